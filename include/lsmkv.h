@@ -485,6 +485,114 @@ int lsmkv_decode_batch_static(const lsmkv_geom_t *geom, int device, void *stream
                               uint32_t n_arenas, const uint32_t *dst_page_table,
                               const lsmkv_pool_t *pool, lsmkv_status_t *status_out);
 
+/*
+ * The step around a hit: new keys and values enter the paged pool, and queries attend to what
+ * the pool holds -- restored prefixes and new tokens alike. These calls work on one layer at a
+ * time, on pools of 16-bit floats (elem_bytes == 2, head_dim a multiple of 8 and at most 256,
+ * LSMKV_EINVAL otherwise); blobs and codecs play no part in them.
+ *
+ * A batch is described once per step and used for every layer. Sequence i has kv_len[i] tokens,
+ * the last n_i = new_off[i+1] - new_off[i] of which are new: new token t of it (row new_off[i] + t
+ * of q, k, v and out) stands at position p = kv_len[i] - n_i + t. A negative p is padding
+ * (kv_len[i] < n_i): nothing is stored for it and its rows of q_out and out are zero. Position p
+ * lies in slot p % page_tokens of page page_table[page_off[i] + p / page_tokens].
+ *   new_off    [dev] u64[n_seq + 1], ascending, new_off[n_seq] == n_new
+ *   kv_len     [dev] u32[n_seq], below 2^31
+ *   page_off   [dev] u64[n_seq + 1], ascending: sequence i has the page_off[i+1] - page_off[i]
+ *              entries of page_table [dev] from page_off[i] on, ceil(kv_len[i]/page_tokens) or more
+ *   max_new    an upper bound of n_i
+ * A sequence that breaks one of these sets LSMKV_ST_BAD_COUNT (item = sequence) and is left out:
+ * its rows are not written. A page id >= num_pages sets LSMKV_ST_BAD_PAGE (item = entry of
+ * page_table); its tokens are not stored by an append and read as zeros by an attend. A pool
+ * buffer that is not 16-byte aligned sets LSMKV_ST_MISALIGNED and the call does nothing.
+ */
+#define LSMKV_BF16 0u
+#define LSMKV_F16 1u
+
+typedef struct {
+    uint64_t n_new;
+    uint32_t n_seq, max_new;
+    const uint64_t *new_off;    /* [dev] */
+    const uint32_t *kv_len;     /* [dev] */
+    const uint64_t *page_off;   /* [dev] */
+    const uint32_t *page_table; /* [dev] */
+} lsmkv_seqs_t;
+
+/* Rows of head_dim contiguous elements: row (t, h) starts at data + t*token_stride +
+ * h*head_stride elements. data 16-byte aligned, strides multiples of 8 (LSMKV_EINVAL). */
+typedef struct {
+    void *data;            /* [dev] */
+    uint64_t token_stride, head_stride;
+} lsmkv_rows_t;
+
+/* Position rotation. table [dev] f32[n_pos][rot_dim]: rot_dim/2 cosines, then rot_dim/2 sines
+ * of every position (scaled variants are the table's business). rot_dim even, <= head_dim; the
+ * elements from rot_dim on stay as they are. interleaved = 0: element e is paired with
+ * e + rot_dim/2; 1: elements 2e and 2e + 1. positions [dev] u32[n_new] or NULL: the row of the
+ * table for every new token, instead of p. A row >= n_pos sets LSMKV_ST_BAD_COUNT (item = new
+ * token) and the token is left out. table 16-byte aligned. */
+typedef struct {
+    const float *table;
+    const uint32_t *positions;
+    uint64_t n_pos;
+    uint32_t rot_dim, interleaved;
+} lsmkv_rope_t;
+
+/*
+ * Append: for every new token, K and V enter the pool pages of `layer`, K after its norm and
+ * rotation; the queries get theirs in the same pass (q_in -> q_out, which may be the same rows).
+ *   norm      x / sqrt(mean_e(x_e^2) + eps) * w_e over the head_dim elements of a head; q_norm,
+ *             k_norm [dev] head_dim elements of `dtype`, 16-byte aligned, NULL = no norm
+ *   rope      [host] NULL = no rotation
+ *   k, v      [host] descriptors of n_new x n_kv_heads rows; q_in, q_out [host] of n_new x
+ *             n_q_heads rows, both NULL (and n_q_heads 0) to append only
+ * Computed in 32 bits and rounded once. V rows, and K rows without norm and rotation, are bit
+ * copies. Slots must be distinct within the call.
+ */
+int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype,
+                       const lsmkv_seqs_t *seqs, const lsmkv_rows_t *k, const lsmkv_rows_t *v,
+                       const lsmkv_pool_t *pool, const lsmkv_rope_t *rope, uint32_t n_q_heads,
+                       const lsmkv_rows_t *q_in, const lsmkv_rows_t *q_out, const void *q_norm,
+                       const void *k_norm, float eps);
+
+/*
+ * Attend: row (t, h) of out, for a new token at position p, is the softmax-weighted mean of the
+ * values of positions 0..p of its sequence under KV head h / (n_q_heads / n_kv_heads), weights
+ * softmax(scale * q . k). n_q_heads must be a multiple of n_kv_heads.
+ *   q, out   [host] descriptors of n_new x n_q_heads rows of `dtype`; out may be q's rows
+ *   lse_out  [dev] f32[n_new][n_q_heads] or NULL: log(sum exp(scale * q . k)) of every row
+ * A row without any key (padding) is zero, its lse -inf. Scores, statistics and sums are held
+ * in 32 bits; weights are rounded to `dtype` before they meet the values.
+ * Uses (and may grow) scratch of the context: two calls must be ordered by the caller.
+ */
+int lsmkv_attend_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype,
+                       const lsmkv_seqs_t *seqs, uint32_t n_q_heads, const lsmkv_rows_t *q,
+                       const lsmkv_pool_t *pool, float scale, const lsmkv_rows_t *out,
+                       float *lse_out);
+
+/*
+ * Attend, for a batch whose sequences share prefixes: sequences group_off[g] .. group_off[g+1]
+ * form group g, and the first shared_pages[g] entries of their page tables name the same pages
+ * (what a get of a common prefix into common pages gives). Same result as lsmkv_attend_batch;
+ * the keys and values of a group's common pages are read once for all its queries instead of
+ * once per sequence. A member with one of its new tokens inside the common pages is computed by
+ * itself; a group of one, and one whose first sequence lists fewer pages, share nothing.
+ *   group_off    [dev] u32[n_group + 1], ascending from 0 to n_seq (else LSMKV_ST_BAD_COUNT,
+ *                item = group, and the results of its sequences are unspecified)
+ *   shared_pages [dev] u32[n_group]
+ */
+typedef struct {
+    uint32_t n_group, reserved;
+    const uint32_t *group_off;    /* [dev] */
+    const uint32_t *shared_pages; /* [dev] */
+} lsmkv_groups_t;
+
+int lsmkv_attend_shared_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype,
+                              const lsmkv_seqs_t *seqs, const lsmkv_groups_t *groups,
+                              uint32_t n_q_heads, const lsmkv_rows_t *q,
+                              const lsmkv_pool_t *pool, float scale, const lsmkv_rows_t *out,
+                              float *lse_out);
+
 /* Synchronise `stream`, copy the device status block to *out [host] and clear it. */
 int lsmkv_last_status(lsmkv_ctx *ctx, void *stream, lsmkv_status_t *out);
 
@@ -496,7 +604,7 @@ int lsmkv_last_status(lsmkv_ctx *ctx, void *stream, lsmkv_status_t *out);
  * turn hit lengths into the list of chunks to copy.
  * Independently of that switch the launches of every call of a context sit inside an NVTX
  * range named after their class ("lsmkv:keys", "lsmkv:pack", "lsmkv:probe", "lsmkv:plan",
- * "lsmkv:unpack", "lsmkv:flush", "lsmkv:merge"): a timeline tool that collects NVTX shows
+ * "lsmkv:unpack", "lsmkv:flush", "lsmkv:merge", "lsmkv:attend"): a timeline tool that collects NVTX shows
  * them, without such a tool the ranges do nothing. lsmkv_decode_batch_static opens none.
  */
 #define LSMKV_K_KEYS 0
@@ -506,6 +614,7 @@ int lsmkv_last_status(lsmkv_ctx *ctx, void *stream, lsmkv_status_t *out);
 #define LSMKV_K_UNPACK 4
 #define LSMKV_K_FLUSH 5
 #define LSMKV_K_MERGE 6
+#define LSMKV_K_ATTEND 7 /* append and attend calls */
 #define LSMKV_K_CLASSES 8
 typedef struct {
     double ms[LSMKV_K_CLASSES];

@@ -4,6 +4,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <mutex>
 #include <new>
@@ -20,6 +21,8 @@
 #include "lsmkv_xp12.cuh"
 #include "lsmkv_xp12_fused.cuh"
 #include "lsmkv_xrun.cuh"
+#include "lsmkv_append.cuh"
+#include "lsmkv_attend.cuh"
 
 using namespace lsmkv;
 
@@ -55,6 +58,11 @@ struct lsmkv_ctx {
     int64_t xp_one_pass, wait_cycles, host_copy_ctas, host_put_device_placed, test_drop_piece;
     int64_t host_copy_piece;
     uint32_t ppc;        // pages per chunk: chunk_tokens / page_tokens
+    // attend: parts of cut tiles with their counters; results of the prefix pass
+    void *d_attend;
+    uint64_t attend_cap;   // bytes
+    void *d_prefix;
+    uint64_t prefix_cap;   // bytes
     // host-buffer calls: device staging and host scratch
     void *d_io[3];
     uint64_t io_cap[3];
@@ -168,7 +176,7 @@ struct LaunchTimer {
     {
         static const char *const names[LSMKV_K_CLASSES] = {
             "lsmkv:keys", "lsmkv:pack", "lsmkv:probe", "lsmkv:plan",
-            "lsmkv:unpack", "lsmkv:flush", "lsmkv:merge", "lsmkv:other"};
+            "lsmkv:unpack", "lsmkv:flush", "lsmkv:merge", "lsmkv:attend"};
         return names[cls >= 0 && cls < LSMKV_K_CLASSES ? cls : LSMKV_K_CLASSES - 1];
     }
     static cudaEvent_t get(lsmkv_ctx *c)
@@ -232,6 +240,15 @@ cudaError_t set_copy_smem_limit(int max_smem_optin)
     if (e == cudaSuccess)
         e = cudaFuncSetAttribute(k_xpf_encode<XpfShape16k>,
                                  cudaFuncAttributeMaxDynamicSharedMemorySize, (int)XpfShape16k::kSmem);
+    for (auto *few : {k_attend_few<__nv_bfloat16, 64, 4, 6>, k_attend_few<__half, 64, 4, 6>})
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FewShape<64, 4, 6>::kSmem);
+    for (auto *few : {k_attend_few<__nv_bfloat16, 128, 4, 3>, k_attend_few<__half, 128, 4, 3>})
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FewShape<128, 4, 3>::kSmem);
+    for (auto *few : {k_attend_few<__nv_bfloat16, 256, 4, 3>, k_attend_few<__half, 256, 4, 3>})
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FewShape<256, 4, 3>::kSmem);
     if (e == cudaSuccess) g_smem_limit_set[dev] = true;
     return e;
 }
@@ -593,6 +610,8 @@ int lsmkv_destroy(lsmkv_ctx *ctx)
     if (release_scratch(ctx, &ctx->d_dir, &ctx->dir_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     if (release_scratch(ctx, &ctx->d_sort, &ctx->sort_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     if (release_scratch(ctx, &ctx->d_xp, &ctx->xp_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
+    if (release_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
+    if (release_scratch(ctx, &ctx->d_prefix, &ctx->prefix_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     for (int k = 0; k < 3; ++k)
         if (release_scratch(ctx, &ctx->d_io[k], &ctx->io_cap[k], __LINE__) != LSMKV_OK)
             note((cudaError_t)ctx->last_cuda);
@@ -1472,3 +1491,4 @@ extern "C" int lsmkv_decode_batch_static(const lsmkv_geom_t *g, int device, void
 }
 
 #include "lsmkv_hostio.cuh"
+#include "lsmkv_serve.cuh"

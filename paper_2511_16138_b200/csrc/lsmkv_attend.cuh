@@ -1,0 +1,733 @@
+// Attention over the paged pool: what both kernels share (the batch as a list of row tiles and
+// its division among the CTAs, partial results and their merge), and the kernel for few rows.
+//
+// For a row (query of one head at position p) with keys k_j, values v_j, j <= p:
+//   m = max_j s_j, s_j = scale * q . k_j;  l = sum_j exp(s_j - m);  o = sum_j exp(s_j - m) v_j / l
+// The sums can be taken in parts: parts (m_1, l_1, o_1), (m_2, l_2, o_2) merge into
+//   m = max(m_1, m_2), l = l_1 e^(m_1-m) + l_2 e^(m_2-m), o = likewise
+// so one pass over the keys suffices, and the keys of a row may be split among warps and CTAs.
+// Exponents are kept in base 2 (scale * log2 e is folded into the scores).
+//
+// Division of work. The query heads of one KV head read the same keys, so a row tile is up to M
+// rows of one sequence under one KV head (row r = token r / G, head r % G), and its cost is the
+// number of key tiles that its last row sees. All tiles in a row -- sequence, KV head, row tile,
+// key tile -- form one line of units that is cut into equal spans, one per CTA: no CTA has more
+// than one unit more than another, whatever the lengths. A row tile cut by a span's end leaves
+// parts in scratch; the CTA that delivers the last part merges them, in order, so that results
+// do not depend on who was last. Every CTA finds its span by itself, from the lengths: no launch
+// before, and nothing for the host to know.
+#pragma once
+#include "lsmkv_append.cuh"
+#include "lsmkv_copy.cuh"
+
+namespace lsmkv {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct AttendJob {
+    SeqArgs seqs;
+    void *const *kv_ptrs;
+    uint64_t num_pages;
+    uint32_t layer, n_layers, page_tokens, n_kv_heads, head_dim, n_q_heads, group;   // group = G
+    uint32_t rows_lo, rows_hi;   // this launch takes the items with rows_lo < rows * G <= rows_hi
+    const void *q;
+    void *out;
+    uint64_t q_ts, q_hs, o_ts, o_hs;
+    float *lse;
+    float scale_log2;
+    // shared prefixes. prefix_pass: the items are the groups, results go to pre_o / pre_lse;
+    // otherwise, with pre_o set, sequence i starts behind its skip[i] shared tokens and merges
+    // the group's result into its own
+    uint32_t prefix_pass, n_group;
+    const uint32_t *group_off, *shared_pages;
+    uint32_t *skip;
+    float *pre_o;                // f32 [n_new][n_q_heads][head_dim]
+    float *pre_lse;              // f32 [n_new][n_q_heads], base 2
+    float *parts;                // two slots per CTA
+    unsigned int *arrived;       // one counter per CTA, zero between calls
+    DevStatus *st;
+};
+
+// An item: a sequence, or in the prefix pass a group.
+struct Item {
+    uint64_t row0, page0;
+    uint32_t tokens;             // new tokens
+    uint32_t kv0, kv1;           // keys [kv0, kv1)
+    uint32_t skip;               // tokens covered by the prefix pass (own pass)
+    bool causal;
+    bool ok;
+};
+
+__device__ __forceinline__ uint32_t shared_tokens(const AttendJob &j, uint32_t g)
+{
+    const uint32_t a = j.group_off[g], b = j.group_off[g + 1];
+    if (a >= b || b > j.seqs.n_seq || b - a < 2) return 0;
+    const uint64_t have = j.seqs.page_off[a + 1] - j.seqs.page_off[a];
+    const uint64_t want = j.shared_pages[g];
+    if (want > have || want * j.page_tokens >= 0x80000000ull) return 0;
+    return (uint32_t)(want * j.page_tokens);
+}
+
+__device__ __forceinline__ Item load_item(const AttendJob &j, uint32_t i)
+{
+    Item it;
+    if (j.prefix_pass) {
+        const uint32_t a = j.group_off[i], b = j.group_off[i + 1];
+        it.kv0 = 0;
+        it.kv1 = shared_tokens(j, i);
+        it.causal = false;
+        it.skip = 0;
+        it.ok = true;
+        it.tokens = 0;
+        it.row0 = it.page0 = 0;
+        if (it.kv1) {
+            const uint64_t r0 = j.seqs.new_off[a], r1 = j.seqs.new_off[b];
+            it.ok = r0 <= r1 && r1 <= j.seqs.n_new;
+            it.row0 = r0;
+            it.tokens = it.ok ? (uint32_t)(r1 - r0) : 0u;
+            it.page0 = j.seqs.page_off[a];
+        }
+        return it;
+    }
+    const SeqInfo s = load_seq(j.seqs, i, j.page_tokens);
+    it.row0 = s.row0;
+    it.page0 = s.page0;
+    it.tokens = s.rows;
+    it.ok = s.ok;
+    it.kv0 = 0;
+    it.kv1 = s.kv;
+    it.causal = true;
+    it.skip = 0;
+    if (j.pre_o && s.ok) {
+        // a member with a new token inside the shared part goes by itself
+        const uint32_t k = j.skip[i];
+        if (k && s.kv >= s.rows && k <= s.kv - s.rows) it.skip = it.kv0 = k;
+    }
+    return it;
+}
+
+// Keys that token t of an item sees: [kv0, limit).
+__device__ __forceinline__ uint32_t token_limit(const Item &it, uint32_t t)
+{
+    if (!it.causal) return it.kv1;
+    const int64_t p = (int64_t)it.kv1 - (int64_t)it.tokens + (int64_t)t + 1;
+    return p > (int64_t)it.kv0 ? (uint32_t)p : it.kv0;
+}
+
+// Key tiles of `tile` keys for row tile rt (M rows): at least one, so that rows without keys are
+// written too.
+__device__ __forceinline__ uint32_t tile_units(const Item &it, uint32_t rt, uint32_t M, uint32_t G,
+                                               uint32_t tile)
+{
+    uint32_t t = (rt * M + M - 1) / G;
+    if (t >= it.tokens) t = it.tokens - 1;
+    const uint32_t n = (token_limit(it, t) - it.kv0 + tile - 1) / tile;
+    return n ? n : 1u;
+}
+
+__device__ __forceinline__ uint32_t item_tiles(const AttendJob &j, const Item &it, uint32_t M)
+{
+    const uint64_t rows = (uint64_t)it.tokens * j.group;
+    if (rows <= j.rows_lo || rows > j.rows_hi) return 0;
+    return (uint32_t)((rows + M - 1) / M);
+}
+
+// Units of one KV head of an item.
+__device__ __forceinline__ uint64_t item_units(const AttendJob &j, const Item &it, uint32_t M,
+                                               uint32_t tile)
+{
+    const uint32_t n = item_tiles(j, it, M);
+    if (!n) return 0;
+    if (!it.causal) return (uint64_t)n * tile_units(it, 0, M, j.group, tile);
+    uint64_t u = 0;
+    for (uint32_t rt = 0; rt < n; ++rt) u += tile_units(it, rt, M, j.group, tile);
+    return u;
+}
+
+// A CTA's place on the line of units.
+struct Span {
+    uint64_t begin, end, per;    // units [begin, end); units per CTA
+    uint32_t item;               // the item that holds `begin`
+    uint64_t before;             // units ahead of that item
+};
+
+// Called by all threads of a CTA (NT of them, a multiple of 32, at most 1024). n items.
+template <int NT>
+__device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t tile)
+{
+    __shared__ uint64_t warp_sum[NT / 32];
+    __shared__ uint64_t found_before;
+    __shared__ uint32_t found_item;
+    const uint32_t tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    const uint32_t each = (n + NT - 1) / NT;
+    const uint32_t i0 = tid * each < n ? tid * each : n;
+    const uint32_t i1 = i0 + each < n ? i0 + each : n;
+    uint64_t mine = 0, first = 0;
+    for (uint32_t i = i0; i < i1; ++i) {
+        const Item it = load_item(j, i);
+        const uint64_t u = item_units(j, it, M, tile) * j.n_kv_heads;
+        if (!it.ok && blockIdx.x == 0) st_flag(j.st, LSMKV_ST_BAD_COUNT, i);
+        if (i == i0) first = u;
+        mine += u;
+    }
+    uint64_t incl = mine;
+    for (int d = 1; d < 32; d <<= 1) {
+        const uint64_t o = __shfl_up_sync(~0u, incl, d);
+        if ((int)lane >= d) incl += o;
+    }
+    if (lane == 31) warp_sum[w] = incl;
+    __syncthreads();
+    uint64_t total = 0, ahead = 0;
+#pragma unroll
+    for (int k = 0; k < NT / 32; ++k) {
+        if (k < (int)w) ahead += warp_sum[k];
+        total += warp_sum[k];
+    }
+    Span s;
+    s.per = (total + gridDim.x - 1) / gridDim.x;
+    s.begin = s.per * blockIdx.x;
+    s.end = s.begin + s.per;
+    if (s.end > total) s.end = total;
+    if (s.begin > total) s.begin = total;
+    uint64_t at = ahead + incl - mine;
+    if (s.begin < s.end && at <= s.begin && s.begin < at + mine) {
+        uint32_t i = i0;
+        if (each > 1 && at + first <= s.begin) {
+            at += first;
+            for (i = i0 + 1; i < i1; ++i) {
+                const uint64_t u = item_units(j, load_item(j, i), M, tile) * j.n_kv_heads;
+                if (at + u > s.begin) break;
+                at += u;
+            }
+        }
+        found_item = i;
+        found_before = at;
+    }
+    __syncthreads();
+    s.item = found_item;
+    s.before = found_before;
+    return s;
+}
+
+// The first item behind i that has units (there is one when the span is not done), looked for by
+// the lanes of every warp together: a launch may pass over many items that are not its own.
+__device__ __forceinline__ uint32_t next_item(const AttendJob &j, uint32_t i, uint32_t n, uint32_t M,
+                                              uint32_t tile, Item *it, uint64_t *per_head)
+{
+    const uint32_t lane = threadIdx.x & 31;
+    for (uint32_t base = i + 1; base < n; base += 32) {
+        uint64_t u = 0;
+        if (base + lane < n) u = item_units(j, load_item(j, base + lane), M, tile);
+        const unsigned some = __ballot_sync(~0u, u != 0);
+        if (some) {
+            const int k = __ffs(some) - 1;
+            *per_head = __shfl_sync(~0u, u, k);
+            *it = load_item(j, base + k);
+            return base + k;
+        }
+    }
+    return i;
+}
+
+// One row tile of the line and the piece of it that lies in a CTA's span.
+struct Cut {
+    uint32_t kv_head, rt, rows;  // rows of the tile
+    uint64_t tile0;              // units ahead of the tile
+    uint32_t units;              // of the whole tile
+    uint32_t k0, k1;             // key tiles [k0, k1) of it are this CTA's
+};
+
+// The tile that holds unit u of an item whose first unit is `before`.
+__device__ __forceinline__ Cut find_cut(const AttendJob &j, const Item &it, uint64_t per_head,
+                                            uint64_t before, uint64_t u, uint64_t end, uint32_t M,
+                                            uint32_t tile)
+{
+    Cut p;
+    const uint64_t rel = u - before;
+    p.kv_head = (uint32_t)(rel / per_head);
+    uint64_t at = rel - (uint64_t)p.kv_head * per_head;
+    uint64_t base = before + (uint64_t)p.kv_head * per_head;
+    p.rt = 0;
+    if (!it.causal) {
+        p.units = tile_units(it, 0, M, j.group, tile);
+        p.rt = (uint32_t)(at / p.units);
+        base += (uint64_t)p.rt * p.units;
+        at -= (uint64_t)p.rt * p.units;
+    } else {
+        while (true) {
+            p.units = tile_units(it, p.rt, M, j.group, tile);
+            if (at < p.units) break;
+            at -= p.units;
+            base += p.units;
+            ++p.rt;
+        }
+    }
+    p.tile0 = base;
+    p.k0 = (uint32_t)at;
+    const uint64_t left = base + p.units < end ? base + p.units : end;
+    p.k1 = (uint32_t)(left - base);
+    const uint64_t rows = (uint64_t)it.tokens * j.group - (uint64_t)p.rt * M;
+    p.rows = rows < M ? (uint32_t)rows : M;
+    return p;
+}
+
+// ---- partial results: per slot, M rows of sums, then M maxima and M sums of weights ----------
+
+__device__ __forceinline__ float *part_slot(const AttendJob &j, uint64_t slot, uint32_t M, uint32_t DP)
+{
+    return j.parts + slot * ((uint64_t)M * (DP + 2));
+}
+
+// 2^(x) with 2^(-inf) = 0; statistics of an empty part are m = -inf, l = 0.
+__device__ __forceinline__ float part_weight(float m, float top)
+{
+    return m == -INFINITY ? 0.f : exp2f(m - top);
+}
+
+// A row tile's products also run over keys that only later rows of it see, with weight zero:
+// an infinite or undefined value there makes the sum undefined although the row must not see
+// it. A row that comes out undefined and has such keys beside it is taken again here, key by key
+// over its own keys alone; finite inputs never come here.
+template <typename T>
+__device__ __noinline__ void redo_row4(const AttendJob &j, const Item &it, uint64_t row, uint32_t head,
+                                       uint32_t limit, uint32_t d, float4 *acc, float *m_out, float *l_out)
+{
+    const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
+    const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
+    const T *const q = static_cast<const T *>(j.q) + row * j.q_ts + (uint64_t)head * j.q_hs;
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (uint32_t k = it.kv0; k < limit; ++k) {
+        const uint32_t page = j.seqs.page_table[it.page0 + k / j.page_tokens];
+        const bool real = page < j.num_pages;
+        const uint64_t at = (((uint64_t)(real ? page : 0) * j.page_tokens + k % j.page_tokens) *
+                                 j.n_kv_heads + head / j.group) * j.head_dim;
+        float s = 0.f;
+        for (uint32_t e = 0; real && e < j.head_dim; ++e) s += Half2<T>::up1(q[e]) * Half2<T>::up1(kbuf[at + e]);
+        s *= j.scale_log2;
+        const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
+        const float c = exp2f(m - base), w = exp2f(s - base);
+        l = l * c + w;
+        for (int e = 0; e < 4; ++e) o[e] = o[e] * c + (real ? w * Half2<T>::up1(vbuf[at + d + e]) : 0.f);
+        m = top;
+    }
+    *acc = make_float4(o[0], o[1], o[2], o[3]);
+    *m_out = m;
+    *l_out = l;
+}
+
+// Write four elements of finished row R of the item: acc = sum of weighted values relative to 2^m, l the sum
+// of weights. Merges the prefix pass's result first when there is one.
+template <typename T>
+__device__ __forceinline__ void finish_row4(const AttendJob &j, const Item &it, const Cut &p, uint32_t R,
+                                            uint32_t d, float4 acc, float m, float l)
+{
+    const uint64_t row = it.row0 + R / j.group;
+    const uint32_t head = p.kv_head * j.group + R % j.group;
+    const uint64_t flat = row * j.n_q_heads + head;
+    if (it.causal && it.tokens > 1 && isnan(acc.x + acc.y + acc.z + acc.w))
+        redo_row4<T>(j, it, row, head, token_limit(it, R / j.group), d, &acc, &m, &l);
+    if (it.skip) {
+        const float pm = j.pre_lse[flat];
+        const float4 po = *reinterpret_cast<const float4 *>(j.pre_o + flat * j.head_dim + d);
+        const float top = fmaxf(m, pm);
+        const float a = part_weight(m, top), b = part_weight(pm, top);
+        acc.x = acc.x * a + po.x * b;
+        acc.y = acc.y * a + po.y * b;
+        acc.z = acc.z * a + po.z * b;
+        acc.w = acc.w * a + po.w * b;
+        l = l * a + b;
+        m = top;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
+    if (l == 0.f) acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+    if (j.prefix_pass) {
+        *reinterpret_cast<float4 *>(j.pre_o + flat * j.head_dim + d) = acc;
+        if (d == 0) j.pre_lse[flat] = lse2;
+        return;
+    }
+    uint2 v;
+    v.x = Half2<T>::down(acc.x, acc.y);
+    v.y = Half2<T>::down(acc.z, acc.w);
+    *reinterpret_cast<uint2 *>(static_cast<T *>(j.out) + row * j.o_ts + head * j.o_hs + d) = v;
+    if (d == 0 && j.lse) j.lse[flat] = lse2 * kLn2;
+}
+
+// Merge the parts of a cut tile. Called by all threads of the CTA that delivered the last one.
+template <typename T, int NT>
+__device__ void merge_parts(const AttendJob &j, const Item &it, const Cut &p, uint64_t per, uint32_t M,
+                            uint32_t DP)
+{
+    const uint32_t c0 = (uint32_t)(p.tile0 / per), c1 = (uint32_t)((p.tile0 + p.units - 1) / per);
+    const uint32_t quads = j.head_dim / 4;
+    for (uint32_t x = threadIdx.x; x < p.rows * quads; x += NT) {
+        const uint32_t r = x / quads, d = (x - r * quads) * 4;
+        float m = -INFINITY, l = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (uint32_t c = c0; c <= c1; ++c) {
+            const float *s = part_slot(j, 2ull * c + (c == c0 ? 1 : 0), M, DP);
+            const float pm = __ldcg(s + (uint64_t)M * DP + r), pl = __ldcg(s + (uint64_t)M * (DP + 1) + r);
+            const float4 o = __ldcg(reinterpret_cast<const float4 *>(s + (uint64_t)r * DP + d));
+            const float top = fmaxf(m, pm);
+            const float a = part_weight(m, top), b = part_weight(pm, top);
+            acc.x = acc.x * a + o.x * b;
+            acc.y = acc.y * a + o.y * b;
+            acc.z = acc.z * a + o.z * b;
+            acc.w = acc.w * a + o.w * b;
+            l = l * a + pl * b;
+            m = top;
+        }
+        finish_row4<T>(j, it, p, p.rt * M + r, d, acc, m, l);
+    }
+}
+
+// The CTA has written its part of a cut tile: true for all its threads when it is the last one.
+__device__ __forceinline__ bool deliver_part(const AttendJob &j, const Cut &p, uint64_t per)
+{
+    __shared__ uint32_t last;
+    const uint32_t c0 = (uint32_t)(p.tile0 / per), c1 = (uint32_t)((p.tile0 + p.units - 1) / per);
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        last = atomicAdd(&j.arrived[c0], 1u) == c1 - c0;
+        if (last) j.arrived[c0] = 0;      // ready for the next call
+    }
+    __syncthreads();
+    if (last) __threadfence();
+    return last;
+}
+
+// ---- few rows ---------------------------------------------------------------------------------
+//
+// Bound by memory: a decode step reads every key and value once and does 4 G operations a byte.
+// A row tile is 16 rows (one m16n8k16 fragment), a warp takes 16 keys at a time in a private ring
+// of ST stages fed by cp.async (no barrier in the loop: the warps of a CTA share nothing until
+// the tile's end), and the NW warps of a CTA take the key tiles in turn. Two CTAs a SM, so that
+// one streams while the other merges. Rows of a page are contiguous for one head only (256
+// bytes at head_dim 128), and page sizes are the caller's: 16-byte copies, swizzled on their
+// way, take any of them.
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool real)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                 :: "r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+__device__ __forceinline__ void ldmatrix4t(uint32_t addr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+template <typename T> __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4],
+                                                               uint32_t b0, uint32_t b1);
+template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4],
+                                                                    uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+                 "{%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <> __device__ __forceinline__ void mma16816<__half>(float (&c)[4], const uint32_t (&a)[4],
+                                                             uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+                 "{%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+template <int DP, int NW, int ST>
+struct FewShape {
+    static constexpr int kM = 16;                          // rows of a tile
+    static constexpr int kKeys = 16;                       // keys a warp takes at a time
+    static constexpr int kThreads = NW * 32;
+    static constexpr uint32_t kStage = kKeys * DP * 2 * 2; // K then V
+    static constexpr size_t kQBytes = 16 * DP * 2;
+    static constexpr size_t kSmem = kQBytes + (size_t)NW * ST * kStage;
+    static_assert((size_t)ST * kStage >= 16 * DP * 4, "a warp's ring takes its sums at the tile's end");
+};
+
+template <typename T, int DP, int NW, int ST>
+__global__ __launch_bounds__(NW * 32) void k_attend_few(const AttendJob j)
+{
+    using Sh = FewShape<DP, NW, ST>;
+    constexpr int NT = Sh::kThreads;
+    constexpr int kChunks = DP / 8;            // 16-byte pieces of a row
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ float sm_m[NW][16], sm_l[NW][16];
+    const uint32_t tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    const uint32_t G = j.group, D = j.head_dim;
+
+    const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
+    const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
+    if ((reinterpret_cast<uintptr_t>(kbuf) | reinterpret_cast<uintptr_t>(vbuf)) & 15u) {
+        if (blockIdx.x == 0 && tid == 0) st_flag(j.st, LSMKV_ST_MISALIGNED, 0);
+        return;
+    }
+    const uint32_t n_items = j.prefix_pass ? j.n_group : j.seqs.n_seq;
+    constexpr uint32_t kTile = Sh::kKeys * NW;
+    const Span span = find_span<NT>(j, n_items, Sh::kM, kTile);
+    if (span.begin >= span.end) return;
+
+    const uint32_t q_s = smem_addr(smem);
+    const uint32_t ring = q_s + (uint32_t)Sh::kQBytes + w * (ST * Sh::kStage);
+    const uint64_t tok_stride = (uint64_t)j.n_kv_heads * D;
+
+    uint64_t u = span.begin, before = span.before;
+    uint32_t i = span.item;
+    Item it = load_item(j, i);
+    uint64_t per_head = item_units(j, it, Sh::kM, kTile);
+    while (u < span.end) {
+        if (u >= before + per_head * j.n_kv_heads) {
+            before += per_head * j.n_kv_heads;
+            i = next_item(j, i, n_items, Sh::kM, kTile, &it, &per_head);
+        }
+        const Cut p = find_cut(j, it, per_head, before, u, span.end, Sh::kM, kTile);
+        const uint32_t row_base = p.rt * Sh::kM;
+
+        // the tile's queries, swizzled like the keys; rows beyond the tile are zero
+        for (uint32_t x = tid; x < 16 * kChunks; x += NT) {
+            const uint32_t r = x / kChunks, c = x % kChunks;
+            const bool real = r < p.rows && c * 8 < D;
+            const uint32_t R = row_base + (r < p.rows ? r : 0);
+            const T *src = static_cast<const T *>(j.q) + (it.row0 + R / G) * j.q_ts +
+                           (uint64_t)(p.kv_head * G + R % G) * j.q_hs + (c * 8 < D ? c * 8 : 0);
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (real) v = *reinterpret_cast<const uint4 *>(src);
+            *reinterpret_cast<uint4 *>(smem + (r * kChunks + (c ^ (r & 7))) * 16) = v;
+        }
+        __syncthreads();
+
+        // rows lane/4 and lane/4 + 8 of the tile, and the keys they see
+        uint32_t lim[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint32_t r = (lane >> 2) + 8 * x;
+            lim[x] = r < p.rows ? token_limit(it, (row_base + r) / G) : it.kv0;
+        }
+        const uint32_t lim_first = token_limit(it, row_base / G);              // least of the tile
+        const uint32_t lim_last = token_limit(it, (row_base + p.rows - 1) / G);
+        const uint32_t key_end = min(lim_last, it.kv0 + p.k1 * kTile);
+        const uint32_t key0 = it.kv0 + p.k0 * kTile + w * Sh::kKeys;
+
+        // the page id of key `key + lane % 16`, one step ahead of its copies
+        auto page_of = [&](uint32_t key) -> uint32_t {
+            const uint32_t k = key + (lane & 15);
+            if (k >= key_end) return 0xFFFFFFFFu;
+            const uint64_t entry = it.page0 + k / j.page_tokens;
+            const uint32_t page = j.seqs.page_table[entry];
+            if (page >= j.num_pages) {
+                st_flag(j.st, LSMKV_ST_BAD_PAGE, entry);
+                return 0xFFFFFFFFu;
+            }
+            return page;
+        };
+        auto fetch = [&](uint32_t key, uint32_t page, uint32_t stage) {
+            const uint32_t k = key + (lane & 15);
+            const bool real = page != 0xFFFFFFFFu;
+            const uint64_t off = real ? ((uint64_t)page * j.page_tokens + k % j.page_tokens) * tok_stride +
+                                            (uint64_t)p.kv_head * D
+                                      : 0;
+            const unsigned live = __ballot_sync(~0u, real);
+            const uint32_t lo = (uint32_t)off, hi = (uint32_t)(off >> 32);
+            const uint32_t dst = ring + stage * Sh::kStage;
+            constexpr int kPer = kChunks / 2;      // 16 rows * kChunks pieces / 32 lanes
+#pragma unroll
+            for (int x = 0; x < kPer; ++x) {
+                const uint32_t piece = x * 32 + lane;
+                const uint32_t r = piece / kChunks, c = piece % kChunks;
+                const uint64_t o = ((uint64_t)__shfl_sync(~0u, hi, r) << 32) | __shfl_sync(~0u, lo, r);
+                const bool in = ((live >> r) & 1u) && c * 8 < D;
+                const uint64_t e = in ? o + c * 8 : 0;
+                const uint32_t at = dst + (r * kChunks + (c ^ (r & 7))) * 16;
+                cp_async16(at, kbuf + e, in);
+                cp_async16(at + Sh::kKeys * DP * 2, vbuf + e, in);
+            }
+        };
+
+        float o[DP / 8][4];
+#pragma unroll
+        for (int x = 0; x < DP / 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+        uint32_t key_load = key0;
+        uint32_t page = page_of(key_load);
+#pragma unroll
+        for (int s = 0; s < ST - 1; ++s) {
+            if (key_load < key_end) {
+                const uint32_t next = page_of(key_load + kTile);
+                fetch(key_load, page, s);
+                page = next;
+                key_load += kTile;
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        uint32_t stage = 0, stage_load = ST - 1;
+        for (uint32_t key = key0; key < key_end; key += kTile) {
+            if (key_load < key_end) {
+                const uint32_t next = page_of(key_load + kTile);
+                fetch(key_load, page, stage_load);
+                page = next;
+                key_load += kTile;
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            stage_load = stage_load + 1 == ST ? 0 : stage_load + 1;
+            asm volatile("cp.async.wait_group %0;" :: "n"(ST - 1) : "memory");
+            __syncwarp();
+            const uint32_t ks = ring + stage * Sh::kStage;
+            const uint32_t vs = ks + Sh::kKeys * DP * 2;
+
+            float s[2][4] = {};
+            {
+                const uint32_t kr = (lane & 7) + ((lane >> 4) << 3);
+                const uint32_t qr = lane & 15;
+#pragma unroll
+                for (int x = 0; x < DP / 16; ++x) {
+                    uint32_t a[4], b[4];
+                    ldmatrix4(q_s + (qr * kChunks + ((2 * x + (lane >> 4)) ^ (qr & 7))) * 16, a);
+                    ldmatrix4(ks + (kr * kChunks + ((2 * x + ((lane >> 3) & 1)) ^ (kr & 7))) * 16, b);
+                    mma16816<T>(s[0], a, b[0], b[1]);
+                    mma16816<T>(s[1], a, b[2], b[3]);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] *= j.scale_log2;
+            if (key + Sh::kKeys > lim_first) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (key + n * 8 + 2 * (lane & 3) + (e & 1) >= lim[e >> 1]) s[n][e] = -INFINITY;
+            }
+            uint32_t pa[4];
+            float corr[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                float t = fmaxf(fmaxf(s[0][2 * x], s[0][2 * x + 1]), fmaxf(s[1][2 * x], s[1][2 * x + 1]));
+                t = fmaxf(t, __shfl_xor_sync(~0u, t, 1));
+                t = fmaxf(t, __shfl_xor_sync(~0u, t, 2));
+                t = fmaxf(t, m[x]);
+                const float base = t == -INFINITY ? 0.f : t;
+                corr[x] = exp2f(m[x] - base);
+                m[x] = t;
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    s[n][2 * x] = exp2f(s[n][2 * x] - base);
+                    s[n][2 * x + 1] = exp2f(s[n][2 * x + 1] - base);
+                }
+                l[x] = l[x] * corr[x] + (s[0][2 * x] + s[0][2 * x + 1]) + (s[1][2 * x] + s[1][2 * x + 1]);
+                // the weights are rounded to the values' type: the tensor cores take both in one
+                pa[x] = Half2<T>::down(s[0][2 * x], s[0][2 * x + 1]);
+                pa[2 + x] = Half2<T>::down(s[1][2 * x], s[1][2 * x + 1]);
+            }
+            if (__any_sync(~0u, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+                for (int x = 0; x < DP / 8; ++x) {
+                    o[x][0] *= corr[0];
+                    o[x][1] *= corr[0];
+                    o[x][2] *= corr[1];
+                    o[x][3] *= corr[1];
+                }
+            }
+            {
+                const uint32_t vr = (lane & 7) + (((lane >> 3) & 1) << 3);
+#pragma unroll
+                for (int x = 0; x < DP / 16; ++x) {
+                    uint32_t b[4];
+                    ldmatrix4t(vs + (vr * kChunks + ((2 * x + (lane >> 4)) ^ (vr & 7))) * 16, b);
+                    mma16816<T>(o[2 * x], pa, b[0], b[1]);
+                    mma16816<T>(o[2 * x + 1], pa, b[2], b[3]);
+                }
+            }
+            __syncwarp();     // the stage is read before it is filled again
+            stage = stage + 1 == ST ? 0 : stage + 1;
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+
+        // merge the warps: sums into the warps' own rings, statistics beside them
+        float *const mine = reinterpret_cast<float *>(smem + Sh::kQBytes + (size_t)w * ST * Sh::kStage);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            l[x] += __shfl_xor_sync(~0u, l[x], 1);
+            l[x] += __shfl_xor_sync(~0u, l[x], 2);
+            const uint32_t r = (lane >> 2) + 8 * x;
+            if ((lane & 3) == 0) {
+                sm_m[w][r] = m[x];
+                sm_l[w][r] = l[x];
+            }
+            if (r < p.rows) {
+#pragma unroll
+                for (int n = 0; n < DP / 8; ++n)
+                    *reinterpret_cast<float2 *>(mine + r * DP + ((n * 8 + 2 * (lane & 3)) ^ ((r & 3) * 8))) =
+                        make_float2(o[n][2 * x], o[n][2 * x + 1]);
+            }
+        }
+        __syncthreads();
+        const bool whole = p.k0 == 0 && p.k1 == p.units;
+        const uint32_t quads = D / 4;
+        float *slot = whole ? nullptr
+                            : part_slot(j, 2ull * blockIdx.x + (p.k0 == 0 ? 1 : 0), Sh::kM, DP);
+        for (uint32_t x = tid; x < p.rows * quads; x += NT) {
+            const uint32_t r = x / quads, d = (x - r * quads) * 4;
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < NW; ++k) top = fmaxf(top, sm_m[k][r]);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < NW; ++k) {
+                const float f = part_weight(sm_m[k][r], top);
+                const float4 v = *reinterpret_cast<const float4 *>(
+                    smem + Sh::kQBytes + (size_t)k * ST * Sh::kStage +
+                    (r * DP + (d ^ ((r & 3) * 8))) * 4);
+                acc.x += f * v.x;
+                acc.y += f * v.y;
+                acc.z += f * v.z;
+                acc.w += f * v.w;
+                sum += f * sm_l[k][r];
+            }
+            if (whole) {
+                finish_row4<T>(j, it, p, row_base + r, d, acc, top, sum);
+            } else {
+                __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)r * DP + d), acc);
+                if (d == 0) {
+                    __stcg(slot + (uint64_t)Sh::kM * DP + r, top);
+                    __stcg(slot + (uint64_t)Sh::kM * (DP + 1) + r, sum);
+                }
+            }
+        }
+        if (!whole && deliver_part(j, p, span.per)) merge_parts<T, NT>(j, it, p, span.per, Sh::kM, DP);
+        __syncthreads();
+        u += p.k1 - p.k0;
+    }
+}
+
+// The prefix pass's companion: how many tokens of every sequence the pass covers.
+__global__ void k_shared_skip(const AttendJob j)
+{
+    const uint32_t i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i == 0 && (j.group_off[0] != 0 || j.group_off[j.n_group] != j.seqs.n_seq))
+        st_flag(j.st, LSMKV_ST_BAD_COUNT, j.n_group);
+    if (i >= j.n_group) return;
+    const uint32_t a = j.group_off[i], b = j.group_off[i + 1];
+    if (a > b || b > j.seqs.n_seq) {
+        st_flag(j.st, LSMKV_ST_BAD_COUNT, i);
+        return;
+    }
+    const uint32_t k = shared_tokens(j, i);
+    for (uint32_t s = a; s < b; ++s) j.skip[s] = k;
+}
+
+}  // namespace lsmkv

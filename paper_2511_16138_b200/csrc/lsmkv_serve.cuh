@@ -1,0 +1,251 @@
+// The calls around a hit: append new keys and values to the paged pool, attend to what it holds.
+// Host side: checks of the arguments, scratch, choice of kernel, launches.
+// Included at the end of lsmkv.cu (needs the context's internals).
+#pragma once
+
+namespace {
+
+// The pools these calls take.
+bool serve_geom_ok(const lsmkv_ctx *ctx, uint32_t layer, uint32_t dtype)
+{
+    const lsmkv_geom_t &g = ctx->geom;
+    return g.elem_bytes == 2 && g.head_dim % 8 == 0 && g.head_dim <= 256 && layer < g.n_layers &&
+           (dtype == LSMKV_BF16 || dtype == LSMKV_F16);
+}
+
+bool seqs_ok(const lsmkv_seqs_t *s)
+{
+    return s && s->n_seq && s->max_new && s->new_off && s->kv_len && s->page_off && s->page_table;
+}
+
+bool rows_ok(const lsmkv_rows_t *r)
+{
+    return r && r->data && aligned16(r->data) && r->token_stride % 8 == 0 && r->head_stride % 8 == 0;
+}
+
+SeqArgs seq_args(const lsmkv_seqs_t *s)
+{
+    SeqArgs a;
+    a.n_new = s->n_new;
+    a.n_seq = s->n_seq;
+    a.max_new = s->max_new;
+    a.new_off = s->new_off;
+    a.kv_len = s->kv_len;
+    a.page_off = s->page_off;
+    a.page_table = s->page_table;
+    return a;
+}
+
+template <typename T>
+int launch_few(lsmkv_ctx *ctx, cudaStream_t s, const AttendJob &job)
+{
+    const unsigned sm = (unsigned)ctx->sm_count;
+    if (job.head_dim <= 64)
+        k_attend_few<T, 64, 4, 6><<<sm * 2, 128, FewShape<64, 4, 6>::kSmem, s>>>(job);
+    else if (job.head_dim <= 128)
+        k_attend_few<T, 128, 4, 3><<<sm * 2, 128, FewShape<128, 4, 3>::kSmem, s>>>(job);
+    else
+        k_attend_few<T, 256, 4, 3><<<sm, 128, FewShape<256, 4, 3>::kSmem, s>>>(job);
+    ++ctx->launches;
+    CU(ctx, cudaGetLastError());
+    return LSMKV_OK;
+}
+
+// Scratch of the attend kernels: counters, then two part slots per CTA of the widest launch.
+int ensure_attend(lsmkv_ctx *ctx, cudaStream_t s)
+{
+    const size_t counters = ((size_t)ctx->sm_count * 2 * 4 + 255) & ~size_t(255);
+    const uint32_t dp = ctx->geom.head_dim <= 64 ? 64 : ctx->geom.head_dim <= 128 ? 128 : 256;
+    const size_t bytes = counters + (size_t)ctx->sm_count * 2 * 2 * 16 * (dp + 2) * 4;
+    if (ctx->d_attend && bytes <= ctx->attend_cap) return LSMKV_OK;
+    const int rc = grow_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, bytes, bytes, __LINE__);
+    if (rc != LSMKV_OK) return rc;
+    const cudaError_t e = cudaMemsetAsync(ctx->d_attend, 0, counters, s);
+    if (e != cudaSuccess) {
+        release_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, __LINE__);
+        return cuda_fail(ctx, e, __LINE__);
+    }
+    return LSMKV_OK;
+}
+
+int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const lsmkv_seqs_t *seqs,
+           const lsmkv_groups_t *groups, uint32_t n_q_heads, const lsmkv_rows_t *q,
+           const lsmkv_pool_t *pool, float scale, const lsmkv_rows_t *out, float *lse_out)
+{
+    if (!ctx || !seqs) return LSMKV_EINVAL;
+    if (!serve_geom_ok(ctx, layer, dtype)) return LSMKV_EINVAL;
+    if (seqs->n_new == 0) return LSMKV_OK;
+    if (!seqs_ok(seqs) || !rows_ok(q) || !rows_ok(out) || !pool || !pool->kv_ptrs) return LSMKV_EINVAL;
+    if (n_q_heads == 0 || n_q_heads % ctx->geom.n_kv_heads != 0 || !std::isfinite(scale)) return LSMKV_EINVAL;
+    if (groups && groups->n_group && (!groups->group_off || !groups->shared_pages)) return LSMKV_EINVAL;
+    if (groups && groups->n_group > seqs->n_seq) return LSMKV_EINVAL;
+    const bool shared = groups && groups->n_group;
+    DeviceGuard guard(ctx->device);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int rc = ensure_attend(ctx, s);
+    if (rc != LSMKV_OK) return rc;
+
+    AttendJob job;
+    std::memset(&job, 0, sizeof(job));
+    job.seqs = seq_args(seqs);
+    job.kv_ptrs = pool->kv_ptrs;
+    job.num_pages = pool->num_pages;
+    job.layer = layer;
+    job.n_layers = ctx->geom.n_layers;
+    job.page_tokens = ctx->geom.page_tokens;
+    job.n_kv_heads = ctx->geom.n_kv_heads;
+    job.head_dim = ctx->geom.head_dim;
+    job.n_q_heads = n_q_heads;
+    job.group = n_q_heads / ctx->geom.n_kv_heads;
+    job.rows_lo = 0;
+    job.rows_hi = 0xFFFFFFFFu;
+    job.q = q->data;
+    job.q_ts = q->token_stride;
+    job.q_hs = q->head_stride;
+    job.out = out->data;
+    job.o_ts = out->token_stride;
+    job.o_hs = out->head_stride;
+    job.lse = lse_out;
+    job.scale_log2 = scale * kLog2e;
+    job.arrived = static_cast<unsigned int *>(ctx->d_attend);
+    job.parts = reinterpret_cast<float *>(static_cast<char *>(ctx->d_attend) +
+                                          (((size_t)ctx->sm_count * 2 * 4 + 255) & ~size_t(255)));
+    job.st = ctx->d_status;
+    if (shared) {
+        const uint64_t heads = seqs->n_new * n_q_heads;
+        const size_t bytes = (size_t)(heads * (ctx->geom.head_dim + 1) + seqs->n_seq) * 4;
+        if (!ctx->d_prefix || bytes > ctx->prefix_cap) {
+            rc = grow_scratch(ctx, &ctx->d_prefix, &ctx->prefix_cap, bytes, bytes, __LINE__);
+            if (rc != LSMKV_OK) return rc;
+        }
+        job.pre_o = static_cast<float *>(ctx->d_prefix);
+        job.pre_lse = job.pre_o + heads * ctx->geom.head_dim;
+        job.skip = reinterpret_cast<uint32_t *>(job.pre_lse + heads);
+        job.n_group = groups->n_group;
+        job.group_off = groups->group_off;
+        job.shared_pages = groups->shared_pages;
+    }
+    LaunchTimer timer(ctx, s, LSMKV_K_ATTEND);
+    auto few = dtype == LSMKV_BF16 ? launch_few<__nv_bfloat16> : launch_few<__half>;
+    if (shared) {
+        k_shared_skip<<<(groups->n_group + 127) / 128, 128, 0, s>>>(job);
+        ++ctx->launches;
+        CU(ctx, cudaGetLastError());
+        job.prefix_pass = 1;
+        rc = few(ctx, s, job);
+        if (rc != LSMKV_OK) return rc;
+        job.prefix_pass = 0;
+    }
+    return few(ctx, s, job);
+}
+
+}  // namespace
+
+extern "C" int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype,
+                                  const lsmkv_seqs_t *seqs, const lsmkv_rows_t *k,
+                                  const lsmkv_rows_t *v, const lsmkv_pool_t *pool,
+                                  const lsmkv_rope_t *rope, uint32_t n_q_heads,
+                                  const lsmkv_rows_t *q_in, const lsmkv_rows_t *q_out,
+                                  const void *q_norm, const void *k_norm, float eps)
+{
+    if (!ctx || !seqs) return LSMKV_EINVAL;
+    if (!serve_geom_ok(ctx, layer, dtype)) return LSMKV_EINVAL;
+    if (seqs->n_new == 0) return LSMKV_OK;
+    if (!seqs_ok(seqs) || !rows_ok(k) || !rows_ok(v) || !pool || !pool->kv_ptrs) return LSMKV_EINVAL;
+    if (n_q_heads ? !rows_ok(q_in) || !rows_ok(q_out) : q_in || q_out || q_norm) return LSMKV_EINVAL;
+    if (!aligned16(q_norm) || !aligned16(k_norm)) return LSMKV_EINVAL;
+    if ((q_norm || k_norm) && !(eps >= 0.f && std::isfinite(eps))) return LSMKV_EINVAL;
+    const lsmkv_geom_t &g = ctx->geom;
+    if (rope && (!rope->table || !aligned16(rope->table) || rope->rot_dim % 2 || rope->rot_dim == 0 ||
+                 rope->rot_dim > g.head_dim || rope->interleaved > 1))
+        return LSMKV_EINVAL;
+    if (n_q_heads > 0x10000u || seqs->n_new > 0xFFFFFFFFull) return LSMKV_EINVAL;
+    AppendJob job;
+    std::memset(&job, 0, sizeof(job));
+    job.seqs = seq_args(seqs);
+    job.kv_ptrs = pool->kv_ptrs;
+    job.num_pages = pool->num_pages;
+    job.layer = layer;
+    job.n_layers = g.n_layers;
+    job.page_tokens = g.page_tokens;
+    job.n_kv_heads = g.n_kv_heads;
+    job.head_dim = g.head_dim;
+    job.n_q_heads = n_q_heads;
+    job.k = k->data;
+    job.k_ts = k->token_stride;
+    job.k_hs = k->head_stride;
+    job.v = v->data;
+    job.v_ts = v->token_stride;
+    job.v_hs = v->head_stride;
+    if (n_q_heads) {
+        job.q = q_in->data;
+        job.q_ts = q_in->token_stride;
+        job.q_hs = q_in->head_stride;
+        job.q_out = q_out->data;
+        job.o_ts = q_out->token_stride;
+        job.o_hs = q_out->head_stride;
+    }
+    if (rope) {
+        job.table = rope->table;
+        job.positions = rope->positions;
+        job.n_pos = rope->n_pos;
+        job.rot_dim = rope->rot_dim;
+        job.interleaved = rope->interleaved;
+    }
+    job.q_norm = q_norm;
+    job.k_norm = k_norm;
+    job.eps = eps;
+    job.st = ctx->d_status;
+
+    DeviceGuard guard(ctx->device);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    LaunchTimer timer(ctx, s, LSMKV_K_ATTEND);
+    const uint32_t slots = n_q_heads + 2 * g.n_kv_heads;
+    // Whole 16-byte pieces on both sides of a pair (or no pair that leaves its piece): vector
+    // form. Otherwise element by element.
+    const bool vec = job.rot_dim % (job.interleaved ? 8 : 16) == 0;
+    uint32_t per_pass = 1;       // head slots that a warp takes at once
+    constexpr uint32_t U = 4;
+    if (vec) {
+        const uint32_t lanes = job.interleaved || !job.rot_dim
+                                   ? (g.head_dim / 8 + 1) / 2
+                                   : job.rot_dim / 16 + (g.head_dim - job.rot_dim + 15) / 16;
+        while ((1u << job.lane_log2) < lanes) ++job.lane_log2;
+        per_pass = (32u >> job.lane_log2) * U;
+    }
+    // A warp per token when there are tokens enough to fill the GPU; with fewer, several warps
+    // share a token's heads, down to one pass each.
+    const uint32_t most = (slots + per_pass - 1) / per_pass;
+    const uint64_t fill = (uint64_t)ctx->sm_count * 16;
+    uint64_t parts = (fill + seqs->n_new - 1) / seqs->n_new;
+    job.parts = (uint32_t)(parts < most ? parts : most);
+    const uint64_t warps = seqs->n_new * job.parts;
+    constexpr unsigned kWarps = 4;
+    const uint64_t grid = (warps + kWarps - 1) / kWarps;
+    if (grid > 0x7FFFFFFFull) return LSMKV_EINVAL;
+    const bool bf = dtype == LSMKV_BF16;
+    void (*kern)(AppendJob) = vec ? (bf ? k_append<__nv_bfloat16, U> : k_append<__half, U>)
+                                  : (bf ? k_append_elements<__nv_bfloat16> : k_append_elements<__half>);
+    kern<<<(unsigned)grid, kWarps * 32, 0, s>>>(job);
+    ++ctx->launches;
+    CU(ctx, cudaGetLastError());
+    return LSMKV_OK;
+}
+
+extern "C" int lsmkv_attend_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype,
+                                  const lsmkv_seqs_t *seqs, uint32_t n_q_heads,
+                                  const lsmkv_rows_t *q, const lsmkv_pool_t *pool, float scale,
+                                  const lsmkv_rows_t *out, float *lse_out)
+{
+    return attend(ctx, stream, layer, dtype, seqs, nullptr, n_q_heads, q, pool, scale, out, lse_out);
+}
+
+extern "C" int lsmkv_attend_shared_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer,
+                                         uint32_t dtype, const lsmkv_seqs_t *seqs,
+                                         const lsmkv_groups_t *groups, uint32_t n_q_heads,
+                                         const lsmkv_rows_t *q, const lsmkv_pool_t *pool,
+                                         float scale, const lsmkv_rows_t *out, float *lse_out)
+{
+    if (!groups) return LSMKV_EINVAL;
+    return attend(ctx, stream, layer, dtype, seqs, groups, n_q_heads, q, pool, scale, out, lse_out);
+}

@@ -28,13 +28,15 @@ EXPORTS = (
     "lsmkv_bloom_blocks", "lsmkv_bloom_build", "lsmkv_encode_bound", "lsmkv_last_cuda_line",
     "lsmkv_hindex_buckets", "lsmkv_hindex_build", "lsmkv_xrun_merge", "lsmkv_plan_compaction",
     "lsmkv_relocate_records", "lsmkv_xrun_build", "lsmkv_xprobe_batch",
+    "lsmkv_append_batch", "lsmkv_attend_batch", "lsmkv_attend_shared_batch",
 )
 ST_OVERFLOW = 32
 CODEC_IDENTITY, CODEC_XP12 = 0, 1
 ETOOBIG = -5
 STATIC_MAX_QUERIES, STATIC_MAX_CHUNKS = 4096, 262144
-K_KEYS, K_PACK, K_PROBE, K_PLAN, K_UNPACK, K_CLASSES = 0, 1, 2, 3, 4, 8
-K_NAMES = ("keys", "pack", "probe", "plan", "unpack", "flush", "merge")
+K_KEYS, K_PACK, K_PROBE, K_PLAN, K_UNPACK, K_ATTEND, K_CLASSES = 0, 1, 2, 3, 4, 7, 8
+K_NAMES = ("keys", "pack", "probe", "plan", "unpack", "flush", "merge", "attend")
+BF16, F16 = 0, 1
 
 
 class LsmkvError(RuntimeError):
@@ -95,6 +97,26 @@ class StatusStruct(C.Structure):
 
 class RelocStruct(C.Structure):
     _fields_ = [("old_file", C.c_uint32), ("new_file", C.c_uint32), ("delta", C.c_uint64)]
+
+
+class SeqsStruct(C.Structure):
+    _fields_ = [("n_new", C.c_uint64), ("n_seq", C.c_uint32), ("max_new", C.c_uint32),
+                ("new_off", C.c_void_p), ("kv_len", C.c_void_p), ("page_off", C.c_void_p),
+                ("page_table", C.c_void_p)]
+
+
+class RowsStruct(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_uint64), ("head_stride", C.c_uint64)]
+
+
+class RopeStruct(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("positions", C.c_void_p), ("n_pos", C.c_uint64),
+                ("rot_dim", C.c_uint32), ("interleaved", C.c_uint32)]
+
+
+class GroupsStruct(C.Structure):
+    _fields_ = [("n_group", C.c_uint32), ("reserved", C.c_uint32), ("group_off", C.c_void_p),
+                ("shared_pages", C.c_void_p)]
 
 
 class ProfileStruct(C.Structure):
@@ -181,6 +203,13 @@ def lib() -> C.CDLL:
     L.lsmkv_xprobe_batch.restype = C.c_int
     L.lsmkv_xprobe_batch.argtypes = [vp, vp, u32, vp, vp, vp, u64, C.POINTER(XRunStruct), u32,
                                      vp, vp]
+    f32 = C.c_float
+    L.lsmkv_append_batch.restype = C.c_int
+    L.lsmkv_append_batch.argtypes = [vp, vp, u32, u32, vp, vp, vp, vp, vp, u32, vp, vp, vp, vp, f32]
+    L.lsmkv_attend_batch.restype = C.c_int
+    L.lsmkv_attend_batch.argtypes = [vp, vp, u32, u32, vp, u32, vp, vp, f32, vp, vp]
+    L.lsmkv_attend_shared_batch.restype = C.c_int
+    L.lsmkv_attend_shared_batch.argtypes = [vp, vp, u32, u32, vp, vp, u32, vp, vp, f32, vp, vp]
     L.lsmkv_encode_bound.restype = u64
     L.lsmkv_encode_bound.argtypes = [vp, u64]
     L.lsmkv_bloom_blocks.restype = u64
@@ -471,6 +500,121 @@ def lsmkv_decode_batch_static(geom: Geom, device, stream, n_query, qchunk_off, n
         raise LsmkvError(rc, "lsmkv_decode_batch_static")
 
 
+def _rows(t, head_dim: int):
+    """[n_new, heads, head_dim] tensor, strided or not -> lsmkv_rows_t."""
+    if t.dim() != 3 or t.shape[2] != head_dim or (t.stride(2) != 1 and head_dim != 1):
+        raise ValueError(f"rows must be [tokens, heads, {head_dim}] with contiguous elements, "
+                         f"got {tuple(t.shape)} with strides {t.stride()}")
+    return RowsStruct(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _dtype(*tensors) -> int:
+    """The one 16-bit float type of the given tensors (None among them is skipped)."""
+    import torch
+    kinds = {t.dtype for t in tensors if t is not None}
+    if len(kinds) != 1 or not kinds <= {torch.bfloat16, torch.float16}:
+        raise TypeError(f"bfloat16 or float16 throughout, got {kinds}")
+    return BF16 if torch.bfloat16 in kinds else F16
+
+
+def _tokens(seqs, geom, *named):
+    for name, t, heads in named:
+        if t is not None and (t.shape[0] != seqs.n_new or t.shape[1] != heads):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, the batch {seqs.n_new} new "
+                             f"tokens of {heads} heads")
+
+
+def _check_lse(lse, q):
+    if lse is not None and (str(lse.dtype) != "torch.float32" or not lse.is_contiguous() or
+                            lse.numel() != q.shape[0] * q.shape[1]):
+        raise ValueError("lse: contiguous float32 [n_new, n_q_heads]")
+
+
+class Seqs:
+    """A step's batch (lsmkv_seqs_t): built once, used for every layer. Keeps its tensors alive.
+    new_off int64[n_seq + 1], kv_len int32[n_seq], page_off int64[n_seq + 1], page_table int32."""
+
+    def __init__(self, new_off, kv_len, page_off, page_table, n_new: int, max_new: int):
+        n_seq = kv_len.numel()
+        for name, t, size, n in (("new_off", new_off, 8, n_seq + 1), ("kv_len", kv_len, 4, n_seq),
+                                 ("page_off", page_off, 8, n_seq + 1),
+                                 ("page_table", page_table, 4, None)):
+            if t.element_size() != size or not t.is_contiguous() or (n and t.numel() != n):
+                raise ValueError(f"{name}: contiguous, {size}-byte integers"
+                                 + (f", {n} of them" if n else ""))
+        self.n_new, self.max_new, self.n_seq = int(n_new), int(max_new), n_seq
+        self.keep = (new_off, kv_len, page_off, page_table)
+        self.c = SeqsStruct(self.n_new, n_seq, self.max_new, *[t.data_ptr() for t in self.keep])
+        self.ref = C.addressof(self.c)
+
+
+class Groups:
+    """Sequences that share prefixes (lsmkv_groups_t): group_off int32[n_group + 1],
+    shared_pages int32[n_group]."""
+
+    def __init__(self, group_off, shared_pages):
+        n = shared_pages.numel()
+        if group_off.numel() != n + 1 or group_off.element_size() != 4 or \
+                shared_pages.element_size() != 4 or not group_off.is_contiguous() or \
+                not shared_pages.is_contiguous():
+            raise ValueError("group_off: n_group + 1, shared_pages: n_group contiguous 4-byte "
+                             "integers")
+        self.keep = (group_off, shared_pages)
+        self.c = GroupsStruct(n, 0, group_off.data_ptr(), shared_pages.data_ptr())
+        self.ref = C.addressof(self.c)
+
+
+class Rope:
+    """Position rotation (lsmkv_rope_t): table float32[n_pos, rot_dim], rot_dim/2 cosines then
+    rot_dim/2 sines a row; positions int32[n_new] or None (the tokens' own positions)."""
+
+    def __init__(self, table, interleaved: bool = False, positions=None):
+        import torch
+        if table.dtype != torch.float32 or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError("table: contiguous float32 [n_pos, rot_dim]")
+        if positions is not None and (positions.element_size() != 4 or
+                                      not positions.is_contiguous()):
+            raise ValueError("positions: contiguous 4-byte integers")
+        self.keep = (table, positions)
+        self.n_positions = None if positions is None else positions.numel()
+        self.c = RopeStruct(table.data_ptr(), None if positions is None else positions.data_ptr(),
+                            table.shape[0], table.shape[1], int(interleaved))
+        self.ref = C.addressof(self.c)
+
+
+def lsmkv_append_batch(ctx, stream, layer, dtype, seqs, k, v, pool, rope, n_q_heads, q_in, q_out,
+                       q_norm, k_norm, eps) -> None:
+    """seqs: Seqs; k, v, q_in, q_out: RowsStruct (or None for the queries); rope: Rope or None."""
+    p = _pool(pool)
+    rc = lib().lsmkv_append_batch(
+        ctx, _stream(stream), layer, dtype, seqs.ref, C.addressof(k), C.addressof(v),
+        C.addressof(p) if p is not None else None, rope.ref if rope is not None else None,
+        n_q_heads, C.addressof(q_in) if q_in is not None else None,
+        C.addressof(q_out) if q_out is not None else None, _ptr(q_norm), _ptr(k_norm), eps)
+    _check(ctx, rc, "lsmkv_append_batch")
+
+
+def lsmkv_attend_batch(ctx, stream, layer, dtype, seqs, n_q_heads, q, pool, scale, out,
+                       lse_out=None) -> None:
+    """seqs: Seqs; q, out: RowsStruct."""
+    p = _pool(pool)
+    rc = lib().lsmkv_attend_batch(ctx, _stream(stream), layer, dtype, seqs.ref, n_q_heads,
+                                  C.addressof(q), C.addressof(p) if p is not None else None,
+                                  scale, C.addressof(out), _ptr(lse_out))
+    _check(ctx, rc, "lsmkv_attend_batch")
+
+
+def lsmkv_attend_shared_batch(ctx, stream, layer, dtype, seqs, groups, n_q_heads, q, pool, scale,
+                              out, lse_out=None) -> None:
+    """seqs: Seqs; groups: Groups; q, out: RowsStruct."""
+    p = _pool(pool)
+    rc = lib().lsmkv_attend_shared_batch(ctx, _stream(stream), layer, dtype, seqs.ref, groups.ref,
+                                         n_q_heads, C.addressof(q),
+                                         C.addressof(p) if p is not None else None, scale,
+                                         C.addressof(out), _ptr(lse_out))
+    _check(ctx, rc, "lsmkv_attend_shared_batch")
+
+
 def lsmkv_last_status(ctx, stream=None) -> dict:
     st = StatusStruct()
     _check(ctx, lib().lsmkv_last_status(ctx, _stream(stream), C.byref(st)), "lsmkv_last_status")
@@ -598,6 +742,44 @@ class Context:
 
     def merge_runs(self, runs, keys_out, vals_out, n_out, stream=None):
         lsmkv_merge_runs(self.handle, stream, runs, keys_out, vals_out, n_out)
+
+    def append_batch(self, layer, seqs, k, v, pool, rope=None, q=None, q_out=None, q_norm=None,
+                     k_norm=None, eps=1e-6, stream=None):
+        """k, v [n_new, n_kv_heads, head_dim] into the pool; q [n_new, n_q_heads, head_dim] ->
+        q_out (q itself when None). Strided views are fine."""
+        g = self.geom
+        if q is not None and q_out is None:
+            q_out = q
+        heads = 0 if q is None else q.shape[1]
+        _tokens(seqs, g, ("k", k, g.n_kv_heads), ("v", v, g.n_kv_heads), ("q_out", q_out, heads))
+        if q is not None and q.shape[0] != seqs.n_new:
+            raise ValueError(f"q has {q.shape[0]} rows, the batch {seqs.n_new} new tokens")
+        for w in (q_norm, k_norm):
+            if w is not None and (w.numel() != g.head_dim or not w.is_contiguous()):
+                raise ValueError(f"norm weights: {g.head_dim} contiguous elements")
+        if rope is not None and rope.n_positions not in (None, seqs.n_new):
+            raise ValueError(f"{rope.n_positions} positions for {seqs.n_new} new tokens")
+        lsmkv_append_batch(self.handle, stream, layer, _dtype(k, v, q, q_out, q_norm, k_norm), seqs,
+                           _rows(k, g.head_dim), _rows(v, g.head_dim), pool, rope, heads,
+                           None if q is None else _rows(q, g.head_dim),
+                           None if q is None else _rows(q_out, g.head_dim), q_norm, k_norm, eps)
+
+    def attend_batch(self, layer, seqs, q, out, pool, scale, lse=None, stream=None):
+        """q, out [n_new, n_q_heads, head_dim]; lse float32 [n_new, n_q_heads] or None."""
+        g = self.geom
+        _tokens(seqs, g, ("q", q, q.shape[1]), ("out", out, q.shape[1]))
+        _check_lse(lse, q)
+        lsmkv_attend_batch(self.handle, stream, layer, _dtype(q, out), seqs, q.shape[1],
+                           _rows(q, g.head_dim), pool, scale, _rows(out, g.head_dim), lse)
+
+    def attend_shared_batch(self, layer, seqs, groups, q, out, pool, scale, lse=None, stream=None):
+        """attend_batch for sequences in groups with common pages ahead (Groups)."""
+        g = self.geom
+        _tokens(seqs, g, ("q", q, q.shape[1]), ("out", out, q.shape[1]))
+        _check_lse(lse, q)
+        lsmkv_attend_shared_batch(self.handle, stream, layer, _dtype(q, out), seqs, groups,
+                                  q.shape[1], _rows(q, g.head_dim), pool, scale,
+                                  _rows(out, g.head_dim), lse)
 
     def last_status(self, stream=None) -> dict:
         return lsmkv_last_status(self.handle, stream)
