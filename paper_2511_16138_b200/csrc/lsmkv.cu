@@ -23,6 +23,7 @@
 #include "lsmkv_xrun.cuh"
 #include "lsmkv_append.cuh"
 #include "lsmkv_attend.cuh"
+#include "lsmkv_attend_mma.cuh"
 
 using namespace lsmkv;
 
@@ -249,6 +250,12 @@ cudaError_t set_copy_smem_limit(int max_smem_optin)
     for (auto *few : {k_attend_few<__nv_bfloat16, 256, 4, 3>, k_attend_few<__half, 256, 4, 3>})
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FewShape<256, 4, 3>::kSmem);
+    for (auto *many : {k_attend_many<__nv_bfloat16, 64>, k_attend_many<__half, 64>})
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ManyShape<64>::kSmem);
+    for (auto *many : {k_attend_many<__nv_bfloat16, 128>, k_attend_many<__half, 128>})
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ManyShape<128>::kSmem);
     if (e == cudaSuccess) g_smem_limit_set[dev] = true;
     return e;
 }
@@ -299,6 +306,12 @@ int ensure_dir(lsmkv_ctx *ctx, uint64_t entries)
     if (entries <= ctx->dir_cap && ctx->d_dir) return LSMKV_OK;
     return grow_scratch(ctx, &ctx->d_dir, &ctx->dir_cap, (size_t)entries * sizeof(uint64_t),
                         entries, __LINE__);
+}
+
+// The attend scratch starts with a counter per CTA of its widest launch (two CTAs a SM).
+size_t attend_counter_bytes(const lsmkv_ctx *ctx)
+{
+    return ((size_t)ctx->sm_count * 2 * 4 + 255) & ~size_t(255);
 }
 
 struct SortWs {
@@ -1183,6 +1196,9 @@ int lsmkv_last_status(lsmkv_ctx *ctx, void *stream, lsmkv_status_t *out)
     std::memset(&z, 0, sizeof(z));
     z.first_bad = ~0ull;
     CU(ctx, cudaMemcpyAsync(ctx->d_status, &z, sizeof(z), cudaMemcpyHostToDevice, s));
+    // an attend that gave up may have left its counters between two calls' values
+    if ((out->flags & LSMKV_ST_WAIT_EXPIRED) && ctx->d_attend)
+        CU(ctx, cudaMemsetAsync(ctx->d_attend, 0, attend_counter_bytes(ctx), s));
     CU(ctx, cudaStreamSynchronize(s));
     return LSMKV_OK;
 }

@@ -46,6 +46,8 @@ struct AttendJob {
     float *pre_lse;              // f32 [n_new][n_q_heads], base 2
     float *parts;                // two slots per CTA
     unsigned int *arrived;       // one counter per CTA, zero between calls
+    long long wait_cycles;
+    uint64_t test_drop;          // test hook: ~0 = off
     DevStatus *st;
 };
 
@@ -213,18 +215,16 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
 // The first item behind i that has units (there is one when the span is not done), looked for by
 // the lanes of every warp together: a launch may pass over many items that are not its own.
 __device__ __forceinline__ uint32_t next_item(const AttendJob &j, uint32_t i, uint32_t n, uint32_t M,
-                                              uint32_t tile, Item *it, uint64_t *per_head)
+                                              Item *it)
 {
     const uint32_t lane = threadIdx.x & 31;
     for (uint32_t base = i + 1; base < n; base += 32) {
-        uint64_t u = 0;
-        if (base + lane < n) u = item_units(j, load_item(j, base + lane), M, tile);
-        const unsigned some = __ballot_sync(~0u, u != 0);
+        const unsigned some =
+            __ballot_sync(~0u, base + lane < n && item_tiles(j, load_item(j, base + lane), M) != 0);
         if (some) {
-            const int k = __ffs(some) - 1;
-            *per_head = __shfl_sync(~0u, u, k);
-            *it = load_item(j, base + k);
-            return base + k;
+            const uint32_t k = base + __ffs(some) - 1;
+            *it = load_item(j, k);
+            return k;
         }
     }
     return i;
@@ -238,39 +238,63 @@ struct Cut {
     uint32_t k0, k1;             // key tiles [k0, k1) of it are this CTA's
 };
 
-// The tile that holds unit u of an item whose first unit is `before`.
-__device__ __forceinline__ Cut find_cut(const AttendJob &j, const Item &it, uint64_t per_head,
-                                            uint64_t before, uint64_t u, uint64_t end, uint32_t M,
-                                            uint32_t tile)
-{
+// Walks the cuts of a span. All threads of a warp go through it together.
+template <int M, int TILE>
+struct Walk {
+    uint64_t u;                  // next unit
+    uint32_t i, tiles;           // item, its row tiles
+    Item it;
     Cut p;
-    const uint64_t rel = u - before;
-    p.kv_head = (uint32_t)(rel / per_head);
-    uint64_t at = rel - (uint64_t)p.kv_head * per_head;
-    uint64_t base = before + (uint64_t)p.kv_head * per_head;
-    p.rt = 0;
-    if (!it.causal) {
-        p.units = tile_units(it, 0, M, j.group, tile);
-        p.rt = (uint32_t)(at / p.units);
-        base += (uint64_t)p.rt * p.units;
-        at -= (uint64_t)p.rt * p.units;
-    } else {
+    bool begun;
+
+    __device__ __forceinline__ void start(const AttendJob &j, const Span &s)
+    {
+        u = s.begin;
+        i = s.item;
+        it = load_item(j, i);
+        tiles = item_tiles(j, it, M);
+        begun = false;
+        if (s.begin >= s.end) return;
+        // the tile that holds unit s.begin
+        const uint64_t per_head = item_units(j, it, M, TILE);
+        const uint64_t rel = u - s.before;
+        p.kv_head = (uint32_t)(rel / per_head);
+        uint64_t at = rel - (uint64_t)p.kv_head * per_head;
+        p.tile0 = s.before + (uint64_t)p.kv_head * per_head;
+        p.rt = 0;
         while (true) {
-            p.units = tile_units(it, p.rt, M, j.group, tile);
-            if (at < p.units) break;
+            p.units = tile_units(it, p.rt, M, j.group, TILE);
+            if (at < p.units || p.rt + 1 >= tiles) break;
             at -= p.units;
-            base += p.units;
+            p.tile0 += p.units;
             ++p.rt;
         }
     }
-    p.tile0 = base;
-    p.k0 = (uint32_t)at;
-    const uint64_t left = base + p.units < end ? base + p.units : end;
-    p.k1 = (uint32_t)(left - base);
-    const uint64_t rows = (uint64_t)it.tokens * j.group - (uint64_t)p.rt * M;
-    p.rows = rows < M ? (uint32_t)rows : M;
-    return p;
-}
+    __device__ __forceinline__ bool next(const AttendJob &j, const Span &s)
+    {
+        if (u >= s.end) return false;
+        if (begun) {
+            p.tile0 = u;
+            if (++p.rt == tiles) {
+                p.rt = 0;
+                if (++p.kv_head == j.n_kv_heads) {
+                    p.kv_head = 0;
+                    i = next_item(j, i, j.prefix_pass ? j.n_group : j.seqs.n_seq, M, &it);
+                    tiles = item_tiles(j, it, M);
+                }
+            }
+            p.units = tile_units(it, p.rt, M, j.group, TILE);
+        }
+        begun = true;
+        p.k0 = (uint32_t)(u - p.tile0);
+        const uint64_t end = p.tile0 + p.units < s.end ? p.tile0 + p.units : s.end;
+        p.k1 = (uint32_t)(end - p.tile0);
+        u = end;
+        const uint64_t rows = (uint64_t)it.tokens * j.group - (uint64_t)p.rt * M;
+        p.rows = rows < M ? (uint32_t)rows : M;
+        return true;
+    }
+};
 
 // ---- partial results: per slot, M rows of sums, then M maxima and M sums of weights ----------
 
@@ -289,16 +313,21 @@ __device__ __forceinline__ float part_weight(float m, float top)
 // an infinite or undefined value there makes the sum undefined although the row must not see
 // it. A row that comes out undefined and has such keys beside it is taken again here, key by key
 // over its own keys alone; finite inputs never come here.
+struct Quad {
+    float4 acc;
+    float m, l;
+};
+
 template <typename T>
-__device__ __noinline__ void redo_row4(const AttendJob &j, const Item &it, uint64_t row, uint32_t head,
-                                       uint32_t limit, uint32_t d, float4 *acc, float *m_out, float *l_out)
+__device__ __noinline__ Quad redo_row4(const AttendJob &j, uint64_t page0, uint64_t row, uint32_t head,
+                                       uint32_t first, uint32_t limit, uint32_t d)
 {
     const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
     const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
     const T *const q = static_cast<const T *>(j.q) + row * j.q_ts + (uint64_t)head * j.q_hs;
     float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t k = it.kv0; k < limit; ++k) {
-        const uint32_t page = j.seqs.page_table[it.page0 + k / j.page_tokens];
+    for (uint32_t k = first; k < limit; ++k) {
+        const uint32_t page = j.seqs.page_table[page0 + k / j.page_tokens];
         const bool real = page < j.num_pages;
         const uint64_t at = (((uint64_t)(real ? page : 0) * j.page_tokens + k % j.page_tokens) *
                                  j.n_kv_heads + head / j.group) * j.head_dim;
@@ -308,12 +337,15 @@ __device__ __noinline__ void redo_row4(const AttendJob &j, const Item &it, uint6
         const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
         const float c = exp2f(m - base), w = exp2f(s - base);
         l = l * c + w;
+#pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = o[e] * c + (real ? w * Half2<T>::up1(vbuf[at + d + e]) : 0.f);
         m = top;
     }
-    *acc = make_float4(o[0], o[1], o[2], o[3]);
-    *m_out = m;
-    *l_out = l;
+    Quad r;
+    r.acc = make_float4(o[0], o[1], o[2], o[3]);
+    r.m = m;
+    r.l = l;
+    return r;
 }
 
 // Write four elements of finished row R of the item: acc = sum of weighted values relative to 2^m, l the sum
@@ -325,8 +357,12 @@ __device__ __forceinline__ void finish_row4(const AttendJob &j, const Item &it, 
     const uint64_t row = it.row0 + R / j.group;
     const uint32_t head = p.kv_head * j.group + R % j.group;
     const uint64_t flat = row * j.n_q_heads + head;
-    if (it.causal && it.tokens > 1 && isnan(acc.x + acc.y + acc.z + acc.w))
-        redo_row4<T>(j, it, row, head, token_limit(it, R / j.group), d, &acc, &m, &l);
+    if (it.causal && it.tokens > 1 && isnan(acc.x + acc.y + acc.z + acc.w)) {
+        const Quad again = redo_row4<T>(j, it.page0, row, head, it.kv0, token_limit(it, R / j.group), d);
+        acc = again.acc;
+        m = again.m;
+        l = again.l;
+    }
     if (it.skip) {
         const float pm = j.pre_lse[flat];
         const float4 po = *reinterpret_cast<const float4 *>(j.pre_o + flat * j.head_dim + d);
@@ -368,7 +404,9 @@ __device__ void merge_parts(const AttendJob &j, const Item &it, const Cut &p, ui
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (uint32_t c = c0; c <= c1; ++c) {
             const float *s = part_slot(j, 2ull * c + (c == c0 ? 1 : 0), M, DP);
-            const float pm = __ldcg(s + (uint64_t)M * DP + r), pl = __ldcg(s + (uint64_t)M * (DP + 1) + r);
+            const float pm = __ldcg(s + (uint64_t)M * DP + r);
+            if (pm == -INFINITY) continue;    // no key of this part was the row's: nothing to add
+            const float pl = __ldcg(s + (uint64_t)M * (DP + 1) + r);
             const float4 o = __ldcg(reinterpret_cast<const float4 *>(s + (uint64_t)r * DP + d));
             const float top = fmaxf(m, pm);
             const float a = part_weight(m, top), b = part_weight(pm, top);
@@ -458,7 +496,7 @@ struct FewShape {
 };
 
 template <typename T, int DP, int NW, int ST>
-__global__ __launch_bounds__(NW * 32) void k_attend_few(const AttendJob j)
+__global__ __launch_bounds__(NW * 32) void k_attend_few(const __grid_constant__ AttendJob j)
 {
     using Sh = FewShape<DP, NW, ST>;
     constexpr int NT = Sh::kThreads;
@@ -483,16 +521,11 @@ __global__ __launch_bounds__(NW * 32) void k_attend_few(const AttendJob j)
     const uint32_t ring = q_s + (uint32_t)Sh::kQBytes + w * (ST * Sh::kStage);
     const uint64_t tok_stride = (uint64_t)j.n_kv_heads * D;
 
-    uint64_t u = span.begin, before = span.before;
-    uint32_t i = span.item;
-    Item it = load_item(j, i);
-    uint64_t per_head = item_units(j, it, Sh::kM, kTile);
-    while (u < span.end) {
-        if (u >= before + per_head * j.n_kv_heads) {
-            before += per_head * j.n_kv_heads;
-            i = next_item(j, i, n_items, Sh::kM, kTile, &it, &per_head);
-        }
-        const Cut p = find_cut(j, it, per_head, before, u, span.end, Sh::kM, kTile);
+    Walk<Sh::kM, (int)kTile> walk;
+    walk.start(j, span);
+    const Item &it = walk.it;
+    const Cut &p = walk.p;
+    while (walk.next(j, span)) {
         const uint32_t row_base = p.rt * Sh::kM;
 
         // the tile's queries, swizzled like the keys; rows beyond the tile are zero
@@ -710,7 +743,6 @@ __global__ __launch_bounds__(NW * 32) void k_attend_few(const AttendJob j)
         }
         if (!whole && deliver_part(j, p, span.per)) merge_parts<T, NT>(j, it, p, span.per, Sh::kM, DP);
         __syncthreads();
-        u += p.k1 - p.k0;
     }
 }
 

@@ -51,12 +51,43 @@ int launch_few(lsmkv_ctx *ctx, cudaStream_t s, const AttendJob &job)
     return LSMKV_OK;
 }
 
+template <typename T>
+int launch_many(lsmkv_ctx *ctx, cudaStream_t s, const AttendJob &job)
+{
+    const unsigned sm = (unsigned)ctx->sm_count;
+    if (job.head_dim <= 64)
+        k_attend_many<T, 64><<<sm, ManyShape<64>::kThreads, ManyShape<64>::kSmem, s>>>(job);
+    else
+        k_attend_many<T, 128><<<sm, ManyShape<128>::kThreads, ManyShape<128>::kSmem, s>>>(job);
+    ++ctx->launches;
+    CU(ctx, cudaGetLastError());
+    return LSMKV_OK;
+}
+
+// One pass over the sequences (or groups): those of few rows and those of many, each by its
+// kernel. most: no item has more rows (query heads of one KV head times new tokens).
+template <typename T>
+int launch_pass(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job, uint64_t most)
+{
+    // Up to 16 rows fill one fragment of the few-row kernel; beyond, it would read the keys once
+    // for every 16 rows, where the many-row kernel reads them once for 256.
+    const bool mma = job.head_dim <= 128;
+    job.rows_lo = 0;
+    job.rows_hi = mma ? 16 : 0xFFFFFFFFu;
+    int rc = launch_few<T>(ctx, s, job);
+    if (rc != LSMKV_OK || !mma || most <= 16) return rc;
+    job.rows_lo = 16;
+    job.rows_hi = 0xFFFFFFFFu;
+    return launch_many<T>(ctx, s, job);
+}
+
 // Scratch of the attend kernels: counters, then two part slots per CTA of the widest launch.
 int ensure_attend(lsmkv_ctx *ctx, cudaStream_t s)
 {
-    const size_t counters = ((size_t)ctx->sm_count * 2 * 4 + 255) & ~size_t(255);
+    const size_t counters = attend_counter_bytes(ctx);
     const uint32_t dp = ctx->geom.head_dim <= 64 ? 64 : ctx->geom.head_dim <= 128 ? 128 : 256;
-    const size_t bytes = counters + (size_t)ctx->sm_count * 2 * 2 * 16 * (dp + 2) * 4;
+    const size_t few = (size_t)ctx->sm_count * 2 * 2 * 16, many = dp > 128 ? 0 : (size_t)ctx->sm_count * 2 * 256;
+    const size_t bytes = counters + std::max(few, many) * (dp + 2) * 4;
     if (ctx->d_attend && bytes <= ctx->attend_cap) return LSMKV_OK;
     const int rc = grow_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, bytes, bytes, __LINE__);
     if (rc != LSMKV_OK) return rc;
@@ -108,8 +139,9 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
     job.lse = lse_out;
     job.scale_log2 = scale * kLog2e;
     job.arrived = static_cast<unsigned int *>(ctx->d_attend);
-    job.parts = reinterpret_cast<float *>(static_cast<char *>(ctx->d_attend) +
-                                          (((size_t)ctx->sm_count * 2 * 4 + 255) & ~size_t(255)));
+    job.parts = reinterpret_cast<float *>(static_cast<char *>(ctx->d_attend) + attend_counter_bytes(ctx));
+    job.wait_cycles = ctx->wait_cycles;
+    job.test_drop = ctx->test_drop_piece < 0 ? ~0ull : (uint64_t)ctx->test_drop_piece;
     job.st = ctx->d_status;
     if (shared) {
         const uint64_t heads = seqs->n_new * n_q_heads;
@@ -126,17 +158,17 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
         job.shared_pages = groups->shared_pages;
     }
     LaunchTimer timer(ctx, s, LSMKV_K_ATTEND);
-    auto few = dtype == LSMKV_BF16 ? launch_few<__nv_bfloat16> : launch_few<__half>;
+    auto pass = dtype == LSMKV_BF16 ? launch_pass<__nv_bfloat16> : launch_pass<__half>;
     if (shared) {
         k_shared_skip<<<(groups->n_group + 127) / 128, 128, 0, s>>>(job);
         ++ctx->launches;
         CU(ctx, cudaGetLastError());
         job.prefix_pass = 1;
-        rc = few(ctx, s, job);
+        rc = pass(ctx, s, job, seqs->n_new * job.group);
         if (rc != LSMKV_OK) return rc;
         job.prefix_pass = 0;
     }
-    return few(ctx, s, job);
+    return pass(ctx, s, job, (uint64_t)seqs->max_new * job.group);
 }
 
 }  // namespace

@@ -108,6 +108,8 @@ CASES = [
     (torch.bfloat16, 64, 16, 64, 4, [33, 1], [9, 5]),
     (torch.bfloat16, 128, 16, 4, 1, [1], [40000]),                   # one row tile, many parts
     (torch.float16, 128, 16, 8, 1, [40], [20000]),
+    # every CTA goes through many items, of either kernel
+    (torch.bfloat16, 128, 16, 8, 2, [1, 33, 70, 2, 150, 0, 4, 5] * 40, [300, 0, 90, 1000, 40, 7, 16, 31] * 40),
 ]
 
 
@@ -384,3 +386,24 @@ def test_members_that_do_not_reach_behind_the_common_pages_go_by_themselves():
         ctx.attend_shared_batch(0, seqs, lsmkv.Groups(t([0, 8, 7]), t([4, 3])), q, out, pt, 0.1)
         st = ctx.last_status()
         assert st["flags"] == lsmkv.ST_BAD_COUNT and st["first_bad"] == 0
+
+
+def test_a_wait_that_runs_out_is_reported_and_the_context_stays_usable():
+    """The many-row kernel with one of its tiles never handed over (the library's test hook) and
+    the limit at about a millisecond: every role leaves, the call reports it, and the next call
+    of the same context is right."""
+    case = (torch.bfloat16, 128, 16, 8, 2, [70, 300], [900, 2000])
+    geom, pool, q, seqs, new_off, kv, page_off, table = setup(case, n_layers=1)
+    out = torch.zeros_like(q)
+    with lsmkv.Context(geom, 0) as ctx:
+        pt = lsmkv.pool_table(list(pool))
+        ctx.set_tuning("wait_cycles", 2_000_000)
+        ctx.set_tuning("test_drop_piece", 3)
+        ctx.attend_batch(0, seqs, q, out, pt, 0.08)
+        assert ctx.last_status()["flags"] == lsmkv.ST_WAIT_EXPIRED
+        ctx.set_tuning("test_drop_piece", -1)
+        ctx.set_tuning("wait_cycles", 2_000_000_000)
+        ctx.attend_batch(0, seqs, q, out, pt, 0.08)
+        assert ctx.last_status()["flags"] == 0
+        assert ctx.last_cuda_error() == 0
+    check(out, None, reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, 0.08), torch.bfloat16)
