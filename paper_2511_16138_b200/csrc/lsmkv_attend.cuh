@@ -13,8 +13,9 @@
 // number of key tiles that its last row sees. All tiles in a row -- sequence, KV head, row tile,
 // key tile -- form one line of units that is cut into equal spans, one per CTA: no CTA has more
 // than one unit more than another, whatever the lengths. A row tile cut by a span's end leaves
-// parts in scratch; the CTA that delivers the last part merges them, in order, so that results
-// do not depend on who was last. Every CTA finds its span by itself, from the lengths: no launch
+// parts in scratch, merged in order by whoever comes after (the CTA that delivers the last part
+// in the few-row kernel, a launch of its own behind the many-row kernel, the own pass for a
+// shared prefix), so that results do not depend on timing. Every CTA finds its span by itself, from the lengths: no launch
 // before, and nothing for the host to know.
 #pragma once
 #include "lsmkv_append.cuh"
@@ -36,19 +37,31 @@ struct AttendJob {
     uint64_t q_ts, q_hs, o_ts, o_hs;
     float *lse;
     float scale_log2;
-    // shared prefixes. prefix_pass: the items are the groups, results go to pre_o / pre_lse;
-    // otherwise, with pre_o set, sequence i starts behind its skip[i] shared tokens and merges
-    // the group's result into its own
+    // Shared prefixes. prefix_pass: the items are the groups; the result of a row tile goes to
+    // pre_o / pre_lse, or stays in pre_parts when the tile is cut; share[] is filled. Otherwise,
+    // with share set, sequence i starts behind its share[i].skip tokens and merges what the
+    // prefix pass left for it into its own result.
     uint32_t prefix_pass, n_group;
     const uint32_t *group_off, *shared_pages;
-    uint32_t *skip;
+    struct Share *share;
     float *pre_o;                // f32 [n_new][n_q_heads][head_dim]
     float *pre_lse;              // f32 [n_new][n_q_heads], base 2
+    float *pre_parts;            // as parts
+    uint32_t pre_rows, dp;       // rows of the prefix pass's tiles; elements of a part's row
     float *parts;                // two slots per CTA
-    unsigned int *arrived;       // one counter per CTA, zero between calls
+    unsigned int *arrived;       // few rows: one counter per CTA, zero between calls
+    struct CutDesc *cuts;        // many rows: the cut tile that starts in a CTA's span
     long long wait_cycles;
     uint64_t test_drop;          // test hook: ~0 = off
     DevStatus *st;
+};
+
+// What the prefix pass has for a sequence: the tokens it covers, and where its group's row tiles
+// lie on that pass's line of units.
+struct __align__(16) Share {
+    uint32_t skip, units, tiles, unused;   // units of a tile; tiles of a KV head
+    uint64_t base, row0;                   // first unit and first row of the group
+    uint64_t per, unused2;
 };
 
 // An item: a sequence, or in the prefix pass a group.
@@ -56,9 +69,10 @@ struct Item {
     uint64_t row0, page0;
     uint32_t tokens;             // new tokens
     uint32_t kv0, kv1;           // keys [kv0, kv1)
-    uint32_t skip;               // tokens covered by the prefix pass (own pass)
     bool causal;
     bool ok;
+    uint32_t index;              // its number
+    uint32_t skip;               // own pass: tokens whose result the prefix pass has, in share[index]
 };
 
 __device__ __forceinline__ uint32_t shared_tokens(const AttendJob &j, uint32_t g)
@@ -74,6 +88,7 @@ __device__ __forceinline__ uint32_t shared_tokens(const AttendJob &j, uint32_t g
 __device__ __forceinline__ Item load_item(const AttendJob &j, uint32_t i)
 {
     Item it;
+    it.index = i;
     if (j.prefix_pass) {
         const uint32_t a = j.group_off[i], b = j.group_off[i + 1];
         it.kv0 = 0;
@@ -101,10 +116,10 @@ __device__ __forceinline__ Item load_item(const AttendJob &j, uint32_t i)
     it.kv1 = s.kv;
     it.causal = true;
     it.skip = 0;
-    if (j.pre_o && s.ok) {
+    if (j.share && s.ok) {
         // a member with a new token inside the shared part goes by itself
-        const uint32_t k = j.skip[i];
-        if (k && s.kv >= s.rows && k <= s.kv - s.rows) it.skip = it.kv0 = k;
+        const uint32_t k = j.share[i].skip;
+        if (s.kv >= s.rows && k <= s.kv - s.rows) it.skip = it.kv0 = k;
     }
     return it;
 }
@@ -145,6 +160,27 @@ __device__ __forceinline__ uint64_t item_units(const AttendJob &j, const Item &i
     uint64_t u = 0;
     for (uint32_t rt = 0; rt < n; ++rt) u += tile_units(it, rt, M, j.group, tile);
     return u;
+}
+
+// Group i's place on the prefix pass's line of units, for its members.
+__device__ __forceinline__ void share_group(const AttendJob &j, uint32_t i, const Item &it, uint64_t base,
+                                            uint64_t per_head, uint64_t per, uint32_t M)
+{
+    const uint32_t a = j.group_off[i], b = j.group_off[i + 1];
+    if (a > b || b > j.seqs.n_seq) {
+        st_flag(j.st, LSMKV_ST_BAD_COUNT, i);
+        return;
+    }
+    Share sh;
+    sh.tiles = item_tiles(j, it, M);
+    sh.skip = sh.tiles ? it.kv1 : 0;
+    sh.units = sh.tiles ? (uint32_t)(per_head / sh.tiles) : 1;
+    sh.base = base;
+    sh.row0 = it.row0;
+    sh.per = per;
+    sh.unused = 0;
+    sh.unused2 = 0;
+    for (uint32_t k = a; k < b; ++k) j.share[k] = sh;
 }
 
 // A CTA's place on the line of units.
@@ -193,6 +229,19 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
     if (s.end > total) s.end = total;
     if (s.begin > total) s.begin = total;
     uint64_t at = ahead + incl - mine;
+    if (j.prefix_pass) {
+        // the groups' places, for the own pass: a CTA writes every gridDim-th group's members
+        uint64_t base = at;
+        for (uint32_t i = i0; i < i1; ++i) {
+            const Item it = load_item(j, i);
+            const uint64_t u = item_units(j, it, M, tile);
+            if (i % gridDim.x == blockIdx.x) share_group(j, i, it, base, u, s.per, M);
+            base += u * j.n_kv_heads;
+        }
+        if (tid == 0 && blockIdx.x == 0 &&
+            (j.group_off[0] != 0 || j.group_off[j.n_group] != j.seqs.n_seq))
+            st_flag(j.st, LSMKV_ST_BAD_COUNT, j.n_group);
+    }
     if (s.begin < s.end && at <= s.begin && s.begin < at + mine) {
         uint32_t i = i0;
         if (each > 1 && at + first <= s.begin) {
@@ -300,13 +349,44 @@ struct Walk {
 
 __device__ __forceinline__ float *part_slot(const AttendJob &j, uint64_t slot, uint32_t M, uint32_t DP)
 {
-    return j.parts + slot * ((uint64_t)M * (DP + 2));
+    return (j.prefix_pass ? j.pre_parts : j.parts) + slot * ((uint64_t)M * (DP + 2));
 }
 
 // 2^(x) with 2^(-inf) = 0; statistics of an empty part are m = -inf, l = 0.
 __device__ __forceinline__ float part_weight(float m, float top)
 {
     return m == -INFINITY ? 0.f : exp2f(m - top);
+}
+
+// Add parts c0..c1 of a cut tile, four elements of one row, to (acc, m, l); four parts in flight.
+__device__ __forceinline__ void add_parts(const float *parts, uint32_t c0, uint32_t c1, uint32_t M,
+                                          uint32_t DP, uint32_t r, uint32_t d, float4 &acc, float &m, float &l)
+{
+    constexpr int U = 4;
+    for (uint32_t c = c0; c <= c1; c += U) {
+        float pm[U], pl[U];
+        float4 o[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t x = c + u <= c1 ? c + u : c1;
+            const float *s = parts + (2ull * x + (x == c0 ? 1 : 0)) * ((uint64_t)M * (DP + 2));
+            pm[u] = __ldcg(s + (uint64_t)M * DP + r);
+            pl[u] = __ldcg(s + (uint64_t)M * (DP + 1) + r);
+            o[u] = __ldcg(reinterpret_cast<const float4 *>(s + (uint64_t)r * DP + d));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (c + u > c1 || pm[u] == -INFINITY) continue;   // no key of this part was the row's
+            const float top = fmaxf(m, pm[u]);
+            const float a = part_weight(m, top), b = part_weight(pm[u], top);
+            acc.x = acc.x * a + o[u].x * b;
+            acc.y = acc.y * a + o[u].y * b;
+            acc.z = acc.z * a + o[u].z * b;
+            acc.w = acc.w * a + o[u].w * b;
+            l = l * a + pl[u] * b;
+            m = top;
+        }
+    }
 }
 
 // A row tile's products also run over keys that only later rows of it see, with weight zero:
@@ -348,14 +428,14 @@ __device__ __noinline__ Quad redo_row4(const AttendJob &j, uint64_t page0, uint6
     return r;
 }
 
-// Write four elements of finished row R of the item: acc = sum of weighted values relative to 2^m, l the sum
-// of weights. Merges the prefix pass's result first when there is one.
+// Write four elements of finished row R of the item: acc = sum of weighted values relative to
+// 2^m, l the sum of weights. Merges the prefix pass's result first when there is one.
 template <typename T>
-__device__ __forceinline__ void finish_row4(const AttendJob &j, const Item &it, const Cut &p, uint32_t R,
+__device__ __forceinline__ void finish_row4(const AttendJob &j, const Item &it, uint32_t kv_head, uint32_t R,
                                             uint32_t d, float4 acc, float m, float l)
 {
     const uint64_t row = it.row0 + R / j.group;
-    const uint32_t head = p.kv_head * j.group + R % j.group;
+    const uint32_t sub = R % j.group, head = kv_head * j.group + sub;
     const uint64_t flat = row * j.n_q_heads + head;
     if (it.causal && it.tokens > 1 && isnan(acc.x + acc.y + acc.z + acc.w)) {
         const Quad again = redo_row4<T>(j, it.page0, row, head, it.kv0, token_limit(it, R / j.group), d);
@@ -364,16 +444,25 @@ __device__ __forceinline__ void finish_row4(const AttendJob &j, const Item &it, 
         l = again.l;
     }
     if (it.skip) {
-        const float pm = j.pre_lse[flat];
-        const float4 po = *reinterpret_cast<const float4 *>(j.pre_o + flat * j.head_dim + d);
-        const float top = fmaxf(m, pm);
-        const float a = part_weight(m, top), b = part_weight(pm, top);
-        acc.x = acc.x * a + po.x * b;
-        acc.y = acc.y * a + po.y * b;
-        acc.z = acc.z * a + po.z * b;
-        acc.w = acc.w * a + po.w * b;
-        l = l * a + b;
-        m = top;
+        // its row tile of the prefix pass: whole, or in parts
+        const Share &sh = j.share[it.index];
+        const uint32_t P = (uint32_t)(row - sh.row0) * j.group + sub, rt = P / j.pre_rows;
+        const uint64_t u0 = sh.base + (uint64_t)(kv_head * sh.tiles + rt) * sh.units;
+        const uint32_t c0 = (uint32_t)(u0 / sh.per), c1 = (uint32_t)((u0 + sh.units - 1) / sh.per);
+        if (c0 != c1) {
+            add_parts(j.pre_parts, c0, c1, j.pre_rows, j.dp, P - rt * j.pre_rows, d, acc, m, l);
+        } else {
+            const float pm = j.pre_lse[flat];
+            const float4 po = *reinterpret_cast<const float4 *>(j.pre_o + flat * j.head_dim + d);
+            const float top = fmaxf(m, pm);
+            const float a = part_weight(m, top), b = part_weight(pm, top);
+            acc.x = acc.x * a + po.x * b;
+            acc.y = acc.y * a + po.y * b;
+            acc.z = acc.z * a + po.z * b;
+            acc.w = acc.w * a + po.w * b;
+            l = l * a + b;
+            m = top;
+        }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
@@ -391,33 +480,27 @@ __device__ __forceinline__ void finish_row4(const AttendJob &j, const Item &it, 
     if (d == 0 && j.lse) j.lse[flat] = lse2 * kLn2;
 }
 
-// Merge the parts of a cut tile. Called by all threads of the CTA that delivered the last one.
+// The same out of line, where the call site is unrolled.
+template <typename T>
+__device__ __noinline__ void finish_row4_call(const AttendJob &j, const Item &it, uint32_t kv_head, uint32_t R,
+                                              uint32_t d, float4 acc, float m, float l)
+{
+    finish_row4<T>(j, it, kv_head, R, d, acc, m, l);
+}
+
+// Merge rows [r0, r1) of a cut tile, by NT threads.
 template <typename T, int NT>
-__device__ void merge_parts(const AttendJob &j, const Item &it, const Cut &p, uint64_t per, uint32_t M,
-                            uint32_t DP)
+__device__ __forceinline__ void merge_parts(const AttendJob &j, const Item &it, const Cut &p, uint64_t per,
+                                            uint32_t M, uint32_t r0, uint32_t r1)
 {
     const uint32_t c0 = (uint32_t)(p.tile0 / per), c1 = (uint32_t)((p.tile0 + p.units - 1) / per);
     const uint32_t quads = j.head_dim / 4;
-    for (uint32_t x = threadIdx.x; x < p.rows * quads; x += NT) {
-        const uint32_t r = x / quads, d = (x - r * quads) * 4;
+    for (uint32_t x = threadIdx.x; x < (r1 - r0) * quads; x += NT) {
+        const uint32_t r = r0 + x / quads, d = x % quads * 4;
         float m = -INFINITY, l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (uint32_t c = c0; c <= c1; ++c) {
-            const float *s = part_slot(j, 2ull * c + (c == c0 ? 1 : 0), M, DP);
-            const float pm = __ldcg(s + (uint64_t)M * DP + r);
-            if (pm == -INFINITY) continue;    // no key of this part was the row's: nothing to add
-            const float pl = __ldcg(s + (uint64_t)M * (DP + 1) + r);
-            const float4 o = __ldcg(reinterpret_cast<const float4 *>(s + (uint64_t)r * DP + d));
-            const float top = fmaxf(m, pm);
-            const float a = part_weight(m, top), b = part_weight(pm, top);
-            acc.x = acc.x * a + o.x * b;
-            acc.y = acc.y * a + o.y * b;
-            acc.z = acc.z * a + o.z * b;
-            acc.w = acc.w * a + o.w * b;
-            l = l * a + pl * b;
-            m = top;
-        }
-        finish_row4<T>(j, it, p, p.rt * M + r, d, acc, m, l);
+        add_parts(j.parts, c0, c1, M, j.dp, r, d, acc, m, l);
+        finish_row4<T>(j, it, p.kv_head, p.rt * M + r, d, acc, m, l);
     }
 }
 
@@ -732,7 +815,7 @@ __global__ __launch_bounds__(NW * 32) void k_attend_few(const __grid_constant__ 
                 sum += f * sm_l[k][r];
             }
             if (whole) {
-                finish_row4<T>(j, it, p, row_base + r, d, acc, top, sum);
+                finish_row4<T>(j, it, p.kv_head, row_base + r, d, acc, top, sum);
             } else {
                 __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)r * DP + d), acc);
                 if (d == 0) {
@@ -741,25 +824,11 @@ __global__ __launch_bounds__(NW * 32) void k_attend_few(const __grid_constant__ 
                 }
             }
         }
-        if (!whole && deliver_part(j, p, span.per)) merge_parts<T, NT>(j, it, p, span.per, Sh::kM, DP);
+        // in the prefix pass the own pass takes the parts from where they are
+        if (!whole && !j.prefix_pass && deliver_part(j, p, span.per))
+            merge_parts<T, NT>(j, it, p, span.per, Sh::kM, 0, p.rows);
         __syncthreads();
     }
-}
-
-// The prefix pass's companion: how many tokens of every sequence the pass covers.
-__global__ void k_shared_skip(const AttendJob j)
-{
-    const uint32_t i = blockIdx.x * blockDim.x + threadIdx.x;
-    if (i == 0 && (j.group_off[0] != 0 || j.group_off[j.n_group] != j.seqs.n_seq))
-        st_flag(j.st, LSMKV_ST_BAD_COUNT, j.n_group);
-    if (i >= j.n_group) return;
-    const uint32_t a = j.group_off[i], b = j.group_off[i + 1];
-    if (a > b || b > j.seqs.n_seq) {
-        st_flag(j.st, LSMKV_ST_BAD_COUNT, i);
-        return;
-    }
-    const uint32_t k = shared_tokens(j, i);
-    for (uint32_t s = a; s < b; ++s) j.skip[s] = k;
 }
 
 }  // namespace lsmkv

@@ -27,12 +27,14 @@ template <int DP>
 struct ManyShape {
     static constexpr int kM = 256, kKeys = 128;
     static constexpr int kStages = DP == 128 ? 5 : 8;
-    static constexpr int kLag = 3;             // copy groups in flight per loader thread
     static constexpr uint32_t kTileBytes = 128 * DP * 2;
     static constexpr int kLoaders = 2;         // warps
-    static constexpr int kThreads = (8 + kLoaders + 1) * 32;   // 11 warps: 168 registers each
+    // 8 softmax warps, then a warpgroup of loaders, issuer and an idle warp. 384 threads start with
+    // 168 registers each (64512); 256 x 208 + 128 x 80 = 63488 of them are in use afterwards.
+    static constexpr int kThreads = 12 * 32;
+    static constexpr int kSoftmaxRegs = 208, kOtherRegs = 80;
     static constexpr size_t kSmem = 1024 + (size_t)(2 + kStages) * kTileBytes;
-    static_assert(kLag <= kStages - 2, "a stage must be handed over before the ring blocks on it");
+    static_assert(kStages >= 4, "both halves' keys and values in flight");
 };
 
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
@@ -83,6 +85,14 @@ __device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr, uint32_t block)
            (1ull << 46) | (2ull << 61);
 }
 
+// True on one lane of a converged warp, always the same one.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add)
 {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -104,7 +114,7 @@ __device__ __forceinline__ void mma_commit(uint32_t bar)
                  :: "r"(bar) : "memory");
 }
 
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32])
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float *v)
 {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -130,14 +140,52 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const float (&v)[32])
            "r"(addr) : "memory");
 }
 
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[16])
+__device__ __forceinline__ void tmem_st32u(uint32_t addr, const uint32_t *v)
 {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
         :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
            "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+           "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+           "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]),
            "r"(addr) : "memory");
+}
+
+// Loaded values may be used behind the wait only: this ties them to its place.
+__device__ __forceinline__ void tmem_pin32(float *v)
+{
+    asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                      "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]));
+    asm volatile("" : "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+                      "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31]));
+}
+
+// Two products and sums in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "add.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -145,15 +193,37 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// Key tiles of half x in a cut: the first half's last row may see fewer than the second's.
+// A tile of up to 128 rows is one half; so that both halves' pipelines work, the key tiles of a
+// cut then go to the halves in turn, over the same queries, and the first half's threads merge
+// the two sums at the end.
+__device__ __forceinline__ bool shares_rows(const Cut &p) { return p.rows <= 128; }
+
+// Key tiles of half x in a cut: of the tile's first half the last row may see fewer.
 __device__ __forceinline__ uint32_t half_tiles(const AttendJob &j, const Item &it, const Cut &p, uint32_t x,
                                                uint32_t M, uint32_t tile)
 {
     const uint32_t n = p.k1 - p.k0;
-    if (p.rows <= 128) return x ? 0 : n;
+    if (shares_rows(p)) return (n + 1 - x) / 2;
     if (x) return n;
     const uint32_t e = (token_limit(it, (p.rt * M + 127) / j.group) - it.kv0 + tile - 1) / tile;
     return e <= p.k0 ? 0 : e >= p.k1 ? n : e - p.k0;
+}
+
+// The cut tile that starts in a CTA's span, for the merge behind the kernel; rows = 0: none.
+struct CutDesc {
+    Item it;
+    Cut p;
+    uint64_t per;
+};
+
+// Merge of the cut tiles: a block takes 32 rows of one.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attend_merge(const __grid_constant__ AttendJob j)
+{
+    const CutDesc &c = j.cuts[blockIdx.x];
+    const uint32_t r0 = blockIdx.y * 32, rows = c.p.rows;
+    if (r0 >= rows) return;
+    merge_parts<T, 256>(j, c.it, c.p, c.per, 256, r0, r0 + 32 < rows ? r0 + 32 : rows);
 }
 
 template <typename T, int DP>
@@ -163,11 +233,13 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
     constexpr int kChunks = DP / 8;
     constexpr uint32_t kBlock = 128 * 128;      // bytes of one block of 128 rows x 64 elements
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * Sh::kStages + 11];
+    __shared__ __align__(8) uint64_t bars[2 * Sh::kStages + 12];
     __shared__ uint32_t tmem_slot;
-    __shared__ volatile uint32_t stop, last_part;
+    __shared__ volatile uint32_t stop;
+    __shared__ float half_m[128], half_l[128];   // the second half's statistics, when the halves share rows
     const uint32_t tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const uint32_t G = j.group, D = j.head_dim;
+    if (tid == 0 && !j.prefix_pass) j.cuts[blockIdx.x].p.rows = 0;
 
     const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
     const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
@@ -187,9 +259,11 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
     auto s_full = [&](uint32_t x) { return q_empty + 8 + 8 * x; };
     auto p_full = [&](uint32_t x) { return q_empty + 24 + 8 * x; };
     auto o_full = [&](uint32_t x) { return q_empty + 40 + 8 * x; };
-    const uint32_t part_bar = q_empty + 56, done_bar = q_empty + 64, spare_bar = q_empty + 72;
+    const uint32_t half_bar = q_empty + 56, half_read = q_empty + 64, done_bar = q_empty + 72,
+                   spare_bar = q_empty + 80;
     if (tid == 0) {
-        mbar_init(part_bar, 256);
+        mbar_init(half_bar, 128);
+        mbar_init(half_read, 128);
         mbar_init(done_bar, 1);
         mbar_init(spare_bar, 32 * Sh::kLoaders);
         for (int s = 0; s < Sh::kStages; ++s) {
@@ -222,18 +296,22 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
     using CutWalk = Walk<Sh::kM, Sh::kKeys>;
 
     if (w < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(Sh::kSoftmaxRegs));
         // ---- softmax: a thread owns row `row` of half x
         const uint32_t x = w >> 2, row = tid & 127;
         const uint32_t lane_base = (w & 3) << 21;            // lanes 32 (w % 4) ..
         const uint32_t s_t = tmem + lane_base + x * 128, o_t = tmem + lane_base + 256 + x * 128;
         const float c = fmaxf(fabsf(j.scale_log2), 1e-37f);  // a negative scale negates the products
-        uint32_t s_cnt = 0, o_cnt = 0, part_cnt = 0;
+        uint32_t s_cnt = 0, o_cnt = 0, half_cnt = 0;
+        bool half_due = false;       // second half: its sums of the cut before are still to be read
         CutWalk cw;
         cw.start(j, span);
         while (cw.next(j, span)) {
             const uint32_t n = half_tiles(j, cw.it, cw.p, x, Sh::kM, Sh::kKeys);
-            const uint32_t row_base = cw.p.rt * Sh::kM + x * 128;
-            const bool real = x * 128 + row < cw.p.rows;
+            const bool both = shares_rows(cw.p);                   // the halves share rows
+            const uint32_t first = both ? 0 : x * 128, step = both ? 2 : 1;
+            const uint32_t row_base = cw.p.rt * Sh::kM + first;
+            const bool real = first + row < cw.p.rows;
             const uint32_t lim = real ? token_limit(cw.it, (row_base + row) / G) : 0x7FFFFFFFu;
             const uint32_t lim_first = token_limit(cw.it, row_base / G);
             float m = -INFINITY, l = 0.f;
@@ -242,24 +320,28 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
                 if (!(alive = wait_warp(s_full(x), s_cnt & 1))) break;
                 ++s_cnt;
                 tc_fence_after();
-                const uint32_t key = cw.it.kv0 + (cw.p.k0 + t) * Sh::kKeys;
+                const uint32_t key = cw.it.kv0 + (cw.p.k0 + (both ? x : 0) + t * step) * Sh::kKeys;
                 const bool masked = key + Sh::kKeys > lim_first;
                 const int see = masked ? (int)(lim > key ? lim - key : 0u) : Sh::kKeys;   // keys of the tile
-                float top = -INFINITY;
+                float v[Sh::kKeys];
+#pragma unroll
+                for (int ch = 0; ch < 4; ++ch) tmem_ld32(s_t + ch * 32, v + ch * 32);
+                tmem_wait_ld();
+#pragma unroll
+                for (int ch = 0; ch < 4; ++ch) tmem_pin32(v + ch * 32);
+                if (masked) {
+#pragma unroll
+                    for (int e = 0; e < Sh::kKeys; ++e)
+                        if (e >= see) v[e] = -INFINITY;
+                }
+                float tops[4];
 #pragma unroll
                 for (int ch = 0; ch < 4; ++ch) {
-                    float v[32];
-                    tmem_ld32(s_t + ch * 32, v);
-                    tmem_wait_ld();
-                    if (masked) {
+                    tops[ch] = fmaxf(v[ch * 32], v[ch * 32 + 1]);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) top = fmaxf(top, ch * 32 + e < see ? v[e] : -INFINITY);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) top = fmaxf(top, v[e]);
-                    }
+                    for (int e = 2; e < 32; e += 2) tops[ch] = max3(tops[ch], v[ch * 32 + e], v[ch * 32 + e + 1]);
                 }
-                top *= c;
+                const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * c;
                 float fix = 1.f;
                 if (t == 0) {
                     m = top;
@@ -268,44 +350,44 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
                     m = top;
                     l *= fix;
                 }
+                const float neg = m == -INFINITY ? 0.f : -m;
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                const float2 cc = make_float2(c, c), nn = make_float2(neg, neg);
+#pragma unroll
+                for (int ch = 0; ch < 2; ++ch) {
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int e = 0; e < 64; e += 2) {
+                        float2 x = fma2(make_float2(v[ch * 64 + e], v[ch * 64 + e + 1]), cc, nn);
+                        x.x = exp2f(x.x);
+                        x.y = exp2f(x.y);
+                        sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], x);
+                        // the weights are rounded to the values' type: the tensor cores take both in one
+                        pk[e / 2] = Half2<T>::down(x.x, x.y);
+                    }
+                    tmem_st32u(s_t + ch * 32, pk);
+                }
+                l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 if (__any_sync(~0u, fix != 1.f)) {
                     // the value product of the tile before is done: its scores came after it
 #pragma unroll 1
                     for (int ch = 0; ch < DP / 32; ++ch) {
-                        float v[32];
-                        tmem_ld32(o_t + ch * 32, v);
+                        float o[32];
+                        tmem_ld32(o_t + ch * 32, o);
                         tmem_wait_ld();
+                        tmem_pin32(o);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] *= fix;
-                        tmem_st32(o_t + ch * 32, v);
+                        for (int e = 0; e < 32; ++e) o[e] *= fix;
+                        tmem_st32(o_t + ch * 32, o);
                     }
-                    tmem_wait_st();
                 }
-                const float neg = m == -INFINITY ? 0.f : -m;
-                float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
-                for (int ch = 0; ch < 4; ++ch) {
-                    float v[32];
-                    uint32_t pk[16];
-                    tmem_ld32(s_t + ch * 32, v);
-                    tmem_wait_ld();
-                    if (masked) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (ch * 32 + e >= see) v[e] = -INFINITY;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        const float a = exp2f(fmaf(v[e], c, neg)), b = exp2f(fmaf(v[e + 1], c, neg));
-                        sum0 += a;
-                        sum1 += b;
-                        // the weights are rounded to the values' type: the tensor cores take both in one
-                        pk[e / 2] = Half2<T>::down(a, b);
-                    }
-                    tmem_st16(s_t + ch * 16, pk);
-                }
-                l += sum0 + sum1;
                 tmem_wait_st();
+                if (half_due) {
+                    // these weights let the issuer overwrite the sums that the first half merges
+                    if (!(alive = wait_warp(half_read, half_cnt & 1))) break;
+                    ++half_cnt;
+                    half_due = false;
+                }
                 tc_fence_before();
                 mbar_arrive(p_full(x));
             }
@@ -318,7 +400,35 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
             const bool whole = cw.p.k0 == 0 && cw.p.k1 == cw.p.units;
             float *slot = whole ? nullptr
                                 : part_slot(j, 2ull * blockIdx.x + (cw.p.k0 == 0 ? 1 : 0), Sh::kM, DP);
-            if (x * 128 < cw.p.rows && (n || whole)) {
+            float f0 = 1.f, f1 = 0.f;            // weights of the two halves' sums, when they share rows
+            const bool two = both && cw.p.k1 - cw.p.k0 > 1;
+            if (two && x) {
+                if (half_due) {                  // (no key tile in the cuts since)
+                    if (!(alive = wait_warp(half_read, half_cnt & 1))) break;
+                    ++half_cnt;
+                }
+                half_m[row] = m;
+                half_l[row] = l;
+                tc_fence_before();
+                mbar_arrive(half_bar);
+                half_due = true;
+            } else if (two) {
+                if (!(alive = wait_warp(half_bar, half_cnt & 1))) break;
+                ++half_cnt;
+                tc_fence_after();
+                const float m1 = half_m[row], top = fmaxf(m, m1);
+                f0 = part_weight(m, top);
+                f1 = part_weight(m1, top);
+                l = l * f0 + half_l[row] * f1;
+                m = top;
+            }
+            if (first < cw.p.rows && (n || whole) && !(both && x)) {
+                // most rows: nothing to merge, l > 0, finite
+                const bool plain = !j.prefix_pass && !cw.it.skip && l != 0.f;
+                const float inv = 1.f / l;
+                const uint32_t R = row_base + (real ? row : 0);
+                const uint64_t out_row = cw.it.row0 + R / G;
+                const uint32_t out_head = cw.p.kv_head * G + R % G;
 #pragma unroll 1
                 for (int ch = 0; ch < DP / 32; ++ch) {
                     float v[32];
@@ -326,96 +436,105 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
                     if (n) {
                         tmem_ld32(o_t + ch * 32, v);
                         tmem_wait_ld();
+                        tmem_pin32(v);
                     } else {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = 0.f;
                     }
-                    if (real) {
+                    if (two) {
+                        float v1[32];
+                        tmem_ld32(o_t + 128 + ch * 32, v1);
+                        tmem_wait_ld();
+                        tmem_pin32(v1);
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4) {
-                            const uint32_t d = ch * 32 + e;
-                            const float4 acc = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-                            if (d >= D) continue;
-                            if (whole)
-                                finish_row4<T>(j, cw.it, cw.p, row_base + row, d, acc, m, l);
-                            else
-                                __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)(x * 128 + row) * DP + d), acc);
+                        for (int e = 0; e < 32; ++e) v[e] = v[e] * f0 + v1[e] * f1;
+                    }
+                    if (!real) continue;
+                    float all = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) all += v[e];
+                    if (!whole) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)(first + row) * DP + ch * 32 + e),
+                                   make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]));
+                    } else if (plain && !isnan(all)) {
+                        T *const dst = static_cast<T *>(j.out) + out_row * j.o_ts + out_head * j.o_hs + ch * 32;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8) {
+                            if (ch * 32 + e >= D) continue;
+                            uint4 pk;
+                            pk.x = Half2<T>::down(v[e] * inv, v[e + 1] * inv);
+                            pk.y = Half2<T>::down(v[e + 2] * inv, v[e + 3] * inv);
+                            pk.z = Half2<T>::down(v[e + 4] * inv, v[e + 5] * inv);
+                            pk.w = Half2<T>::down(v[e + 6] * inv, v[e + 7] * inv);
+                            *reinterpret_cast<uint4 *>(dst + e) = pk;
                         }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            if (ch * 32 + e < D)
+                                finish_row4_call<T>(j, cw.it, cw.p.kv_head, row_base + row, ch * 32 + e,
+                                                    make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]), m, l);
                     }
                 }
+                if (plain && real && whole && j.lse)
+                    j.lse[out_row * j.n_q_heads + out_head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+                __syncwarp();
                 tc_fence_before();
             }
-            if (!whole) {
-                if (real) {
-                    __stcg(slot + (uint64_t)Sh::kM * DP + x * 128 + row, m);
-                    __stcg(slot + (uint64_t)Sh::kM * (DP + 1) + x * 128 + row, l);
-                }
-                // as deliver_part, for the 256 threads of this role and with bounded waits
-                const uint32_t c0 = (uint32_t)(cw.p.tile0 / span.per);
-                __threadfence();
-                mbar_arrive(part_bar);
-                if (!(alive = wait_warp(part_bar, part_cnt & 1))) break;
-                ++part_cnt;
-                if (tid == 0) {
-                    const uint32_t c1 = (uint32_t)((cw.p.tile0 + cw.p.units - 1) / span.per);
-                    __threadfence();
-                    last_part = atomicAdd(&j.arrived[c0], 1u) == c1 - c0;
-                    if (last_part) j.arrived[c0] = 0;
-                    __threadfence();
-                }
-                mbar_arrive(part_bar);
-                if (!(alive = wait_warp(part_bar, part_cnt & 1))) break;
-                ++part_cnt;
-                if (last_part) {
-                    __threadfence();
-                    merge_parts<T, 256>(j, cw.it, cw.p, span.per, Sh::kM, DP);
-                }
+            if (two && !x) mbar_arrive(half_read);
+            if (!whole && real && !(both && x)) {
+                __stcg(slot + (uint64_t)Sh::kM * DP + first + row, m);
+                __stcg(slot + (uint64_t)Sh::kM * (DP + 1) + first + row, l);
+            }
+            if (!whole && cw.p.k0 == 0 && tid == 0 && !j.prefix_pass) {
+                CutDesc &c = j.cuts[blockIdx.x];
+                c.it = cw.it;
+                c.p = cw.p;
+                c.per = span.per;
             }
         }
-    } else if (w < 8 + Sh::kLoaders) {
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(Sh::kOtherRegs));
+    }
+    if (w >= 8 && w < 8 + Sh::kLoaders) {
         // ---- loaders
         constexpr int kSets = 4 / Sh::kLoaders;              // sets of 32 rows a warp takes of a block of 128
         const uint32_t r0 = (w - 8) * 32 * kSets;
         const uint64_t tok_stride = (uint64_t)j.n_kv_heads * D;
         uint32_t stage = 0, laps = 0, q_cnt = 0;
-        uint32_t fifo[Sh::kLag] = {};
-        uint32_t pending = 0;
         bool alive = true;
 
+        // The barrier is arrived at, for this thread, when its copies so far have landed; the
+        // issuer's proxy fence behind its wait makes them visible to the matrix unit.
         auto hand_over = [&](uint32_t bar) {
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            mbar_arrive(bar);
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" :: "r"(bar) : "memory");
         };
-        auto push = [&](uint32_t bar) {                      // a group of copies that ends at `bar`
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            if (pending == Sh::kLag) {
-                asm volatile("cp.async.wait_group %0;" :: "n"(Sh::kLag) : "memory");
-                hand_over(fifo[0]);
-            } else {
-                ++pending;
-            }
+        // 32 rows of a block of 128 from row `first` on; row r at src + off(lane r), if ok(lane r).
+        // Four lanes take 64 bytes of a row, eight rows at a time: with the swizzle (piece c of row r
+        // at c ^ r % 8) a lane's places differ by constants.
+        uint32_t piece_at[2], bytes[kChunks / 4];
 #pragma unroll
-            for (int k = 0; k + 1 < Sh::kLag; ++k) fifo[k] = fifo[k + 1];
-            fifo[Sh::kLag - 1] = bar;
-        };
-        auto flush = [&]() {
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        for (int y = 0; y < 2; ++y)
+            piece_at[y] = (lane >> 2) * 128 + (((y * 4 + (lane & 3)) ^ (lane >> 2)) << 4);
 #pragma unroll
-            for (int k = 0; k < Sh::kLag; ++k)
-                if (k + pending >= Sh::kLag) hand_over(fifo[k]);
-            pending = 0;
-        };
-        // 32 rows of a block, row r at src + off(lane r): 16-byte pieces to their swizzled places
+        for (int y = 0; y < kChunks / 4; ++y) bytes[y] = (y * 4 + (lane & 3)) * 8 < D ? 16 : 0;
         auto copy_rows = [&](uint32_t dst, const T *src, uint64_t off, bool ok, uint32_t first) {
-            const unsigned live = __ballot_sync(~0u, ok);
-            const uint32_t lo = (uint32_t)off, hi = (uint32_t)(off >> 32);
+            const uint32_t lo = (uint32_t)off, hi = (uint32_t)(off >> 32) | (ok ? 0u : 0x80000000u);
 #pragma unroll
-            for (int y = 0; y < kChunks; ++y) {
-                const uint32_t piece = y * 32 + lane, r = piece / kChunks, ck = piece % kChunks;
-                const uint64_t o = ((uint64_t)__shfl_sync(~0u, hi, r) << 32) | __shfl_sync(~0u, lo, r);
-                const bool in = ((live >> r) & 1u) && ck * 8 < D;
-                const uint32_t at = dst + (ck >> 3) * kBlock + (first + r) * 128 + (((ck & 7) ^ (r & 7)) << 4);
-                cp_async16(at, src + (in ? o + ck * 8 : 0), in);
+            for (int i = 0; i < 4; ++i) {
+                const int r = i * 8 + (lane >> 2);
+                const uint32_t h = __shfl_sync(~0u, hi, r);
+                const bool in = !(h >> 31);
+                const uint64_t o = ((uint64_t)(h & 0x7FFFFFFFu) << 32) | __shfl_sync(~0u, lo, r);
+                const T *row = src + o + (lane & 3) * 8;
+                const uint32_t at = dst + (first + i * 8) * 128;
+#pragma unroll
+                for (int y = 0; y < kChunks / 4; ++y)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                                 :: "r"(at + piece_at[y & 1] + (y >> 1) * kBlock),
+                                    "l"(bytes[y] ? row + y * 32 : src), "r"(in ? bytes[y] : 0u) : "memory");
             }
         };
         auto take_stage = [&]() {
@@ -424,7 +543,7 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
         };
         // hands the stage just filled to the issuer
         auto push_stage = [&]() {
-            push(blockIdx.x == 0 && (uint64_t)laps * Sh::kStages + stage == j.test_drop ? spare_bar : full(stage));
+            hand_over(blockIdx.x == 0 && (uint64_t)laps * Sh::kStages + stage == j.test_drop ? spare_bar : full(stage));
             if (++stage == Sh::kStages) {
                 stage = 0;
                 ++laps;
@@ -472,7 +591,6 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
                 push_stage();
                 if (t == 0) {
                     // the queries, once the products of the cut before have read theirs
-                    flush();
                     if (!(alive = wait_warp(q_empty, (q_cnt & 1) ^ 1))) break;
                     ++q_cnt;
                     for (uint32_t x = 0; x < 2 && x * 128 < cw.p.rows; ++x) {
@@ -486,7 +604,7 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
                             copy_rows(q_s + x * Sh::kTileBytes, static_cast<const T *>(j.q), q_off, in, r0 + y * 32);
                         }
                     }
-                    push(q_full);
+                    hand_over(q_full);
                 }
                 if (!take_stage()) break;
 #pragma unroll
@@ -495,8 +613,7 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
                 push_stage();
             }
         }
-        flush();
-    } else {
+    } else if (w == 8 + Sh::kLoaders) {
         // ---- issuer: the warp walks and waits together, one lane issues
         const uint32_t type = std::is_same<T, __half>::value ? 0u : 1u;
         const uint32_t common = (1u << 4) | (type << 7) | (type << 10) | (8u << 24);   // f32 sums, M = 128
@@ -508,22 +625,30 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
         bool alive = true;
         auto stage_of = [&](uint32_t at) { return at % Sh::kStages; };
         auto lap_of = [&](uint32_t at) { return (at / Sh::kStages) & 1; };
-        auto scores = [&](uint32_t x, uint32_t st) {
-            if (lane) return;
-            const uint64_t a = desc_k_major(q_s + x * Sh::kTileBytes), b = desc_k_major(ring + st * Sh::kTileBytes);
-            for (uint32_t k = 0; k < k_steps; ++k) {
+        auto scores = [&](uint32_t x, uint32_t q, uint32_t st) {      // S_x = Q_q K^T
+            if (!elect_one()) return;
+            const uint64_t a = desc_k_major(q_s + q * Sh::kTileBytes), b = desc_k_major(ring + st * Sh::kTileBytes);
+#pragma unroll
+            for (uint32_t k = 0; k < DP / 16; ++k) {
                 const uint64_t step = (k >> 2) * (kBlock >> 4) + (k & 3) * 2;   // 64 elements a block, 16 a step
-                mma_ss(tmem + x * 128, a + step, b + step, id_s, k != 0);
+                if (k < k_steps) mma_ss(tmem + x * 128, a + step, b + step, id_s, k != 0);
             }
         };
         auto values = [&](uint32_t x, uint32_t st, bool add) {
-            if (lane) return;
+            if (!elect_one()) return;
             const uint64_t b = desc_mn_major(ring + st * Sh::kTileBytes, kBlock);
+#pragma unroll
             for (uint32_t k = 0; k < Sh::kKeys / 16; ++k)
                 mma_ts(tmem + 256 + x * 128, tmem + x * 128 + k * 8, b + k * (2048 >> 4), id_o, add || k != 0);
         };
+        // copies have landed: order them before the matrix unit's reads
+        auto wait_tile = [&](uint32_t bar, uint32_t parity) {
+            const bool ok = wait_warp(bar, parity);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            return ok;
+        };
         auto commit = [&](uint32_t bar) {
-            if (lane == 0) mma_commit(bar);
+            if (elect_one()) mma_commit(bar);
         };
         CutWalk cw;
         cw.start(j, span);
@@ -531,22 +656,49 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
             const uint32_t n = cw.p.k1 - cw.p.k0;
             const uint32_t nx[2] = {half_tiles(j, cw.it, cw.p, 0, Sh::kM, Sh::kKeys),
                                     half_tiles(j, cw.it, cw.p, 1, Sh::kM, Sh::kKeys)};
-            const uint32_t at = pos;
+            const bool both = shares_rows(cw.p);
+            const uint32_t at = pos;      // keys of tile t at position at + 2 t, values behind them
             pos += 2 * n;
-            if (!(alive = wait_warp(q_full, q_cnt & 1))) break;
+            if (!(alive = wait_tile(q_full, q_cnt & 1))) break;
             ++q_cnt;
-            if (!(alive = wait_warp(full(stage_of(at)), lap_of(at)))) break;
+            if (both) {
+                // tile t belongs to half t % 2
+                for (uint32_t t = 0; t < n + 2; ++t) {
+                    const uint32_t x = t & 1;
+                    if (t >= 2) {
+                        const uint32_t v_at = at + 2 * (t - 2) + 1;
+                        if (!(alive = wait_tile(full(stage_of(v_at)), lap_of(v_at)))) break;
+                        if (!(alive = wait_warp(p_full(x), p_cnt[x] & 1))) break;
+                        ++p_cnt[x];
+                        tc_fence_after();
+                        values(x, stage_of(v_at), t >= 4);
+                        commit(empty(stage_of(v_at)));
+                        if (t >= n) commit(o_full(x));
+                    }
+                    if (t < n) {
+                        const uint32_t k_at = at + 2 * t;
+                        if (!(alive = wait_tile(full(stage_of(k_at)), lap_of(k_at)))) break;
+                        tc_fence_after();
+                        scores(x, 0, stage_of(k_at));
+                        commit(s_full(x));
+                        commit(empty(stage_of(k_at)));
+                        if (t + 1 == n) commit(q_empty);
+                    }
+                }
+                continue;
+            }
+            if (!(alive = wait_tile(full(stage_of(at)), lap_of(at)))) break;
             tc_fence_after();
             for (uint32_t x = 0; x < 2; ++x)
                 if (nx[x]) {
-                    scores(x, stage_of(at));
+                    scores(x, x, stage_of(at));
                     commit(s_full(x));
                 }
             commit(empty(stage_of(at)));
             if (n == 1) commit(q_empty);
             for (uint32_t t = 0; t < n && alive; ++t) {
                 const uint32_t v_at = at + 2 * t + 1, k_at = v_at + 1;
-                if (!(alive = wait_warp(full(stage_of(v_at)), lap_of(v_at)))) break;
+                if (!(alive = wait_tile(full(stage_of(v_at)), lap_of(v_at)))) break;
                 bool key_here = false;
                 for (uint32_t x = 0; x < 2; ++x) {
                     if (t < nx[x]) {
@@ -556,9 +708,10 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
                         values(x, stage_of(v_at), t != 0);
                     }
                     if (t + 1 < nx[x]) {
-                        if (!key_here && !(alive = wait_warp(full(stage_of(k_at)), lap_of(k_at)))) break;
+                        if (!key_here && !(alive = wait_tile(full(stage_of(k_at)), lap_of(k_at)))) break;
                         key_here = true;
-                        scores(x, stage_of(k_at));
+                        tc_fence_after();
+                        scores(x, x, stage_of(k_at));
                         commit(s_full(x));
                     } else if (t + 1 == nx[x]) {
                         commit(o_full(x));

@@ -61,33 +61,63 @@ int launch_many(lsmkv_ctx *ctx, cudaStream_t s, const AttendJob &job)
         k_attend_many<T, 128><<<sm, ManyShape<128>::kThreads, ManyShape<128>::kSmem, s>>>(job);
     ++ctx->launches;
     CU(ctx, cudaGetLastError());
+    if (job.prefix_pass) return LSMKV_OK;
+    k_attend_merge<T><<<dim3(sm, 256 / 32), 256, 0, s>>>(job);
+    ++ctx->launches;
+    CU(ctx, cudaGetLastError());
     return LSMKV_OK;
 }
 
-// One pass over the sequences (or groups): those of few rows and those of many, each by its
-// kernel. most: no item has more rows (query heads of one KV head times new tokens).
+// The tcgen05 kernel takes heads of up to 128 elements.
+bool many_takes(const lsmkv_ctx *ctx) { return ctx->geom.head_dim <= 128; }
+
+uint32_t part_dp(const lsmkv_ctx *ctx)
+{
+    return ctx->geom.head_dim <= 64 ? 64 : ctx->geom.head_dim <= 128 ? 128 : 256;
+}
+
+// The groups' common keys, all groups by one kernel: whatever their rows, reading the keys once
+// is what counts.
 template <typename T>
-int launch_pass(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job, uint64_t most)
+int launch_prefix(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
+{
+    job.prefix_pass = 1;
+    job.rows_lo = 0;
+    job.rows_hi = 0xFFFFFFFFu;
+    const int rc = many_takes(ctx) ? launch_many<T>(ctx, s, job) : launch_few<T>(ctx, s, job);
+    job.prefix_pass = 0;
+    return rc;
+}
+
+// The sequences: those of few rows and those of many, each by its kernel.
+template <typename T>
+int launch_own(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
 {
     // Up to 16 rows fill one fragment of the few-row kernel; beyond, it would read the keys once
     // for every 16 rows, where the many-row kernel reads them once for 256.
-    const bool mma = job.head_dim <= 128;
+    const bool mma = many_takes(ctx);
     job.rows_lo = 0;
     job.rows_hi = mma ? 16 : 0xFFFFFFFFu;
-    int rc = launch_few<T>(ctx, s, job);
-    if (rc != LSMKV_OK || !mma || most <= 16) return rc;
+    const int rc = launch_few<T>(ctx, s, job);
+    if (rc != LSMKV_OK || !mma || (uint64_t)job.seqs.max_new * job.group <= 16) return rc;
     job.rows_lo = 16;
     job.rows_hi = 0xFFFFFFFFu;
     return launch_many<T>(ctx, s, job);
 }
 
-// Scratch of the attend kernels: counters, then two part slots per CTA of the widest launch.
+// Two part slots for every CTA of the widest launch.
+size_t part_bytes(const lsmkv_ctx *ctx, bool few, bool many)
+{
+    const size_t a = few ? (size_t)ctx->sm_count * 2 * 2 * 16 : 0;
+    const size_t b = many && many_takes(ctx) ? (size_t)ctx->sm_count * 2 * 256 : 0;
+    return std::max(a, b) * (part_dp(ctx) + 2) * 4;
+}
+
+// Scratch of the attend kernels: counters, descriptors of cut tiles, parts.
 int ensure_attend(lsmkv_ctx *ctx, cudaStream_t s)
 {
     const size_t counters = attend_counter_bytes(ctx);
-    const uint32_t dp = ctx->geom.head_dim <= 64 ? 64 : ctx->geom.head_dim <= 128 ? 128 : 256;
-    const size_t few = (size_t)ctx->sm_count * 2 * 2 * 16, many = dp > 128 ? 0 : (size_t)ctx->sm_count * 2 * 256;
-    const size_t bytes = counters + std::max(few, many) * (dp + 2) * 4;
+    const size_t bytes = counters + (size_t)ctx->sm_count * sizeof(CutDesc) + 256 + part_bytes(ctx, true, true);
     if (ctx->d_attend && bytes <= ctx->attend_cap) return LSMKV_OK;
     const int rc = grow_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, bytes, bytes, __LINE__);
     if (rc != LSMKV_OK) return rc;
@@ -138,37 +168,42 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
     job.o_hs = out->head_stride;
     job.lse = lse_out;
     job.scale_log2 = scale * kLog2e;
-    job.arrived = static_cast<unsigned int *>(ctx->d_attend);
-    job.parts = reinterpret_cast<float *>(static_cast<char *>(ctx->d_attend) + attend_counter_bytes(ctx));
+    IoLayout lay(ctx->d_attend);
+    job.arrived = reinterpret_cast<unsigned int *>(lay.take<unsigned char>(attend_counter_bytes(ctx)));
+    job.cuts = lay.take<CutDesc>((size_t)ctx->sm_count);
+    job.parts = lay.take<float>(0);
+    job.dp = part_dp(ctx);
     job.wait_cycles = ctx->wait_cycles;
     job.test_drop = ctx->test_drop_piece < 0 ? ~0ull : (uint64_t)ctx->test_drop_piece;
     job.st = ctx->d_status;
     if (shared) {
         const uint64_t heads = seqs->n_new * n_q_heads;
-        const size_t bytes = (size_t)(heads * (ctx->geom.head_dim + 1) + seqs->n_seq) * 4;
+        auto place = [&](void *at) {
+            IoLayout l(at);
+            job.share = l.take<Share>(seqs->n_seq);
+            job.pre_o = l.take<float>(heads * ctx->geom.head_dim);
+            job.pre_lse = l.take<float>(heads);
+            job.pre_parts = l.take<float>(part_bytes(ctx, !many_takes(ctx), true) / 4);
+            return l.at;
+        };
+        const size_t bytes = place(nullptr);
         if (!ctx->d_prefix || bytes > ctx->prefix_cap) {
             rc = grow_scratch(ctx, &ctx->d_prefix, &ctx->prefix_cap, bytes, bytes, __LINE__);
             if (rc != LSMKV_OK) return rc;
         }
-        job.pre_o = static_cast<float *>(ctx->d_prefix);
-        job.pre_lse = job.pre_o + heads * ctx->geom.head_dim;
-        job.skip = reinterpret_cast<uint32_t *>(job.pre_lse + heads);
+        place(ctx->d_prefix);
+        job.pre_rows = many_takes(ctx) ? 256 : 16;
         job.n_group = groups->n_group;
         job.group_off = groups->group_off;
         job.shared_pages = groups->shared_pages;
     }
     LaunchTimer timer(ctx, s, LSMKV_K_ATTEND);
-    auto pass = dtype == LSMKV_BF16 ? launch_pass<__nv_bfloat16> : launch_pass<__half>;
+    const bool bf = dtype == LSMKV_BF16;
     if (shared) {
-        k_shared_skip<<<(groups->n_group + 127) / 128, 128, 0, s>>>(job);
-        ++ctx->launches;
-        CU(ctx, cudaGetLastError());
-        job.prefix_pass = 1;
-        rc = pass(ctx, s, job, seqs->n_new * job.group);
+        rc = bf ? launch_prefix<__nv_bfloat16>(ctx, s, job) : launch_prefix<__half>(ctx, s, job);
         if (rc != LSMKV_OK) return rc;
-        job.prefix_pass = 0;
     }
-    return pass(ctx, s, job, (uint64_t)seqs->max_new * job.group);
+    return bf ? launch_own<__nv_bfloat16>(ctx, s, job) : launch_own<__half>(ctx, s, job);
 }
 
 }  // namespace
