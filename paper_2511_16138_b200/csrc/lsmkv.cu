@@ -250,10 +250,12 @@ cudaError_t set_copy_smem_limit(int max_smem_optin)
     for (auto *few : {k_attend_few<__nv_bfloat16, 256, 4, 3>, k_attend_few<__half, 256, 4, 3>})
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FewShape<256, 4, 3>::kSmem);
-    for (auto *many : {k_attend_many<__nv_bfloat16, 64>, k_attend_many<__half, 64>})
+    for (auto *many : {k_attend_many<__nv_bfloat16, 64, true>, k_attend_many<__half, 64, true>,
+                       k_attend_many<__nv_bfloat16, 64, false>, k_attend_many<__half, 64, false>})
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ManyShape<64>::kSmem);
-    for (auto *many : {k_attend_many<__nv_bfloat16, 128>, k_attend_many<__half, 128>})
+    for (auto *many : {k_attend_many<__nv_bfloat16, 128, true>, k_attend_many<__half, 128, true>,
+                       k_attend_many<__nv_bfloat16, 128, false>, k_attend_many<__half, 128, false>})
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ManyShape<128>::kSmem);
     if (e == cudaSuccess) g_smem_limit_set[dev] = true;

@@ -51,6 +51,8 @@ struct AttendJob {
     float *parts;                // two slots per CTA
     unsigned int *arrived;       // few rows: one counter per CTA, zero between calls
     struct CutDesc *cuts;        // many rows: the cut tile that starts in a CTA's span
+    void *maps;                  // many rows: two tensor maps per CTA
+    uint32_t box_rows;           // tokens of a box, dividing page_tokens
     long long wait_cycles;
     uint64_t test_drop;          // test hook: ~0 = off
     DevStatus *st;

@@ -4,9 +4,10 @@
 // A row tile is 256 rows, two halves of 128 (one TMEM lane a row). A persistent CTA walks its span
 // of units (key tiles of 128 keys); its warps have roles that run side by side:
 //   loaders (2 warps)  gather the tile's queries, then keys and values of one key tile after the
-//                      other through a ring of stages: 16-byte cp.async, each to its place in the
-//                      128-byte-swizzled layout that the matrix unit reads, so that any page size
-//                      and any page order costs the same
+//                      other through a ring of stages, in the 128-byte-swizzled layout that the
+//                      matrix unit reads. Pages of a multiple of 8 tokens come by the copy engine
+//                      in boxes of 64 elements x up to 64 tokens; others, like the queries, by
+//                      16-byte cp.async, each to its place
 //   issuer (1 warp)    S_x = Q_x K^T of the next key tile and O_x += P_x V of this one, for the
 //                      halves x in turn: while one half's softmax runs, the other half's products do
 //   softmax (2 x 4 warps) a thread owns a row: scores from TMEM, running maximum and sum in
@@ -17,6 +18,8 @@
 // either (16 exponentials a cycle and SM; 8192 operations a cycle and SM at head_dim 128).
 // Every wait is bounded; one that runs out ends all roles and is reported.
 #pragma once
+#include <cuda.h>
+
 #include <type_traits>
 
 #include "lsmkv_attend.cuh"
@@ -112,6 +115,31 @@ __device__ __forceinline__ void mma_commit(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];"
                  :: "r"(bar) : "memory");
+}
+
+// The key (or value) buffer of a layer as the copy engine sees it: elements, heads, tokens. The
+// host knows all of it but the address, which lies in the pool's table on the device: a warp puts
+// it into a copy of the map and publishes that for its CTA.
+__device__ __forceinline__ void publish_map(void *dst, unsigned char *work, const CUtensorMap &map,
+                                            const void *address)
+{
+    const uint32_t lane = threadIdx.x & 31;
+    reinterpret_cast<uint32_t *>(work)[lane] = reinterpret_cast<const uint32_t *>(&map)[lane];
+    __syncwarp();
+    if (lane == 0)
+        asm volatile("tensormap.replace.tile.global_address.shared::cta.b1024.b64 [%0], %1;"
+                     :: "r"(smem_addr(work)), "l"(address) : "memory");
+    __syncwarp();
+    asm volatile("tensormap.cp_fenceproxy.global.shared::cta.tensormap::generic.release.gpu.sync.aligned [%0], [%1], 128;"
+                 :: "l"(dst), "r"(smem_addr(work)) : "memory");
+    asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" :: "l"(dst) : "memory");
+}
+
+__device__ __forceinline__ void tma_box(uint32_t dst, const void *map, int e, int head, int token, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4}], [%5];"
+                 :: "r"(dst), "l"(map), "r"(e), "r"(head), "r"(token), "r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, float *v)
@@ -226,8 +254,9 @@ __global__ __launch_bounds__(256) void k_attend_merge(const __grid_constant__ At
     merge_parts<T, 256>(j, c.it, c.p, c.per, 256, r0, r0 + 32 < rows ? r0 + 32 : rows);
 }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(const __grid_constant__ AttendJob j)
+template <typename T, int DP, bool kBoxes>
+__global__ __launch_bounds__(ManyShape<DP>::kThreads, 1)
+void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ CUtensorMap map)
 {
     using Sh = ManyShape<DP>;
     constexpr int kChunks = DP / 8;
@@ -235,6 +264,7 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * Sh::kStages + 12];
     __shared__ uint32_t tmem_slot;
+    __shared__ __align__(128) unsigned char map_work[128];
     __shared__ volatile uint32_t stop;
     __shared__ float half_m[128], half_l[128];   // the second half's statistics, when the halves share rows
     const uint32_t tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
@@ -267,7 +297,7 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
         mbar_init(done_bar, 1);
         mbar_init(spare_bar, 32 * Sh::kLoaders);
         for (int s = 0; s < Sh::kStages; ++s) {
-            mbar_init(full(s), 32 * Sh::kLoaders);
+            mbar_init(full(s), kBoxes ? 1 : 32 * Sh::kLoaders);
             mbar_init(empty(s), 1);
         }
         mbar_init(q_full, 32 * Sh::kLoaders);
@@ -284,6 +314,11 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      :: "r"(smem_addr(&tmem_slot)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    unsigned char *const maps = reinterpret_cast<unsigned char *>(j.maps) + blockIdx.x * 256;
+    if (kBoxes && w == 8) {
+        publish_map(maps, map_work, map, kbuf);
+        publish_map(maps + 128, map_work, map, vbuf);
     }
     tc_fence_before();
     __syncthreads();
@@ -541,9 +576,11 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
             alive = alive && wait_warp(empty(stage), (laps & 1) ^ 1);
             return alive;
         };
-        // hands the stage just filled to the issuer
-        auto push_stage = [&]() {
-            hand_over(blockIdx.x == 0 && (uint64_t)laps * Sh::kStages + stage == j.test_drop ? spare_bar : full(stage));
+        // the barrier of the stage that is filled next (test hook: another one's)
+        auto stage_bar = [&]() {
+            return blockIdx.x == 0 && (uint64_t)laps * Sh::kStages + stage == j.test_drop ? spare_bar : full(stage);
+        };
+        auto next_stage = [&]() {
             if (++stage == Sh::kStages) {
                 stage = 0;
                 ++laps;
@@ -557,60 +594,105 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
             const uint32_t row_base = cw.p.rt * Sh::kM;
             const uint32_t key_end = min(token_limit(it, (row_base + cw.p.rows - 1) / G),
                                          it.kv0 + cw.p.k1 * Sh::kKeys);
-            auto page_of = [&](uint32_t t, int set) -> uint32_t {
-                const uint32_t k = it.kv0 + (cw.p.k0 + t) * Sh::kKeys + r0 + set * 32 + lane;
-                if (k >= key_end) return 0xFFFFFFFFu;
+            const uint32_t n = cw.p.k1 - cw.p.k0;
+            const uint32_t key0 = it.kv0 + cw.p.k0 * Sh::kKeys;
+            // the queries, once the products of the cut before have read theirs
+            auto fetch_queries = [&]() {
+                if (!(alive = wait_warp(q_empty, (q_cnt & 1) ^ 1))) return;
+                ++q_cnt;
+                for (uint32_t x = 0; x < 2 && x * 128 < cw.p.rows; ++x) {
+#pragma unroll
+                    for (int y = 0; y < kSets; ++y) {
+                        const uint32_t r = x * 128 + r0 + y * 32 + lane;
+                        const bool in = r < cw.p.rows;
+                        const uint32_t R = row_base + (in ? r : 0);
+                        const uint64_t q_off =
+                            (it.row0 + R / G) * j.q_ts + (uint64_t)(cw.p.kv_head * G + R % G) * j.q_hs;
+                        copy_rows(q_s + x * Sh::kTileBytes, static_cast<const T *>(j.q), q_off, in, r0 + y * 32);
+                    }
+                }
+                hand_over(q_full);
+            };
+            // page id of key k; kNone for a key that is not loaded
+            constexpr uint32_t kNone = 0xFFFFFFFFu;
+            auto page_of = [&](uint32_t k) -> uint32_t {
+                if (k >= key_end) return kNone;
                 const uint64_t entry = it.page0 + k / j.page_tokens;
                 const uint32_t page = j.seqs.page_table[entry];
-                if (page >= j.num_pages) {
-                    st_flag(j.st, LSMKV_ST_BAD_PAGE, entry);
-                    return 0xFFFFFFFFu;
-                }
-                return page;
+                if (page < j.num_pages) return page;
+                st_flag(j.st, LSMKV_ST_BAD_PAGE, entry);
+                return kBoxes ? (uint32_t)j.num_pages : kNone;    // the copy engine reads zeros there
             };
-            const uint32_t n = cw.p.k1 - cw.p.k0;
-            uint32_t page[kSets];                            // a tile ahead of the copies
-#pragma unroll
-            for (int y = 0; y < kSets; ++y) page[y] = page_of(0, y);
-            for (uint32_t t = 0; t < n; ++t) {
-                uint64_t off[kSets];
-                bool ok[kSets];
-#pragma unroll
-                for (int y = 0; y < kSets; ++y) {
-                    const uint32_t k = it.kv0 + (cw.p.k0 + t) * Sh::kKeys + r0 + y * 32 + lane;
-                    ok[y] = page[y] != 0xFFFFFFFFu;
-                    off[y] = ok[y] ? ((uint64_t)page[y] * j.page_tokens + k % j.page_tokens) * tok_stride +
-                                         (uint64_t)cw.p.kv_head * D
-                                   : 0;
-                    if (t + 1 < n) page[y] = page_of(t + 1, y);
+            if constexpr (kBoxes) {
+                // lane g takes tokens [g box_rows, (g + 1) box_rows) of every key tile, one page's
+                if (w != 8) {
+                    fetch_queries();
+                    continue;
                 }
-                if (!take_stage()) break;
+                const uint32_t g0 = lane * j.box_rows;
+                uint32_t page = g0 < Sh::kKeys ? page_of(key0 + g0) : kNone;
+                for (uint32_t t = 0; t < n; ++t) {
+                    const uint32_t k = key0 + t * Sh::kKeys + g0;
+                    const bool ok = page != kNone;
+                    const int token = (int)(page * j.page_tokens + k % j.page_tokens);
+                    if (t + 1 < n && g0 < Sh::kKeys) page = page_of(k + Sh::kKeys);
+                    const uint32_t bytes = __popc(__ballot_sync(~0u, ok)) * (DP / 64) * j.box_rows * 128;
 #pragma unroll
-                for (int y = 0; y < kSets; ++y)
-                    copy_rows(ring + stage * Sh::kTileBytes, kbuf, off[y], ok[y], r0 + y * 32);
-                push_stage();
-                if (t == 0) {
-                    // the queries, once the products of the cut before have read theirs
-                    if (!(alive = wait_warp(q_empty, (q_cnt & 1) ^ 1))) break;
-                    ++q_cnt;
-                    for (uint32_t x = 0; x < 2 && x * 128 < cw.p.rows; ++x) {
+                    for (int kv = 0; kv < 2; ++kv) {
+                        if (!take_stage()) break;
+                        const uint32_t bar = stage_bar();
+                        if (lane == 0)
+                            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
+                                         :: "r"(bar), "r"(bytes) : "memory");
+                        __syncwarp();
+                        if (ok) {
 #pragma unroll
-                        for (int y = 0; y < kSets; ++y) {
-                            const uint32_t r = x * 128 + r0 + y * 32 + lane;
-                            const bool in = r < cw.p.rows;
-                            const uint32_t R = row_base + (in ? r : 0);
-                            const uint64_t q_off =
-                                (it.row0 + R / G) * j.q_ts + (uint64_t)(cw.p.kv_head * G + R % G) * j.q_hs;
-                            copy_rows(q_s + x * Sh::kTileBytes, static_cast<const T *>(j.q), q_off, in, r0 + y * 32);
+                            for (int e = 0; e < DP / 64; ++e)
+                                tma_box(ring + stage * Sh::kTileBytes + e * kBlock + g0 * 128, maps + kv * 128, e * 64,
+                                        (int)cw.p.kv_head, token, bar);
                         }
+                        next_stage();
+                        if (t == 0 && kv == 0) fetch_queries();
+                        if (!alive) break;
                     }
-                    hand_over(q_full);
+                    if (!alive) break;
                 }
-                if (!take_stage()) break;
+            } else {
+                uint32_t page[kSets];                            // a tile ahead of the copies
 #pragma unroll
-                for (int y = 0; y < kSets; ++y)
-                    copy_rows(ring + stage * Sh::kTileBytes, vbuf, off[y], ok[y], r0 + y * 32);
-                push_stage();
+                for (int y = 0; y < kSets; ++y) page[y] = page_of(key0 + r0 + y * 32 + lane);
+                for (uint32_t t = 0; t < n; ++t) {
+                    uint64_t off[kSets];
+                    bool ok[kSets];
+#pragma unroll
+                    for (int y = 0; y < kSets; ++y) {
+                        const uint32_t k = key0 + t * Sh::kKeys + r0 + y * 32 + lane;
+                        ok[y] = page[y] != kNone;
+                        off[y] = ok[y] ? ((uint64_t)page[y] * j.page_tokens + k % j.page_tokens) * tok_stride +
+                                             (uint64_t)cw.p.kv_head * D
+                                       : 0;
+                        if (t + 1 < n) page[y] = page_of(k + Sh::kKeys);
+                    }
+#pragma unroll
+                    for (int kv = 0; kv < 2; ++kv) {
+                        if (!take_stage()) break;
+#pragma unroll
+                        for (int y = 0; y < kSets; ++y)
+                            copy_rows(ring + stage * Sh::kTileBytes, kv ? vbuf : kbuf, off[y], ok[y], r0 + y * 32);
+                        hand_over(stage_bar());
+                        next_stage();
+                        if (t == 0 && kv == 0) fetch_queries();
+                        if (!alive) break;
+                    }
+                    if (!alive) break;
+                }
+            }
+        }
+        if (kBoxes && w == 8) {
+            // boxes still under way write shared memory: let them land
+            for (int s = 0; s < Sh::kStages; ++s) {
+                const uint32_t lap = laps + (stage > (uint32_t)s ? 1 : 0);        // times this stage was filled
+                if (lap) (void)mbar_wait_bounded(full(s), (lap - 1) & 1, j.wait_cycles);
             }
         }
     } else if (w == 8 + Sh::kLoaders) {
@@ -647,6 +729,19 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             return ok;
         };
+        // Boxes are whole: rows behind the last key hold whatever the page holds there, or nothing
+        // new at all. Keys are masked, but a value times zero need not be zero.
+        auto wipe = [&](uint32_t st, uint32_t key, uint32_t key_end) {
+            if (!kBoxes || key + Sh::kKeys <= key_end) return;
+            const uint32_t first = key < key_end ? key_end - key : 0;
+            for (uint32_t x = first * 8 + lane; x < Sh::kKeys * 8; x += 32)
+#pragma unroll
+                for (int e = 0; e < DP / 64; ++e)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};"
+                                 :: "r"(ring + st * Sh::kTileBytes + e * kBlock + x * 16), "r"(0) : "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+        };
         auto commit = [&](uint32_t bar) {
             if (elect_one()) mma_commit(bar);
         };
@@ -657,6 +752,8 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
             const uint32_t nx[2] = {half_tiles(j, cw.it, cw.p, 0, Sh::kM, Sh::kKeys),
                                     half_tiles(j, cw.it, cw.p, 1, Sh::kM, Sh::kKeys)};
             const bool both = shares_rows(cw.p);
+            const uint32_t key0 = cw.it.kv0 + cw.p.k0 * Sh::kKeys;
+            const uint32_t key_end = token_limit(cw.it, (cw.p.rt * Sh::kM + cw.p.rows - 1) / G);
             const uint32_t at = pos;      // keys of tile t at position at + 2 t, values behind them
             pos += 2 * n;
             if (!(alive = wait_tile(q_full, q_cnt & 1))) break;
@@ -671,6 +768,7 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
                         if (!(alive = wait_warp(p_full(x), p_cnt[x] & 1))) break;
                         ++p_cnt[x];
                         tc_fence_after();
+                        wipe(stage_of(v_at), key0 + (t - 2) * Sh::kKeys, key_end);
                         values(x, stage_of(v_at), t >= 4);
                         commit(empty(stage_of(v_at)));
                         if (t >= n) commit(o_full(x));
@@ -699,6 +797,7 @@ __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1) void k_attend_many(cons
             for (uint32_t t = 0; t < n && alive; ++t) {
                 const uint32_t v_at = at + 2 * t + 1, k_at = v_at + 1;
                 if (!(alive = wait_tile(full(stage_of(v_at)), lap_of(v_at)))) break;
+                wipe(stage_of(v_at), key0 + t * Sh::kKeys, key_end);
                 bool key_here = false;
                 for (uint32_t x = 0; x < 2; ++x) {
                     if (t < nx[x]) {

@@ -3,6 +3,8 @@
 // Included at the end of lsmkv.cu (needs the context's internals).
 #pragma once
 
+#include <cudaTypedefs.h>
+
 namespace {
 
 // The pools these calls take.
@@ -51,14 +53,54 @@ int launch_few(lsmkv_ctx *ctx, cudaStream_t s, const AttendJob &job)
     return LSMKV_OK;
 }
 
+// A layer's key or value buffer as the copy engine sees it -- elements, heads, tokens; boxes of 64
+// elements of one head x box_rows tokens, swizzled -- all but its address, which the kernel fills
+// in. False: the pool is none that the copy engine can take that way.
+bool make_pool_map(const lsmkv_ctx *ctx, uint32_t dtype, uint64_t num_pages, uint32_t box_rows, CUtensorMap *map)
+{
+    static const PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) !=
+                cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    }();
+    const lsmkv_geom_t &g = ctx->geom;
+    const uint64_t tokens = num_pages * g.page_tokens;
+    if (!encode || num_pages == 0 || tokens / g.page_tokens != num_pages ||
+        tokens + g.page_tokens > 0x7FFFFFFFull)              // coordinates are 32-bit
+        return false;
+    const cuuint64_t dims[3] = {g.head_dim, g.n_kv_heads, tokens};
+    const cuuint64_t strides[2] = {g.head_dim * 2ull, (cuuint64_t)g.n_kv_heads * g.head_dim * 2};
+    const cuuint32_t box[3] = {64, 1, box_rows}, step[3] = {1, 1, 1};
+    return encode(map, dtype == LSMKV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                  3, ctx->d_attend, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T>
-int launch_many(lsmkv_ctx *ctx, cudaStream_t s, const AttendJob &job)
+int launch_many(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
 {
     const unsigned sm = (unsigned)ctx->sm_count;
-    if (job.head_dim <= 64)
-        k_attend_many<T, 64><<<sm, ManyShape<64>::kThreads, ManyShape<64>::kSmem, s>>>(job);
-    else
-        k_attend_many<T, 128><<<sm, ManyShape<128>::kThreads, ManyShape<128>::kSmem, s>>>(job);
+    // Tokens of a box: the largest power of two that divides the page, at most 64. The swizzle's
+    // unit is 8 rows, so boxes of fewer than 8 are out and cp.async takes such pages.
+    job.box_rows = std::min(job.page_tokens & (~job.page_tokens + 1), 64u);
+    CUtensorMap map;
+    std::memset(&map, 0, sizeof(map));
+    const bool boxes = job.box_rows >= 8 &&
+                       make_pool_map(ctx, std::is_same<T, __half>::value ? LSMKV_F16 : LSMKV_BF16, job.num_pages,
+                                     job.box_rows, &map);
+    if (job.head_dim <= 64) {
+        auto kern = boxes ? k_attend_many<T, 64, true> : k_attend_many<T, 64, false>;
+        kern<<<sm, ManyShape<64>::kThreads, ManyShape<64>::kSmem, s>>>(job, map);
+    } else {
+        auto kern = boxes ? k_attend_many<T, 128, true> : k_attend_many<T, 128, false>;
+        kern<<<sm, ManyShape<128>::kThreads, ManyShape<128>::kSmem, s>>>(job, map);
+    }
     ++ctx->launches;
     CU(ctx, cudaGetLastError());
     if (job.prefix_pass) return LSMKV_OK;
@@ -117,7 +159,7 @@ size_t part_bytes(const lsmkv_ctx *ctx, bool few, bool many)
 int ensure_attend(lsmkv_ctx *ctx, cudaStream_t s)
 {
     const size_t counters = attend_counter_bytes(ctx);
-    const size_t bytes = counters + (size_t)ctx->sm_count * sizeof(CutDesc) + 256 + part_bytes(ctx, true, true);
+    const size_t bytes = counters + (size_t)ctx->sm_count * (sizeof(CutDesc) + 256) + 512 + part_bytes(ctx, true, true);
     if (ctx->d_attend && bytes <= ctx->attend_cap) return LSMKV_OK;
     const int rc = grow_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, bytes, bytes, __LINE__);
     if (rc != LSMKV_OK) return rc;
@@ -171,6 +213,7 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
     IoLayout lay(ctx->d_attend);
     job.arrived = reinterpret_cast<unsigned int *>(lay.take<unsigned char>(attend_counter_bytes(ctx)));
     job.cuts = lay.take<CutDesc>((size_t)ctx->sm_count);
+    job.maps = lay.take<unsigned char>((size_t)ctx->sm_count * 256);
     job.parts = lay.take<float>(0);
     job.dp = part_dp(ctx);
     job.wait_cycles = ctx->wait_cycles;
