@@ -53,6 +53,7 @@ struct AttendJob {
     struct CutDesc *cuts;        // many rows: the cut tile that starts in a CTA's span
     void *maps;                  // many rows: two tensor maps per CTA
     uint32_t box_rows;           // tokens of a box, dividing page_tokens
+    uint32_t q_boxes;            // the queries come by boxes too
     long long wait_cycles;
     uint64_t test_drop;          // test hook: ~0 = off
     DevStatus *st;

@@ -31,8 +31,8 @@ struct ManyShape {
     static constexpr int kM = 256, kKeys = 128;
     static constexpr int kStages = DP == 128 ? 5 : 8;
     static constexpr uint32_t kTileBytes = 128 * DP * 2;
-    static constexpr int kLoaders = 2;         // warps
-    // 8 softmax warps, then a warpgroup of loaders, issuer and an idle warp. 384 threads start with
+    static constexpr int kLoaders = 2;         // warps that share a block's rows, by cp.async
+    // 8 softmax warps, then a warpgroup of loaders and the issuer. 384 threads start with
     // 168 registers each (64512); 256 x 208 + 128 x 80 = 63488 of them are in use afterwards.
     static constexpr int kThreads = 12 * 32;
     static constexpr int kSoftmaxRegs = 208, kOtherRegs = 80;
@@ -168,16 +168,13 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const float (&v)[32])
            "r"(addr) : "memory");
 }
 
-__device__ __forceinline__ void tmem_st32u(uint32_t addr, const uint32_t *v)
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[16])
 {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
         :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
            "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
-           "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
-           "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]),
            "r"(addr) : "memory");
 }
 
@@ -256,13 +253,15 @@ __global__ __launch_bounds__(256) void k_attend_merge(const __grid_constant__ At
 
 template <typename T, int DP, bool kBoxes>
 __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1)
-void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ CUtensorMap map)
+void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ CUtensorMap map,
+                   const __grid_constant__ CUtensorMap q_map)
 {
     using Sh = ManyShape<DP>;
     constexpr int kChunks = DP / 8;
     constexpr uint32_t kBlock = 128 * 128;      // bytes of one block of 128 rows x 64 elements
+    constexpr uint32_t kIssuer = 10;            // its warp
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * Sh::kStages + 12];
+    __shared__ __align__(8) uint64_t bars[3 * Sh::kStages + 14];
     __shared__ uint32_t tmem_slot;
     __shared__ __align__(128) unsigned char map_work[128];
     __shared__ volatile uint32_t stop;
@@ -291,6 +290,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     auto o_full = [&](uint32_t x) { return q_empty + 40 + 8 * x; };
     const uint32_t half_bar = q_empty + 56, half_read = q_empty + 64, done_bar = q_empty + 72,
                    spare_bar = q_empty + 80;
+    auto p_half = [&](uint32_t x) { return q_empty + 88 + 8 * x; };
+    auto landed = [&](uint32_t s) { return q_empty + 104 + 8 * s; };   // boxes that are still to be wiped
     if (tid == 0) {
         mbar_init(half_bar, 128);
         mbar_init(half_read, 128);
@@ -299,12 +300,14 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         for (int s = 0; s < Sh::kStages; ++s) {
             mbar_init(full(s), kBoxes ? 1 : 32 * Sh::kLoaders);
             mbar_init(empty(s), 1);
+            mbar_init(landed(s), 1);
         }
-        mbar_init(q_full, 32 * Sh::kLoaders);
+        mbar_init(q_full, kBoxes && j.q_boxes ? 1 : 32 * Sh::kLoaders);
         mbar_init(q_empty, 1);
         for (int x = 0; x < 2; ++x) {
             mbar_init(s_full(x), 1);
-            mbar_init(p_full(x), 128);
+            mbar_init(p_half(x), 4);
+            mbar_init(p_full(x), 4);
             mbar_init(o_full(x), 1);
         }
         stop = 0;
@@ -386,23 +389,6 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     l *= fix;
                 }
                 const float neg = m == -INFINITY ? 0.f : -m;
-                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                const float2 cc = make_float2(c, c), nn = make_float2(neg, neg);
-#pragma unroll
-                for (int ch = 0; ch < 2; ++ch) {
-                    uint32_t pk[32];
-#pragma unroll
-                    for (int e = 0; e < 64; e += 2) {
-                        float2 x = fma2(make_float2(v[ch * 64 + e], v[ch * 64 + e + 1]), cc, nn);
-                        x.x = exp2f(x.x);
-                        x.y = exp2f(x.y);
-                        sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], x);
-                        // the weights are rounded to the values' type: the tensor cores take both in one
-                        pk[e / 2] = Half2<T>::down(x.x, x.y);
-                    }
-                    tmem_st32u(s_t + ch * 32, pk);
-                }
-                l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 if (__any_sync(~0u, fix != 1.f)) {
                     // the value product of the tile before is done: its scores came after it
 #pragma unroll 1
@@ -416,15 +402,40 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                         tmem_st32(o_t + ch * 32, o);
                     }
                 }
-                tmem_wait_st();
                 if (half_due) {
-                    // these weights let the issuer overwrite the sums that the first half merges
+                    // the weights let the issuer overwrite the sums that the first half merges
                     if (!(alive = wait_warp(half_read, half_cnt & 1))) break;
                     ++half_cnt;
                     half_due = false;
                 }
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                const float2 cc = make_float2(c, c), nn = make_float2(neg, neg);
+#pragma unroll
+                for (int ch = 0; ch < 4; ++ch) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float2 x = fma2(make_float2(v[ch * 32 + e], v[ch * 32 + e + 1]), cc, nn);
+                        x.x = exp2f(x.x);
+                        x.y = exp2f(x.y);
+                        sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], x);
+                        // the weights are rounded to the values' type: the tensor cores take both in one
+                        pk[e / 2] = Half2<T>::down(x.x, x.y);
+                    }
+                    if (ch == 2) {
+                        // the weights of the first 64 keys are in place: their product may begin
+                        tmem_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(p_half(x));
+                    }
+                    tmem_st16(s_t + ch * 16, pk);
+                }
+                l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                tmem_wait_st();
                 tc_fence_before();
-                mbar_arrive(p_full(x));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full(x));
             }
             if (alive && n) {
                 alive = wait_warp(o_full(x), o_cnt & 1);
@@ -533,18 +544,23 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(Sh::kOtherRegs));
     }
-    if (w >= 8 && w < 8 + Sh::kLoaders) {
-        // ---- loaders
+    if (w >= 8 && w != kIssuer) {
+        // ---- loaders. With boxes: warp 8 keys and values, warp 9 queries (and warp 11, if by
+        // cp.async) and what is left to wipe. Otherwise warps 8 and 9 everything, half the rows each.
         constexpr int kSets = 4 / Sh::kLoaders;              // sets of 32 rows a warp takes of a block of 128
-        const uint32_t r0 = (w - 8) * 32 * kSets;
+        const uint32_t r0 = ((kBoxes ? w == 11 : w == 9) ? 1 : 0) * 32 * kSets;
         const uint64_t tok_stride = (uint64_t)j.n_kv_heads * D;
-        uint32_t stage = 0, laps = 0, q_cnt = 0;
-        bool alive = true;
+        uint32_t stage = 0, laps = 0, q_cnt = 0, wiped = 0;     // wiped: a parity per stage
+        bool alive = kBoxes ? w != 11 || !j.q_boxes : w != 11;
 
         // The barrier is arrived at, for this thread, when its copies so far have landed; the
         // issuer's proxy fence behind its wait makes them visible to the matrix unit.
         auto hand_over = [&](uint32_t bar) {
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" :: "r"(bar) : "memory");
+        };
+        auto expect = [&](uint32_t bar, uint32_t bytes) {
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
+                         :: "r"(bar), "r"(bytes) : "memory");
         };
         // 32 rows of a block of 128 from row `first` on; row r at src + off(lane r), if ok(lane r).
         // Four lanes take 64 bytes of a row, eight rows at a time: with the swizzle (piece c of row r
@@ -592,15 +608,29 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         while (alive && cw.next(j, span)) {
             const Item &it = cw.it;
             const uint32_t row_base = cw.p.rt * Sh::kM;
-            const uint32_t key_end = min(token_limit(it, (row_base + cw.p.rows - 1) / G),
-                                         it.kv0 + cw.p.k1 * Sh::kKeys);
             const uint32_t n = cw.p.k1 - cw.p.k0;
             const uint32_t key0 = it.kv0 + cw.p.k0 * Sh::kKeys;
+            const uint32_t key_end = min(token_limit(it, (row_base + cw.p.rows - 1) / G), key0 + n * Sh::kKeys);
+            // Boxes are whole: rows behind the last key hold whatever the page holds there, or what
+            // the stage held before. Keys are masked, but a value times zero need not be zero.
+            const bool ragged = kBoxes && key_end < key0 + n * Sh::kKeys;
             // the queries, once the products of the cut before have read theirs
             auto fetch_queries = [&]() {
                 if (!(alive = wait_warp(q_empty, (q_cnt & 1) ^ 1))) return;
                 ++q_cnt;
-                for (uint32_t x = 0; x < 2 && x * 128 < cw.p.rows; ++x) {
+                const uint32_t halves = cw.p.rows > 128 ? 2 : 1;
+                if (kBoxes && j.q_boxes) {
+                    if (lane == 0) {
+                        expect(q_full, halves * Sh::kTileBytes);
+                        for (uint32_t x = 0; x < halves; ++x)
+                            for (int e = 0; e < DP / 64; ++e)
+                                tma_box(q_s + x * Sh::kTileBytes + e * kBlock, &q_map, e * 64, (int)(cw.p.kv_head * G),
+                                        (int)(it.row0 + (row_base + x * 128) / G), q_full);
+                    }
+                    __syncwarp();
+                    return;
+                }
+                for (uint32_t x = 0; x < halves; ++x) {
 #pragma unroll
                     for (int y = 0; y < kSets; ++y) {
                         const uint32_t r = x * 128 + r0 + y * 32 + lane;
@@ -623,12 +653,31 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 st_flag(j.st, LSMKV_ST_BAD_PAGE, entry);
                 return kBoxes ? (uint32_t)j.num_pages : kNone;    // the copy engine reads zeros there
             };
-            if constexpr (kBoxes) {
-                // lane g takes tokens [g box_rows, (g + 1) box_rows) of every key tile, one page's
-                if (w != 8) {
-                    fetch_queries();
-                    continue;
+            if (kBoxes && w != 8) {
+                fetch_queries();
+                if (w != 9) continue;
+                // the last values of the cut: stage of position 2n - 1 from here
+                stage += 2 * n - 1;
+                laps += stage / Sh::kStages;
+                stage %= Sh::kStages;
+                if (ragged && alive) {
+                    if (!(alive = wait_warp(landed(stage), (wiped >> stage) & 1))) break;
+                    wiped ^= 1u << stage;
+                    const uint32_t at = ring + stage * Sh::kTileBytes;
+                    const uint32_t last0 = key0 + (n - 1) * Sh::kKeys;
+                    const uint32_t first = key_end > last0 ? key_end - last0 : 0;
+                    for (uint32_t y = first * 8 + lane; y < Sh::kKeys * 8; y += 32)
+#pragma unroll
+                        for (int e = 0; e < DP / 64; ++e)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};"
+                                         :: "r"(at + e * kBlock + y * 16), "r"(0) : "memory");
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(full(stage));
                 }
+                next_stage();
+            } else if (kBoxes) {
+                // lane g takes tokens [g box_rows, (g + 1) box_rows) of every key tile, one page's
                 const uint32_t g0 = lane * j.box_rows;
                 uint32_t page = g0 < Sh::kKeys ? page_of(key0 + g0) : kNone;
                 for (uint32_t t = 0; t < n; ++t) {
@@ -636,14 +685,12 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     const bool ok = page != kNone;
                     const int token = (int)(page * j.page_tokens + k % j.page_tokens);
                     if (t + 1 < n && g0 < Sh::kKeys) page = page_of(k + Sh::kKeys);
-                    const uint32_t bytes = __popc(__ballot_sync(~0u, ok)) * (DP / 64) * j.box_rows * 128;
+                    const uint32_t total = __popc(__ballot_sync(~0u, ok)) * (DP / 64) * j.box_rows * 128;
 #pragma unroll
                     for (int kv = 0; kv < 2; ++kv) {
                         if (!take_stage()) break;
-                        const uint32_t bar = stage_bar();
-                        if (lane == 0)
-                            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
-                                         :: "r"(bar), "r"(bytes) : "memory");
+                        const uint32_t bar = kv && ragged && t + 1 == n ? landed(stage) : stage_bar();
+                        if (lane == 0) expect(bar, total);
                         __syncwarp();
                         if (ok) {
 #pragma unroll
@@ -652,8 +699,6 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                                         (int)cw.p.kv_head, token, bar);
                         }
                         next_stage();
-                        if (t == 0 && kv == 0) fetch_queries();
-                        if (!alive) break;
                     }
                     if (!alive) break;
                 }
@@ -695,138 +740,126 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 if (lap) (void)mbar_wait_bounded(full(s), (lap - 1) & 1, j.wait_cycles);
             }
         }
-    } else if (w == 8 + Sh::kLoaders) {
-        // ---- issuer: the warp walks and waits together, one lane issues
+    } else if (w == kIssuer) {
+        // ---- issuer: the warp walks together, one lane waits and issues
         const uint32_t type = std::is_same<T, __half>::value ? 0u : 1u;
         const uint32_t common = (1u << 4) | (type << 7) | (type << 10) | (8u << 24);   // f32 sums, M = 128
         const uint32_t k_steps = (D + 15) / 16, n_out = k_steps * 16;
         const uint32_t id_s = common | ((Sh::kKeys / 8) << 17) | (j.scale_log2 < 0.f ? 1u << 13 : 0u);
         const uint32_t id_o = common | ((n_out / 8) << 17) | (1u << 16);
-        uint32_t pos = 0;             // tiles taken from the ring: keys and values in turn
-        uint32_t q_cnt = 0, p_cnt[2] = {0, 0};
-        bool alive = true;
-        auto stage_of = [&](uint32_t at) { return at % Sh::kStages; };
-        auto lap_of = [&](uint32_t at) { return (at / Sh::kStages) & 1; };
+        const bool leader = elect_one();
+        const bool fenced = !kBoxes;
+        // places in the ring: keys of tile t at 2 t, values behind them
+        struct Place {
+            uint32_t st, ph;
+            __device__ __forceinline__ void step(uint32_t by)
+            {
+                st += by;
+                if (st >= Sh::kStages) {
+                    st -= Sh::kStages;
+                    ph ^= 1;
+                }
+            }
+        };
+        Place kp = {0, 0};
+        uint32_t q_par = 0, p_par = 0;
+        const uint64_t q_desc = desc_k_major(q_s), k_desc = desc_k_major(ring), v_desc = desc_mn_major(ring, kBlock);
+        // cp.async wrote through another proxy than the matrix unit reads through
+        auto wait_tile = [&](const Place &at) {
+            if (!wait(full(at.st), at.ph)) return false;
+            if (fenced) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            return true;
+        };
         auto scores = [&](uint32_t x, uint32_t q, uint32_t st) {      // S_x = Q_q K^T
-            if (!elect_one()) return;
-            const uint64_t a = desc_k_major(q_s + q * Sh::kTileBytes), b = desc_k_major(ring + st * Sh::kTileBytes);
+            const uint64_t a = q_desc + q * (Sh::kTileBytes >> 4), b = k_desc + st * (Sh::kTileBytes >> 4);
 #pragma unroll
             for (uint32_t k = 0; k < DP / 16; ++k) {
                 const uint64_t step = (k >> 2) * (kBlock >> 4) + (k & 3) * 2;   // 64 elements a block, 16 a step
                 if (k < k_steps) mma_ss(tmem + x * 128, a + step, b + step, id_s, k != 0);
             }
+            mma_commit(s_full(x));
         };
+        // O_x += P_x V, the first 64 keys as soon as their weights are there
         auto values = [&](uint32_t x, uint32_t st, bool add) {
-            if (!elect_one()) return;
-            const uint64_t b = desc_mn_major(ring + st * Sh::kTileBytes, kBlock);
+            const uint64_t b = v_desc + st * (Sh::kTileBytes >> 4);
+            const uint32_t par = (p_par >> x) & 1;
+            p_par ^= 1u << x;
 #pragma unroll
-            for (uint32_t k = 0; k < Sh::kKeys / 16; ++k)
-                mma_ts(tmem + 256 + x * 128, tmem + x * 128 + k * 8, b + k * (2048 >> 4), id_o, add || k != 0);
-        };
-        // copies have landed: order them before the matrix unit's reads
-        auto wait_tile = [&](uint32_t bar, uint32_t parity) {
-            const bool ok = wait_warp(bar, parity);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            return ok;
-        };
-        // Boxes are whole: rows behind the last key hold whatever the page holds there, or nothing
-        // new at all. Keys are masked, but a value times zero need not be zero.
-        auto wipe = [&](uint32_t st, uint32_t key, uint32_t key_end) {
-            if (!kBoxes || key + Sh::kKeys <= key_end) return;
-            const uint32_t first = key < key_end ? key_end - key : 0;
-            for (uint32_t x = first * 8 + lane; x < Sh::kKeys * 8; x += 32)
+            for (uint32_t h = 0; h < 2; ++h) {
+                if (!wait(h ? p_full(x) : p_half(x), par)) return false;
+                tc_fence_after();
 #pragma unroll
-                for (int e = 0; e < DP / 64; ++e)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};"
-                                 :: "r"(ring + st * Sh::kTileBytes + e * kBlock + x * 16), "r"(0) : "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
+                for (uint32_t k = h * 4; k < h * 4 + 4; ++k)
+                    mma_ts(tmem + 256 + x * 128, tmem + x * 128 + k * 8, b + k * (2048 >> 4), id_o, add || k != 0);
+            }
+            return true;
         };
-        auto commit = [&](uint32_t bar) {
-            if (elect_one()) mma_commit(bar);
-        };
-        CutWalk cw;
-        cw.start(j, span);
-        while (alive && cw.next(j, span)) {
-            const uint32_t n = cw.p.k1 - cw.p.k0;
-            const uint32_t nx[2] = {half_tiles(j, cw.it, cw.p, 0, Sh::kM, Sh::kKeys),
-                                    half_tiles(j, cw.it, cw.p, 1, Sh::kM, Sh::kKeys)};
-            const bool both = shares_rows(cw.p);
-            const uint32_t key0 = cw.it.kv0 + cw.p.k0 * Sh::kKeys;
-            const uint32_t key_end = token_limit(cw.it, (cw.p.rt * Sh::kM + cw.p.rows - 1) / G);
-            const uint32_t at = pos;      // keys of tile t at position at + 2 t, values behind them
-            pos += 2 * n;
-            if (!(alive = wait_tile(q_full, q_cnt & 1))) break;
-            ++q_cnt;
+        auto run_cut = [&](uint32_t n, uint32_t n0, uint32_t n1, bool both) -> bool {
+            Place vp = kp;
+            vp.step(1);
+            if (!wait(q_full, q_par)) return false;
+            q_par ^= 1;
+            if (!kBoxes || !j.q_boxes) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             if (both) {
                 // tile t belongs to half t % 2
                 for (uint32_t t = 0; t < n + 2; ++t) {
                     const uint32_t x = t & 1;
                     if (t >= 2) {
-                        const uint32_t v_at = at + 2 * (t - 2) + 1;
-                        if (!(alive = wait_tile(full(stage_of(v_at)), lap_of(v_at)))) break;
-                        if (!(alive = wait_warp(p_full(x), p_cnt[x] & 1))) break;
-                        ++p_cnt[x];
-                        tc_fence_after();
-                        wipe(stage_of(v_at), key0 + (t - 2) * Sh::kKeys, key_end);
-                        values(x, stage_of(v_at), t >= 4);
-                        commit(empty(stage_of(v_at)));
-                        if (t >= n) commit(o_full(x));
+                        if (!wait_tile(vp) || !values(x, vp.st, t >= 4)) return false;
+                        mma_commit(empty(vp.st));
+                        if (t >= n) mma_commit(o_full(x));
+                        vp.step(2);
                     }
                     if (t < n) {
-                        const uint32_t k_at = at + 2 * t;
-                        if (!(alive = wait_tile(full(stage_of(k_at)), lap_of(k_at)))) break;
-                        tc_fence_after();
-                        scores(x, 0, stage_of(k_at));
-                        commit(s_full(x));
-                        commit(empty(stage_of(k_at)));
-                        if (t + 1 == n) commit(q_empty);
+                        if (!wait_tile(kp)) return false;
+                        scores(x, 0, kp.st);
+                        mma_commit(empty(kp.st));
+                        if (t + 1 == n) mma_commit(q_empty);
+                        kp.step(2);
                     }
                 }
-                continue;
+                return true;
             }
-            if (!(alive = wait_tile(full(stage_of(at)), lap_of(at)))) break;
-            tc_fence_after();
-            for (uint32_t x = 0; x < 2; ++x)
-                if (nx[x]) {
-                    scores(x, x, stage_of(at));
-                    commit(s_full(x));
-                }
-            commit(empty(stage_of(at)));
-            if (n == 1) commit(q_empty);
-            for (uint32_t t = 0; t < n && alive; ++t) {
-                const uint32_t v_at = at + 2 * t + 1, k_at = v_at + 1;
-                if (!(alive = wait_tile(full(stage_of(v_at)), lap_of(v_at)))) break;
-                wipe(stage_of(v_at), key0 + t * Sh::kKeys, key_end);
-                bool key_here = false;
+            if (!wait_tile(kp)) return false;
+            if (n0) scores(0, 0, kp.st);
+            if (n1) scores(1, 1, kp.st);
+            mma_commit(empty(kp.st));
+            if (n == 1) mma_commit(q_empty);
+            kp.step(2);
+            for (uint32_t t = 0; t < n; ++t) {
+                const bool more = t + 1 < n;
+                if (!wait_tile(vp) || (more && !wait_tile(kp))) return false;
+#pragma unroll
                 for (uint32_t x = 0; x < 2; ++x) {
-                    if (t < nx[x]) {
-                        if (!(alive = wait_warp(p_full(x), p_cnt[x] & 1))) break;
-                        ++p_cnt[x];
-                        tc_fence_after();
-                        values(x, stage_of(v_at), t != 0);
-                    }
-                    if (t + 1 < nx[x]) {
-                        if (!key_here && !(alive = wait_tile(full(stage_of(k_at)), lap_of(k_at)))) break;
-                        key_here = true;
-                        tc_fence_after();
-                        scores(x, x, stage_of(k_at));
-                        commit(s_full(x));
-                    } else if (t + 1 == nx[x]) {
-                        commit(o_full(x));
-                    }
+                    const uint32_t nx = x ? n1 : n0;
+                    if (t < nx && !values(x, vp.st, t != 0)) return false;
+                    if (t + 1 < nx) scores(x, x, kp.st);
+                    else if (t + 1 == nx) mma_commit(o_full(x));
                 }
-                if (!alive) break;
-                commit(empty(stage_of(v_at)));
-                if (t + 1 < n) {
-                    commit(empty(stage_of(k_at)));
-                    if (t + 2 == n) commit(q_empty);
+                mma_commit(empty(vp.st));
+                vp.step(2);
+                if (more) {
+                    mma_commit(empty(kp.st));
+                    if (t + 2 == n) mma_commit(q_empty);
+                    kp.step(2);
                 }
             }
+            return true;
+        };
+        CutWalk cw;
+        cw.start(j, span);
+        while (cw.next(j, span)) {
+            bool ok = true;
+            if (leader)
+                ok = run_cut(cw.p.k1 - cw.p.k0, half_tiles(j, cw.it, cw.p, 0, Sh::kM, Sh::kKeys),
+                             half_tiles(j, cw.it, cw.p, 1, Sh::kM, Sh::kKeys), shares_rows(cw.p));
+            if (!__all_sync(~0u, ok)) break;
         }
         // products still under way read shared memory and write TMEM: let them end
-        commit(done_bar);
-        (void)mbar_wait_bounded(done_bar, 0, j.wait_cycles);
+        if (leader) {
+            mma_commit(done_bar);
+            (void)mbar_wait_bounded(done_bar, 0, j.wait_cycles);
+        }
     }
     __syncwarp();
     asm volatile("cp.async.wait_all;" ::: "memory");

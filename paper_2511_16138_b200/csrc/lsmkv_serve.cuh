@@ -53,10 +53,9 @@ int launch_few(lsmkv_ctx *ctx, cudaStream_t s, const AttendJob &job)
     return LSMKV_OK;
 }
 
-// A layer's key or value buffer as the copy engine sees it -- elements, heads, tokens; boxes of 64
-// elements of one head x box_rows tokens, swizzled -- all but its address, which the kernel fills
-// in. False: the pool is none that the copy engine can take that way.
-bool make_pool_map(const lsmkv_ctx *ctx, uint32_t dtype, uint64_t num_pages, uint32_t box_rows, CUtensorMap *map)
+// Rows as the copy engine sees them: elements, heads, tokens; boxes of 64 elements, swizzled.
+bool make_map(uint32_t dtype, const void *base, const uint64_t (&dims)[3], uint64_t head_stride,
+              uint64_t token_stride, uint32_t box_heads, uint32_t box_tokens, CUtensorMap *map)
 {
     static const PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
         void *p = nullptr;
@@ -68,16 +67,12 @@ bool make_pool_map(const lsmkv_ctx *ctx, uint32_t dtype, uint64_t num_pages, uin
         }
         return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
     }();
-    const lsmkv_geom_t &g = ctx->geom;
-    const uint64_t tokens = num_pages * g.page_tokens;
-    if (!encode || num_pages == 0 || tokens / g.page_tokens != num_pages ||
-        tokens + g.page_tokens > 0x7FFFFFFFull)              // coordinates are 32-bit
-        return false;
-    const cuuint64_t dims[3] = {g.head_dim, g.n_kv_heads, tokens};
-    const cuuint64_t strides[2] = {g.head_dim * 2ull, (cuuint64_t)g.n_kv_heads * g.head_dim * 2};
-    const cuuint32_t box[3] = {64, 1, box_rows}, step[3] = {1, 1, 1};
+    if (!encode || dims[2] == 0 || dims[2] > 0x7FFFFFFFull) return false;     // coordinates are 32-bit
+    const cuuint64_t d[3] = {dims[0], dims[1], dims[2]};
+    const cuuint64_t strides[2] = {head_stride * 2, token_stride * 2};
+    const cuuint32_t box[3] = {64, box_heads, box_tokens}, step[3] = {1, 1, 1};
     return encode(map, dtype == LSMKV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                  3, ctx->d_attend, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  3, const_cast<void *>(base), d, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -88,18 +83,27 @@ int launch_many(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
     const unsigned sm = (unsigned)ctx->sm_count;
     // Tokens of a box: the largest power of two that divides the page, at most 64. The swizzle's
     // unit is 8 rows, so boxes of fewer than 8 are out and cp.async takes such pages.
-    job.box_rows = std::min(job.page_tokens & (~job.page_tokens + 1), 64u);
-    CUtensorMap map;
+    const lsmkv_geom_t &g = ctx->geom;
+    const uint32_t dtype = std::is_same<T, __half>::value ? LSMKV_F16 : LSMKV_BF16;
+    job.box_rows = std::min(g.page_tokens & (~g.page_tokens + 1), 64u);
+    CUtensorMap map, q_map;
     std::memset(&map, 0, sizeof(map));
-    const bool boxes = job.box_rows >= 8 &&
-                       make_pool_map(ctx, std::is_same<T, __half>::value ? LSMKV_F16 : LSMKV_BF16, job.num_pages,
-                                     job.box_rows, &map);
+    std::memset(&q_map, 0, sizeof(q_map));
+    // (the map's address is filled in by the kernel, which finds it in the pool's table)
+    const uint64_t row = (uint64_t)g.n_kv_heads * g.head_dim;
+    const bool boxes = job.box_rows >= 8 && job.num_pages < 0x7FFFFFFFull / g.page_tokens &&
+                       make_map(dtype, ctx->d_attend, {g.head_dim, g.n_kv_heads, job.num_pages * g.page_tokens},
+                                g.head_dim, row, 1, job.box_rows, &map);
+    // The 128 rows of half a tile are a box of queries when the heads of a KV head divide them.
+    job.q_boxes = boxes && job.group <= 128 && (job.group & (job.group - 1)) == 0 &&
+                  make_map(dtype, job.q, {g.head_dim, job.n_q_heads, job.seqs.n_new}, job.q_hs, job.q_ts, job.group,
+                           128 / job.group, &q_map);
     if (job.head_dim <= 64) {
         auto kern = boxes ? k_attend_many<T, 64, true> : k_attend_many<T, 64, false>;
-        kern<<<sm, ManyShape<64>::kThreads, ManyShape<64>::kSmem, s>>>(job, map);
+        kern<<<sm, ManyShape<64>::kThreads, ManyShape<64>::kSmem, s>>>(job, map, q_map);
     } else {
         auto kern = boxes ? k_attend_many<T, 128, true> : k_attend_many<T, 128, false>;
-        kern<<<sm, ManyShape<128>::kThreads, ManyShape<128>::kSmem, s>>>(job, map);
+        kern<<<sm, ManyShape<128>::kThreads, ManyShape<128>::kSmem, s>>>(job, map, q_map);
     }
     ++ctx->launches;
     CU(ctx, cudaGetLastError());
