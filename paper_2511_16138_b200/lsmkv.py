@@ -105,10 +105,6 @@ class SeqsStruct(C.Structure):
                 ("page_table", C.c_void_p)]
 
 
-class RowsStruct(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_uint64), ("head_stride", C.c_uint64)]
-
-
 class RopeStruct(C.Structure):
     _fields_ = [("table", C.c_void_p), ("positions", C.c_void_p), ("n_pos", C.c_uint64),
                 ("rot_dim", C.c_uint32), ("interleaved", C.c_uint32)]
@@ -264,10 +260,18 @@ def _ptr(x):
     return x.data_ptr()
 
 
+_raw_stream = None
+
+
 def _stream(stream):
+    global _raw_stream
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _raw_stream is None:
+            import torch
+            get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            _raw_stream = ((lambda: get(torch._C._cuda_getDevice())) if get is not None else
+                           lambda: torch.cuda.current_stream().cuda_stream)
+        return _raw_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -500,33 +504,40 @@ def lsmkv_decode_batch_static(geom: Geom, device, stream, n_query, qchunk_off, n
         raise LsmkvError(rc, "lsmkv_decode_batch_static")
 
 
-def _rows(t, head_dim: int):
-    """[n_new, heads, head_dim] tensor, strided or not -> lsmkv_rows_t."""
-    if t.dim() != 3 or t.shape[2] != head_dim or (t.stride(2) != 1 and head_dim != 1):
-        raise ValueError(f"rows must be [tokens, heads, {head_dim}] with contiguous elements, "
-                         f"got {tuple(t.shape)} with strides {t.stride()}")
-    return RowsStruct(t.data_ptr(), t.stride(0), t.stride(1))
+_NO_ROWS = (None, 0, 0)
 
 
-def _dtype(*tensors) -> int:
+def _rows(name, t, n_new: int, heads: int, head_dim: int):
+    """(address, token stride, head stride) of a [n_new, heads, head_dim] tensor, strided or not."""
+    if t.shape != (n_new, heads, head_dim):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, the batch {n_new} new tokens of "
+                         f"{heads} heads of {head_dim}")
+    token, head, element = t.stride()
+    if element != 1 and head_dim != 1:
+        raise ValueError(f"{name}: the elements of a head must be contiguous, strides {t.stride()}")
+    return t.data_ptr(), token, head
+
+
+_DTYPES = {}
+
+
+def _dtype(first, *others) -> int:
     """The one 16-bit float type of the given tensors (None among them is skipped)."""
-    import torch
-    kinds = {t.dtype for t in tensors if t is not None}
-    if len(kinds) != 1 or not kinds <= {torch.bfloat16, torch.float16}:
-        raise TypeError(f"bfloat16 or float16 throughout, got {kinds}")
-    return BF16 if torch.bfloat16 in kinds else F16
-
-
-def _tokens(seqs, geom, *named):
-    for name, t, heads in named:
-        if t is not None and (t.shape[0] != seqs.n_new or t.shape[1] != heads):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, the batch {seqs.n_new} new "
-                             f"tokens of {heads} heads")
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.bfloat16: BF16, torch.float16: F16})
+    kind = first.dtype
+    for t in others:
+        if t is not None and t.dtype is not kind:
+            raise TypeError(f"one type throughout, got {kind} and {t.dtype}")
+    if kind not in _DTYPES:
+        raise TypeError(f"bfloat16 or float16, got {kind}")
+    return _DTYPES[kind]
 
 
 def _check_lse(lse, q):
-    if lse is not None and (str(lse.dtype) != "torch.float32" or not lse.is_contiguous() or
-                            lse.numel() != q.shape[0] * q.shape[1]):
+    if (str(lse.dtype) != "torch.float32" or not lse.is_contiguous() or
+            lse.numel() != q.shape[0] * q.shape[1]):
         raise ValueError("lse: contiguous float32 [n_new, n_q_heads]")
 
 
@@ -582,37 +593,51 @@ class Rope:
         self.ref = C.addressof(self.c)
 
 
+_address = C.addressof
+
+
+class _AttendArgs(C.Structure):
+    """What an attend call points at, in one piece: q and out (lsmkv_rows_t), the pool."""
+    _fields_ = [("q", C.c_void_p), ("q_token", C.c_uint64), ("q_head", C.c_uint64),
+                ("out", C.c_void_p), ("out_token", C.c_uint64), ("out_head", C.c_uint64),
+                ("kv_ptrs", C.c_void_p), ("num_pages", C.c_uint64)]
+    OUT, POOL = 24, 48
+
+
+class _AppendArgs(C.Structure):
+    """The same of an append call: k, v, q, q_out, the pool."""
+    _fields_ = [(name + part, kind) for name in ("k", "v", "q", "out")
+                for part, kind in (("", C.c_void_p), ("_token", C.c_uint64), ("_head", C.c_uint64))]
+    _fields_ += [("kv_ptrs", C.c_void_p), ("num_pages", C.c_uint64)]
+    V, Q, OUT, POOL = 24, 48, 72, 96
+
+
 def lsmkv_append_batch(ctx, stream, layer, dtype, seqs, k, v, pool, rope, n_q_heads, q_in, q_out,
                        q_norm, k_norm, eps) -> None:
-    """seqs: Seqs; k, v, q_in, q_out: RowsStruct (or None for the queries); rope: Rope or None."""
-    p = _pool(pool)
-    rc = lib().lsmkv_append_batch(
-        ctx, _stream(stream), layer, dtype, seqs.ref, C.addressof(k), C.addressof(v),
-        C.addressof(p) if p is not None else None, rope.ref if rope is not None else None,
-        n_q_heads, C.addressof(q_in) if q_in is not None else None,
-        C.addressof(q_out) if q_out is not None else None, _ptr(q_norm), _ptr(k_norm), eps)
-    _check(ctx, rc, "lsmkv_append_batch")
+    """The C call; seqs, rope, k, v, q_in, q_out, pool: addresses of their structs, or None."""
+    rc = (_lib or lib()).lsmkv_append_batch(ctx, _stream(stream), layer, dtype, seqs, k, v, pool,
+                                            rope, n_q_heads, q_in, q_out, _ptr(q_norm),
+                                            _ptr(k_norm), eps)
+    if rc:
+        _check(ctx, rc, "lsmkv_append_batch")
 
 
 def lsmkv_attend_batch(ctx, stream, layer, dtype, seqs, n_q_heads, q, pool, scale, out,
                        lse_out=None) -> None:
-    """seqs: Seqs; q, out: RowsStruct."""
-    p = _pool(pool)
-    rc = lib().lsmkv_attend_batch(ctx, _stream(stream), layer, dtype, seqs.ref, n_q_heads,
-                                  C.addressof(q), C.addressof(p) if p is not None else None,
-                                  scale, C.addressof(out), _ptr(lse_out))
-    _check(ctx, rc, "lsmkv_attend_batch")
+    """The C call; seqs, q, pool, out: addresses of their structs."""
+    rc = (_lib or lib()).lsmkv_attend_batch(ctx, _stream(stream), layer, dtype, seqs, n_q_heads, q,
+                                            pool, scale, out, _ptr(lse_out))
+    if rc:
+        _check(ctx, rc, "lsmkv_attend_batch")
 
 
 def lsmkv_attend_shared_batch(ctx, stream, layer, dtype, seqs, groups, n_q_heads, q, pool, scale,
                               out, lse_out=None) -> None:
-    """seqs: Seqs; groups: Groups; q, out: RowsStruct."""
-    p = _pool(pool)
-    rc = lib().lsmkv_attend_shared_batch(ctx, _stream(stream), layer, dtype, seqs.ref, groups.ref,
-                                         n_q_heads, C.addressof(q),
-                                         C.addressof(p) if p is not None else None, scale,
-                                         C.addressof(out), _ptr(lse_out))
-    _check(ctx, rc, "lsmkv_attend_shared_batch")
+    """The C call; seqs, groups, q, pool, out: addresses of their structs."""
+    rc = (_lib or lib()).lsmkv_attend_shared_batch(ctx, _stream(stream), layer, dtype, seqs, groups,
+                                                   n_q_heads, q, pool, scale, out, _ptr(lse_out))
+    if rc:
+        _check(ctx, rc, "lsmkv_attend_shared_batch")
 
 
 def lsmkv_last_status(ctx, stream=None) -> dict:
@@ -748,38 +773,48 @@ class Context:
         """k, v [n_new, n_kv_heads, head_dim] into the pool; q [n_new, n_q_heads, head_dim] ->
         q_out (q itself when None). Strided views are fine."""
         g = self.geom
-        if q is not None and q_out is None:
-            q_out = q
-        heads = 0 if q is None else q.shape[1]
-        _tokens(seqs, g, ("k", k, g.n_kv_heads), ("v", v, g.n_kv_heads), ("q_out", q_out, heads))
-        if q is not None and q.shape[0] != seqs.n_new:
-            raise ValueError(f"q has {q.shape[0]} rows, the batch {seqs.n_new} new tokens")
+        dim, n = g.head_dim, seqs.n_new
+        kk, vv = _rows("k", k, n, g.n_kv_heads, dim), _rows("v", v, n, g.n_kv_heads, dim)
+        heads, qq, oo = 0, _NO_ROWS, _NO_ROWS
+        if q is not None:
+            if q_out is None:
+                q_out = q
+            heads = q.shape[1]
+            qq, oo = _rows("q", q, n, heads, dim), _rows("q_out", q_out, n, heads, dim)
         for w in (q_norm, k_norm):
-            if w is not None and (w.numel() != g.head_dim or not w.is_contiguous()):
-                raise ValueError(f"norm weights: {g.head_dim} contiguous elements")
-        if rope is not None and rope.n_positions not in (None, seqs.n_new):
-            raise ValueError(f"{rope.n_positions} positions for {seqs.n_new} new tokens")
-        lsmkv_append_batch(self.handle, stream, layer, _dtype(k, v, q, q_out, q_norm, k_norm), seqs,
-                           _rows(k, g.head_dim), _rows(v, g.head_dim), pool, rope, heads,
-                           None if q is None else _rows(q, g.head_dim),
-                           None if q is None else _rows(q_out, g.head_dim), q_norm, k_norm, eps)
+            if w is not None and (w.numel() != dim or not w.is_contiguous()):
+                raise ValueError(f"norm weights: {dim} contiguous elements")
+        if rope is not None and rope.n_positions not in (None, n):
+            raise ValueError(f"{rope.n_positions} positions for {n} new tokens")
+        kv_ptrs, num_pages = pool
+        args = _AppendArgs(*kk, *vv, *qq, *oo, _ptr(kv_ptrs), num_pages)
+        at = _address(args)
+        lsmkv_append_batch(self.handle, stream, layer, _dtype(k, v, q, q_out, q_norm, k_norm),
+                           seqs.ref, at, at + args.V, at + args.POOL,
+                           None if rope is None else rope.ref, heads, at + args.Q if heads else None,
+                           at + args.OUT if heads else None, q_norm, k_norm, eps)
+
+    def _attend_args(self, seqs, q, out, pool, lse):
+        dim, n, heads = self.geom.head_dim, seqs.n_new, q.shape[1]
+        if lse is not None:
+            _check_lse(lse, q)
+        kv_ptrs, num_pages = pool
+        return heads, _AttendArgs(*_rows("q", q, n, heads, dim), *_rows("out", out, n, heads, dim),
+                                  _ptr(kv_ptrs), num_pages)
 
     def attend_batch(self, layer, seqs, q, out, pool, scale, lse=None, stream=None):
         """q, out [n_new, n_q_heads, head_dim]; lse float32 [n_new, n_q_heads] or None."""
-        g = self.geom
-        _tokens(seqs, g, ("q", q, q.shape[1]), ("out", out, q.shape[1]))
-        _check_lse(lse, q)
-        lsmkv_attend_batch(self.handle, stream, layer, _dtype(q, out), seqs, q.shape[1],
-                           _rows(q, g.head_dim), pool, scale, _rows(out, g.head_dim), lse)
+        heads, args = self._attend_args(seqs, q, out, pool, lse)
+        at = _address(args)
+        lsmkv_attend_batch(self.handle, stream, layer, _dtype(q, out), seqs.ref, heads, at,
+                           at + args.POOL, scale, at + args.OUT, lse)
 
     def attend_shared_batch(self, layer, seqs, groups, q, out, pool, scale, lse=None, stream=None):
         """attend_batch for sequences in groups with common pages ahead (Groups)."""
-        g = self.geom
-        _tokens(seqs, g, ("q", q, q.shape[1]), ("out", out, q.shape[1]))
-        _check_lse(lse, q)
-        lsmkv_attend_shared_batch(self.handle, stream, layer, _dtype(q, out), seqs, groups,
-                                  q.shape[1], _rows(q, g.head_dim), pool, scale,
-                                  _rows(out, g.head_dim), lse)
+        heads, args = self._attend_args(seqs, q, out, pool, lse)
+        at = _address(args)
+        lsmkv_attend_shared_batch(self.handle, stream, layer, _dtype(q, out), seqs.ref, groups.ref,
+                                  heads, at, at + args.POOL, scale, at + args.OUT, lse)
 
     def last_status(self, stream=None) -> dict:
         return lsmkv_last_status(self.handle, stream)
