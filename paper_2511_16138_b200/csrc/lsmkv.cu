@@ -241,15 +241,22 @@ cudaError_t set_copy_smem_limit(int max_smem_optin)
     if (e == cudaSuccess)
         e = cudaFuncSetAttribute(k_xpf_encode<XpfShape16k>,
                                  cudaFuncAttributeMaxDynamicSharedMemorySize, (int)XpfShape16k::kSmem);
-    for (auto *few : {k_attend_few<__nv_bfloat16, 64, 4, 6>, k_attend_few<__half, 64, 4, 6>})
+    auto raise_few = [&](auto shape, auto *kern) {
         if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FewShape<64, 4, 6>::kSmem);
-    for (auto *few : {k_attend_few<__nv_bfloat16, 128, 4, 3>, k_attend_few<__half, 128, 4, 3>})
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FewShape<128, 4, 3>::kSmem);
-    for (auto *few : {k_attend_few<__nv_bfloat16, 256, 4, 3>, k_attend_few<__half, 256, 4, 3>})
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(few, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FewShape<256, 4, 3>::kSmem);
+            e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)decltype(shape)::kSmem);
+    };
+    raise_few(FewShape<64, 1>(), k_attend_few<__nv_bfloat16, 64, 1>);
+    raise_few(FewShape<64, 2>(), k_attend_few<__nv_bfloat16, 64, 2>);
+    raise_few(FewShape<128, 1>(), k_attend_few<__nv_bfloat16, 128, 1>);
+    raise_few(FewShape<128, 2>(), k_attend_few<__nv_bfloat16, 128, 2>);
+    raise_few(FewShape<256, 1>(), k_attend_few<__nv_bfloat16, 256, 1>);
+    raise_few(FewShape<256, 2>(), k_attend_few<__nv_bfloat16, 256, 2>);
+    raise_few(FewShape<64, 1>(), k_attend_few<__half, 64, 1>);
+    raise_few(FewShape<64, 2>(), k_attend_few<__half, 64, 2>);
+    raise_few(FewShape<128, 1>(), k_attend_few<__half, 128, 1>);
+    raise_few(FewShape<128, 2>(), k_attend_few<__half, 128, 2>);
+    raise_few(FewShape<256, 1>(), k_attend_few<__half, 256, 1>);
+    raise_few(FewShape<256, 2>(), k_attend_few<__half, 256, 2>);
     for (auto *many : {k_attend_many<__nv_bfloat16, 64, true>, k_attend_many<__half, 64, true>,
                        k_attend_many<__nv_bfloat16, 64, false>, k_attend_many<__half, 64, false>})
         if (e == cudaSuccess)
@@ -310,10 +317,10 @@ int ensure_dir(lsmkv_ctx *ctx, uint64_t entries)
                         entries, __LINE__);
 }
 
-// The attend scratch starts with a counter per CTA of its widest launch (two CTAs a SM).
+// The attend scratch starts with a counter per CTA (one CTA a SM).
 size_t attend_counter_bytes(const lsmkv_ctx *ctx)
 {
-    return ((size_t)ctx->sm_count * 2 * 4 + 255) & ~size_t(255);
+    return ((size_t)ctx->sm_count * 4 + 255) & ~size_t(255);
 }
 
 struct SortWs {

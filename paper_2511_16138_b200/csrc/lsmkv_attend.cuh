@@ -14,8 +14,7 @@
 // key tile -- form one line of units that is cut into equal spans, one per CTA: no CTA has more
 // than one unit more than another, whatever the lengths. A row tile cut by a span's end leaves
 // parts in scratch, merged in order by whoever comes after (the CTA that delivers the last part
-// in the few-row kernel, a launch of its own behind the many-row kernel, the own pass for a
-// shared prefix), so that results do not depend on timing. Every CTA finds its span by itself, from the lengths: no launch
+// in the few-row kernel, a launch of its own behind the many-row kernel), so that results do not depend on timing. Every CTA finds its span by itself, from the lengths: no launch
 // before, and nothing for the host to know.
 #pragma once
 #include "lsmkv_append.cuh"
@@ -37,17 +36,15 @@ struct AttendJob {
     uint64_t q_ts, q_hs, o_ts, o_hs;
     float *lse;
     float scale_log2;
-    // Shared prefixes. prefix_pass: the items are the groups; the result of a row tile goes to
-    // pre_o / pre_lse, or stays in pre_parts when the tile is cut; share[] is filled. Otherwise,
-    // with share set, sequence i starts behind its share[i].skip tokens and merges what the
-    // prefix pass left for it into its own result.
+    // Shared prefixes. prefix_pass: the items are the groups, results go to pre_o / pre_lse, and
+    // skip[] is filled; otherwise, with skip set, sequence i starts behind its skip[i] tokens and
+    // merges the prefix pass's result into its own.
     uint32_t prefix_pass, n_group;
     const uint32_t *group_off, *shared_pages;
-    struct Share *share;
+    uint32_t *skip;
     float *pre_o;                // f32 [n_new][n_q_heads][head_dim]
     float *pre_lse;              // f32 [n_new][n_q_heads], base 2
-    float *pre_parts;            // as parts
-    uint32_t pre_rows, dp;       // rows of the prefix pass's tiles; elements of a part's row
+    uint32_t dp;                 // elements of a part's row
     float *parts;                // two slots per CTA
     unsigned int *arrived;       // few rows: one counter per CTA, zero between calls
     struct CutDesc *cuts;        // many rows: the cut tile that starts in a CTA's span
@@ -59,14 +56,6 @@ struct AttendJob {
     DevStatus *st;
 };
 
-// What the prefix pass has for a sequence: the tokens it covers, and where its group's row tiles
-// lie on that pass's line of units.
-struct __align__(16) Share {
-    uint32_t skip, units, tiles, unused;   // units of a tile; tiles of a KV head
-    uint64_t base, row0;                   // first unit and first row of the group
-    uint64_t per, unused2;
-};
-
 // An item: a sequence, or in the prefix pass a group.
 struct Item {
     uint64_t row0, page0;
@@ -74,8 +63,7 @@ struct Item {
     uint32_t kv0, kv1;           // keys [kv0, kv1)
     bool causal;
     bool ok;
-    uint32_t index;              // its number
-    uint32_t skip;               // own pass: tokens whose result the prefix pass has, in share[index]
+    uint32_t skip;               // own pass: tokens whose result the prefix pass has
 };
 
 __device__ __forceinline__ uint32_t shared_tokens(const AttendJob &j, uint32_t g)
@@ -91,7 +79,6 @@ __device__ __forceinline__ uint32_t shared_tokens(const AttendJob &j, uint32_t g
 __device__ __forceinline__ Item load_item(const AttendJob &j, uint32_t i)
 {
     Item it;
-    it.index = i;
     if (j.prefix_pass) {
         const uint32_t a = j.group_off[i], b = j.group_off[i + 1];
         it.kv0 = 0;
@@ -119,10 +106,10 @@ __device__ __forceinline__ Item load_item(const AttendJob &j, uint32_t i)
     it.kv1 = s.kv;
     it.causal = true;
     it.skip = 0;
-    if (j.share && s.ok) {
+    if (j.skip) {
         // a member with a new token inside the shared part goes by itself
-        const uint32_t k = j.share[i].skip;
-        if (s.kv >= s.rows && k <= s.kv - s.rows) it.skip = it.kv0 = k;
+        const uint32_t k = j.skip[i];
+        if (s.ok && s.kv >= s.rows && k <= s.kv - s.rows) it.skip = it.kv0 = k;
     }
     return it;
 }
@@ -165,33 +152,20 @@ __device__ __forceinline__ uint64_t item_units(const AttendJob &j, const Item &i
     return u;
 }
 
-// Group i's place on the prefix pass's line of units, for its members.
-__device__ __forceinline__ void share_group(const AttendJob &j, uint32_t i, const Item &it, uint64_t base,
-                                            uint64_t per_head, uint64_t per, uint32_t M)
-{
-    const uint32_t a = j.group_off[i], b = j.group_off[i + 1];
-    if (a > b || b > j.seqs.n_seq) {
-        st_flag(j.st, LSMKV_ST_BAD_COUNT, i);
-        return;
-    }
-    Share sh;
-    sh.tiles = item_tiles(j, it, M);
-    sh.skip = sh.tiles ? it.kv1 : 0;
-    sh.units = sh.tiles ? (uint32_t)(per_head / sh.tiles) : 1;
-    sh.base = base;
-    sh.row0 = it.row0;
-    sh.per = per;
-    sh.unused = 0;
-    sh.unused2 = 0;
-    for (uint32_t k = a; k < b; ++k) j.share[k] = sh;
-}
-
 // A CTA's place on the line of units.
 struct Span {
     uint64_t begin, end, per;    // units [begin, end); units per CTA
     uint32_t item;               // the item that holds `begin`
     uint64_t before;             // units ahead of that item
 };
+
+// A call's launches follow each other closely: each lets the next one start while it still runs
+// and itself waits, first of all, for what the one before has written.
+__device__ __forceinline__ void follow_launch()
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
 
 // Called by all threads of a CTA (NT of them, a multiple of 32, at most 1024). n items.
 template <int NT>
@@ -233,13 +207,16 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
     if (s.begin > total) s.begin = total;
     uint64_t at = ahead + incl - mine;
     if (j.prefix_pass) {
-        // the groups' places, for the own pass: a CTA writes every gridDim-th group's members
-        uint64_t base = at;
-        for (uint32_t i = i0; i < i1; ++i) {
-            const Item it = load_item(j, i);
-            const uint64_t u = item_units(j, it, M, tile);
-            if (i % gridDim.x == blockIdx.x) share_group(j, i, it, base, u, s.per, M);
-            base += u * j.n_kv_heads;
+        // for the own pass: a CTA fills in every gridDim-th group's members
+        for (uint32_t g = blockIdx.x + tid * gridDim.x; g < n; g += gridDim.x * NT) {
+            const uint32_t a = j.group_off[g], b = j.group_off[g + 1];
+            if (a > b || b > j.seqs.n_seq) {
+                st_flag(j.st, LSMKV_ST_BAD_COUNT, g);
+                continue;
+            }
+            const Item it = load_item(j, g);
+            const uint32_t k = item_tiles(j, it, M) ? it.kv1 : 0;
+            for (uint32_t i = a; i < b; ++i) j.skip[i] = k;
         }
         if (tid == 0 && blockIdx.x == 0 &&
             (j.group_off[0] != 0 || j.group_off[j.n_group] != j.seqs.n_seq))
@@ -352,7 +329,7 @@ struct Walk {
 
 __device__ __forceinline__ float *part_slot(const AttendJob &j, uint64_t slot, uint32_t M, uint32_t DP)
 {
-    return (j.prefix_pass ? j.pre_parts : j.parts) + slot * ((uint64_t)M * (DP + 2));
+    return j.parts + slot * ((uint64_t)M * (DP + 2));
 }
 
 // 2^(x) with 2^(-inf) = 0; statistics of an empty part are m = -inf, l = 0.
@@ -361,46 +338,56 @@ __device__ __forceinline__ float part_weight(float m, float top)
     return m == -INFINITY ? 0.f : exp2f(m - top);
 }
 
-// Add parts c0..c1 of a cut tile, four elements of one row, to (acc, m, l); four parts in flight.
-__device__ __forceinline__ void add_parts(const float *parts, uint32_t c0, uint32_t c1, uint32_t M,
-                                          uint32_t DP, uint32_t r, uint32_t d, float4 &acc, float &m, float &l)
+struct Quad {
+    float4 acc;
+    float m, l;
+};
+
+__device__ __forceinline__ void add_quad(Quad &a, const float4 &o, float m, float l)
+{
+    const float top = fmaxf(a.m, m);
+    const float f = part_weight(a.m, top), g = part_weight(m, top);
+    a.acc.x = a.acc.x * f + o.x * g;
+    a.acc.y = a.acc.y * f + o.y * g;
+    a.acc.z = a.acc.z * f + o.z * g;
+    a.acc.w = a.acc.w * f + o.w * g;
+    a.l = a.l * f + l * g;
+    a.m = top;
+}
+
+// Parts c0..c1 of a cut tile, four elements of row r, merged in order; four parts in flight. (Out
+// of line, like what else ends a row: the loops that come before want the registers.)
+__device__ __noinline__ Quad sum_parts(const float *parts, uint32_t c0, uint32_t c1, uint32_t M, uint32_t DP,
+                                       uint32_t r, uint32_t d)
 {
     constexpr int U = 4;
+    Quad sum;
+    sum.acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    sum.m = -INFINITY;
+    sum.l = 0.f;
     for (uint32_t c = c0; c <= c1; c += U) {
         float pm[U], pl[U];
         float4 o[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint32_t x = c + u <= c1 ? c + u : c1;
-            const float *s = parts + (2ull * x + (x == c0 ? 1 : 0)) * ((uint64_t)M * (DP + 2));
+            pm[u] = -INFINITY;
+            if (c + u > c1) continue;
+            const float *s = parts + (2ull * (c + u) + (c + u == c0 ? 1 : 0)) * ((uint64_t)M * (DP + 2));
             pm[u] = __ldcg(s + (uint64_t)M * DP + r);
             pl[u] = __ldcg(s + (uint64_t)M * (DP + 1) + r);
             o[u] = __ldcg(reinterpret_cast<const float4 *>(s + (uint64_t)r * DP + d));
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (c + u > c1 || pm[u] == -INFINITY) continue;   // no key of this part was the row's
-            const float top = fmaxf(m, pm[u]);
-            const float a = part_weight(m, top), b = part_weight(pm[u], top);
-            acc.x = acc.x * a + o[u].x * b;
-            acc.y = acc.y * a + o[u].y * b;
-            acc.z = acc.z * a + o[u].z * b;
-            acc.w = acc.w * a + o[u].w * b;
-            l = l * a + pl[u] * b;
-            m = top;
-        }
+        for (int u = 0; u < U; ++u)
+            if (pm[u] != -INFINITY) add_quad(sum, o[u], pm[u], pl[u]);   // else no key of it was the row's
     }
+    return sum;
 }
 
 // A row tile's products also run over keys that only later rows of it see, with weight zero:
 // an infinite or undefined value there makes the sum undefined although the row must not see
 // it. A row that comes out undefined and has such keys beside it is taken again here, key by key
 // over its own keys alone; finite inputs never come here.
-struct Quad {
-    float4 acc;
-    float m, l;
-};
-
 template <typename T>
 __device__ __noinline__ Quad redo_row4(const AttendJob &j, uint64_t page0, uint64_t row, uint32_t head,
                                        uint32_t first, uint32_t limit, uint32_t d)
@@ -447,25 +434,16 @@ __device__ __forceinline__ void finish_row4(const AttendJob &j, const Item &it, 
         l = again.l;
     }
     if (it.skip) {
-        // its row tile of the prefix pass: whole, or in parts
-        const Share &sh = j.share[it.index];
-        const uint32_t P = (uint32_t)(row - sh.row0) * j.group + sub, rt = P / j.pre_rows;
-        const uint64_t u0 = sh.base + (uint64_t)(kv_head * sh.tiles + rt) * sh.units;
-        const uint32_t c0 = (uint32_t)(u0 / sh.per), c1 = (uint32_t)((u0 + sh.units - 1) / sh.per);
-        if (c0 != c1) {
-            add_parts(j.pre_parts, c0, c1, j.pre_rows, j.dp, P - rt * j.pre_rows, d, acc, m, l);
-        } else {
-            const float pm = j.pre_lse[flat];
-            const float4 po = *reinterpret_cast<const float4 *>(j.pre_o + flat * j.head_dim + d);
-            const float top = fmaxf(m, pm);
-            const float a = part_weight(m, top), b = part_weight(pm, top);
-            acc.x = acc.x * a + po.x * b;
-            acc.y = acc.y * a + po.y * b;
-            acc.z = acc.z * a + po.z * b;
-            acc.w = acc.w * a + po.w * b;
-            l = l * a + b;
-            m = top;
-        }
+        Quad sum;
+        sum.acc = acc;
+        sum.m = m;
+        sum.l = l;
+        const float pm = j.pre_lse[flat];
+        add_quad(sum, *reinterpret_cast<const float4 *>(j.pre_o + flat * j.head_dim + d), pm,
+                 pm == -INFINITY ? 0.f : 1.f);
+        acc = sum.acc;
+        m = sum.m;
+        l = sum.l;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
@@ -500,10 +478,8 @@ __device__ __forceinline__ void merge_parts(const AttendJob &j, const Item &it, 
     const uint32_t quads = j.head_dim / 4;
     for (uint32_t x = threadIdx.x; x < (r1 - r0) * quads; x += NT) {
         const uint32_t r = r0 + x / quads, d = x % quads * 4;
-        float m = -INFINITY, l = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        add_parts(j.parts, c0, c1, M, j.dp, r, d, acc, m, l);
-        finish_row4<T>(j, it, p.kv_head, p.rt * M + r, d, acc, m, l);
+        const Quad q = sum_parts(j.parts, c0, c1, M, j.dp, r, d);
+        finish_row4<T>(j, it, p.kv_head, p.rt * M + r, d, q.acc, q.m, q.l);
     }
 }
 
@@ -526,12 +502,15 @@ __device__ __forceinline__ bool deliver_part(const AttendJob &j, const Cut &p, u
 // ---- few rows ---------------------------------------------------------------------------------
 //
 // Bound by memory: a decode step reads every key and value once and does 4 G operations a byte.
-// A row tile is 16 rows (one m16n8k16 fragment), a warp takes 16 keys at a time in a private ring
-// of ST stages fed by cp.async (no barrier in the loop: the warps of a CTA share nothing until
-// the tile's end), and the NW warps of a CTA take the key tiles in turn. Two CTAs a SM, so that
-// one streams while the other merges. Rows of a page are contiguous for one head only (256
-// bytes at head_dim 128), and page sizes are the caller's: 16-byte copies, swizzled on their
-// way, take any of them.
+// A row tile is NB blocks of 8 rows. The products are taken the other way round, S^T = K Q^T and
+// O^T = V^T P^T, with the keys (or the elements) as the 16 rows of an m16n8k16 fragment and 8
+// queries as its columns: the legacy matrix path is slow enough here that 16 query rows, of which
+// a decode step has G, would cost more than the memory (823 us instead of 718 for 256 requests
+// of 4.6k tokens). P^T goes from accumulator to operand layout by movmatrix.
+// A warp takes 16 keys at a time in a private ring of ST stages fed by cp.async (no barrier in the
+// loop: the warps of a CTA share nothing until the cut's end), and the NW warps of a CTA take the
+// key tiles in turn. One CTA a SM, and the ring runs ahead over the cuts' ends: the next cut's
+// keys travel while this one's warps merge, which is what short sequences need.
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool real)
 {
@@ -570,267 +549,381 @@ template <> __device__ __forceinline__ void mma16816<__half>(float (&c)[4], cons
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <int DP, int NW, int ST>
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+
+template <int DP, int NB>
 struct FewShape {
-    static constexpr int kM = 16;                          // rows of a tile
+    static constexpr int kM = 8 * NB;                      // rows of a tile
     static constexpr int kKeys = 16;                       // keys a warp takes at a time
-    static constexpr int kThreads = NW * 32;
+    static constexpr int kWarps = DP <= 128 ? 8 : 4;
+    static constexpr int kStages = DP <= 64 ? 6 : 3;       // 192 KB of keys and values a SM
+    static constexpr int kThreads = kWarps * 32;
     static constexpr uint32_t kStage = kKeys * DP * 2 * 2; // K then V
-    static constexpr size_t kQBytes = 16 * DP * 2;
-    static constexpr size_t kSmem = kQBytes + (size_t)NW * ST * kStage;
-    static_assert((size_t)ST * kStage >= 16 * DP * 4, "a warp's ring takes its sums at the tile's end");
+    static constexpr size_t kQBytes = kM * DP * 2;
+    // rows merged at a time: all of them where they fit beside the ring
+    static constexpr uint32_t kMergeRows = (NB == 1 && DP <= 128 ? 32768 : 24576) / (kWarps * DP * 4);
+    static constexpr size_t kMergeBytes = (size_t)kMergeRows * kWarps * DP * 4;
+    static constexpr size_t kSmem = kQBytes + kMergeBytes + (size_t)kWarps * kStages * kStage;
+    // operand fragments of the queries stay in registers while there are few
+    static constexpr bool kQInRegs = DP * NB <= 256;
 };
 
-template <typename T, int DP, int NW, int ST>
-__global__ __launch_bounds__(NW * 32) void k_attend_few(const __grid_constant__ AttendJob j)
+template <typename T, int DP, int NB>
+__global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(const __grid_constant__ AttendJob j)
 {
-    using Sh = FewShape<DP, NW, ST>;
-    constexpr int NT = Sh::kThreads;
+    using Sh = FewShape<DP, NB>;
+    constexpr int NT = Sh::kThreads, NW = Sh::kWarps, ST = Sh::kStages;
     constexpr int kChunks = DP / 8;            // 16-byte pieces of a row
+    constexpr uint32_t kTile = Sh::kKeys * NW, kNone = 0xFFFFFFFFu;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ float sm_m[NW][16], sm_l[NW][16];
+    __shared__ float sm_m[NW][Sh::kM], sm_l[NW][Sh::kM];
     const uint32_t tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const uint32_t G = j.group, D = j.head_dim;
 
+    follow_launch();
     const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
     const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
+    const uint32_t n_items = j.prefix_pass ? j.n_group : j.seqs.n_seq;
+    const Span span = find_span<NT>(j, n_items, Sh::kM, kTile);
     if ((reinterpret_cast<uintptr_t>(kbuf) | reinterpret_cast<uintptr_t>(vbuf)) & 15u) {
         if (blockIdx.x == 0 && tid == 0) st_flag(j.st, LSMKV_ST_MISALIGNED, 0);
         return;
     }
-    const uint32_t n_items = j.prefix_pass ? j.n_group : j.seqs.n_seq;
-    constexpr uint32_t kTile = Sh::kKeys * NW;
-    const Span span = find_span<NT>(j, n_items, Sh::kM, kTile);
     if (span.begin >= span.end) return;
 
     const uint32_t q_s = smem_addr(smem);
-    const uint32_t ring = q_s + (uint32_t)Sh::kQBytes + w * (ST * Sh::kStage);
+    float *const merge = reinterpret_cast<float *>(smem + Sh::kQBytes);
+    const uint32_t ring = q_s + (uint32_t)(Sh::kQBytes + Sh::kMergeBytes) + w * (ST * Sh::kStage);
     const uint64_t tok_stride = (uint64_t)j.n_kv_heads * D;
+    using CutWalk = Walk<Sh::kM, (int)kTile>;
 
-    Walk<Sh::kM, (int)kTile> walk;
+    // The load side, ahead of the other: its cut, and the keys and page ids of this warp's next
+    // 16-key tile.
+    CutWalk ahead;
+    ahead.start(j, span);
+    uint32_t load_key = 0, load_end = 0, load_page = kNone;
+    auto page_of = [&](uint32_t key) -> uint32_t {      // of key + lane % 16
+        const uint32_t k = key + (lane & 15);
+        if (k >= load_end) return kNone;
+        const uint64_t entry = ahead.it.page0 + k / j.page_tokens;
+        const uint32_t page = j.seqs.page_table[entry];
+        if (page < j.num_pages) return page;
+        st_flag(j.st, LSMKV_ST_BAD_PAGE, entry);
+        return kNone;
+    };
+    auto next_load_cut = [&]() {
+        load_key = load_end = 0;
+        while (load_key >= load_end && ahead.next(j, span)) {
+            const Item &it = ahead.it;
+            const Cut &p = ahead.p;
+            load_key = it.kv0 + p.k0 * kTile + w * Sh::kKeys;
+            load_end = min(token_limit(it, (p.rt * Sh::kM + p.rows - 1) / G), it.kv0 + p.k1 * kTile);
+        }
+        load_page = page_of(load_key);
+    };
+    // Piece c = lane % kChunks of rows kRows x + lane / kChunks: whole rows side by side (256 bytes in
+    // one request at head_dim 128), swizzled (piece c of row r at c ^ r % 8).
+    constexpr int kRows = 32 / kChunks > 0 ? 32 / kChunks : 1;
+    constexpr int kCopies = 16 * kChunks / 32;
+    const uint32_t piece_r = lane / kChunks, piece_c = lane % kChunks;
+    const uint32_t piece_at = (piece_r * kChunks + (piece_c ^ piece_r)) * 16;
+    const bool one_page = j.page_tokens % 16 == 0;      // of a 16-key tile
+    const uint64_t step = kRows * tok_stride;
+    auto fetch = [&](uint32_t stage) {
+        if (load_key < load_end) {
+            const uint32_t k = load_key + (lane & 15), page = load_page;
+            const bool real = page != kNone;
+            const uint32_t left = load_end - load_key;
+            uint64_t off = real ? ((uint64_t)page * j.page_tokens + k % j.page_tokens) * tok_stride +
+                                      (uint64_t)ahead.p.kv_head * D
+                                : 0;
+            load_key += kTile;
+            if (load_key < load_end) load_page = page_of(load_key);
+            const uint32_t dst = ring + stage * Sh::kStage;
+            if (one_page) {
+                // the rows of the tile lie one behind the other; lane 0's is the first
+                off = __shfl_sync(~0u, off, 0) + piece_r * tok_stride + piece_c * 8;
+                const bool there = __shfl_sync(~0u, real, 0) && piece_c * 8 < D;
+                const T *kp = kbuf + off, *vp = vbuf + off;
+#pragma unroll
+                for (int x = 0; x < kCopies; ++x) {
+                    const uint32_t r = x * kRows;            // and piece_r more
+                    const bool in = there && r + piece_r < left;
+                    const uint32_t to = dst + r * kChunks * 16 + (piece_at ^ ((r & 7) << 4));
+                    cp_async16(to, in ? kp : kbuf, in);
+                    cp_async16(to + Sh::kKeys * DP * 2, in ? vp : vbuf, in);
+                    kp += step;
+                    vp += step;
+                }
+            } else {
+                const uint32_t lo = (uint32_t)off, hi = (uint32_t)(off >> 32) | (real ? 0u : 0x80000000u);
+#pragma unroll
+                for (int x = 0; x < kCopies; ++x) {
+                    const uint32_t r = x * kRows + piece_r;
+                    const uint32_t h = __shfl_sync(~0u, hi, r);
+                    const uint64_t o = ((uint64_t)(h & 0x7FFFFFFFu) << 32) | __shfl_sync(~0u, lo, r);
+                    const bool in = !(h >> 31) && piece_c * 8 < D;
+                    const uint64_t e = in ? o + piece_c * 8 : 0;
+                    const uint32_t to = dst + x * kRows * kChunks * 16 + (piece_at ^ (((x * kRows) & 7) << 4));
+                    cp_async16(to, kbuf + e, in);
+                    cp_async16(to + Sh::kKeys * DP * 2, vbuf + e, in);
+                }
+            }
+            if (load_key >= load_end) next_load_cut();
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    next_load_cut();
+#pragma unroll
+    for (int s = 0; s < ST - 1; ++s) fetch(s);
+
+    CutWalk walk;
     walk.start(j, span);
     const Item &it = walk.it;
     const Cut &p = walk.p;
-    while (walk.next(j, span)) {
-        const uint32_t row_base = p.rt * Sh::kM;
-
-        // the tile's queries, swizzled like the keys; rows beyond the tile are zero
-        for (uint32_t x = tid; x < 16 * kChunks; x += NT) {
-            const uint32_t r = x / kChunks, c = x % kChunks;
-            const bool real = r < p.rows && c * 8 < D;
-            const uint32_t R = row_base + (r < p.rows ? r : 0);
-            const T *src = static_cast<const T *>(j.q) + (it.row0 + R / G) * j.q_ts +
-                           (uint64_t)(p.kv_head * G + R % G) * j.q_hs + (c * 8 < D ? c * 8 : 0);
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (real) v = *reinterpret_cast<const uint4 *>(src);
-            *reinterpret_cast<uint4 *>(smem + (r * kChunks + (c ^ (r & 7))) * 16) = v;
-        }
-        __syncthreads();
-
-        // rows lane/4 and lane/4 + 8 of the tile, and the keys they see
-        uint32_t lim[2];
+    // a 16-byte piece (or several, at few threads) of the tile's queries a thread; rows beyond
+    // the tile are zero
+    constexpr int kPieces = (Sh::kM * kChunks + NT - 1) / NT;
+    uint4 q_piece[kPieces];
+    auto load_queries = [&]() {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const uint32_t r = (lane >> 2) + 8 * x;
-            lim[x] = r < p.rows ? token_limit(it, (row_base + r) / G) : it.kv0;
+        for (int y = 0; y < kPieces; ++y) {
+            const uint32_t x = tid + y * NT, r = x / kChunks, c = x % kChunks;
+            q_piece[y] = make_uint4(0, 0, 0, 0);
+            if (r < p.rows && c * 8 < D) {
+                const uint32_t R = p.rt * Sh::kM + r;
+                q_piece[y] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(j.q) + (it.row0 + R / G) * j.q_ts +
+                                                              (uint64_t)(p.kv_head * G + R % G) * j.q_hs + c * 8);
+            }
+        }
+    };
+    auto store_queries = [&]() {
+#pragma unroll
+        for (int y = 0; y < kPieces; ++y) {
+            const uint32_t x = tid + y * NT, r = x / kChunks, c = x % kChunks;
+            if (r < Sh::kM) *reinterpret_cast<uint4 *>(smem + (r * kChunks + (c ^ (r & 7))) * 16) = q_piece[y];
+        }
+    };
+    uint32_t stage = 0, stage_load = ST - 1;
+    bool more = walk.next(j, span);
+    if (more) {
+        load_queries();
+        store_queries();
+    }
+    __syncthreads();
+    while (more) {
+        const Cut cut = p;
+        const uint32_t row_base = cut.rt * Sh::kM;
+        // this lane's rows are 8 nb + 2 (lane % 4) and the one behind it; the keys they see
+        uint32_t lim[NB][2];
+#pragma unroll
+        for (int x = 0; x < 2 * NB; ++x) {
+            const uint32_t r = (x >> 1) * 8 + 2 * (lane & 3) + (x & 1);
+            lim[x >> 1][x & 1] = r < cut.rows ? token_limit(it, (row_base + r) / G) : it.kv0;
         }
         const uint32_t lim_first = token_limit(it, row_base / G);              // least of the tile
-        const uint32_t lim_last = token_limit(it, (row_base + p.rows - 1) / G);
-        const uint32_t key_end = min(lim_last, it.kv0 + p.k1 * kTile);
-        const uint32_t key0 = it.kv0 + p.k0 * kTile + w * Sh::kKeys;
+        const uint32_t key_end = min(token_limit(it, (row_base + cut.rows - 1) / G), it.kv0 + cut.k1 * kTile);
+        const uint32_t key0 = it.kv0 + cut.k0 * kTile + w * Sh::kKeys;
 
-        // the page id of key `key + lane % 16`, one step ahead of its copies
-        auto page_of = [&](uint32_t key) -> uint32_t {
-            const uint32_t k = key + (lane & 15);
-            if (k >= key_end) return 0xFFFFFFFFu;
-            const uint64_t entry = it.page0 + k / j.page_tokens;
-            const uint32_t page = j.seqs.page_table[entry];
-            if (page >= j.num_pages) {
-                st_flag(j.st, LSMKV_ST_BAD_PAGE, entry);
-                return 0xFFFFFFFFu;
-            }
-            return page;
-        };
-        auto fetch = [&](uint32_t key, uint32_t page, uint32_t stage) {
-            const uint32_t k = key + (lane & 15);
-            const bool real = page != 0xFFFFFFFFu;
-            const uint64_t off = real ? ((uint64_t)page * j.page_tokens + k % j.page_tokens) * tok_stride +
-                                            (uint64_t)p.kv_head * D
-                                      : 0;
-            const unsigned live = __ballot_sync(~0u, real);
-            const uint32_t lo = (uint32_t)off, hi = (uint32_t)(off >> 32);
-            const uint32_t dst = ring + stage * Sh::kStage;
-            constexpr int kPer = kChunks / 2;      // 16 rows * kChunks pieces / 32 lanes
+        // queries as the right operand: 16 elements x 8 rows a fragment, two fragments a load
+        uint32_t qf[Sh::kQInRegs ? DP / 16 : 1][NB][2];
+        auto load_q = [&](int x, uint32_t (&f)[2][NB][2]) {       // elements 32 x ..
 #pragma unroll
-            for (int x = 0; x < kPer; ++x) {
-                const uint32_t piece = x * 32 + lane;
-                const uint32_t r = piece / kChunks, c = piece % kChunks;
-                const uint64_t o = ((uint64_t)__shfl_sync(~0u, hi, r) << 32) | __shfl_sync(~0u, lo, r);
-                const bool in = ((live >> r) & 1u) && c * 8 < D;
-                const uint64_t e = in ? o + c * 8 : 0;
-                const uint32_t at = dst + (r * kChunks + (c ^ (r & 7))) * 16;
-                cp_async16(at, kbuf + e, in);
-                cp_async16(at + Sh::kKeys * DP * 2, vbuf + e, in);
+            for (int nb = 0; nb < NB; ++nb) {
+                const uint32_t r = nb * 8 + (lane & 7), ck = 4 * x + (lane >> 3);
+                uint32_t q[4];
+                ldmatrix4(q_s + (r * kChunks + (ck ^ (r & 7))) * 16, q);
+                f[0][nb][0] = q[0];
+                f[0][nb][1] = q[1];
+                f[1][nb][0] = q[2];
+                f[1][nb][1] = q[3];
             }
         };
-
-        float o[DP / 8][4];
+        if constexpr (Sh::kQInRegs) {
 #pragma unroll
-        for (int x = 0; x < DP / 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-
-        uint32_t key_load = key0;
-        uint32_t page = page_of(key_load);
-#pragma unroll
-        for (int s = 0; s < ST - 1; ++s) {
-            if (key_load < key_end) {
-                const uint32_t next = page_of(key_load + kTile);
-                fetch(key_load, page, s);
-                page = next;
-                key_load += kTile;
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
+            for (int x = 0; x < DP / 32; ++x) load_q(x, *reinterpret_cast<uint32_t(*)[2][NB][2]>(&qf[2 * x]));
         }
-        uint32_t stage = 0, stage_load = ST - 1;
+
+        float o[DP / 16][NB][4];
+#pragma unroll
+        for (int x = 0; x < DP / 16; ++x)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) o[x][nb][0] = o[x][nb][1] = o[x][nb][2] = o[x][nb][3] = 0.f;
+        float m[NB][2], l[NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            m[nb][0] = m[nb][1] = -INFINITY;
+            l[nb][0] = l[nb][1] = 0.f;
+        }
         for (uint32_t key = key0; key < key_end; key += kTile) {
-            if (key_load < key_end) {
-                const uint32_t next = page_of(key_load + kTile);
-                fetch(key_load, page, stage_load);
-                page = next;
-                key_load += kTile;
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
+            fetch(stage_load);
             stage_load = stage_load + 1 == ST ? 0 : stage_load + 1;
             asm volatile("cp.async.wait_group %0;" :: "n"(ST - 1) : "memory");
             __syncwarp();
             const uint32_t ks = ring + stage * Sh::kStage;
             const uint32_t vs = ks + Sh::kKeys * DP * 2;
 
-            float s[2][4] = {};
+            // scores of 16 keys (lane/4 and lane/4 + 8) x 8 rows
+            float s[NB][4];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.f;
             {
-                const uint32_t kr = (lane & 7) + ((lane >> 4) << 3);
-                const uint32_t qr = lane & 15;
+                const uint32_t kr = lane & 15;
+                uint32_t f[2][NB][2];
 #pragma unroll
                 for (int x = 0; x < DP / 16; ++x) {
-                    uint32_t a[4], b[4];
-                    ldmatrix4(q_s + (qr * kChunks + ((2 * x + (lane >> 4)) ^ (qr & 7))) * 16, a);
-                    ldmatrix4(ks + (kr * kChunks + ((2 * x + ((lane >> 3) & 1)) ^ (kr & 7))) * 16, b);
-                    mma16816<T>(s[0], a, b[0], b[1]);
-                    mma16816<T>(s[1], a, b[2], b[3]);
+                    uint32_t a[4];
+                    ldmatrix4(ks + (kr * kChunks + ((2 * x + (lane >> 4)) ^ (kr & 7))) * 16, a);
+                    if constexpr (!Sh::kQInRegs) {
+                        if (x % 2 == 0) load_q(x / 2, f);
+                    }
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        if constexpr (Sh::kQInRegs) mma16816<T>(s[nb], a, qf[x][nb][0], qf[x][nb][1]);
+                        else mma16816<T>(s[nb], a, f[x & 1][nb][0], f[x & 1][nb][1]);
+                    }
                 }
             }
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][e] *= j.scale_log2;
+                for (int e = 0; e < 4; ++e) s[nb][e] *= j.scale_log2;
             if (key + Sh::kKeys > lim_first) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (key + n * 8 + 2 * (lane & 3) + (e & 1) >= lim[e >> 1]) s[n][e] = -INFINITY;
+                        if (key + (lane >> 2) + 8 * (e >> 1) >= lim[nb][e & 1]) s[nb][e] = -INFINITY;
             }
-            uint32_t pa[4];
-            float corr[2];
+            // The maximum that the weights refer to is the row's over all lanes. It moves only when
+            // a score passes it by more than 2^8: most tiles need one vote, no exchange.
+            bool over = false;
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                float t = fmaxf(fmaxf(s[0][2 * x], s[0][2 * x + 1]), fmaxf(s[1][2 * x], s[1][2 * x + 1]));
-                t = fmaxf(t, __shfl_xor_sync(~0u, t, 1));
-                t = fmaxf(t, __shfl_xor_sync(~0u, t, 2));
-                t = fmaxf(t, m[x]);
-                const float base = t == -INFINITY ? 0.f : t;
-                corr[x] = exp2f(m[x] - base);
-                m[x] = t;
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    s[n][2 * x] = exp2f(s[n][2 * x] - base);
-                    s[n][2 * x + 1] = exp2f(s[n][2 * x + 1] - base);
+                for (int x = 0; x < 2; ++x) over |= fmaxf(s[nb][x], s[nb][2 + x]) > m[nb][x] + 8.f;
+            if (__any_sync(~0u, over)) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    float fix[2];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        float t = fmaxf(s[nb][x], s[nb][2 + x]);
+                        t = fmaxf(t, __shfl_xor_sync(~0u, t, 4));
+                        t = fmaxf(t, __shfl_xor_sync(~0u, t, 8));
+                        t = fmaxf(t, __shfl_xor_sync(~0u, t, 16));
+                        t = fmaxf(t, m[nb][x]);
+                        fix[x] = t == -INFINITY ? 1.f : exp2f(m[nb][x] - t);
+                        m[nb][x] = t;
+                        l[nb][x] *= fix[x];
+                    }
+#pragma unroll
+                    for (int x = 0; x < DP / 16; ++x) {
+                        o[x][nb][0] *= fix[0];
+                        o[x][nb][1] *= fix[1];
+                        o[x][nb][2] *= fix[0];
+                        o[x][nb][3] *= fix[1];
+                    }
                 }
-                l[x] = l[x] * corr[x] + (s[0][2 * x] + s[0][2 * x + 1]) + (s[1][2 * x] + s[1][2 * x + 1]);
+            }
+            uint32_t pf[NB][2];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float base = m[nb][e & 1] == -INFINITY ? 0.f : m[nb][e & 1];
+                    s[nb][e] = exp2f(s[nb][e] - base);
+                    l[nb][e & 1] += s[nb][e];
+                }
                 // the weights are rounded to the values' type: the tensor cores take both in one
-                pa[x] = Half2<T>::down(s[0][2 * x], s[0][2 * x + 1]);
-                pa[2 + x] = Half2<T>::down(s[1][2 * x], s[1][2 * x + 1]);
-            }
-            if (__any_sync(~0u, corr[0] != 1.f || corr[1] != 1.f)) {
-#pragma unroll
-                for (int x = 0; x < DP / 8; ++x) {
-                    o[x][0] *= corr[0];
-                    o[x][1] *= corr[0];
-                    o[x][2] *= corr[1];
-                    o[x][3] *= corr[1];
-                }
+                pf[nb][0] = transpose8x8(Half2<T>::down(s[nb][0], s[nb][1]));
+                pf[nb][1] = transpose8x8(Half2<T>::down(s[nb][2], s[nb][3]));
             }
             {
-                const uint32_t vr = (lane & 7) + (((lane >> 3) & 1) << 3);
+                const uint32_t vr = (lane & 7) + ((lane >> 4) << 3);
 #pragma unroll
                 for (int x = 0; x < DP / 16; ++x) {
-                    uint32_t b[4];
-                    ldmatrix4t(vs + (vr * kChunks + ((2 * x + (lane >> 4)) ^ (vr & 7))) * 16, b);
-                    mma16816<T>(o[2 * x], pa, b[0], b[1]);
-                    mma16816<T>(o[2 * x + 1], pa, b[2], b[3]);
+                    uint32_t a[4];
+                    ldmatrix4t(vs + (vr * kChunks + ((2 * x + ((lane >> 3) & 1)) ^ (vr & 7))) * 16, a);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma16816<T>(o[x][nb], a, pf[nb][0], pf[nb][1]);
                 }
             }
             __syncwarp();     // the stage is read before it is filled again
             stage = stage + 1 == ST ? 0 : stage + 1;
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        __syncwarp();
 
-        // merge the warps: sums into the warps' own rings, statistics beside them
-        float *const mine = reinterpret_cast<float *>(smem + Sh::kQBytes + (size_t)w * ST * Sh::kStage);
+        // merge the warps, kMergeRows rows at a time; the next cut's queries are on their way
+        const Item done = it;
+        more = walk.next(j, span);
+        if (more) load_queries();
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            l[x] += __shfl_xor_sync(~0u, l[x], 1);
-            l[x] += __shfl_xor_sync(~0u, l[x], 2);
-            const uint32_t r = (lane >> 2) + 8 * x;
-            if ((lane & 3) == 0) {
-                sm_m[w][r] = m[x];
-                sm_l[w][r] = l[x];
-            }
-            if (r < p.rows) {
-#pragma unroll
-                for (int n = 0; n < DP / 8; ++n)
-                    *reinterpret_cast<float2 *>(mine + r * DP + ((n * 8 + 2 * (lane & 3)) ^ ((r & 3) * 8))) =
-                        make_float2(o[n][2 * x], o[n][2 * x + 1]);
+        for (int x = 0; x < 2 * NB; ++x) {
+            float &sum = l[x >> 1][x & 1];
+            sum += __shfl_xor_sync(~0u, sum, 4);
+            sum += __shfl_xor_sync(~0u, sum, 8);
+            sum += __shfl_xor_sync(~0u, sum, 16);
+            if (lane < 4) {
+                sm_m[w][(x >> 1) * 8 + 2 * lane + (x & 1)] = m[x >> 1][x & 1];
+                sm_l[w][(x >> 1) * 8 + 2 * lane + (x & 1)] = sum;
             }
         }
-        __syncthreads();
-        const bool whole = p.k0 == 0 && p.k1 == p.units;
+        const bool whole = cut.k0 == 0 && cut.k1 == cut.units;
         const uint32_t quads = D / 4;
         float *slot = whole ? nullptr
-                            : part_slot(j, 2ull * blockIdx.x + (p.k0 == 0 ? 1 : 0), Sh::kM, DP);
-        for (uint32_t x = tid; x < p.rows * quads; x += NT) {
-            const uint32_t r = x / quads, d = (x - r * quads) * 4;
-            float top = -INFINITY, sum = 0.f;
+                            : part_slot(j, 2ull * blockIdx.x + (cut.k0 == 0 ? 1 : 0), Sh::kM, DP);
+        for (uint32_t r0 = 0; r0 < cut.rows; r0 += Sh::kMergeRows) {
+            const uint32_t r1 = min(r0 + Sh::kMergeRows, cut.rows);
 #pragma unroll
-            for (int k = 0; k < NW; ++k) top = fmaxf(top, sm_m[k][r]);
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int x = 0; x < 2 * NB; ++x) {
+                const uint32_t r = (x >> 1) * 8 + 2 * (lane & 3) + (x & 1);
+                if (r >= r0 && r < r1) {
+                    float *const mine = merge + ((r - r0) * NW + w) * DP;
 #pragma unroll
-            for (int k = 0; k < NW; ++k) {
-                const float f = part_weight(sm_m[k][r], top);
-                const float4 v = *reinterpret_cast<const float4 *>(
-                    smem + Sh::kQBytes + (size_t)k * ST * Sh::kStage +
-                    (r * DP + (d ^ ((r & 3) * 8))) * 4);
-                acc.x += f * v.x;
-                acc.y += f * v.y;
-                acc.z += f * v.z;
-                acc.w += f * v.w;
-                sum += f * sm_l[k][r];
-            }
-            if (whole) {
-                finish_row4<T>(j, it, p.kv_head, row_base + r, d, acc, top, sum);
-            } else {
-                __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)r * DP + d), acc);
-                if (d == 0) {
-                    __stcg(slot + (uint64_t)Sh::kM * DP + r, top);
-                    __stcg(slot + (uint64_t)Sh::kM * (DP + 1) + r, sum);
+                    for (int n = 0; n < DP / 16; ++n) {
+                        mine[(n * 16 + (lane >> 2)) ^ ((r & 6) << 2)] = o[n][x >> 1][x & 1];
+                        mine[(n * 16 + 8 + (lane >> 2)) ^ ((r & 6) << 2)] = o[n][x >> 1][2 + (x & 1)];
+                    }
                 }
             }
+            __syncthreads();
+            if (r0 == 0 && more) store_queries();      // all warps are done with this cut's
+            for (uint32_t x = tid; x < (r1 - r0) * quads; x += NT) {
+                const uint32_t r = r0 + x / quads, d = x % quads * 4;
+                float top = -INFINITY, sum = 0.f;
+#pragma unroll
+                for (int k = 0; k < NW; ++k) top = fmaxf(top, sm_m[k][r]);
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int k = 0; k < NW; ++k) {
+                    const float f = part_weight(sm_m[k][r], top);
+                    const float4 v = *reinterpret_cast<const float4 *>(
+                        merge + ((r - r0) * NW + k) * DP + (d ^ ((r & 6) << 2)));
+                    acc.x += f * v.x;
+                    acc.y += f * v.y;
+                    acc.z += f * v.z;
+                    acc.w += f * v.w;
+                    sum += f * sm_l[k][r];
+                }
+                if (whole) {
+                    finish_row4<T>(j, done, cut.kv_head, row_base + r, d, acc, top, sum);
+                } else {
+                    __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)r * DP + d), acc);
+                    if (d == 0) {
+                        __stcg(slot + (uint64_t)Sh::kM * DP + r, top);
+                        __stcg(slot + (uint64_t)Sh::kM * (DP + 1) + r, sum);
+                    }
+                }
+            }
+            __syncthreads();
         }
-        // in the prefix pass the own pass takes the parts from where they are
-        if (!whole && !j.prefix_pass && deliver_part(j, p, span.per))
-            merge_parts<T, NT>(j, it, p, span.per, Sh::kM, 0, p.rows);
-        __syncthreads();
+        if (!whole && deliver_part(j, cut, span.per))
+            merge_parts<T, NT>(j, done, cut, span.per, Sh::kM, 0, cut.rows);
     }
 }
 

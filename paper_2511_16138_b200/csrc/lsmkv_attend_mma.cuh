@@ -241,14 +241,16 @@ struct CutDesc {
     uint64_t per;
 };
 
-// Merge of the cut tiles: a block takes 32 rows of one.
+// Merge of the cut tiles: a block takes a few rows of one, four elements a thread at head_dim 128.
+constexpr uint32_t kMergeBlockRows = 8;
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_merge(const __grid_constant__ AttendJob j)
 {
+    follow_launch();
     const CutDesc &c = j.cuts[blockIdx.x];
-    const uint32_t r0 = blockIdx.y * 32, rows = c.p.rows;
+    const uint32_t r0 = blockIdx.y * kMergeBlockRows, rows = c.p.rows;
     if (r0 >= rows) return;
-    merge_parts<T, 256>(j, c.it, c.p, c.per, 256, r0, r0 + 32 < rows ? r0 + 32 : rows);
+    merge_parts<T, 256>(j, c.it, c.p, c.per, 256, r0, min(r0 + kMergeBlockRows, rows));
 }
 
 template <typename T, int DP, bool kBoxes>
@@ -268,15 +270,16 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     __shared__ float half_m[128], half_l[128];   // the second half's statistics, when the halves share rows
     const uint32_t tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const uint32_t G = j.group, D = j.head_dim;
-    if (tid == 0 && !j.prefix_pass) j.cuts[blockIdx.x].p.rows = 0;
+    follow_launch();
+    if (tid == 0) j.cuts[blockIdx.x].p.rows = 0;
 
     const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
     const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
+    const Span span = find_span<Sh::kThreads>(j, j.prefix_pass ? j.n_group : j.seqs.n_seq, Sh::kM, Sh::kKeys);
     if ((reinterpret_cast<uintptr_t>(kbuf) | reinterpret_cast<uintptr_t>(vbuf)) & 15u) {
         if (blockIdx.x == 0 && tid == 0) st_flag(j.st, LSMKV_ST_MISALIGNED, 0);
         return;
     }
-    const Span span = find_span<Sh::kThreads>(j, j.prefix_pass ? j.n_group : j.seqs.n_seq, Sh::kM, Sh::kKeys);
     if (span.begin >= span.end) return;
 
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -534,7 +537,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 __stcg(slot + (uint64_t)Sh::kM * DP + first + row, m);
                 __stcg(slot + (uint64_t)Sh::kM * (DP + 1) + first + row, l);
             }
-            if (!whole && cw.p.k0 == 0 && tid == 0 && !j.prefix_pass) {
+            if (!whole && cw.p.k0 == 0 && tid == 0) {
                 CutDesc &c = j.cuts[blockIdx.x];
                 c.it = cw.it;
                 c.p = cw.p;

@@ -38,18 +38,43 @@ SeqArgs seq_args(const lsmkv_seqs_t *s)
     return a;
 }
 
-template <typename T>
-int launch_few(lsmkv_ctx *ctx, cudaStream_t s, const AttendJob &job)
+// A launch of an attend call: behind another one of the same call (follows) it may start before
+// that one has ended (the kernels wait for it themselves).
+template <typename... P, typename... A>
+cudaError_t start(lsmkv_ctx *ctx, cudaStream_t s, bool follows, void (*kern)(P...), dim3 grid, unsigned threads,
+                  size_t smem, const A &...args)
 {
-    const unsigned sm = (unsigned)ctx->sm_count;
-    if (job.head_dim <= 64)
-        k_attend_few<T, 64, 4, 6><<<sm * 2, 128, FewShape<64, 4, 6>::kSmem, s>>>(job);
-    else if (job.head_dim <= 128)
-        k_attend_few<T, 128, 4, 3><<<sm * 2, 128, FewShape<128, 4, 3>::kSmem, s>>>(job);
-    else
-        k_attend_few<T, 256, 4, 3><<<sm, 128, FewShape<256, 4, 3>::kSmem, s>>>(job);
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = grid;
+    c.blockDim = threads;
+    c.dynamicSmemBytes = smem;
+    c.stream = s;
+    c.attrs = &early;
+    c.numAttrs = follows ? 1 : 0;
     ++ctx->launches;
-    CU(ctx, cudaGetLastError());
+    return cudaLaunchKernelEx(&c, kern, args...);
+}
+
+template <typename T, int DP, int NB>
+cudaError_t start_few(lsmkv_ctx *ctx, cudaStream_t s, bool follows, const AttendJob &job)
+{
+    using Sh = FewShape<DP, NB>;
+    return start(ctx, s, follows, k_attend_few<T, DP, NB>, (unsigned)ctx->sm_count, Sh::kThreads, Sh::kSmem, job);
+}
+
+// rows8: no row tile has more than 8 rows.
+template <typename T>
+int launch_few(lsmkv_ctx *ctx, cudaStream_t s, bool follows, const AttendJob &job, bool rows8)
+{
+    if (job.head_dim <= 64)
+        CU(ctx, (rows8 ? start_few<T, 64, 1> : start_few<T, 64, 2>)(ctx, s, follows, job));
+    else if (job.head_dim <= 128)
+        CU(ctx, (rows8 ? start_few<T, 128, 1> : start_few<T, 128, 2>)(ctx, s, follows, job));
+    else
+        CU(ctx, (rows8 ? start_few<T, 256, 1> : start_few<T, 256, 2>)(ctx, s, follows, job));
     return LSMKV_OK;
 }
 
@@ -78,7 +103,7 @@ bool make_map(uint32_t dtype, const void *base, const uint64_t (&dims)[3], uint6
 }
 
 template <typename T>
-int launch_many(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
+int launch_many(lsmkv_ctx *ctx, cudaStream_t s, bool follows, AttendJob &job)
 {
     const unsigned sm = (unsigned)ctx->sm_count;
     // Tokens of a box: the largest power of two that divides the page, at most 64. The swizzle's
@@ -98,19 +123,13 @@ int launch_many(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
     job.q_boxes = boxes && job.group <= 128 && (job.group & (job.group - 1)) == 0 &&
                   make_map(dtype, job.q, {g.head_dim, job.n_q_heads, job.seqs.n_new}, job.q_hs, job.q_ts, job.group,
                            128 / job.group, &q_map);
-    if (job.head_dim <= 64) {
-        auto kern = boxes ? k_attend_many<T, 64, true> : k_attend_many<T, 64, false>;
-        kern<<<sm, ManyShape<64>::kThreads, ManyShape<64>::kSmem, s>>>(job, map, q_map);
-    } else {
-        auto kern = boxes ? k_attend_many<T, 128, true> : k_attend_many<T, 128, false>;
-        kern<<<sm, ManyShape<128>::kThreads, ManyShape<128>::kSmem, s>>>(job, map, q_map);
-    }
-    ++ctx->launches;
-    CU(ctx, cudaGetLastError());
-    if (job.prefix_pass) return LSMKV_OK;
-    k_attend_merge<T><<<dim3(sm, 256 / 32), 256, 0, s>>>(job);
-    ++ctx->launches;
-    CU(ctx, cudaGetLastError());
+    if (job.head_dim <= 64)
+        CU(ctx, start(ctx, s, follows, boxes ? k_attend_many<T, 64, true> : k_attend_many<T, 64, false>, sm,
+                      ManyShape<64>::kThreads, ManyShape<64>::kSmem, job, map, q_map));
+    else
+        CU(ctx, start(ctx, s, follows, boxes ? k_attend_many<T, 128, true> : k_attend_many<T, 128, false>, sm,
+                      ManyShape<128>::kThreads, ManyShape<128>::kSmem, job, map, q_map));
+    CU(ctx, start(ctx, s, true, k_attend_merge<T>, dim3(sm, 256 / kMergeBlockRows), 256, 0, job));
     return LSMKV_OK;
 }
 
@@ -130,7 +149,7 @@ int launch_prefix(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
     job.prefix_pass = 1;
     job.rows_lo = 0;
     job.rows_hi = 0xFFFFFFFFu;
-    const int rc = many_takes(ctx) ? launch_many<T>(ctx, s, job) : launch_few<T>(ctx, s, job);
+    const int rc = many_takes(ctx) ? launch_many<T>(ctx, s, false, job) : launch_few<T>(ctx, s, false, job, false);
     job.prefix_pass = 0;
     return rc;
 }
@@ -139,31 +158,30 @@ int launch_prefix(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
 template <typename T>
 int launch_own(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
 {
-    // Up to 16 rows fill one fragment of the few-row kernel; beyond, it would read the keys once
-    // for every 16 rows, where the many-row kernel reads them once for 256.
+    // Up to 16 rows are one tile of the few-row kernel; beyond, it would read the keys once for
+    // every 16 rows, where the many-row kernel reads them once for 256.
     const bool mma = many_takes(ctx);
     job.rows_lo = 0;
     job.rows_hi = mma ? 16 : 0xFFFFFFFFu;
-    const int rc = launch_few<T>(ctx, s, job);
-    if (rc != LSMKV_OK || !mma || (uint64_t)job.seqs.max_new * job.group <= 16) return rc;
+    const uint64_t most = (uint64_t)job.seqs.max_new * job.group;
+    const int rc = launch_few<T>(ctx, s, job.skip != nullptr, job, most <= 8);
+    if (rc != LSMKV_OK || !mma || most <= 16) return rc;
     job.rows_lo = 16;
     job.rows_hi = 0xFFFFFFFFu;
-    return launch_many<T>(ctx, s, job);
+    return launch_many<T>(ctx, s, true, job);
 }
 
-// Two part slots for every CTA of the widest launch.
-size_t part_bytes(const lsmkv_ctx *ctx, bool few, bool many)
+// Two part slots for every CTA.
+size_t part_bytes(const lsmkv_ctx *ctx)
 {
-    const size_t a = few ? (size_t)ctx->sm_count * 2 * 2 * 16 : 0;
-    const size_t b = many && many_takes(ctx) ? (size_t)ctx->sm_count * 2 * 256 : 0;
-    return std::max(a, b) * (part_dp(ctx) + 2) * 4;
+    return (size_t)ctx->sm_count * 2 * (many_takes(ctx) ? 256 : 16) * (part_dp(ctx) + 2) * 4;
 }
 
 // Scratch of the attend kernels: counters, descriptors of cut tiles, parts.
 int ensure_attend(lsmkv_ctx *ctx, cudaStream_t s)
 {
     const size_t counters = attend_counter_bytes(ctx);
-    const size_t bytes = counters + (size_t)ctx->sm_count * (sizeof(CutDesc) + 256) + 512 + part_bytes(ctx, true, true);
+    const size_t bytes = counters + (size_t)ctx->sm_count * (sizeof(CutDesc) + 256) + 512 + part_bytes(ctx);
     if (ctx->d_attend && bytes <= ctx->attend_cap) return LSMKV_OK;
     const int rc = grow_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, bytes, bytes, __LINE__);
     if (rc != LSMKV_OK) return rc;
@@ -227,10 +245,9 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
         const uint64_t heads = seqs->n_new * n_q_heads;
         auto place = [&](void *at) {
             IoLayout l(at);
-            job.share = l.take<Share>(seqs->n_seq);
+            job.skip = l.take<uint32_t>(seqs->n_seq);
             job.pre_o = l.take<float>(heads * ctx->geom.head_dim);
             job.pre_lse = l.take<float>(heads);
-            job.pre_parts = l.take<float>(part_bytes(ctx, !many_takes(ctx), true) / 4);
             return l.at;
         };
         const size_t bytes = place(nullptr);
@@ -239,7 +256,6 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
             if (rc != LSMKV_OK) return rc;
         }
         place(ctx->d_prefix);
-        job.pre_rows = many_takes(ctx) ? 256 : 16;
         job.n_group = groups->n_group;
         job.group_off = groups->group_off;
         job.shared_pages = groups->shared_pages;
