@@ -140,15 +140,20 @@ __device__ __forceinline__ uint32_t item_tiles(const AttendJob &j, const Item &i
     return (uint32_t)((rows + M - 1) / M);
 }
 
+// A tile's length on the line: its units and one more, about what its beginning and end cost (its
+// queries, the merge of the warps, the result: 5k cycles, where a unit of the few-row kernel takes
+// 2.9k). No work lies in that last unit.
+constexpr uint32_t kTileCost = 1;
+
 // Units of one KV head of an item.
 __device__ __forceinline__ uint64_t item_units(const AttendJob &j, const Item &it, uint32_t M,
                                                uint32_t tile)
 {
     const uint32_t n = item_tiles(j, it, M);
     if (!n) return 0;
-    if (!it.causal) return (uint64_t)n * tile_units(it, 0, M, j.group, tile);
+    if (!it.causal) return (uint64_t)n * (tile_units(it, 0, M, j.group, tile) + kTileCost);
     uint64_t u = 0;
-    for (uint32_t rt = 0; rt < n; ++rt) u += tile_units(it, rt, M, j.group, tile);
+    for (uint32_t rt = 0; rt < n; ++rt) u += tile_units(it, rt, M, j.group, tile) + kTileCost;
     return u;
 }
 
@@ -293,35 +298,38 @@ struct Walk {
         p.rt = 0;
         while (true) {
             p.units = tile_units(it, p.rt, M, j.group, TILE);
-            if (at < p.units || p.rt + 1 >= tiles) break;
-            at -= p.units;
-            p.tile0 += p.units;
+            if (at < p.units + kTileCost || p.rt + 1 >= tiles) break;
+            at -= p.units + kTileCost;
+            p.tile0 += p.units + kTileCost;
             ++p.rt;
         }
     }
     __device__ __forceinline__ bool next(const AttendJob &j, const Span &s)
     {
-        if (u >= s.end) return false;
-        if (begun) {
-            p.tile0 = u;
-            if (++p.rt == tiles) {
-                p.rt = 0;
-                if (++p.kv_head == j.n_kv_heads) {
-                    p.kv_head = 0;
-                    i = next_item(j, i, j.prefix_pass ? j.n_group : j.seqs.n_seq, M, &it);
-                    tiles = item_tiles(j, it, M);
+        while (u < s.end) {
+            if (begun) {
+                p.tile0 = u;
+                if (++p.rt == tiles) {
+                    p.rt = 0;
+                    if (++p.kv_head == j.n_kv_heads) {
+                        p.kv_head = 0;
+                        i = next_item(j, i, j.prefix_pass ? j.n_group : j.seqs.n_seq, M, &it);
+                        tiles = item_tiles(j, it, M);
+                    }
                 }
+                p.units = tile_units(it, p.rt, M, j.group, TILE);
             }
-            p.units = tile_units(it, p.rt, M, j.group, TILE);
+            begun = true;
+            p.k0 = (uint32_t)(u - p.tile0);
+            const uint64_t end = p.tile0 + p.units;
+            u = end + kTileCost < s.end ? end + kTileCost : s.end;
+            if (p.k0 >= p.units) continue;      // the span begins behind the tile's last unit
+            p.k1 = (uint32_t)((end < s.end ? end : s.end) - p.tile0);
+            const uint64_t rows = (uint64_t)it.tokens * j.group - (uint64_t)p.rt * M;
+            p.rows = rows < M ? (uint32_t)rows : M;
+            return true;
         }
-        begun = true;
-        p.k0 = (uint32_t)(u - p.tile0);
-        const uint64_t end = p.tile0 + p.units < s.end ? p.tile0 + p.units : s.end;
-        p.k1 = (uint32_t)(end - p.tile0);
-        u = end;
-        const uint64_t rows = (uint64_t)it.tokens * j.group - (uint64_t)p.rt * M;
-        p.rows = rows < M ? (uint32_t)rows : M;
-        return true;
+        return false;
     }
 };
 
@@ -602,13 +610,18 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
     const uint64_t tok_stride = (uint64_t)j.n_kv_heads * D;
     using CutWalk = Walk<Sh::kM, (int)kTile>;
 
-    // The load side, ahead of the other: its cut, and the keys and page ids of this warp's next
-    // 16-key tile.
-    CutWalk ahead;
-    ahead.start(j, span);
-    uint32_t load_key = 0, load_end = 0, load_page = kNone;
-    auto page_of = [&](uint32_t key) -> uint32_t {      // of key + lane % 16
-        const uint32_t k = key + (lane & 15);
+    CutWalk walk;
+    walk.start(j, span);
+    bool more = walk.next(j, span);
+    const Item &it = walk.it;
+    const Cut &p = walk.p;
+    // The load side, ahead of the other: its cut, and this warp's next 16-key tile. Where such a
+    // tile lies in one page, a lane holds the page id of one of the next 32 tiles; else, of key
+    // lane % 16 of the next tile.
+    CutWalk ahead = walk;
+    const bool one_page = j.page_tokens % 16 == 0;
+    uint32_t load_key = 0, load_end = 0, load_page = kNone, tiles_known = 0;
+    auto page_of = [&](uint32_t k) -> uint32_t {
         if (k >= load_end) return kNone;
         const uint64_t entry = ahead.it.page0 + k / j.page_tokens;
         const uint32_t page = j.seqs.page_table[entry];
@@ -616,15 +629,18 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
         st_flag(j.st, LSMKV_ST_BAD_PAGE, entry);
         return kNone;
     };
+    auto load_pages = [&]() {
+        load_page = page_of(load_key + (one_page ? lane * kTile : lane & 15));
+        tiles_known = one_page ? 32 : 1;
+    };
+    auto take_load_cut = [&]() {
+        const Item &on = ahead.it;
+        load_key = on.kv0 + ahead.p.k0 * kTile + w * Sh::kKeys;
+        load_end = min(token_limit(on, (ahead.p.rt * Sh::kM + ahead.p.rows - 1) / G), on.kv0 + ahead.p.k1 * kTile);
+    };
     auto next_load_cut = [&]() {
-        load_key = load_end = 0;
-        while (load_key >= load_end && ahead.next(j, span)) {
-            const Item &it = ahead.it;
-            const Cut &p = ahead.p;
-            load_key = it.kv0 + p.k0 * kTile + w * Sh::kKeys;
-            load_end = min(token_limit(it, (p.rt * Sh::kM + p.rows - 1) / G), it.kv0 + p.k1 * kTile);
-        }
-        load_page = page_of(load_key);
+        while (load_key >= load_end && ahead.next(j, span)) take_load_cut();
+        load_pages();
     };
     // Piece c = lane % kChunks of rows kRows x + lane / kChunks: whole rows side by side (256 bytes in
     // one request at head_dim 128), swizzled (piece c of row r at c ^ r % 8).
@@ -632,23 +648,23 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
     constexpr int kCopies = 16 * kChunks / 32;
     const uint32_t piece_r = lane / kChunks, piece_c = lane % kChunks;
     const uint32_t piece_at = (piece_r * kChunks + (piece_c ^ piece_r)) * 16;
-    const bool one_page = j.page_tokens % 16 == 0;      // of a 16-key tile
     const uint64_t step = kRows * tok_stride;
     auto fetch = [&](uint32_t stage) {
         if (load_key < load_end) {
-            const uint32_t k = load_key + (lane & 15), page = load_page;
+            const uint32_t k = load_key + (one_page ? 0 : lane & 15);
+            const uint32_t page = one_page ? __shfl_sync(~0u, load_page, 32 - tiles_known) : load_page;
             const bool real = page != kNone;
             const uint32_t left = load_end - load_key;
             uint64_t off = real ? ((uint64_t)page * j.page_tokens + k % j.page_tokens) * tok_stride +
                                       (uint64_t)ahead.p.kv_head * D
                                 : 0;
             load_key += kTile;
-            if (load_key < load_end) load_page = page_of(load_key);
+            if (--tiles_known == 0 && load_key < load_end) load_pages();
             const uint32_t dst = ring + stage * Sh::kStage;
             if (one_page) {
-                // the rows of the tile lie one behind the other; lane 0's is the first
-                off = __shfl_sync(~0u, off, 0) + piece_r * tok_stride + piece_c * 8;
-                const bool there = __shfl_sync(~0u, real, 0) && piece_c * 8 < D;
+                // the rows of the tile lie one behind the other
+                off += piece_r * tok_stride + piece_c * 8;
+                const bool there = real && piece_c * 8 < D;
                 const T *kp = kbuf + off, *vp = vbuf + off;
 #pragma unroll
                 for (int x = 0; x < kCopies; ++x) {
@@ -678,14 +694,6 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    next_load_cut();
-#pragma unroll
-    for (int s = 0; s < ST - 1; ++s) fetch(s);
-
-    CutWalk walk;
-    walk.start(j, span);
-    const Item &it = walk.it;
-    const Cut &p = walk.p;
     // a 16-byte piece (or several, at few threads) of the tile's queries a thread; rows beyond
     // the tile are zero
     constexpr int kPieces = (Sh::kM * kChunks + NT - 1) / NT;
@@ -710,9 +718,12 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
         }
     };
     uint32_t stage = 0, stage_load = ST - 1;
-    bool more = walk.next(j, span);
     if (more) {
+        take_load_cut();
+        next_load_cut();
         load_queries();
+#pragma unroll
+        for (int s = 0; s < ST - 1; ++s) fetch(s);
         store_queries();
     }
     __syncthreads();

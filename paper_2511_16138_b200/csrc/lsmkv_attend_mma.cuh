@@ -244,7 +244,7 @@ struct CutDesc {
 // Merge of the cut tiles: a block takes a few rows of one, four elements a thread at head_dim 128.
 constexpr uint32_t kMergeBlockRows = 8;
 template <typename T>
-__global__ __launch_bounds__(256) void k_attend_merge(const __grid_constant__ AttendJob j)
+__global__ __launch_bounds__(256, 5) void k_attend_merge(const __grid_constant__ AttendJob j)
 {
     follow_launch();
     const CutDesc &c = j.cuts[blockIdx.x];

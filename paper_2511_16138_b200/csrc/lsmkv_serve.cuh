@@ -142,14 +142,18 @@ uint32_t part_dp(const lsmkv_ctx *ctx)
 }
 
 // The groups' common keys, all groups by one kernel: whatever their rows, reading the keys once
-// is what counts.
+// is what counts. A batch of at most 64 rows in all goes by the few-row kernel all the same: its up
+// to four row tiles find the keys in L2, and it starts and ends faster (one group of 8 sequences,
+// G = 4, 1024 common tokens: FEW us a call against MANY).
 template <typename T>
 int launch_prefix(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
 {
     job.prefix_pass = 1;
     job.rows_lo = 0;
     job.rows_hi = 0xFFFFFFFFu;
-    const int rc = many_takes(ctx) ? launch_many<T>(ctx, s, false, job) : launch_few<T>(ctx, s, false, job, false);
+    const uint64_t rows = job.seqs.n_new * job.group;
+    const int rc = many_takes(ctx) && rows > 64 ? launch_many<T>(ctx, s, false, job)
+                                                 : launch_few<T>(ctx, s, false, job, rows <= 8);
     job.prefix_pass = 0;
     return rc;
 }
