@@ -238,7 +238,7 @@ __device__ __forceinline__ uint32_t half_tiles(const AttendJob &j, const Item &i
 struct CutDesc {
     Item it;
     Cut p;
-    uint64_t per;
+    uint32_t c0, c1;             // its parts
 };
 
 // Merge of the cut tiles: a block takes a few rows of one, four elements a thread at head_dim 128.
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(256, 5) void k_attend_merge(const __grid_constant__
     const CutDesc &c = j.cuts[blockIdx.x];
     const uint32_t r0 = blockIdx.y * kMergeBlockRows, rows = c.p.rows;
     if (r0 >= rows) return;
-    merge_parts<T, 256>(j, c.it, c.p, c.per, 256, r0, min(r0 + kMergeBlockRows, rows));
+    merge_parts<T, 256>(j, c.it, c.p, c.c0, c.c1, 256, r0, min(r0 + kMergeBlockRows, rows));
 }
 
 template <typename T, int DP, bool kBoxes>
@@ -275,12 +275,13 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
 
     const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
     const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
-    const Span span = find_span<Sh::kThreads>(j, j.prefix_pass ? j.n_group : j.seqs.n_seq, Sh::kM, Sh::kKeys);
+    const Span span = find_span<Sh::kThreads, true>(j, j.prefix_pass ? j.n_group : j.seqs.n_seq, Sh::kM, Sh::kKeys,
+                                                    reinterpret_cast<uint32_t *>(smem_raw));
     if ((reinterpret_cast<uintptr_t>(kbuf) | reinterpret_cast<uintptr_t>(vbuf)) & 15u) {
         if (blockIdx.x == 0 && tid == 0) st_flag(j.st, LSMKV_ST_MISALIGNED, 0);
         return;
     }
-    if (span.begin >= span.end) return;
+    if (span.begin >= span.end && !span.waves) return;
 
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t q_s = base, ring = base + 2 * Sh::kTileBytes;
@@ -448,7 +449,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
             if (!alive) break;
             const bool whole = cw.p.k0 == 0 && cw.p.k1 == cw.p.units;
             float *slot = whole ? nullptr
-                                : part_slot(j, 2ull * blockIdx.x + (cw.p.k0 == 0 ? 1 : 0), Sh::kM, DP);
+                                : part_slot(j, 2ull * span.rank + (cw.p.k0 == 0 ? 1 : 0), Sh::kM, DP);
             float f0 = 1.f, f1 = 0.f;            // weights of the two halves' sums, when they share rows
             const bool two = both && cw.p.k1 - cw.p.k0 > 1;
             if (two && x) {
@@ -541,7 +542,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 CutDesc &c = j.cuts[blockIdx.x];
                 c.it = cw.it;
                 c.p = cw.p;
-                c.per = span.per;
+                c.c0 = c.c1 = span.rank;
+                while (j.span_begin[c.c1 + 1] < cw.p.tile0 + cw.p.units) ++c.c1;
             }
         }
     } else {

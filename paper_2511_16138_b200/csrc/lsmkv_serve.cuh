@@ -181,19 +181,36 @@ size_t part_bytes(const lsmkv_ctx *ctx)
     return (size_t)ctx->sm_count * 2 * (many_takes(ctx) ? 256 : 16) * (part_dp(ctx) + 2) * 4;
 }
 
-// Scratch of the attend kernels: counters, descriptors of cut tiles, parts.
-int ensure_attend(lsmkv_ctx *ctx, cudaStream_t s)
+// Scratch of the attend kernels for n_seq sequences: counters, descriptors of cut tiles, tensor
+// maps, the spans' beginnings, the items' tiles, parts. Returns its size.
+size_t place_attend(const lsmkv_ctx *ctx, void *at, uint32_t n_seq, AttendJob *job)
 {
-    const size_t counters = attend_counter_bytes(ctx);
-    const size_t bytes = counters + (size_t)ctx->sm_count * (sizeof(CutDesc) + 256) + 512 + part_bytes(ctx);
-    if (ctx->d_attend && bytes <= ctx->attend_cap) return LSMKV_OK;
-    const int rc = grow_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, bytes, bytes, __LINE__);
-    if (rc != LSMKV_OK) return rc;
-    const cudaError_t e = cudaMemsetAsync(ctx->d_attend, 0, counters, s);
-    if (e != cudaSuccess) {
-        release_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, __LINE__);
-        return cuda_fail(ctx, e, __LINE__);
+    IoLayout l(at);
+    const size_t sm = (size_t)ctx->sm_count;
+    job->arrived = reinterpret_cast<unsigned int *>(l.take<unsigned char>(attend_counter_bytes(ctx)));
+    job->cuts = l.take<CutDesc>(sm);
+    job->maps = l.take<unsigned char>(sm * 256);
+    job->span_begin = l.take<uint64_t>(sm + 1);
+    job->parts = l.take<float>(part_bytes(ctx) / 4);
+    job->tile_base = l.take<uint32_t>((size_t)n_seq + 1);
+    return l.at;
+}
+
+int ensure_attend(lsmkv_ctx *ctx, cudaStream_t s, uint32_t n_seq, AttendJob *job)
+{
+    // room for a few sequences more than asked for: a growing batch does not allocate every time
+    size_t bytes = place_attend(ctx, nullptr, n_seq, job);
+    if (!ctx->d_attend || bytes > ctx->attend_cap) {
+        bytes += 16384;
+        const int rc = grow_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, bytes, bytes, __LINE__);
+        if (rc != LSMKV_OK) return rc;
+        const cudaError_t e = cudaMemsetAsync(ctx->d_attend, 0, attend_counter_bytes(ctx), s);
+        if (e != cudaSuccess) {
+            release_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, __LINE__);
+            return cuda_fail(ctx, e, __LINE__);
+        }
     }
+    place_attend(ctx, ctx->d_attend, n_seq, job);
     return LSMKV_OK;
 }
 
@@ -211,11 +228,10 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
     const bool shared = groups && groups->n_group;
     DeviceGuard guard(ctx->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    int rc = ensure_attend(ctx, s);
-    if (rc != LSMKV_OK) return rc;
-
     AttendJob job;
     std::memset(&job, 0, sizeof(job));
+    int rc = ensure_attend(ctx, s, seqs->n_seq, &job);
+    if (rc != LSMKV_OK) return rc;
     job.seqs = seq_args(seqs);
     job.kv_ptrs = pool->kv_ptrs;
     job.num_pages = pool->num_pages;
@@ -236,11 +252,6 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
     job.o_hs = out->head_stride;
     job.lse = lse_out;
     job.scale_log2 = scale * kLog2e;
-    IoLayout lay(ctx->d_attend);
-    job.arrived = reinterpret_cast<unsigned int *>(lay.take<unsigned char>(attend_counter_bytes(ctx)));
-    job.cuts = lay.take<CutDesc>((size_t)ctx->sm_count);
-    job.maps = lay.take<unsigned char>((size_t)ctx->sm_count * 256);
-    job.parts = lay.take<float>(0);
     job.dp = part_dp(ctx);
     job.wait_cycles = ctx->wait_cycles;
     job.test_drop = ctx->test_drop_piece < 0 ? ~0ull : (uint64_t)ctx->test_drop_piece;
