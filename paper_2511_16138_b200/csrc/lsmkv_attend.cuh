@@ -52,6 +52,7 @@ struct AttendJob {
     uint32_t *tile_base;         // many rows: row tiles ahead of every item
     void *maps;                  // many rows: two tensor maps per CTA
     uint32_t box_rows;           // tokens of a box, dividing page_tokens
+    uint32_t wide_boxes;         // a box has all elements of a head, not 64
     uint32_t q_boxes;            // the queries come by boxes too
     long long wait_cycles;
     uint64_t test_drop;          // test hook: ~0 = off
@@ -204,9 +205,11 @@ __device__ __forceinline__ uint64_t block_scan(uint64_t mine, uint64_t *scratch,
 // kWaves: where there are more row tiles than CTAs, the CTAs first take whole tiles in turn, wave
 // by wave -- tiles of one sequence and head side by side, so that the CTAs read the same keys at
 // the same time and L2 has them -- and only the tiles that are left are cut into spans, which even
-// out what the waves left uneven. (Two requests of 32768 tokens, 1024 new, 64/8 heads: spans alone
-// read 6.1 GB from memory in 2.0 ms, where the keys and values are 0.27 GB.) load: gridDim words of
-// shared memory.
+// out what the waves left uneven. (Two requests of 32768 tokens, 1024 new, 64/8 heads, 0.27 GB of
+// keys and values: spans alone read 6.1 GB from memory and take 2.40 ms, with waves 0.35 GB and
+// 2.12 ms.) Keys that L2 holds anyway need none, and spans even out better (six prompts of 700 to
+// 3000 tokens, 45 MB: 133 us against 147). load: gridDim words of shared memory.
+constexpr uint64_t kL2Keeps = 64ull << 20;   // bytes of keys and values, of 126 MB
 template <int NT, bool kWaves>
 __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t tile, uint32_t *load)
 {
@@ -219,13 +222,17 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
     const uint32_t i1 = i0 + each < n ? i0 + each : n;
     uint64_t mine = 0, first = 0;
     uint32_t tiles = 0;
+    uint64_t bytes = 0;
     for (uint32_t i = i0; i < i1; ++i) {
         const Item it = load_item(j, i);
         const uint64_t u = item_units(j, it, M, tile) * j.n_kv_heads;
         if (!it.ok && blockIdx.x == 0) st_flag(j.st, LSMKV_ST_BAD_COUNT, i);
         if (i == i0) first = u;
         mine += u;
-        if (kWaves) tiles += item_tiles(j, it, M) * j.n_kv_heads;
+        if (kWaves && item_tiles(j, it, M)) {
+            tiles += item_tiles(j, it, M) * j.n_kv_heads;
+            bytes += (uint64_t)(it.kv1 - it.kv0) * j.n_kv_heads * j.head_dim * 4;
+        }
     }
     uint64_t total;
     const uint64_t incl = block_scan<NT>(mine, scan, &total);
@@ -246,7 +253,9 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
             base += item_tiles(j, load_item(j, i), M) * j.n_kv_heads;
         }
         if (i1 == n && i0 < i1) j.tile_base[n] = base;
-        uint32_t waves = j.prefix_pass ? 0 : (uint32_t)(all_tiles / N);
+        uint64_t all_bytes;
+        block_scan<NT>(bytes, scan, &all_bytes);
+        uint32_t waves = j.prefix_pass || all_bytes <= kL2Keeps ? 0 : (uint32_t)(all_tiles / N);
         uint64_t capacity = s.per;                       // of CTA tid, behind its waves
         const uint32_t team = n < NT ? NT / n : 1;       // threads that go through an item's tiles
         while (waves) {

@@ -73,18 +73,19 @@ __device__ __forceinline__ bool mbar_wait_or_stop(uint32_t bar, uint32_t parity,
     }
 }
 
-// Shared-memory operand descriptors of 128-byte-swizzled tiles [rows][64 elements], one block of
-// 128 rows after the other. K-major (rows are M or N, elements run along K): groups of 8 rows are
-// 1024 bytes apart. MN-major (elements run along N, rows along K): blocks of 64 elements are
-// `block` bytes apart, groups of 8 rows 1024.
-__device__ __forceinline__ uint64_t desc_k_major(uint32_t addr)
+// Shared-memory operand descriptors of 128-byte-swizzled tiles: cells of 8 rows x 64 elements (1024
+// bytes), cells of the next 8 rows `group` bytes on, of the next 64 elements `half` bytes on. K-major
+// (rows are M or N, elements run along K; `half` is the caller's to add) and MN-major (elements run
+// along N, rows along K).
+__device__ __forceinline__ uint64_t desc_k_major(uint32_t addr, uint32_t group)
 {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(group >> 4) << 32) | (1ull << 46) |
+           (2ull << 61);
 }
 
-__device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr, uint32_t block)
+__device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr, uint32_t group, uint32_t half)
 {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(block >> 4) << 16) | (64ull << 32) |
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(half >> 4) << 16) | ((uint64_t)(group >> 4) << 32) |
            (1ull << 46) | (2ull << 61);
 }
 
@@ -140,6 +141,15 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const void *map, int e, in
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
                  "[%0], [%1, {%2, %3, %4}], [%5];"
                  :: "r"(dst), "l"(map), "r"(e), "r"(head), "r"(token), "r"(bar) : "memory");
+}
+
+// All elements of a head of several tokens: elements, tokens mod 8, blocks of 64 elements, tokens
+// div 8, heads.
+__device__ __forceinline__ void tma_wide_box(uint32_t dst, const void *map, int head, int group, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %2, %2, %3, %4}], [%5];"
+                 :: "r"(dst), "l"(map), "r"(0), "r"(group), "r"(head), "r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, float *v)
@@ -331,6 +341,10 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
+    // layout of keys and values in their stages: cells of all elements of 8 tokens side by side, as
+    // wide boxes leave them, or block after block of 64 elements, like the queries
+    const bool wide = kBoxes && j.wide_boxes;
+    const uint32_t kv_group = wide ? 1024 * (DP / 64) : 1024, kv_half = wide ? 1024 : kBlock;
     // columns: scores (and weights over them) of the halves at 0 and 128, sums at 256 and 384
     auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_or_stop(bar, parity, j.wait_cycles, &stop); };
     // for roles whose lanes act together: all of a warp go on, or none
@@ -675,7 +689,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
 #pragma unroll
                         for (int e = 0; e < DP / 64; ++e)
                             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};"
-                                         :: "r"(at + e * kBlock + y * 16), "r"(0) : "memory");
+                                         :: "r"(at + e * kv_half + (y >> 6) * kv_group + (y & 63) * 16), "r"(0)
+                                         : "memory");
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) mbar_arrive(full(stage));
@@ -697,7 +712,10 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                         const uint32_t bar = kv && ragged && t + 1 == n ? landed(stage) : stage_bar();
                         if (lane == 0) expect(bar, total);
                         __syncwarp();
-                        if (ok) {
+                        if (ok && wide) {
+                            tma_wide_box(ring + stage * Sh::kTileBytes + (g0 >> 3) * kv_group, maps + kv * 128,
+                                         (int)cw.p.kv_head, token >> 3, bar);
+                        } else if (ok) {
 #pragma unroll
                             for (int e = 0; e < DP / 64; ++e)
                                 tma_box(ring + stage * Sh::kTileBytes + e * kBlock + g0 * 128, maps + kv * 128, e * 64,
@@ -768,7 +786,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         };
         Place kp = {0, 0};
         uint32_t q_par = 0, p_par = 0;
-        const uint64_t q_desc = desc_k_major(q_s), k_desc = desc_k_major(ring), v_desc = desc_mn_major(ring, kBlock);
+        const uint64_t q_desc = desc_k_major(q_s, 1024), k_desc = desc_k_major(ring, kv_group),
+                       v_desc = desc_mn_major(ring, kv_group, kv_half);
         // cp.async wrote through another proxy than the matrix unit reads through
         auto wait_tile = [&](const Place &at) {
             if (!wait(full(at.st), at.ph)) return false;
@@ -779,8 +798,10 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
             const uint64_t a = q_desc + q * (Sh::kTileBytes >> 4), b = k_desc + st * (Sh::kTileBytes >> 4);
 #pragma unroll
             for (uint32_t k = 0; k < DP / 16; ++k) {
-                const uint64_t step = (k >> 2) * (kBlock >> 4) + (k & 3) * 2;   // 64 elements a block, 16 a step
-                if (k < k_steps) mma_ss(tmem + x * 128, a + step, b + step, id_s, k != 0);
+                // 64 elements a block, 16 a step
+                if (k < k_steps)
+                    mma_ss(tmem + x * 128, a + (k >> 2) * (kBlock >> 4) + (k & 3) * 2,
+                           b + (k >> 2) * (kv_half >> 4) + (k & 3) * 2, id_s, k != 0);
             }
             mma_commit(s_full(x));
         };
@@ -795,7 +816,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 tc_fence_after();
 #pragma unroll
                 for (uint32_t k = h * 4; k < h * 4 + 4; ++k)
-                    mma_ts(tmem + 256 + x * 128, tmem + x * 128 + k * 8, b + k * (2048 >> 4), id_o, add || k != 0);
+                    mma_ts(tmem + 256 + x * 128, tmem + x * 128 + k * 8, b + k * (2 * kv_group >> 4), id_o, add || k != 0);
             }
             return true;
         };

@@ -78,9 +78,11 @@ int launch_few(lsmkv_ctx *ctx, cudaStream_t s, bool follows, const AttendJob &jo
     return LSMKV_OK;
 }
 
-// Rows as the copy engine sees them: elements, heads, tokens; boxes of 64 elements, swizzled.
-bool make_map(uint32_t dtype, const void *base, const uint64_t (&dims)[3], uint64_t head_stride,
-              uint64_t token_stride, uint32_t box_heads, uint32_t box_tokens, CUtensorMap *map)
+// A tensor map of 16-bit floats, swizzled; dims and box from the innermost on, strides in elements
+// of the dimensions behind it.
+template <int R>
+bool make_map(uint32_t dtype, const void *base, const uint64_t (&dims)[R], const uint64_t (&strides)[R - 1],
+              const uint32_t (&box)[R], CUtensorMap *map)
 {
     static const PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
         void *p = nullptr;
@@ -92,12 +94,18 @@ bool make_map(uint32_t dtype, const void *base, const uint64_t (&dims)[3], uint6
         }
         return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
     }();
-    if (!encode || dims[2] == 0 || dims[2] > 0x7FFFFFFFull) return false;     // coordinates are 32-bit
-    const cuuint64_t d[3] = {dims[0], dims[1], dims[2]};
-    const cuuint64_t strides[2] = {head_stride * 2, token_stride * 2};
-    const cuuint32_t box[3] = {64, box_heads, box_tokens}, step[3] = {1, 1, 1};
-    return encode(map, dtype == LSMKV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                  3, const_cast<void *>(base), d, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    if (!encode) return false;
+    cuuint64_t d[R], st[R - 1];
+    cuuint32_t bx[R], step[R];
+    for (int i = 0; i < R; ++i) {
+        if (dims[i] == 0 || dims[i] > 0x7FFFFFFFull) return false;       // coordinates are 32-bit
+        d[i] = dims[i];
+        bx[i] = box[i];
+        step[i] = 1;
+        if (i) st[i - 1] = strides[i - 1] * 2;
+    }
+    return encode(map, dtype == LSMKV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, R,
+                  const_cast<void *>(base), d, st, bx, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -115,14 +123,21 @@ int launch_many(lsmkv_ctx *ctx, cudaStream_t s, bool follows, AttendJob &job)
     std::memset(&map, 0, sizeof(map));
     std::memset(&q_map, 0, sizeof(q_map));
     // (the map's address is filled in by the kernel, which finds it in the pool's table)
-    const uint64_t row = (uint64_t)g.n_kv_heads * g.head_dim;
-    const bool boxes = job.box_rows >= 8 && job.num_pages < 0x7FFFFFFFull / g.page_tokens &&
-                       make_map(dtype, ctx->d_attend, {g.head_dim, g.n_kv_heads, job.num_pages * g.page_tokens},
-                                g.head_dim, row, 1, job.box_rows, &map);
+    const uint64_t row = (uint64_t)g.n_kv_heads * g.head_dim, D = g.head_dim;
+    bool boxes = job.box_rows >= 8 && job.num_pages < 0x7FFFFFFFull / g.page_tokens;
+    // A box with all elements of a head, where they are whole blocks of 64: half as many boxes at
+    // head_dim 128, and the engine's time goes by boxes (pages of 16: 909 -> WIDE TFLOP/s).
+    job.wide_boxes = D % 64 == 0;
+    if (boxes && job.wide_boxes)
+        boxes = make_map<5>(dtype, ctx->d_attend, {64, 8, D / 64, job.num_pages * g.page_tokens / 8, g.n_kv_heads},
+                            {row, 64, 8 * row, D}, {64, 8, (uint32_t)D / 64, job.box_rows / 8, 1}, &map);
+    else if (boxes)
+        boxes = make_map<3>(dtype, ctx->d_attend, {D, g.n_kv_heads, job.num_pages * g.page_tokens}, {D, row},
+                            {64, 1, job.box_rows}, &map);
     // The 128 rows of half a tile are a box of queries when the heads of a KV head divide them.
     job.q_boxes = boxes && job.group <= 128 && (job.group & (job.group - 1)) == 0 &&
-                  make_map(dtype, job.q, {g.head_dim, job.n_q_heads, job.seqs.n_new}, job.q_hs, job.q_ts, job.group,
-                           128 / job.group, &q_map);
+                  make_map<3>(dtype, job.q, {D, job.n_q_heads, job.seqs.n_new}, {job.q_hs, job.q_ts},
+                              {64, job.group, 128 / job.group}, &q_map);
     if (job.head_dim <= 64)
         CU(ctx, start(ctx, s, follows, boxes ? k_attend_many<T, 64, true> : k_attend_many<T, 64, false>, sm,
                       ManyShape<64>::kThreads, ManyShape<64>::kSmem, job, map, q_map));
