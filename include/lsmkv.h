@@ -519,7 +519,7 @@ typedef struct {
 } lsmkv_seqs_t;
 
 /* Rows of head_dim contiguous elements: row (t, h) starts at data + t*token_stride +
- * h*head_stride elements. data 16-byte aligned, strides multiples of 8 (LSMKV_EINVAL). */
+ * h*head_stride elements. data 16-byte aligned, strides multiples of 8 below 2^32 (LSMKV_EINVAL). */
 typedef struct {
     void *data;            /* [dev] */
     uint64_t token_stride, head_stride;

@@ -45,6 +45,34 @@ template <> struct Half2<__half> {
     static __device__ __forceinline__ __half down1(float v) { return __float2half_rn(v); }
 };
 
+// Two operations of a kind in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "add.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "mul.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
 // The batch as the kernels take it.
 struct SeqArgs {
     uint64_t n_new;
@@ -92,18 +120,18 @@ struct AppendJob {
     uint32_t rot_dim, interleaved;
     const void *q_norm, *k_norm;
     float eps;
-    uint32_t parts;      // warps that share a token's heads
+    uint32_t tokens;     // vector form: tokens of a block
+    uint32_t parts;      // element form: warps that share a token's heads
     uint32_t lane_log2;  // vector form: lanes per head, as a power of two
     DevStatus *st;
 };
 
 // The sequence of row t: the largest i with new_off[i] <= t, found by the warp's lanes together
-// (33 parts a trip: two trips up to 1088 sequences). A batch of equal lengths needs one guess.
+// (33 parts a trip: two trips up to 1088 sequences). A batch of one token each needs one look.
 __device__ __forceinline__ uint32_t find_seq(const uint64_t *off, uint32_t n_seq, uint64_t n_new,
                                              uint64_t t, unsigned lane)
 {
-    const uint32_t guess = n_seq == n_new ? (uint32_t)t : (uint32_t)(t * n_seq / n_new);
-    if (off[guess] <= t && off[guess + 1] > t) return guess;
+    if (n_seq == n_new && off[t] <= t && off[t + 1] > t) return (uint32_t)t;
     uint32_t lo = 0, hi = n_seq;   // off[lo] <= t, and off[hi] > t or hi == n_seq
     while (hi - lo > 1) {
         const uint32_t span = hi - lo;
@@ -193,23 +221,26 @@ __device__ __forceinline__ T *head_dst(const AppendJob &j, uint64_t t, uint32_t 
 // Vector form. 2^lane_log2 lanes per head, two 16-byte pieces a lane: for half-split pairs the
 // lanes below rot_dim/16 hold piece l and its partner piece l + rot_dim/16; all others (and
 // interleaved pairs, which lie inside a piece) hold neighbouring pieces.
-// A warp's U heads-per-lane-group loads are in flight together.
-template <typename T, int U>
-__global__ __launch_bounds__(128) void k_append(const AppendJob j)
+// A block takes `tokens` tokens: its warps first look up the tokens' places and angles, one each,
+// then go through all query heads, all keys, all values, a head per lane group and pass, the next
+// pass's pieces loaded ahead. Instructions count as much as bytes: with kinds, addresses and
+// weights worked out head by head (400 instructions a pass) the same traffic ran at 4.4 TB/s.
+// kOne: a token a block, for small batches: the first pass of all three kinds is loaded before
+// anything is looked up.
+constexpr int kAppendWarps = 8;
+template <typename T, bool kOne>
+__global__ __launch_bounds__(kAppendWarps * 32, kOne ? 2 : 4) void k_append(const __grid_constant__ AppendJob j)
 {
-    const unsigned lane = lane_id();
-    const uint64_t warp = (uint64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    const uint64_t t = warp / j.parts;
-    const uint32_t part = (uint32_t)(warp % j.parts);
-    if (t >= j.seqs.n_new) return;
+    __shared__ TokenPlace places[kAppendWarps];
+    __shared__ __align__(16) float angles[kAppendWarps][256];    // cosines and sines of the tokens
+    const unsigned lane = lane_id(), w = threadIdx.x >> 5;
+    const uint32_t t0 = blockIdx.x * j.tokens;
+    const uint32_t here = min((uint32_t)j.seqs.n_new - t0, j.tokens);
     T *const kbuf = static_cast<T *>(j.kv_ptrs[j.layer]);
     T *const vbuf = static_cast<T *>(j.kv_ptrs[j.n_layers + j.layer]);
 
-    const uint32_t slots = j.n_q_heads + 2 * j.n_kv_heads;
     const uint32_t lanes = 1u << j.lane_log2, groups = 32u >> j.lane_log2;
-    const uint32_t l = lane & (lanes - 1), g = lane >> j.lane_log2;
-    const uint32_t pieces = j.head_dim / 8;
-    const uint32_t half = j.rot_dim / 2;
+    const uint32_t l = lane & (lanes - 1), pieces = j.head_dim / 8, half = j.rot_dim / 2;
     const bool split = !j.interleaved && j.rot_dim;
     uint32_t pa, pb;      // this lane's pieces; >= pieces: none
     if (split && l < half / 8) {
@@ -223,130 +254,166 @@ __global__ __launch_bounds__(128) void k_append(const AppendJob j)
         pb = pa + 1;
     }
     const bool has_a = pa < pieces, has_b = pb < pieces;
+    // pairs (P, Q) of this lane that are turned: all, none, or (interleaved) the first few
+    const uint32_t turned = split ? (l < half / 8 ? 8u : 0u) : half > pa * 4 ? min(8u, half - pa * 4) : 0u;
+    const uint32_t angle_at = split ? pa * 8 : pa * 4;
+    const float per_element = 1.f / (float)j.head_dim;
+    const uint32_t stride = kAppendWarps * groups, r0 = w * groups + (lane >> j.lane_log2);
 
-    TokenPlace at;
-    float c[8], s[8];
-    bool known = false;
-    const uint32_t step = groups * j.parts;
-    for (uint32_t h0 = part * groups; h0 < slots; h0 += step * U) {
-        uint4 a[U], b[U];
-        int kind[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t h = h0 + u * step + g;
-            a[u] = b[u] = make_uint4(0, 0, 0, 0);
-            kind[u] = 3;
-            if (h < slots) {
-                const uint4 *src = reinterpret_cast<const uint4 *>(head_src<T>(j, t, h, &kind[u]));
-                if (has_a) a[u] = src[pa];
-                if (has_b) b[u] = src[pb];
-            }
-        }
-        if (!known) {
-            known = true;
-            at = place_token(j, t, lane, part == 0);
-            if (((reinterpret_cast<uintptr_t>(kbuf) | reinterpret_cast<uintptr_t>(vbuf)) & 15u)) {
-                if (lane == 0) st_flag(j.st, LSMKV_ST_MISALIGNED, 0);
-                return;
-            }
-            if (at.state == 0) return;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { c[e] = 1.f; s[e] = 0.f; }
-            if (at.state == 2 && j.rot_dim) {
-                const float *row = j.table + at.angle * j.rot_dim;
-                // half-split: eight pairs of pieces a and b; interleaved: four pairs of each
-                const uint32_t first = split ? pa * 8 : pa * 4;
-                const uint32_t n_a = split ? (l < half / 8 ? 8u : 0u)
-                                           : (first < half ? min(8u, half - first) : 0u);
-#pragma unroll
-                for (int e = 0; e < 8; e += 4) {
-                    if ((uint32_t)e < n_a) {
-                        const float4 cc = *reinterpret_cast<const float4 *>(row + first + e);
-                        const float4 ss = *reinterpret_cast<const float4 *>(row + half + first + e);
-                        c[e] = cc.x; c[e + 1] = cc.y; c[e + 2] = cc.z; c[e + 3] = cc.w;
-                        s[e] = ss.x; s[e + 1] = ss.y; s[e + 2] = ss.z; s[e + 3] = ss.w;
-                    }
-                }
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t h = h0 + u * step + g;
-            const void *w = kind[u] == 0 ? j.q_norm : kind[u] == 1 ? j.k_norm : nullptr;
-            const bool touch = kind[u] < 2 && (w || j.rot_dim);
-            float scale = 1.f;
-            // the sum of squares needs every lane of the warp, whatever its head's kind
-            if (j.q_norm || j.k_norm) {
-                float sum = 0.f;
-                const uint32_t *ra = &a[u].x, *rb = &b[u].x;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 x = Half2<T>::up(ra[e]), y = Half2<T>::up(rb[e]);
-                    sum += x.x * x.x + x.y * x.y + y.x * y.x + y.y * y.y;
-                }
-                for (uint32_t d = lanes >> 1; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-                if (w) scale = rsqrtf(sum / (float)j.head_dim + j.eps);
-            }
-            if (touch && at.state == 2) {
-                float x[16];
-                uint32_t *ra = &a[u].x, *rb = &b[u].x;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 p = Half2<T>::up(ra[e]), q = Half2<T>::up(rb[e]);
-                    x[2 * e] = p.x; x[2 * e + 1] = p.y;
-                    x[8 + 2 * e] = q.x; x[8 + 2 * e + 1] = q.y;
-                }
-                if (w) {
-                    const uint4 *wv = static_cast<const uint4 *>(w);
-                    const uint4 wa = has_a ? wv[pa] : make_uint4(0, 0, 0, 0);
-                    const uint4 wb = has_b ? wv[pb] : make_uint4(0, 0, 0, 0);
-                    const uint32_t *qa = &wa.x, *qb = &wb.x;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 p = Half2<T>::up(qa[e]), q = Half2<T>::up(qb[e]);
-                        x[2 * e] *= scale * p.x; x[2 * e + 1] *= scale * p.y;
-                        x[8 + 2 * e] *= scale * q.x; x[8 + 2 * e + 1] *= scale * q.y;
-                    }
-                }
-                if (split && l < half / 8) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float p = x[e], q = x[8 + e];
-                        x[e] = p * c[e] - q * s[e];
-                        x[8 + e] = q * c[e] + p * s[e];
-                    }
-                } else if (!split && j.rot_dim) {
-                    const uint32_t first = pa * 4;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if (first + e < half) {
-                            const float p = x[2 * e], q = x[2 * e + 1];
-                            x[2 * e] = p * c[e] - q * s[e];
-                            x[2 * e + 1] = q * c[e] + p * s[e];
-                        }
-                    }
-                }
-                // elements that neither norm nor rotation touched keep their bits
-                const uint32_t turned = split ? (l < half / 8 ? 8u : 0u)
-                                              : half > pa * 4 ? half - pa * 4 : 0u;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (w || (uint32_t)e < turned) ra[e] = Half2<T>::down(x[2 * e], x[2 * e + 1]);
-                    if (w || (uint32_t)e + 4 < turned)
-                        rb[e] = Half2<T>::down(x[8 + 2 * e], x[8 + 2 * e + 1]);
-                }
-            }
-            if (kind[u] == 3) continue;
-            if (at.state == 1) {
-                if (kind[u] != 0) continue;
-                a[u] = b[u] = make_uint4(0, 0, 0, 0);
-            }
-            uint4 *dst = reinterpret_cast<uint4 *>(head_dst<T>(j, t, h, at, kbuf, vbuf));
-            if (!dst) continue;
-            if (has_a) dst[pa] = a[u];
-            if (has_b) dst[pb] = b[u];
-        }
+    auto fetch = [&](const T *src, uint32_t ts, uint32_t hs, uint32_t tok, uint32_t h, uint4 &a, uint4 &b) {
+        a = b = make_uint4(0, 0, 0, 0);
+        if (tok >= here) return;
+        const uint4 *row = reinterpret_cast<const uint4 *>(src + ((uint64_t)(t0 + tok) * ts + (uint64_t)h * hs));
+        if (has_a) a = row[pa];
+        if (has_b) b = row[pb];
+    };
+    auto put = [&](T *dst, uint64_t off, const uint4 &a, const uint4 &b) {
+        uint4 *row = reinterpret_cast<uint4 *>(dst + off);
+        if (has_a) row[pa] = a;
+        if (has_b) row[pb] = b;
+    };
+    // All heads of a kind, in passes of `stride` heads: work(token of the block, head, pieces). The
+    // lanes of a warp stay together until its last lane group has no head left.
+    auto first_pass = [&](const T *src, uint32_t ts, uint32_t hs, uint32_t n, uint4 &a, uint4 &b) {
+        fetch(src, ts, hs, r0 / n, r0 % n, a, b);
+    };
+    uint4 q_a, q_b, k_a, k_b, v_a, v_b;
+    if (kOne) {
+        if (j.n_q_heads) first_pass(static_cast<const T *>(j.q), (uint32_t)j.q_ts, (uint32_t)j.q_hs, j.n_q_heads, q_a, q_b);
+        first_pass(static_cast<const T *>(j.k), (uint32_t)j.k_ts, (uint32_t)j.k_hs, j.n_kv_heads, k_a, k_b);
+        first_pass(static_cast<const T *>(j.v), (uint32_t)j.v_ts, (uint32_t)j.v_hs, j.n_kv_heads, v_a, v_b);
     }
+    auto sweep = [&](const T *src, uint32_t ts, uint32_t hs, uint32_t n, uint4 &a, uint4 &b, auto work) {
+        uint32_t tok = r0 / n, h = r0 - tok * n;
+        uint4 na, nb;
+        if (!kOne) fetch(src, ts, hs, tok, h, a, b);
+        while (__any_sync(~0u, tok < here)) {
+            const uint32_t on = tok, at = h;
+            h += stride;
+            while (h >= n) {
+                h -= n;
+                ++tok;
+            }
+            fetch(src, ts, hs, tok, h, na, nb);
+            work(on, at, a, b);
+            a = na;
+            b = nb;
+        }
+    };
+    if (w < here) {
+        const TokenPlace at = place_token(j, t0 + w, lane, true);
+        if (lane == 0) places[w] = at;
+        if (at.state == 2)
+            for (uint32_t e = lane * 4; e < j.rot_dim; e += 128)
+                *reinterpret_cast<float4 *>(&angles[w][e]) =
+                    *reinterpret_cast<const float4 *>(j.table + at.angle * j.rot_dim + e);
+    }
+    if (((reinterpret_cast<uintptr_t>(kbuf) | reinterpret_cast<uintptr_t>(vbuf)) & 15u)) {
+        if (threadIdx.x == 0) st_flag(j.st, LSMKV_ST_MISALIGNED, 0);
+        return;
+    }
+    __syncthreads();
+
+    // norm and rotation of the queries or keys, then write(token, head, place, pieces)
+    auto turn_heads = [&](const T *src, uint32_t ts, uint32_t hs, uint32_t n, uint4 &a0, uint4 &b0, const void *weights, auto write) {
+        float2 wa[4], wb[4];
+        if (weights) {
+            const uint4 *wv = static_cast<const uint4 *>(weights);
+            const uint4 qa = has_a ? wv[pa] : make_uint4(0, 0, 0, 0), qb = has_b ? wv[pb] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                wa[e] = Half2<T>::up((&qa.x)[e]);
+                wb[e] = Half2<T>::up((&qb.x)[e]);
+            }
+        }
+        sweep(src, ts, hs, n, a0, b0, [&](uint32_t tok, uint32_t h, uint4 &a, uint4 &b) {
+            uint32_t *ra = &a.x, *rb = &b.x;
+            float2 x[4], y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] = Half2<T>::up(ra[e]);
+                y[e] = Half2<T>::up(rb[e]);
+            }
+            float scale = 1.f;
+            if (weights) {
+                float2 sum = mul2(x[0], x[0]), more = mul2(y[0], y[0]);
+#pragma unroll
+                for (int e = 1; e < 4; ++e) {
+                    sum = fma2(x[e], x[e], sum);
+                    more = fma2(y[e], y[e], more);
+                }
+                sum = add2(sum, more);
+                float all = sum.x + sum.y;
+                for (uint32_t d = lanes >> 1; d; d >>= 1) all += __shfl_xor_sync(~0u, all, d);
+                scale = rsqrtf(all * per_element + j.eps);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = mul2(x[e], wa[e]);
+                    y[e] = mul2(y[e], wb[e]);
+                }
+            }
+            if (tok >= here) return;
+            const float *row = angles[tok] + angle_at;
+            if (split && turned) {
+                const float2 minus = make_float2(-1.f, -1.f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float4 cs = *reinterpret_cast<const float4 *>(row + (e & 2) * 2);
+                    const float4 ss = *reinterpret_cast<const float4 *>(row + half + (e & 2) * 2);
+                    const float2 c = e & 1 ? make_float2(cs.z, cs.w) : make_float2(cs.x, cs.y);
+                    const float2 s = e & 1 ? make_float2(ss.z, ss.w) : make_float2(ss.x, ss.y);
+                    const float2 p = fma2(mul2(y[e], s), minus, mul2(x[e], c));
+                    y[e] = fma2(y[e], c, mul2(x[e], s));
+                    x[e] = p;
+                }
+            } else if (!split) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if ((uint32_t)e < turned) {
+                        float2 &v = e < 4 ? x[e] : y[e - 4];
+                        const float c = row[e], s = row[half + e], p = v.x;
+                        v.x = p * c - v.y * s;
+                        v.y = v.y * c + p * s;
+                    }
+                }
+            }
+            // what neither norm nor rotation touched keeps its bits
+            const float2 sc = make_float2(scale, scale);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (weights) {
+                    x[e] = mul2(x[e], sc);
+                    y[e] = mul2(y[e], sc);
+                }
+                if (weights || (uint32_t)e < turned) ra[e] = Half2<T>::down(x[e].x, x[e].y);
+                if (weights || (uint32_t)e + 4 < turned) rb[e] = Half2<T>::down(y[e].x, y[e].y);
+            }
+            write(tok, h, a, b);
+        });
+    };
+    // slot of a stored token, ~0 for one that is not stored
+    auto slot_of = [&](uint32_t tok) { return places[tok].state == 2 ? places[tok].slot : ~0ull; };
+    const uint32_t D = j.head_dim, H = j.n_kv_heads;
+    if (j.n_q_heads)
+        turn_heads(static_cast<const T *>(j.q), (uint32_t)j.q_ts, (uint32_t)j.q_hs, j.n_q_heads, q_a, q_b, j.q_norm,
+                   [&](uint32_t tok, uint32_t h, uint4 &a, uint4 &b) {
+                       const int state = places[tok].state;
+                       if (state == 1) a = b = make_uint4(0, 0, 0, 0);      // padding
+                       if (state)
+                           put(static_cast<T *>(j.q_out),
+                               (uint64_t)(t0 + tok) * (uint32_t)j.o_ts + (uint64_t)h * (uint32_t)j.o_hs, a, b);
+                   });
+    turn_heads(static_cast<const T *>(j.k), (uint32_t)j.k_ts, (uint32_t)j.k_hs, H, k_a, k_b, j.k_norm,
+               [&](uint32_t tok, uint32_t h, uint4 &a, uint4 &b) {
+                   const uint64_t slot = slot_of(tok);
+                   if (slot != ~0ull) put(kbuf, (slot * H + h) * D, a, b);
+               });
+    sweep(static_cast<const T *>(j.v), (uint32_t)j.v_ts, (uint32_t)j.v_hs, H, v_a, v_b,
+          [&](uint32_t tok, uint32_t h, uint4 &a, uint4 &b) {
+              if (tok >= here) return;
+              const uint64_t slot = slot_of(tok);
+              if (slot != ~0ull) put(vbuf, (slot * H + h) * D, a, b);
+          });
 }
 
 // Element form, for rotations whose halves are not whole 16-byte pieces: a warp takes a head at

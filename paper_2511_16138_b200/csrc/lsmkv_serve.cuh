@@ -22,7 +22,8 @@ bool seqs_ok(const lsmkv_seqs_t *s)
 
 bool rows_ok(const lsmkv_rows_t *r)
 {
-    return r && r->data && aligned16(r->data) && r->token_stride % 8 == 0 && r->head_stride % 8 == 0;
+    return r && r->data && aligned16(r->data) && r->token_stride % 8 == 0 && r->head_stride % 8 == 0 &&
+           r->token_stride <= 0xFFFFFFFFull && r->head_stride <= 0xFFFFFFFFull;
 }
 
 SeqArgs seq_args(const lsmkv_seqs_t *s)
@@ -319,7 +320,7 @@ extern "C" int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, 
     if (rope && (!rope->table || !aligned16(rope->table) || rope->rot_dim % 2 || rope->rot_dim == 0 ||
                  rope->rot_dim > g.head_dim || rope->interleaved > 1))
         return LSMKV_EINVAL;
-    if (n_q_heads > 0x10000u || seqs->n_new > 0xFFFFFFFFull) return LSMKV_EINVAL;
+    if (n_q_heads > 0x10000u || seqs->n_new > 0x7FFFFFFFull) return LSMKV_EINVAL;
     AppendJob job;
     std::memset(&job, 0, sizeof(job));
     job.seqs = seq_args(seqs);
@@ -364,29 +365,28 @@ extern "C" int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, 
     // Whole 16-byte pieces on both sides of a pair (or no pair that leaves its piece): vector
     // form. Otherwise element by element.
     const bool vec = job.rot_dim % (job.interleaved ? 8 : 16) == 0;
-    uint32_t per_pass = 1;       // head slots that a warp takes at once
-    constexpr uint32_t U = 4;
+    const bool bf = dtype == LSMKV_BF16;
     if (vec) {
         const uint32_t lanes = job.interleaved || !job.rot_dim
                                    ? (g.head_dim / 8 + 1) / 2
                                    : job.rot_dim / 16 + (g.head_dim - job.rot_dim + 15) / 16;
         while ((1u << job.lane_log2) < lanes) ++job.lane_log2;
-        per_pass = (32u >> job.lane_log2) * U;
+        // as many tokens a block as one round of blocks, four a SM, leaves; at most one a warp
+        const uint64_t round = (uint64_t)ctx->sm_count * 4;
+        job.tokens = (uint32_t)std::min<uint64_t>(kAppendWarps, (seqs->n_new + round - 1) / round);
+        const uint64_t grid = (seqs->n_new + job.tokens - 1) / job.tokens;
+        // (that form has more registers: two blocks a SM; 512 tokens of 36 heads 8.9 us, 7.3 without)
+        auto kern = seqs->n_new <= (uint64_t)ctx->sm_count * 2
+                        ? (bf ? k_append<__nv_bfloat16, true> : k_append<__half, true>)
+                        : (bf ? k_append<__nv_bfloat16, false> : k_append<__half, false>);
+        kern<<<(unsigned)grid, kAppendWarps * 32, 0, s>>>(job);
+    } else {
+        // as many warps a token as keep the GPU busy
+        const uint64_t fill = (uint64_t)ctx->sm_count * 16;
+        job.parts = (uint32_t)std::min<uint64_t>((fill + seqs->n_new - 1) / seqs->n_new, slots);
+        const uint64_t grid = (seqs->n_new * job.parts + 3) / 4;
+        (bf ? k_append_elements<__nv_bfloat16> : k_append_elements<__half>)<<<(unsigned)grid, 128, 0, s>>>(job);
     }
-    // A warp per token when there are tokens enough to fill the GPU; with fewer, several warps
-    // share a token's heads, down to one pass each.
-    const uint32_t most = (slots + per_pass - 1) / per_pass;
-    const uint64_t fill = (uint64_t)ctx->sm_count * 16;
-    uint64_t parts = (fill + seqs->n_new - 1) / seqs->n_new;
-    job.parts = (uint32_t)(parts < most ? parts : most);
-    const uint64_t warps = seqs->n_new * job.parts;
-    constexpr unsigned kWarps = 4;
-    const uint64_t grid = (warps + kWarps - 1) / kWarps;
-    if (grid > 0x7FFFFFFFull) return LSMKV_EINVAL;
-    const bool bf = dtype == LSMKV_BF16;
-    void (*kern)(AppendJob) = vec ? (bf ? k_append<__nv_bfloat16, U> : k_append<__half, U>)
-                                  : (bf ? k_append_elements<__nv_bfloat16> : k_append_elements<__half>);
-    kern<<<(unsigned)grid, kWarps * 32, 0, s>>>(job);
     ++ctx->launches;
     CU(ctx, cudaGetLastError());
     return LSMKV_OK;
