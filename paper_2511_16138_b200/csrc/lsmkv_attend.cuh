@@ -46,12 +46,14 @@ struct AttendJob {
     float *pre_lse;              // f32 [n_new][n_q_heads], base 2
     uint32_t dp;                 // elements of a part's row
     float *parts;                // two slots per CTA
+    float *few_parts;            // (host side: the few-row kernel's, which may run beside the other)
     unsigned int *arrived;       // few rows: one counter per CTA, zero between calls
     struct CutDesc *cuts;        // many rows: the cut tile that starts in a CTA's span
     uint64_t *span_begin;        // many rows: where the spans begin on the line, and its end
     uint32_t *tile_base;         // many rows: row tiles ahead of every item
     void *maps;                  // many rows: two tensor maps per CTA
     uint32_t box_rows;           // tokens of a box, dividing page_tokens
+    uint32_t beside;             // the launch before has nothing for this one: wait for it at the end
     uint32_t wide_boxes;         // a box has all elements of a head, not 64
     uint32_t q_boxes;            // the queries come by boxes too
     long long wait_cycles;
@@ -171,10 +173,18 @@ struct Span {
 
 // A call's launches follow each other closely: each lets the next one start while it still runs
 // and itself waits, first of all, for what the one before has written.
+__device__ __forceinline__ void wait_launch() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 __device__ __forceinline__ void follow_launch()
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_launch();
+}
+
+// 64-bit division takes hundreds of cycles; most quotients here are of small numbers.
+__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b)
+{
+    return (a | b) >> 32 ? a / b : (uint32_t)a / (uint32_t)b;
 }
 
 // Inclusive sum over a CTA's threads, and the total; scratch: NT / 32 words of shared memory.
@@ -215,7 +225,8 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
 {
     __shared__ uint64_t scan[NT / 32];
     __shared__ uint64_t found_before, mine_begin, mine_end;
-    __shared__ uint32_t found_item, mine_rank;
+    __shared__ unsigned long long all_bytes;
+    __shared__ uint32_t found_item, mine_rank, all_tiles;
     const uint32_t tid = threadIdx.x, N = gridDim.x;
     const uint32_t each = (n + NT - 1) / NT;
     const uint32_t i0 = tid * each < n ? tid * each : n;
@@ -234,28 +245,42 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
             bytes += (uint64_t)(it.kv1 - it.kv0) * j.n_kv_heads * j.head_dim * 4;
         }
     }
+    const bool may_wave = kWaves && !j.prefix_pass;
+    if (may_wave) {
+        if (tid == 0) {
+            all_bytes = 0;
+            all_tiles = 0;
+        }
+        __syncthreads();
+        if (tiles) {
+            atomicAdd(&all_bytes, (unsigned long long)bytes);
+            atomicAdd(&all_tiles, tiles);
+        }
+    }
     uint64_t total;
     const uint64_t incl = block_scan<NT>(mine, scan, &total);
     Span s;
-    s.per = (total + N - 1) / N;
+    s.per = quotient(total + N - 1, N);
     s.begin = s.per * blockIdx.x;
     s.end = s.begin + s.per;
     if (s.end > total) s.end = total;
     if (s.begin > total) s.begin = total;
     s.waves = 0;
     s.rank = blockIdx.x;
-    if (kWaves) {
-        uint64_t all_tiles;
-        uint32_t base = (uint32_t)(block_scan<NT>(tiles, scan, &all_tiles) - tiles);
-        // every CTA writes all of tile_base and span_begin, the same values, and reads its own
+    uint32_t waves = may_wave && all_bytes > kL2Keeps ? all_tiles / N : 0;
+    if (kWaves && !waves) {
+        // equal spans; every CTA writes all of span_begin, the same values, and reads its own
+        for (uint32_t c = tid; c <= N; c += NT) j.span_begin[c] = c * s.per < total ? c * s.per : total;
+    }
+    if (waves) {
+        uint64_t ignored;
+        uint32_t base = (uint32_t)(block_scan<NT>(tiles, scan, &ignored) - tiles);
+        // (tile_base likewise)
         for (uint32_t i = i0; i < i1; ++i) {
             j.tile_base[i] = base;
             base += item_tiles(j, load_item(j, i), M) * j.n_kv_heads;
         }
         if (i1 == n && i0 < i1) j.tile_base[n] = base;
-        uint64_t all_bytes;
-        block_scan<NT>(bytes, scan, &all_bytes);
-        uint32_t waves = j.prefix_pass || all_bytes <= kL2Keeps ? 0 : (uint32_t)(all_tiles / N);
         uint64_t capacity = s.per;                       // of CTA tid, behind its waves
         const uint32_t team = n < NT ? NT / n : 1;       // threads that go through an item's tiles
         while (waves) {
@@ -274,7 +299,7 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
         }
         if (waves) capacity = tid < N ? s.per - load[tid] : 0;
         if (tid >= N) capacity = 0;
-        uint64_t sum, ignored;
+        uint64_t sum;
         const uint64_t taken = waves && tid < N ? load[tid] : 0;
         block_scan<NT>(taken, scan, &sum);               // units of the waves: the line goes on there
         const uint64_t upto = sum + block_scan<NT>(capacity, scan, &ignored);
@@ -381,7 +406,7 @@ struct Walk {
         // the tile that holds unit s.begin
         const uint64_t per_head = item_units(j, it, M, TILE);
         const uint64_t rel = u - s.before;
-        p.kv_head = (uint32_t)(rel / per_head);
+        p.kv_head = (uint32_t)quotient(rel, per_head);
         uint64_t at = rel - (uint64_t)p.kv_head * per_head;
         p.tile0 = s.before + (uint64_t)p.kv_head * per_head;
         p.rt = 0;
@@ -1056,8 +1081,8 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
             __syncthreads();
         }
         if (!whole) {
-            const uint32_t c0 = (uint32_t)(cut.tile0 / span.per),
-                           c1 = (uint32_t)((cut.tile0 + cut.units - 1) / span.per);
+            const uint32_t c0 = (uint32_t)quotient(cut.tile0, span.per),
+                           c1 = (uint32_t)quotient(cut.tile0 + cut.units - 1, span.per);
             if (deliver_part(j, c0, c1)) merge_parts<T, NT>(j, done, cut, c0, c1, Sh::kM, 0, cut.rows);
         }
     }

@@ -298,7 +298,9 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     __shared__ float half_m[128], half_l[128];   // the second half's statistics, when the halves share rows
     const uint32_t tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const uint32_t G = j.group, D = j.head_dim;
-    follow_launch();
+    // (what comes behind may count on the launch before this one: nobody leaves ahead of it)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (!j.beside) wait_launch();
     if (tid == 0) j.cuts[blockIdx.x].p.rows = 0;
 
     const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
@@ -307,9 +309,13 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                                                     reinterpret_cast<uint32_t *>(smem_raw));
     if ((reinterpret_cast<uintptr_t>(kbuf) | reinterpret_cast<uintptr_t>(vbuf)) & 15u) {
         if (blockIdx.x == 0 && tid == 0) st_flag(j.st, LSMKV_ST_MISALIGNED, 0);
+        wait_launch();
         return;
     }
-    if (span.begin >= span.end && !span.waves) return;
+    if (span.begin >= span.end && !span.waves) {
+        wait_launch();
+        return;
+    }
 
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t q_s = base, ring = base + 2 * Sh::kTileBytes;
@@ -354,6 +360,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     if (kBoxes && w == 8) {
         publish_map(maps, map_work, map, kbuf);
         publish_map(maps + 128, map_work, map, vbuf);
+        if (lane < 2) asm volatile("prefetch.tensormap [%0];" :: "l"(maps + lane * 128) : "memory");
     }
     tc_fence_before();
     __syncthreads();
@@ -913,6 +920,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     if (w == Sh::kThreads / 32 - 1)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512u) : "memory");
     if (tid == 0 && stop) st_flag(j.st, LSMKV_ST_WAIT_EXPIRED, blockIdx.x);
+    wait_launch();
 }
 
 }  // namespace lsmkv

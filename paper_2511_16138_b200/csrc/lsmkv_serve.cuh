@@ -168,6 +168,7 @@ int launch_prefix(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
     job.rows_lo = 0;
     job.rows_hi = 0xFFFFFFFFu;
     const uint64_t rows = job.seqs.n_new * job.group;
+    job.beside = 0;
     const int rc = many_takes(ctx) && rows > 64 ? launch_many<T>(ctx, s, false, job)
                                                  : launch_few<T>(ctx, s, false, job, rows <= 8);
     job.prefix_pass = 0;
@@ -184,17 +185,22 @@ int launch_own(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
     job.rows_lo = 0;
     job.rows_hi = mma ? 16 : 0xFFFFFFFFu;
     const uint64_t most = (uint64_t)job.seqs.max_new * job.group;
+    float *const many_parts = job.parts;
+    job.parts = job.few_parts;
     const int rc = launch_few<T>(ctx, s, job.skip != nullptr, job, most <= 8);
+    job.parts = many_parts;
     if (rc != LSMKV_OK || !mma || most <= 16) return rc;
+    // side by side, unless a prefix pass is still ahead of both
+    job.beside = job.skip == nullptr;
     job.rows_lo = 16;
     job.rows_hi = 0xFFFFFFFFu;
     return launch_many<T>(ctx, s, true, job);
 }
 
-// Two part slots for every CTA.
-size_t part_bytes(const lsmkv_ctx *ctx)
+// Two part slots of so many rows for every CTA.
+size_t part_bytes(const lsmkv_ctx *ctx, uint32_t rows)
 {
-    return (size_t)ctx->sm_count * 2 * (many_takes(ctx) ? 256 : 16) * (part_dp(ctx) + 2) * 4;
+    return (size_t)ctx->sm_count * 2 * rows * (part_dp(ctx) + 2) * 4;
 }
 
 // Scratch of the attend kernels for n_seq sequences: counters, descriptors of cut tiles, tensor
@@ -207,7 +213,8 @@ size_t place_attend(const lsmkv_ctx *ctx, void *at, uint32_t n_seq, AttendJob *j
     job->cuts = l.take<CutDesc>(sm);
     job->maps = l.take<unsigned char>(sm * 256);
     job->span_begin = l.take<uint64_t>(sm + 1);
-    job->parts = l.take<float>(part_bytes(ctx) / 4);
+    job->few_parts = l.take<float>(part_bytes(ctx, 16) / 4);
+    job->parts = many_takes(ctx) ? l.take<float>(part_bytes(ctx, 256) / 4) : job->few_parts;
     job->tile_base = l.take<uint32_t>((size_t)n_seq + 1);
     return l.at;
 }
