@@ -4,11 +4,8 @@
 //   y = x * rsqrt(mean(x^2) + eps) * w           (norm, per head, optional)
 //   (a, b) -> (a cos p - b sin p, b cos p + a sin p)   (rotation, per pair, optional)
 //
-// Bound by memory: every element is read once and written once. A warp owns a part of the heads
-// of one token: a lane always holds the same element pairs of a head, so the token's cosines and
-// sines are fetched once into registers and serve all its heads, and no pair crosses lanes. The
-// loads of the heads are issued before the token's sequence is looked up, because only the
-// destination and the angle depend on it.
+// Bound by memory -- every element is read once and written once -- and close behind it by
+// instructions. A lane always holds whole element pairs of a head, so no pair crosses lanes.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -223,8 +220,9 @@ __device__ __forceinline__ T *head_dst(const AppendJob &j, uint64_t t, uint32_t 
 // interleaved pairs, which lie inside a piece) hold neighbouring pieces.
 // A block takes `tokens` tokens: its warps first look up the tokens' places and angles, one each,
 // then go through all query heads, all keys, all values, a head per lane group and pass, the next
-// pass's pieces loaded ahead. Instructions count as much as bytes: with kinds, addresses and
-// weights worked out head by head (400 instructions a pass) the same traffic ran at 4.4 TB/s.
+// pass's pieces loaded ahead. Measured on 64 turns of 256 to 1024 tokens (41k in all) with 28 + 2 x 4
+// heads of 128 and norms, 0.77 GB: 152 us, 5.1 TB/s; with kinds, addresses and weights worked out head
+// by head (400 instructions a pass of four heads) 174 us; a warp per token, its angles in registers, 208.
 // kOne: a token a block, for small batches: the first pass of all three kinds is loaded before
 // anything is looked up.
 constexpr int kAppendWarps = 8;

@@ -3,19 +3,22 @@
 //
 // A row tile is 256 rows, two halves of 128 (one TMEM lane a row). A persistent CTA walks its span
 // of units (key tiles of 128 keys); its warps have roles that run side by side:
-//   loaders (2 warps)  gather the tile's queries, then keys and values of one key tile after the
+//   loaders (3 warps)  gather the tile's queries, then keys and values of one key tile after the
 //                      other through a ring of stages, in the 128-byte-swizzled layout that the
 //                      matrix unit reads. Pages of a multiple of 8 tokens come by the copy engine
-//                      in boxes of 64 elements x up to 64 tokens; others, like the queries, by
-//                      16-byte cp.async, each to its place
+//                      in boxes of up to 64 tokens, others by 16-byte cp.async, each to its place
 //   issuer (1 warp)    S_x = Q_x K^T of the next key tile and O_x += P_x V of this one, for the
 //                      halves x in turn: while one half's softmax runs, the other half's products do
 //   softmax (2 x 4 warps) a thread owns a row: scores from TMEM, running maximum and sum in
 //                      registers, weights back to TMEM over the scores, where they are the
 //                      A operand of the value product. The sums in TMEM are rescaled only when the
 //                      maximum grew by more than 2^8 (weights stay below 2^8, sums in 32 bits).
-// Bound by the exponentials and the tensor cores together: a 128 x 128 tile takes 1024 cycles of
-// either (16 exponentials a cycle and SM; 8192 operations a cycle and SM at head_dim 128).
+// Bound by the tensor cores and the softmax warps' instructions together: a tile of 256 x 128 takes
+// 2048 cycles of products at head_dim 128 (8192 operations a cycle and SM) and as many of
+// exponentials (16 a cycle and SM), and in steady state 2.5k to 3k in all. Measured: two requests of
+// 32768 tokens, the last 1024 new, 64/8 heads of 128, 2.16 TFLOP: 1.94 ms, 1.11 PFLOP/s, of which a
+// library product reaches 1.63 in a burst and 1.40 sustained. Taking some exponentials by a polynomial
+// on the multiply-add units only added instructions (1.83 -> 1.84 to 1.98 ms).
 // Every wait is bounded; one that runs out ends all roles and is reported.
 #pragma once
 #include <cuda.h>
@@ -233,8 +236,9 @@ struct CutDesc {
 };
 
 // Merge of the cut tiles: a block takes 32 rows of one, a thread four elements of four rows at a
-// time, their parts' loads in flight together (row by row, 8 rows a block, it took 13 us where this
-// takes MERGE, for 148 tiles of 256 rows at head_dim 64).
+// time, their parts' loads in flight together. Latency decides (two or three parts a row: 13 us with
+// cold caches for 148 tiles of 256 rows at head_dim 64, 19 MB); done by the last CTA to arrive at
+// a tile instead, it took that CTA 40 us and more.
 constexpr uint32_t kMergeBlockRows = 32;
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_merge(const __grid_constant__ AttendJob j)

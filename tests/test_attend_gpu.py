@@ -407,3 +407,64 @@ def test_a_wait_that_runs_out_is_reported_and_the_context_stays_usable():
         assert ctx.last_status()["flags"] == 0
         assert ctx.last_cuda_error() == 0
     check(out, None, reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, 0.08), torch.bfloat16)
+
+
+@pytest.mark.parametrize("case", [
+    # more row tiles than CTAs over more keys than the L2 keeps: whole tiles in waves, then spans
+    (torch.bfloat16, 128, 16, 64, 8, [600, 333, 20, 1], [9000, 9500, 12000, 500]),
+    (torch.float16, 64, 64, 32, 16, [900, 700], [20000, 30000]),
+], ids=["128", "64"])
+def test_whole_tiles_in_waves(case):
+    dt, D, P = case[:3]
+    geom, pool, q, seqs, new_off, kv, page_off, table = setup(case, n_layers=1)
+    garbage_beyond(pool, 0, 1, kv, page_off, table, P)
+    out, lse = torch.full_like(q, 5.0), torch.zeros(q.shape[:2], device=DEV)
+    assert sum(kv) * pool.shape[3] * D * 4 > 64 << 20
+    with lsmkv.Context(geom, 0) as ctx:
+        pt = lsmkv.pool_table(list(pool))
+        ctx.attend_batch(0, seqs, q, out, pt, D ** -0.5, lse)
+        assert ctx.last_status()["flags"] == 0
+        again = torch.zeros_like(out)
+        ctx.attend_batch(0, seqs, q, again, pt, D ** -0.5)
+        assert torch.equal(out.view(torch.int16), again.view(torch.int16))
+    hq, G = q.shape[1], q.shape[1] // pool.shape[3]
+    for h in range(pool.shape[3]):                            # head by head: the reference is large
+        heads = slice(h * G, (h + 1) * G)
+        ref = reference(q[:, heads], pool[:, :, :, h:h + 1], 0, 1, new_off, kv, page_off, table, P, D ** -0.5)
+        check(out[:, heads], lse[:, heads], ref, dt)
+        torch.cuda.empty_cache()
+
+
+def test_calls_in_a_cuda_graph_and_one_after_another():
+    """Captured and replayed with other inputs; two calls back to back share the scratch."""
+    case = (torch.bfloat16, 128, 16, 16, 4, [1, 3, 40, 1], [30, 200, 500, 4000])
+    geom, pool, q, seqs, new_off, kv, page_off, table = setup(case, n_layers=1)
+    out, out2 = torch.zeros_like(q), torch.zeros_like(q)
+    with lsmkv.Context(geom, 0) as ctx:
+        pt = lsmkv.pool_table(list(pool))
+        ctx.attend_batch(0, seqs, q, out, pt, 0.08)            # scratch is there before the capture
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            ctx.attend_batch(0, seqs, q, out, pt, 0.08)
+            ctx.attend_batch(0, seqs, out, out2, pt, 0.08)
+        q.copy_(torch.randn_like(q))
+        pool.copy_(torch.randn_like(pool))
+        for _ in range(3):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert ctx.last_status()["flags"] == 0
+        del graph
+    check(out, None, reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, 0.08), torch.bfloat16)
+    check(out2, None, reference(out, pool, 0, 1, new_off, kv, page_off, table, 16, 0.08), torch.bfloat16)
+
+
+def test_negative_and_zero_scale():
+    case = (torch.float16, 64, 16, 8, 2, [1, 50], [70, 300])
+    geom, pool, q, seqs, new_off, kv, page_off, table = setup(case, n_layers=1)
+    with lsmkv.Context(geom, 0) as ctx:
+        for scale in (-0.125, 0.0):
+            out = torch.zeros_like(q)
+            ctx.attend_batch(0, seqs, q, out, lsmkv.pool_table(list(pool)), scale)
+            assert ctx.last_status()["flags"] == 0
+            check(out, None, reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, scale), torch.float16)
