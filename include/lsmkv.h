@@ -563,7 +563,10 @@ int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dt
  *   lse_out  [dev] f32[n_new][n_q_heads] or NULL: log(sum exp(scale * q . k)) of every row
  * A row without any key (padding) is zero, its lse -inf. Scores, statistics and sums are held
  * in 32 bits; weights are rounded to `dtype` before they meet the values.
- * Uses (and may grow) scratch of the context: two calls must be ordered by the caller.
+ * Uses (and may grow) scratch of the context: two attends must be ordered by the caller, and the
+ * first of a size comes before any stream capture. A wait that runs out sets
+ * LSMKV_ST_WAIT_EXPIRED; results are then unspecified until lsmkv_last_status() has been called.
+ * Infinities and NaN among the keys and values reach the rows that see them, and no others.
  */
 int lsmkv_attend_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype,
                        const lsmkv_seqs_t *seqs, uint32_t n_q_heads, const lsmkv_rows_t *q,
@@ -663,7 +666,9 @@ uint64_t lsmkv_launch_count(const lsmkv_ctx *ctx);
  *                       one-pass encoder of the compressing codec does the same with the fetch of
  *                       the slab of this number (slabs numbered over the whole batch): the wait
  *                       for it runs out, every role of every CTA leaves through its bounded
- *                       waits, and the records of chunks that were not finished are zeroed
+ *                       waits, and the records of chunks that were not finished are zeroed. The
+ *                       attend kernel for many rows does the same with the key or value tile of
+ *                       this number of its first CTA
  *   "wait_cycles"       limit, in GPU clock cycles, of every bounded wait inside a kernel (the bulk
  *                       copies' completion, the one-pass encoder's hand-offs); default 2e9, about
  *                       a second; 1e5..1e11. A wait that runs out sets LSMKV_ST_WAIT_EXPIRED
