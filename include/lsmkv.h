@@ -24,7 +24,7 @@
  *   - No call allocates device memory except lsmkv_create(), lsmkv_reserve() and a call whose
  *     batch is larger than any before it (the internal scratch of that kind of call grows;
  *     lsmkv_reserve() pre-sizes the scratch of probe and decode, a first full-size call that
- *     of flush, merge, the compressing codec and the host-buffer calls; the first host-buffer
+ *     of flush, merge, the compressing codec, the host-buffer calls and the attends; the first host-buffer
  *     put with the compressing codec also creates a stream and three events of the context's).
  *
  * Formats (version 1). The paper states properties (key order follows token-prefix order;
@@ -559,7 +559,8 @@ int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dt
  * Attend: row (t, h) of out, for a new token at position p, is the softmax-weighted mean of the
  * values of positions 0..p of its sequence under KV head h / (n_q_heads / n_kv_heads), weights
  * softmax(scale * q . k). n_q_heads must be a multiple of n_kv_heads.
- *   q, out   [host] descriptors of n_new x n_q_heads rows of `dtype`; out may be q's rows
+ *   q, out   [host] descriptors of n_new x n_q_heads rows of `dtype`; out may be q's rows (where
+ *            their memory meets and max_new > 1 the queries are copied first)
  *   lse_out  [dev] f32[n_new][n_q_heads] or NULL: log(sum exp(scale * q . k)) of every row
  * A row without any key (padding) is zero, its lse -inf. Scores, statistics and sums are held
  * in 32 bits; weights are rounded to `dtype` before they meet the values.

@@ -64,6 +64,8 @@ struct lsmkv_ctx {
     uint64_t attend_cap;   // bytes
     void *d_prefix;
     uint64_t prefix_cap;   // bytes
+    void *d_queries;       // copy of queries that share memory with the output
+    uint64_t queries_cap;  // bytes
     // host-buffer calls: device staging and host scratch
     void *d_io[3];
     uint64_t io_cap[3];
@@ -634,6 +636,7 @@ int lsmkv_destroy(lsmkv_ctx *ctx)
     if (release_scratch(ctx, &ctx->d_xp, &ctx->xp_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     if (release_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     if (release_scratch(ctx, &ctx->d_prefix, &ctx->prefix_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
+    if (release_scratch(ctx, &ctx->d_queries, &ctx->queries_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     for (int k = 0; k < 3; ++k)
         if (release_scratch(ctx, &ctx->d_io[k], &ctx->io_cap[k], __LINE__) != LSMKV_OK)
             note((cudaError_t)ctx->last_cuda);

@@ -545,50 +545,60 @@ __device__ __noinline__ Quad sum_parts(const float *parts, uint32_t c0, uint32_t
 // an infinite or undefined value there makes the sum undefined although the row must not see
 // it. A row that comes out undefined and has such keys beside it is taken again here, key by key
 // over its own keys alone; finite inputs never come here.
-template <typename T>
-__device__ __noinline__ Quad redo_row4(const AttendJob &j, uint64_t page0, uint64_t row, uint32_t head,
-                                       uint32_t first, uint32_t limit, uint32_t d)
+// W elements from d on, into out; returns the maximum and the sum of weights.
+template <typename T, int W>
+__device__ __noinline__ float2 redo_row(const AttendJob &j, uint64_t page0, uint64_t row, uint32_t head,
+                                        uint32_t first, uint32_t limit, uint32_t d, float *out)
 {
     const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
     const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
-    const T *const q = static_cast<const T *>(j.q) + row * j.q_ts + (uint64_t)head * j.q_hs;
-    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    const uint4 *const q = reinterpret_cast<const uint4 *>(static_cast<const T *>(j.q) + row * j.q_ts +
+                                                           (uint64_t)head * j.q_hs);
+    float m = -INFINITY, l = 0.f, o[W];
+#pragma unroll
+    for (int e = 0; e < W; ++e) o[e] = 0.f;
     for (uint32_t k = first; k < limit; ++k) {
         const uint32_t page = j.seqs.page_table[page0 + k / j.page_tokens];
         const bool real = page < j.num_pages;
         const uint64_t at = (((uint64_t)(real ? page : 0) * j.page_tokens + k % j.page_tokens) *
                                  j.n_kv_heads + head / j.group) * j.head_dim;
-        float s = 0.f;
-        for (uint32_t e = 0; real && e < j.head_dim; ++e) s += Half2<T>::up1(q[e]) * Half2<T>::up1(kbuf[at + e]);
-        s *= j.scale_log2;
+        const uint4 *const key = reinterpret_cast<const uint4 *>(kbuf + at);
+        float2 dot = make_float2(0.f, 0.f);
+        for (uint32_t e = 0; real && e < j.head_dim / 8; ++e) {
+            const uint4 a = q[e], b = key[e];
+            const uint32_t *x = &a.x, *y = &b.x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dot = fma2(Half2<T>::up(x[i]), Half2<T>::up(y[i]), dot);
+        }
+        const float s = (dot.x + dot.y) * j.scale_log2;
         const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
         const float c = exp2f(m - base), w = exp2f(s - base);
         l = l * c + w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = o[e] * c + (real ? w * Half2<T>::up1(vbuf[at + d + e]) : 0.f);
+        for (int e = 0; e < W; ++e)
+            o[e] = o[e] * c + (real && d + e < j.head_dim ? w * Half2<T>::up1(vbuf[at + d + e]) : 0.f);
         m = top;
     }
-    Quad r;
-    r.acc = make_float4(o[0], o[1], o[2], o[3]);
-    r.m = m;
-    r.l = l;
-    return r;
+#pragma unroll
+    for (int e = 0; e < W; ++e) out[e] = o[e];
+    return make_float2(m, l);
 }
 
 // Write four elements of finished row R of the item: acc = sum of weighted values relative to
 // 2^m, l the sum of weights. Merges the prefix pass's result first when there is one.
 template <typename T>
 __device__ __forceinline__ void finish_row4(const AttendJob &j, const Item &it, uint32_t kv_head, uint32_t R,
-                                            uint32_t d, float4 acc, float m, float l)
+                                            uint32_t d, float4 acc, float m, float l, bool may_redo = true)
 {
     const uint64_t row = it.row0 + R / j.group;
     const uint32_t sub = R % j.group, head = kv_head * j.group + sub;
     const uint64_t flat = row * j.n_q_heads + head;
-    if (it.causal && it.tokens > 1 && isnan(acc.x + acc.y + acc.z + acc.w)) {
-        const Quad again = redo_row4<T>(j, it.page0, row, head, it.kv0, token_limit(it, R / j.group), d);
-        acc = again.acc;
-        m = again.m;
-        l = again.l;
+    if (may_redo && it.causal && it.tokens > 1 && isnan(acc.x + acc.y + acc.z + acc.w)) {
+        float o[4];
+        const float2 ml = redo_row<T, 4>(j, it.page0, row, head, it.kv0, token_limit(it, R / j.group), d, o);
+        acc = make_float4(o[0], o[1], o[2], o[3]);
+        m = ml.x;
+        l = ml.y;
     }
     if (it.skip) {
         Quad sum;
@@ -618,12 +628,12 @@ __device__ __forceinline__ void finish_row4(const AttendJob &j, const Item &it, 
     if (d == 0 && j.lse) j.lse[flat] = lse2 * kLn2;
 }
 
-// The same out of line, where the call site is unrolled.
+// The same out of line, where the call site is unrolled (and has taken undefined rows again itself).
 template <typename T>
 __device__ __noinline__ void finish_row4_call(const AttendJob &j, const Item &it, uint32_t kv_head, uint32_t R,
                                               uint32_t d, float4 acc, float m, float l)
 {
-    finish_row4<T>(j, it, kv_head, R, d, acc, m, l);
+    finish_row4<T>(j, it, kv_head, R, d, acc, m, l, false);
 }
 
 // Merge rows [r0, r1) of a cut tile with parts c0..c1, by NT threads.
@@ -1087,6 +1097,17 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
                            c1 = (uint32_t)quotient(cut.tile0 + cut.units - 1, span.per);
             if (deliver_part(j, c0, c1)) merge_parts<T, NT>(j, done, cut, c0, c1, Sh::kM, 0, cut.rows);
         }
+    }
+}
+
+// Rows of a strided tensor to contiguous ones, 16 bytes at a time.
+__global__ void k_gather_rows(const uint4 *src, uint64_t token_stride, uint64_t head_stride, uint64_t n_new,
+                              uint32_t heads, uint32_t pieces, uint4 *dst)
+{
+    const uint64_t all = n_new * heads * pieces;
+    for (uint64_t x = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; x < all; x += (uint64_t)gridDim.x * blockDim.x) {
+        const uint64_t row = x / pieces, t = row / heads;
+        dst[x] = src[t * token_stride + (row - t * heads) * head_stride + (x - row * pieces)];
     }
 }
 

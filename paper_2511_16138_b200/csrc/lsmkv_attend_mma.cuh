@@ -564,11 +564,18 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                             *reinterpret_cast<uint4 *>(dst + e) = pk;
                         }
                     } else {
+                        float2 ml = make_float2(m, l);
+                        if (isnan(all) && cw.it.causal && cw.it.tokens > 1) {
+                            float o[32];
+                            ml = redo_row<T, 32>(j, cw.it.page0, out_row, out_head, cw.it.kv0, lim, ch * 32, o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = o[e];
+                        }
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
                             if (ch * 32 + e < D)
                                 finish_row4_call<T>(j, cw.it, cw.p.kv_head, row_base + row, ch * 32 + e,
-                                                    make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]), m, l);
+                                                    make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]), ml.x, ml.y);
                     }
                 }
                 if (plain && real && whole && j.lse)

@@ -26,6 +26,16 @@ bool rows_ok(const lsmkv_rows_t *r)
            r->token_stride <= 0xFFFFFFFFull && r->head_stride <= 0xFFFFFFFFull;
 }
 
+// Whether the memory that two sets of rows span meets.
+bool rows_meet(const lsmkv_rows_t &a, const lsmkv_rows_t &b, uint64_t n_new, uint32_t heads, uint32_t head_dim)
+{
+    auto end = [&](const lsmkv_rows_t &r) {
+        return reinterpret_cast<uintptr_t>(r.data) +
+               2 * ((n_new - 1) * r.token_stride + (heads - 1ull) * r.head_stride + head_dim);
+    };
+    return reinterpret_cast<uintptr_t>(a.data) < end(b) && reinterpret_cast<uintptr_t>(b.data) < end(a);
+}
+
 SeqArgs seq_args(const lsmkv_seqs_t *s)
 {
     SeqArgs a;
@@ -299,6 +309,23 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
         job.shared_pages = groups->shared_pages;
     }
     LaunchTimer timer(ctx, s, LSMKV_K_ATTEND);
+    // A row that comes out undefined beside later tokens is computed once more from its query, which
+    // must not have become output by then. One token a sequence has no later tokens.
+    if (seqs->max_new > 1 && rows_meet(*q, *out, seqs->n_new, n_q_heads, ctx->geom.head_dim)) {
+        const uint64_t pieces = seqs->n_new * n_q_heads * (ctx->geom.head_dim / 8);
+        if (!ctx->d_queries || pieces * 16 > ctx->queries_cap) {
+            rc = grow_scratch(ctx, &ctx->d_queries, &ctx->queries_cap, pieces * 16, pieces * 16, __LINE__);
+            if (rc != LSMKV_OK) return rc;
+        }
+        k_gather_rows<<<merge_grid(ctx, pieces), 256, 0, s>>>(
+            static_cast<const uint4 *>(q->data), q->token_stride / 8, q->head_stride / 8, seqs->n_new, n_q_heads,
+            ctx->geom.head_dim / 8, static_cast<uint4 *>(ctx->d_queries));
+        ++ctx->launches;
+        CU(ctx, cudaGetLastError());
+        job.q = ctx->d_queries;
+        job.q_hs = ctx->geom.head_dim;
+        job.q_ts = (uint64_t)n_q_heads * ctx->geom.head_dim;
+    }
     const bool bf = dtype == LSMKV_BF16;
     if (shared) {
         rc = bf ? launch_prefix<__nv_bfloat16>(ctx, s, job) : launch_prefix<__half>(ctx, s, job);

@@ -468,3 +468,20 @@ def test_negative_and_zero_scale():
             ctx.attend_batch(0, seqs, q, out, lsmkv.pool_table(list(pool)), scale)
             assert ctx.last_status()["flags"] == 0
             check(out, None, reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, scale), torch.float16)
+
+
+@pytest.mark.parametrize("new,history,D", [(3, 50, 128), (70, 50, 128), (300, 4000, 64), (20, 9000, 128), (40, 30, 256)])
+def test_infinities_and_output_in_the_queries_own_rows(new, history, D):
+    """Undefined values in the last token, output written over the queries: the rows before it are
+    what they are without, whole tiles and cut ones."""
+    case = (torch.bfloat16, D, 16, 8, 2, [new, 2], [history, 30])
+    geom, pool, q, seqs, new_off, kv, page_off, table = setup(case, n_layers=1)
+    last = kv[0] - 1
+    pool[1, int(table[last // 16]), last % 16] = math.nan
+    ref = reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, 0.08)
+    with lsmkv.Context(geom, 0) as ctx:
+        ctx.attend_batch(0, seqs, q, q, lsmkv.pool_table(list(pool)), 0.08)
+        assert ctx.last_status()["flags"] == 0
+    keep = [r for r in range(new + 2) if r != new - 1]
+    assert torch.isfinite(q[keep]).all() and torch.isnan(q[new - 1]).all()
+    check(q[keep], None, (ref[0][keep], ref[1][keep], None, ref[3][keep]), torch.bfloat16)
