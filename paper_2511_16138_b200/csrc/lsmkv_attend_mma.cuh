@@ -13,12 +13,13 @@
 //                      registers, weights back to TMEM over the scores, where they are the
 //                      A operand of the value product. The sums in TMEM are rescaled only when the
 //                      maximum grew by more than 2^8 (weights stay below 2^8, sums in 32 bits).
-// Bound by the tensor cores and the softmax warps' instructions together: a tile of 256 x 128 takes
-// 2048 cycles of products at head_dim 128 (8192 operations a cycle and SM) and as many of
-// exponentials (16 a cycle and SM), and in steady state 2.5k to 3k in all. Measured: two requests of
-// 32768 tokens, the last 1024 new, 64/8 heads of 128, 2.16 TFLOP: 1.94 ms, 1.11 PFLOP/s, of which a
-// library product reaches 1.63 in a burst and 1.40 sustained. Taking some exponentials by a polynomial
-// on the multiply-add units only added instructions (1.83 -> 1.84 to 1.98 ms).
+// Bound by the chain of a half -- scores, softmax (1.9k cycles for 128 x 128 alone), value product,
+// next scores -- that alternates with the other's: 2.5k to 3k cycles for a tile of 256 x 128, whose
+// products take 2048 at head_dim 128 (8192 operations a cycle and SM) and whose exponentials as many (16
+// a cycle and SM). Measured: two requests of 32768 tokens, the last 1024 new, 64/8 heads of 128, 2.16
+// TFLOP: 1.94 ms, 1.11 PFLOP/s, of which a library product reaches 1.63 in a burst and 1.40 sustained.
+// Taking some exponentials by a polynomial on the multiply-add units lengthened the chain (1.83 -> 1.84
+// to 1.98 ms).
 // Every wait is bounded; one that runs out ends all roles and is reported.
 #pragma once
 #include <cuda.h>
