@@ -489,7 +489,10 @@ __device__ __forceinline__ float *part_slot(const AttendJob &j, uint64_t slot, u
     return j.parts + slot * ((uint64_t)M * (DP + 2));
 }
 
-// 2^(x) with 2^(-inf) = 0; statistics of an empty part are m = -inf, l = 0.
+// A part is empty when its sum of weights is zero (m is -inf then, the sums are not looked at). An undefined
+// score never becomes the maximum, so a part of undefined scores alone has m = -inf too, but l and the
+// sums are NaN: it counts, and NaN times a weight of zero keeps the row undefined.
+// 2^(m - top), 0 for m = -inf
 __device__ __forceinline__ float part_weight(float m, float top)
 {
     return m == -INFINITY ? 0.f : exp2f(m - top);
@@ -527,7 +530,7 @@ __device__ __noinline__ Quad sum_parts(const float *parts, uint32_t c0, uint32_t
         float4 o[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            pm[u] = -INFINITY;
+            pl[u] = 0.f;
             if (c + u > c1) continue;
             const float *s = parts + (2ull * (c + u) + (c + u == c0 ? 1 : 0)) * ((uint64_t)M * (DP + 2));
             pm[u] = __ldcg(s + (uint64_t)M * DP + r);
@@ -536,7 +539,7 @@ __device__ __noinline__ Quad sum_parts(const float *parts, uint32_t c0, uint32_t
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (pm[u] != -INFINITY) add_quad(sum, o[u], pm[u], pl[u]);   // else no key of it was the row's
+            if (pl[u] != 0.f) add_quad(sum, o[u], pm[u], pl[u]);   // else no key of it was the row's
     }
     return sum;
 }

@@ -275,7 +275,7 @@ __global__ __launch_bounds__(256) void k_attend_merge(const __grid_constant__ At
             }
 #pragma unroll
             for (int k = 0; k < R; ++k)
-                if (pm[k] != -INFINITY) add_quad(sum[k], o[k], pm[k], pl[k]);   // else no key of it was the row's
+                if (pl[k] != 0.f) add_quad(sum[k], o[k], pm[k], pl[k]);   // else no key of it was the row's
         }
 #pragma unroll 1
         for (int k = 0; k < R; ++k) {
