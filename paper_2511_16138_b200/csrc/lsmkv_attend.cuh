@@ -75,9 +75,9 @@ __device__ __forceinline__ uint32_t shared_tokens(const AttendJob &j, uint32_t g
 {
     const uint32_t a = j.group_off[g], b = j.group_off[g + 1];
     if (a >= b || b > j.seqs.n_seq || b - a < 2) return 0;
-    const uint64_t have = j.seqs.page_off[a + 1] - j.seqs.page_off[a];
+    const uint64_t p0 = j.seqs.page_off[a], p1 = j.seqs.page_off[a + 1];
     const uint64_t want = j.shared_pages[g];
-    if (want > have || want * j.page_tokens >= 0x80000000ull) return 0;
+    if (p1 < p0 || want > p1 - p0 || want * j.page_tokens >= 0x80000000ull) return 0;
     return (uint32_t)(want * j.page_tokens);
 }
 

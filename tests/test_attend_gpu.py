@@ -485,3 +485,25 @@ def test_infinities_and_output_in_the_queries_own_rows(new, history, D):
     keep = [r for r in range(new + 2) if r != new - 1]
     assert torch.isfinite(q[keep]).all() and torch.isnan(q[new - 1]).all()
     check(q[keep], None, (ref[0][keep], ref[1][keep], None, ref[3][keep]), torch.bfloat16)
+
+
+def test_shared_attend_leaves_out_a_first_member_with_descending_page_offsets():
+    """The group shares nothing then and its other members go by themselves. (The table goes on far
+    behind the entries that the first member would claim, so that no reading of it leaves it.)"""
+    case = (torch.bfloat16, 128, 16, 8, 2, [4, 3], [2, 5], 1, (0, 30))
+    geom, pool, q, seqs, groups, new_off, kv, page_off, table = shared_batch(case)
+    # sequence 0 now begins behind everything and ends where it did; its claimed pages are no pages
+    end = len(table)
+    wide = torch.full((end + 64,), 2 ** 31 - 1, dtype=torch.int32, device=DEV)
+    wide[:end] = seqs.keep[3]
+    off = seqs.keep[2].clone()
+    off[0] = end
+    bad = lsmkv.Seqs(seqs.keep[0], seqs.keep[1], off, wide, seqs.n_new, seqs.max_new)
+    out = torch.full_like(q, 5.0)
+    ref = reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, 0.08)
+    with lsmkv.Context(geom, 0) as ctx:
+        ctx.attend_shared_batch(0, bad, groups, q, out, lsmkv.pool_table(list(pool)), 0.08)
+        st = ctx.last_status()
+    assert st["flags"] == lsmkv.ST_BAD_COUNT and st["first_bad"] == 0
+    assert (out[0] == 5.0).all()
+    check(out[1:], None, tuple(x[1:] for x in ref), torch.bfloat16)
