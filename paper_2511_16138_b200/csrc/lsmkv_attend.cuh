@@ -237,7 +237,8 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
     for (uint32_t i = i0; i < i1; ++i) {
         const Item it = load_item(j, i);
         const uint64_t u = item_units(j, it, M, tile) * j.n_kv_heads;
-        if (!it.ok && blockIdx.x == 0) st_flag(j.st, LSMKV_ST_BAD_COUNT, i);
+        // (a group left out for its offsets holds a sequence that the own pass reports)
+        if (!it.ok && !j.prefix_pass && blockIdx.x == 0) st_flag(j.st, LSMKV_ST_BAD_COUNT, i);
         if (i == i0) first = u;
         mine += u;
         if (kWaves && item_tiles(j, it, M)) {

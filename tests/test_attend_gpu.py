@@ -507,3 +507,19 @@ def test_shared_attend_leaves_out_a_first_member_with_descending_page_offsets():
     assert st["flags"] == lsmkv.ST_BAD_COUNT and st["first_bad"] == 0
     assert (out[0] == 5.0).all()
     check(out[1:], None, tuple(x[1:] for x in ref), torch.bfloat16)
+
+
+def test_shared_attend_names_the_sequence_that_breaks_the_rules():
+    """A bad offset between two groups: the item is the first of the two sequences, not a group."""
+    case = (torch.bfloat16, 128, 16, 8, 2, [4, 3], [2, 2], 1, (0, 30))
+    geom, pool, q, seqs, groups, new_off, kv, page_off, table = shared_batch(case)
+    seqs.keep[0][4] = 9999
+    out = torch.full_like(q, 5.0)
+    with lsmkv.Context(geom, 0) as ctx:
+        ctx.attend_shared_batch(0, seqs, groups, q, out, lsmkv.pool_table(list(pool)), 0.08)
+        st = ctx.last_status()
+    assert st["flags"] == lsmkv.ST_BAD_COUNT and st["first_bad"] == 3
+    ref = reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, 0.08)
+    ok = torch.tensor([0, 1, 2, 5, 6], device=DEV)
+    check(out[ok], None, tuple(x[ok] for x in ref), torch.bfloat16)
+    assert (out[3:5] == 5.0).all()
