@@ -440,7 +440,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 if (__any_sync(~0u, fix != 1.f)) {
                     // the value product of the tile before is done: its scores came after it
 #pragma unroll 1
-                    for (int ch = 0; ch < DP / 32; ++ch) {
+                    for (int ch = 0; ch * 32 < (int)D; ++ch) {
                         float o[32];
                         tmem_ld32(o_t + ch * 32, o);
                         tmem_wait_ld();
@@ -523,8 +523,9 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 const uint32_t R = row_base + (real ? row : 0);
                 const uint64_t out_row = cw.it.row0 + R / G;
                 const uint32_t out_head = cw.p.kv_head * G + R % G;
+                // (columns behind the head's elements hold what an earlier kernel left)
 #pragma unroll 1
-                for (int ch = 0; ch < DP / 32; ++ch) {
+                for (int ch = 0; ch * 32 < (int)D; ++ch) {
                     float v[32];
                     __syncwarp();
                     if (n) {
@@ -546,12 +547,14 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     if (!real) continue;
                     float all = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) all += v[e];
+                    for (int e = 0; e < 32; ++e)
+                        if (ch * 32 + (e & ~7) < (int)D) all += v[e];
                     if (!whole) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
-                            __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)(first + row) * DP + ch * 32 + e),
-                                   make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]));
+                            if (ch * 32 + e < (int)D)
+                                __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)(first + row) * DP + ch * 32 + e),
+                                       make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]));
                     } else if (plain && !isnan(all)) {
                         T *const dst = static_cast<T *>(j.out) + out_row * j.o_ts + out_head * j.o_hs + ch * 32;
 #pragma unroll

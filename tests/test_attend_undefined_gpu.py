@@ -107,3 +107,25 @@ def test_undefined_rows_over_shared_prefixes(case, what):
         ctx.attend_shared_batch(0, seqs, groups, q, out, lsmkv.pool_table(list(pool)), 0.08, lse)
         assert ctx.last_status()["flags"] == 0
     undefined_exactly(out, lse, ref, lost, dt)
+
+
+@pytest.mark.parametrize("D", [80, 96])
+def test_what_an_earlier_kernel_left_on_chip_does_not_matter(D):
+    """A call whose sums are all NaN, then one with narrower heads over long histories, every wait
+    limited to about a millisecond: nothing of the first shows in the second, in time either."""
+    case = (torch.bfloat16, 128, 16, 32, 8, [2048], [0])
+    geom, pool, q, seqs, *_ = setup(case, n_layers=1)
+    pool[1] = math.nan
+    with lsmkv.Context(geom, 0) as ctx:
+        out = torch.zeros_like(q)
+        ctx.attend_batch(0, seqs, q, out, lsmkv.pool_table(list(pool)), 0.08)
+        assert ctx.last_status()["flags"] == 0 and torch.isnan(out).all()
+    case = (torch.bfloat16, D, 16, 8, 2, [100] * 100, [20000] + [900] * 99)
+    geom, pool, q, seqs, new_off, kv, page_off, table = setup(case, n_layers=1)
+    ref = reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, 0.1)
+    with lsmkv.Context(geom, 0) as ctx:
+        ctx.set_tuning("wait_cycles", 2_000_000)
+        out, lse = torch.full_like(q, 5.0), torch.zeros(q.shape[:2], device=DEV)
+        ctx.attend_batch(0, seqs, q, out, lsmkv.pool_table(list(pool)), 0.1, lse)
+        assert ctx.last_status()["flags"] == 0
+    check(out, lse, ref, torch.bfloat16)
