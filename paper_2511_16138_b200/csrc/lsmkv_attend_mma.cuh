@@ -312,6 +312,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
     const Span span = find_span<Sh::kThreads, true>(j, j.prefix_pass ? j.n_group : j.seqs.n_seq, Sh::kM, Sh::kKeys,
                                                     reinterpret_cast<uint32_t *>(smem_raw));
+    // the loads of the waves lay where the copy engine writes queries later; ordered by the barrier below
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     if ((reinterpret_cast<uintptr_t>(kbuf) | reinterpret_cast<uintptr_t>(vbuf)) & 15u) {
         if (blockIdx.x == 0 && tid == 0) st_flag(j.st, LSMKV_ST_MISALIGNED, 0);
         wait_launch();
