@@ -805,6 +805,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 if (lap) (void)mbar_wait_bounded(full(s), (lap - 1) & 1, j.wait_cycles);
             }
         }
+        if (kBoxes && w == 9 && j.q_boxes && q_cnt)
+            (void)mbar_wait_bounded(q_full, (q_cnt - 1) & 1, j.wait_cycles);      // boxes of queries likewise
     } else if (w == kIssuer) {
         // ---- issuer: the warp walks together, one lane waits and issues
         const uint32_t type = std::is_same<T, __half>::value ? 0u : 1u;
