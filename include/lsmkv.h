@@ -560,14 +560,17 @@ int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dt
  * values of positions 0..p of its sequence under KV head h / (n_q_heads / n_kv_heads), weights
  * softmax(scale * q . k). n_q_heads must be a multiple of n_kv_heads.
  *   q, out   [host] descriptors of n_new x n_q_heads rows of `dtype`; out may be q's rows (where
- *            their memory meets and max_new > 1 the queries are copied first)
+ *            their memory meets and a sequence may have several new tokens and more than 16 rows
+ *            under a KV head, the queries are copied first)
  *   lse_out  [dev] f32[n_new][n_q_heads] or NULL: log(sum exp(scale * q . k)) of every row
  * A row without any key (padding) is zero, its lse -inf. Scores, statistics and sums are held
  * in 32 bits; weights are rounded to `dtype` before they meet the values.
  * Uses (and may grow) scratch of the context: two attends must be ordered by the caller, and the
  * first of a size comes before any stream capture. A wait that runs out sets
  * LSMKV_ST_WAIT_EXPIRED; results are then unspecified until lsmkv_last_status() has been called.
- * Infinities and NaN among the keys and values reach the rows that see them, and no others.
+ * Infinities and NaN among the keys and values reach the rows that see them, and no others. (Where
+ * a value is undefined that some rows of a tile of 256 see and others do not, those others are
+ * computed twice.)
  */
 int lsmkv_attend_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype,
                        const lsmkv_seqs_t *seqs, uint32_t n_q_heads, const lsmkv_rows_t *q,

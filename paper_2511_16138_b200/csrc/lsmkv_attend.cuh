@@ -17,6 +17,8 @@
 // in the few-row kernel, a launch of its own behind the many-row kernel), so that results do not depend on timing. Every CTA finds its span by itself, from the lengths: no launch
 // before, and nothing for the host to know.
 #pragma once
+#include <type_traits>
+
 #include "lsmkv_append.cuh"
 #include "lsmkv_copy.cuh"
 
@@ -545,65 +547,31 @@ __device__ __noinline__ Quad sum_parts(const float *parts, uint32_t c0, uint32_t
     return sum;
 }
 
-// A row tile's products also run over keys that only later rows of it see, with weight zero:
-// an infinite or undefined value there makes the sum undefined although the row must not see
-// it. A row that comes out undefined and has such keys beside it is taken again here, key by key
-// over its own keys alone; finite inputs never come here.
-// W elements from d on, into out; returns the maximum and the sum of weights.
-template <typename T, int W>
-__device__ __noinline__ float2 redo_row(const AttendJob &j, uint64_t page0, uint64_t row, uint32_t head,
-                                        uint32_t first, uint32_t limit, uint32_t d, float *out)
+// A row tile's products also run over keys that only later rows of it see, with weight zero: an
+// infinite or undefined value there would make the sum undefined although the row must not see it.
+// Whether any of eight elements is one.
+template <typename T>
+__device__ __forceinline__ bool any_undefined(const uint4 &v)
 {
-    const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
-    const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
-    const uint4 *const q = reinterpret_cast<const uint4 *>(static_cast<const T *>(j.q) + row * j.q_ts +
-                                                           (uint64_t)head * j.q_hs);
-    float m = -INFINITY, l = 0.f, o[W];
+    constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
+    bool any = false;
 #pragma unroll
-    for (int e = 0; e < W; ++e) o[e] = 0.f;
-    for (uint32_t k = first; k < limit; ++k) {
-        const uint32_t page = j.seqs.page_table[page0 + k / j.page_tokens];
-        const bool real = page < j.num_pages;
-        const uint64_t at = (((uint64_t)(real ? page : 0) * j.page_tokens + k % j.page_tokens) *
-                                 j.n_kv_heads + head / j.group) * j.head_dim;
-        const uint4 *const key = reinterpret_cast<const uint4 *>(kbuf + at);
-        float2 dot = make_float2(0.f, 0.f);
-        for (uint32_t e = 0; real && e < j.head_dim / 8; ++e) {
-            const uint4 a = q[e], b = key[e];
-            const uint32_t *x = &a.x, *y = &b.x;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) dot = fma2(Half2<T>::up(x[i]), Half2<T>::up(y[i]), dot);
-        }
-        const float s = (dot.x + dot.y) * j.scale_log2;
-        const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
-        const float c = exp2f(m - base), w = exp2f(s - base);
-        l = l * c + w;
-#pragma unroll
-        for (int e = 0; e < W; ++e)
-            o[e] = o[e] * c + (real && d + e < j.head_dim ? w * Half2<T>::up1(vbuf[at + d + e]) : 0.f);
-        m = top;
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = (&v.x)[i];
+        any |= (x & kExp) == kExp || (x >> 16 & kExp) == kExp;
     }
-#pragma unroll
-    for (int e = 0; e < W; ++e) out[e] = o[e];
-    return make_float2(m, l);
+    return any;
 }
 
 // Write four elements of finished row R of the item: acc = sum of weighted values relative to
 // 2^m, l the sum of weights. Merges the prefix pass's result first when there is one.
 template <typename T>
 __device__ __forceinline__ void finish_row4(const AttendJob &j, const Item &it, uint32_t kv_head, uint32_t R,
-                                            uint32_t d, float4 acc, float m, float l, bool may_redo = true)
+                                            uint32_t d, float4 acc, float m, float l)
 {
     const uint64_t row = it.row0 + R / j.group;
     const uint32_t sub = R % j.group, head = kv_head * j.group + sub;
     const uint64_t flat = row * j.n_q_heads + head;
-    if (may_redo && it.causal && it.tokens > 1 && isnan(acc.x + acc.y + acc.z + acc.w)) {
-        float o[4];
-        const float2 ml = redo_row<T, 4>(j, it.page0, row, head, it.kv0, token_limit(it, R / j.group), d, o);
-        acc = make_float4(o[0], o[1], o[2], o[3]);
-        m = ml.x;
-        l = ml.y;
-    }
     if (it.skip) {
         Quad sum;
         sum.acc = acc;
@@ -632,12 +600,12 @@ __device__ __forceinline__ void finish_row4(const AttendJob &j, const Item &it, 
     if (d == 0 && j.lse) j.lse[flat] = lse2 * kLn2;
 }
 
-// The same out of line, where the call site is unrolled (and has taken undefined rows again itself).
+// The same out of line, where the call site is unrolled.
 template <typename T>
 __device__ __noinline__ void finish_row4_call(const AttendJob &j, const Item &it, uint32_t kv_head, uint32_t R,
                                               uint32_t d, float4 acc, float m, float l)
 {
-    finish_row4<T>(j, it, kv_head, R, d, acc, m, l, false);
+    finish_row4<T>(j, it, kv_head, R, d, acc, m, l);
 }
 
 // Merge rows [r0, r1) of a cut tile with parts c0..c1, by NT threads.
@@ -901,7 +869,8 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
             lim[x >> 1][x & 1] = r < cut.rows ? token_limit(it, (row_base + r) / G) : it.kv0;
         }
         const uint32_t lim_first = token_limit(it, row_base / G);              // least of the tile
-        const uint32_t key_end = min(token_limit(it, (row_base + cut.rows - 1) / G), it.kv0 + cut.k1 * kTile);
+        const uint32_t lim_last = token_limit(it, (row_base + cut.rows - 1) / G);
+        const uint32_t key_end = min(lim_last, it.kv0 + cut.k1 * kTile);
         const uint32_t key0 = it.kv0 + cut.k0 * kTile + w * Sh::kKeys;
 
         // queries as the right operand: 16 elements x 8 rows a fragment, two fragments a load
@@ -1018,14 +987,52 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
                 pf[nb][0] = transpose8x8(Half2<T>::down(s[nb][0], s[nb][1]));
                 pf[nb][1] = transpose8x8(Half2<T>::down(s[nb][2], s[nb][3]));
             }
-            {
-                const uint32_t vr = (lane & 7) + ((lane >> 4) << 3);
+            const uint32_t vr = (lane & 7) + ((lane >> 4) << 3);
+            auto value_fragment = [&](int x, uint32_t (&a)[4]) {
+                ldmatrix4t(vs + (vr * kChunks + ((2 * x + ((lane >> 3) & 1)) ^ (vr & 7))) * 16, a);
+            };
+            // A tile with keys that some rows see and others do not, and an undefined value among them
+            // (16 keys at the end of a sequence with several new tokens, at most two warps' tiles)
+            bool apart = false;
+            if (lim_first < lim_last && key + Sh::kKeys > lim_first) {
+                for (uint32_t x = lane; x < Sh::kKeys * kChunks; x += 32)
+                    apart |= any_undefined<T>(*reinterpret_cast<const uint4 *>(smem + (vs - q_s) + x * 16));
+                apart = __any_sync(~0u, apart);
+            }
+            if (!apart) {
 #pragma unroll
                 for (int x = 0; x < DP / 16; ++x) {
                     uint32_t a[4];
-                    ldmatrix4t(vs + (vr * kChunks + ((2 * x + ((lane >> 3) & 1)) ^ (vr & 7))) * 16, a);
+                    value_fragment(x, a);
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) mma16816<T>(o[x][nb], a, pf[nb][0], pf[nb][1]);
+                }
+            } else {
+                // token by token, over the keys that it sees
+                const uint32_t t1 = (row_base + cut.rows - 1) / G;
+                for (uint32_t t = row_base / G; t <= t1; ++t) {
+                    const uint32_t lim_t = token_limit(it, t), see = lim_t > key ? lim_t - key : 0;
+                    uint32_t mask[2];                // of this lane's keys 2 (lane % 4), + 1, + 8, + 9
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t k = 8 * h + 2 * (lane & 3);
+                        mask[h] = (k < see ? 0xFFFFu : 0u) | (k + 1 < see ? 0xFFFF0000u : 0u);
+                    }
+#pragma unroll
+                    for (int x = 0; x < DP / 16; ++x) {
+                        uint32_t a[4];
+                        value_fragment(x, a);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) a[e] &= mask[e >> 1];
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) {
+                            float part[4] = {0.f, 0.f, 0.f, 0.f};
+                            mma16816<T>(part, a, pf[nb][0], pf[nb][1]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (lim[nb][e & 1] == lim_t) o[x][nb][e] += part[e];
+                        }
+                    }
                 }
             }
             __syncwarp();     // the stage is read before it is filled again

@@ -286,6 +286,280 @@ __global__ __launch_bounds__(256) void k_attend_merge(const __grid_constant__ At
     }
 }
 
+// ---- rows that came out undefined ---------------------------------------------------------------
+//
+// A row may have come out undefined for a value that only later rows of its tile see (see any_undefined). When
+// a CTA is done and has met undefined rows, its softmax warps go through its cuts once more: a scan of
+// the values that some rows of the cut see and others do not (at most 256 keys) finds the last undefined
+// one, and only rows that end ahead of it are computed anew, over the cut's keys alone; all others are undefined by
+// themselves and stay. So an undefined value that its rows see costs the scan; one that rows beside them do
+// not see, their share of the CTA's work once more, at the rate of m16n8k16 products. Nobody waits for the
+// softmax warps by then, so no bounded wait depends on how long it takes, and the pipeline's shared
+// memory is theirs. Measured, 1024 new tokens behind 30000, 64/8 heads of 128, 0.81 ms: 0.80 with a NaN in the first
+// value, 3.6 with one in the last (248 rows of eight CTAs over all keys; 14 with the fragments straight from
+// memory). In the merge launch instead, its registers lengthened that launch by 3.6 us in every call.
+
+// Barriers of the 256 threads of the softmax warps; the second tells whether a condition holds for all of them.
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+__device__ __forceinline__ bool softmax_all(bool c)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)c) : "memory");
+    return r != 0;
+}
+
+template <int DP>
+struct RedoShape {
+    static constexpr uint32_t kKeys = 64;                    // keys of a stage
+    static constexpr uint32_t kRow = DP * 2 + 16;            // 16 bytes more: ldmatrix without conflicts
+    static constexpr uint32_t kHalf = kKeys * kRow;          // keys, then values
+    static constexpr uint32_t kOffsets = 4 * kHalf;          // behind two stages: places of two stages' keys
+    static constexpr uint32_t kBehind = kOffsets + 2 * kKeys * 8;
+};
+
+// 16 rows a warp from row r0 of the cut's tile on, 128 in all; smem: RedoShape's, free.
+template <typename T, int DP, int M, int TILE>
+__device__ __forceinline__ void redo_rows(const AttendJob &j, const Walk<M, TILE> &cw, float *slot, uint32_t r0,
+                                          unsigned char *smem, uint32_t behind)
+{
+    using Sh = RedoShape<DP>;
+    constexpr uint64_t kNone = ~0ull;
+    const Item &it = cw.it;
+    const uint32_t tid = threadIdx.x, lane = tid & 31, g = lane >> 2, c4 = lane & 3, D = j.head_dim, G = j.group;
+    const uint32_t kv_head = cw.p.kv_head, r1 = min(r0 + 128, cw.p.rows), row_base = cw.p.rt * M;
+    const uint32_t key0 = it.kv0 + cw.p.k0 * TILE;
+    const uint32_t key_end = min(token_limit(it, (row_base + r1 - 1) / G), it.kv0 + cw.p.k1 * TILE);
+    if (key_end <= key0) return;                 // (no row here has a key in the cut)
+    // a warp's rows; this lane's are g and g + 8
+    const uint32_t w0 = r0 + (tid >> 5) * 16, n_rows = w0 < r1 ? min(r1 - w0, 16u) : 0;
+    const uint32_t t0 = n_rows ? (row_base + w0) / G : 0, t1 = n_rows ? (row_base + w0 + n_rows - 1) / G : 0;
+    const uint32_t lim_first = token_limit(it, t0);
+    uint32_t lim[2], q[DP / 16][4];
+    bool anew[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const bool in = g + 8 * h < n_rows;
+        const uint32_t R = row_base + (in ? w0 + g + 8 * h : 0);
+        lim[h] = in ? token_limit(it, R / G) : it.kv0;
+        anew[h] = in && lim[h] < behind;
+        const T *row = static_cast<const T *>(j.q) + (it.row0 + R / G) * j.q_ts + (uint64_t)(kv_head * G + R % G) * j.q_hs;
+#pragma unroll
+        for (int x = 0; x < DP / 8; ++x)
+            q[x >> 1][h + 2 * (x & 1)] =
+                in && x * 8u < D ? *reinterpret_cast<const uint32_t *>(row + x * 8 + c4 * 2) : 0u;
+    }
+    uint64_t *const offsets = reinterpret_cast<uint64_t *>(smem + Sh::kOffsets);
+    const uint32_t n_stages = (key_end - key0 + Sh::kKeys - 1) / Sh::kKeys;
+    auto look_up = [&](uint32_t st) {            // places of stage st's keys
+        const uint32_t k = key0 + st * Sh::kKeys + tid;
+        if (tid >= Sh::kKeys) return;
+        uint64_t at = kNone;                     // zeros
+        if (k < key_end) {
+            const uint32_t page = j.seqs.page_table[it.page0 + k / j.page_tokens];
+            if (page < j.num_pages)
+                at = (((uint64_t)page * j.page_tokens + k % j.page_tokens) * j.n_kv_heads + kv_head) * D;
+        }
+        offsets[(st & 1) * Sh::kKeys + tid] = at;
+    };
+    const uint32_t base = smem_addr(smem);
+    auto load = [&](uint32_t st) {
+        const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
+        const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
+        const uint32_t dst = base + (st & 1) * 2 * Sh::kHalf;
+        for (uint32_t x = tid; x < Sh::kKeys * (DP / 8); x += 256) {
+            const uint32_t r = x / (DP / 8), c = x % (DP / 8);
+            const uint64_t at = offsets[(st & 1) * Sh::kKeys + r];
+            const bool in = at != kNone && c * 8 < D;
+            const uint64_t e = in ? at + c * 8 : 0;
+            cp_async16(dst + r * Sh::kRow + c * 16, kbuf + e, in);
+            cp_async16(dst + Sh::kHalf + r * Sh::kRow + c * 16, vbuf + e, in);
+        }
+    };
+    float o[DP / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < DP / 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
+    bool done = !__any_sync(~0u, anew[0] || anew[1]);
+    softmax_sync();                              // whatever lay here is read
+    look_up(0);
+    softmax_sync();
+    load(0);
+    look_up(1);
+    for (uint32_t st = 0; st < n_stages; ++st) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        if (softmax_all(done)) break;
+        if (st + 1 < n_stages) load(st + 1);
+        look_up(st + 2);
+        if (done) continue;
+        const uint32_t ks = base + (st & 1) * 2 * Sh::kHalf, vs = ks + Sh::kHalf;
+#pragma unroll 1
+        for (uint32_t sub = 0; sub < Sh::kKeys; sub += 32) {
+            const uint32_t key = key0 + st * Sh::kKeys + sub;
+            if (key >= key_end) break;
+            float s[4][4] = {};                  // keys 8 n ..
+#pragma unroll
+            for (int x = 0; x < DP / 16; ++x)    // elements 16 x ..
+#pragma unroll
+                for (int n = 0; n < 4; n += 2) {
+                    uint32_t f[4];
+                    ldmatrix4(ks + (sub + n * 8 + (lane & 7) + (lane >> 4) * 8) * Sh::kRow + (2 * x + (lane >> 3 & 1)) * 16, f);
+                    mma16816<T>(s[n], q[x], f[0], f[1]);
+                    mma16816<T>(s[n + 1], q[x], f[2], f[3]);
+                }
+            float top[2] = {m[0], m[1]};
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[n][e] = key + 8 * n + 2 * c4 + (e & 1) < min(lim[e >> 1], key_end) ? s[n][e] * j.scale_log2 : -INFINITY;
+                    top[e >> 1] = fmaxf(top[e >> 1], s[n][e]);
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                top[h] = fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 1));
+                top[h] = fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 2));
+                const float ref = top[h] == -INFINITY ? 0.f : top[h];
+                if (__any_sync(~0u, top[h] > m[h])) {
+                    const float f = exp2f(m[h] - ref);
+                    m[h] = top[h];
+                    l[h] *= f;
+#pragma unroll
+                    for (int x = 0; x < DP / 8; ++x) {
+                        o[x][2 * h] *= f;
+                        o[x][2 * h + 1] *= f;
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int e = 2 * h; e < 2 * h + 2; ++e) {
+                        s[n][e] = exp2f(s[n][e] - ref);
+                        l[h] += s[n][e];
+                    }
+            }
+            uint32_t p[2][4];                    // (rounded to the values' type, as everywhere)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                p[n >> 1][2 * (n & 1)] = Half2<T>::down(s[n][0], s[n][1]);
+                p[n >> 1][2 * (n & 1) + 1] = Half2<T>::down(s[n][2], s[n][3]);
+            }
+            auto value_fragment = [&](int x, int k, uint32_t (&f)[4]) {      // elements 16 x .., keys 16 k ..
+                ldmatrix4t(vs + (sub + k * 16 + (lane & 15)) * Sh::kRow + (2 * x + (lane >> 4)) * 16, f);
+            };
+            if (key + 32 <= lim_first) {
+#pragma unroll
+                for (int x = 0; x < DP / 16; ++x)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        uint32_t f[4];
+                        value_fragment(x, k, f);
+                        mma16816<T>(o[2 * x], p[k], f[0], f[1]);
+                        mma16816<T>(o[2 * x + 1], p[k], f[2], f[3]);
+                    }
+            } else {
+                // keys that some of these rows do not see: token by token
+                for (uint32_t t = t0; t <= t1; ++t) {
+                    const uint32_t lim_t = token_limit(it, t);
+#pragma unroll
+                    for (int x = 0; x < DP / 16; ++x) {
+                        float part[2][4] = {};
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            uint32_t f[4];
+                            value_fragment(x, k, f);
+                            const uint32_t k0 = key + k * 16 + 2 * c4;
+                            const uint32_t m0 = (k0 < lim_t ? 0xFFFFu : 0u) | (k0 + 1 < lim_t ? 0xFFFF0000u : 0u);
+                            const uint32_t m1 = (k0 + 8 < lim_t ? 0xFFFFu : 0u) | (k0 + 9 < lim_t ? 0xFFFF0000u : 0u);
+                            mma16816<T>(part[0], p[k], f[0] & m0, f[1] & m1);
+                            mma16816<T>(part[1], p[k], f[2] & m0, f[3] & m1);
+                        }
+#pragma unroll
+                        for (int n = 0; n < 2; ++n)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (lim[e >> 1] == lim_t) o[2 * x + n][e] += part[n][e];
+                    }
+                }
+            }
+        }
+        if (st % 4 != 3 && st + 1 != n_stages) continue;
+        // rows undefined in all their elements are right as they are
+        bool lost[2] = {true, true};
+#pragma unroll
+        for (int x = 0; x < DP / 8; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) lost[e >> 1] = lost[e >> 1] && (x * 8u >= D || isnan(o[x][e]));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const unsigned votes = __ballot_sync(~0u, lost[h]);
+            if ((votes >> (lane & 28) & 15) == 15) anew[h] = false;
+        }
+        done = !__any_sync(~0u, anew[0] || anew[1]);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        l[h] += __shfl_xor_sync(~0u, l[h], 1);
+        l[h] += __shfl_xor_sync(~0u, l[h], 2);
+        const uint32_t r = w0 + g + 8 * h;
+        // elements 8 x + 2 c4, + 1 of two x: a lane and its neighbour turn them into four of one
+#pragma unroll
+        for (int x = 0; x < DP / 8; x += 2) {
+            const bool odd = c4 & 1;
+            float give[2] = {odd ? o[x][2 * h] : o[x + 1][2 * h], odd ? o[x][2 * h + 1] : o[x + 1][2 * h + 1]};
+            float keep[2] = {odd ? o[x + 1][2 * h] : o[x][2 * h], odd ? o[x + 1][2 * h + 1] : o[x][2 * h + 1]};
+            give[0] = __shfl_xor_sync(~0u, give[0], 1);
+            give[1] = __shfl_xor_sync(~0u, give[1], 1);
+            const float4 acc = odd ? make_float4(give[0], give[1], keep[0], keep[1])
+                                   : make_float4(keep[0], keep[1], give[0], give[1]);
+            const uint32_t d = (x + odd) * 8 + (c4 >> 1) * 4;
+            if (!anew[h] || d >= D) continue;
+            if (slot)
+                __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)r * DP + d), acc);
+            else
+                finish_row4_call<T>(j, it, kv_head, row_base + r, d, acc, m[h], l[h]);
+        }
+        if (slot && anew[h] && c4 == 0) {
+            __stcg(slot + (uint64_t)M * DP + r, m[h]);
+            __stcg(slot + (uint64_t)M * (DP + 1) + r, l[h]);
+        }
+    }
+}
+
+// The cuts of a CTA once more, by its softmax warps.
+template <typename T, int DP, int M, int TILE>
+__device__ __noinline__ void redo_cuts(const AttendJob &j, const Span span, unsigned char *smem)
+{
+    uint32_t *const behind = reinterpret_cast<uint32_t *>(smem + RedoShape<DP>::kBehind);
+    const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
+    const uint32_t tid = threadIdx.x, pieces = j.head_dim / 8;
+    Walk<M, TILE> cw;
+    cw.start(j, span);
+    while (cw.next(j, span)) {
+        const Item &it = cw.it;
+        if (!it.causal || it.tokens < 2) continue;
+        const uint32_t row_base = cw.p.rt * M;
+        const uint32_t from = max(token_limit(it, row_base / j.group), it.kv0 + cw.p.k0 * TILE);
+        const uint32_t end = min(token_limit(it, (row_base + cw.p.rows - 1) / j.group), it.kv0 + cw.p.k1 * TILE);
+        if (end <= from) continue;
+        softmax_sync();
+        if (tid == 0) *behind = 0;
+        softmax_sync();
+        for (uint32_t x = tid; x < (end - from) * pieces; x += 256) {
+            const uint32_t k = from + x / pieces, page = j.seqs.page_table[it.page0 + k / j.page_tokens];
+            if (page >= j.num_pages) continue;
+            const uint64_t at = (((uint64_t)page * j.page_tokens + k % j.page_tokens) * j.n_kv_heads + cw.p.kv_head) * j.head_dim;
+            if (any_undefined<T>(*reinterpret_cast<const uint4 *>(vbuf + at + x % pieces * 8))) atomicMax(behind, k + 1);
+        }
+        softmax_sync();
+        const uint32_t last = *behind;
+        const bool whole = cw.p.k0 == 0 && cw.p.k1 == cw.p.units;
+        float *slot = whole ? nullptr : part_slot(j, 2ull * span.rank + (cw.p.k0 == 0 ? 1 : 0), M, DP);
+        for (uint32_t r0 = 0; r0 < cw.p.rows && token_limit(it, (row_base + r0) / j.group) < last; r0 += 128)
+            redo_rows<T, DP>(j, cw, slot, r0, smem, last);
+    }
+}
+
 template <typename T, int DP, bool kBoxes>
 __global__ __launch_bounds__(ManyShape<DP>::kThreads, 1)
 void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ CUtensorMap map,
@@ -299,7 +573,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     __shared__ __align__(8) uint64_t bars[3 * Sh::kStages + 14];
     __shared__ uint32_t tmem_slot;
     __shared__ __align__(128) unsigned char map_work[128];
-    __shared__ volatile uint32_t stop;
+    __shared__ volatile uint32_t stop, undefined[8];   // (a softmax warp's rows have come out undefined)
     __shared__ float half_m[128], half_l[128];   // the second half's statistics, when the halves share rows
     const uint32_t tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const uint32_t G = j.group, D = j.head_dim;
@@ -356,6 +630,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
             mbar_init(o_full(x), 1);
         }
         stop = 0;
+        for (int x = 0; x < 8; ++x) undefined[x] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (w == Sh::kThreads / 32 - 1) {
@@ -390,6 +665,12 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         const uint32_t lane_base = (w & 3) << 21;            // lanes 32 (w % 4) ..
         const uint32_t s_t = tmem + lane_base + x * 128, o_t = tmem + lane_base + 256 + x * 128;
         const float c = fmaxf(fabsf(j.scale_log2), 1e-37f);  // a negative scale negates the products
+        if ((D + 15) / 16 * 16 < DP) {
+            // columns of the sums that no product writes: they are read with the others, and an earlier kernel
+            // may have left anything there
+            float zero[32] = {};
+            for (int ch = 0; ch < DP / 32; ++ch) tmem_st32(o_t + ch * 32, zero);
+        }
         uint32_t s_cnt = 0, o_cnt = 0, half_cnt = 0;
         bool half_due = false;       // second half: its sums of the cut before are still to be read
         CutWalk cw;
@@ -442,7 +723,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 if (__any_sync(~0u, fix != 1.f)) {
                     // the value product of the tile before is done: its scores came after it
 #pragma unroll 1
-                    for (int ch = 0; ch * 32 < (int)D; ++ch) {
+                    for (int ch = 0; ch < DP / 32; ++ch) {
                         float o[32];
                         tmem_ld32(o_t + ch * 32, o);
                         tmem_wait_ld();
@@ -519,15 +800,15 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 m = top;
             }
             if (first < cw.p.rows && (n || whole) && !(both && x)) {
-                // most rows: nothing to merge, l > 0, finite
+                // most rows: nothing to merge, l > 0
                 const bool plain = !j.prefix_pass && !cw.it.skip && l != 0.f;
                 const float inv = 1.f / l;
                 const uint32_t R = row_base + (real ? row : 0);
                 const uint64_t out_row = cw.it.row0 + R / G;
                 const uint32_t out_head = cw.p.kv_head * G + R % G;
-                // (columns behind the head's elements hold what an earlier kernel left)
+                bool lost = false;
 #pragma unroll 1
-                for (int ch = 0; ch * 32 < (int)D; ++ch) {
+                for (int ch = 0; ch < DP / 32; ++ch) {
                     float v[32];
                     __syncwarp();
                     if (n) {
@@ -549,15 +830,14 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     if (!real) continue;
                     float all = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (ch * 32 + (e & ~7) < (int)D) all += v[e];
+                    for (int e = 0; e < 32; ++e) all += v[e];
+                    lost |= isnan(all);
                     if (!whole) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
-                            if (ch * 32 + e < (int)D)
-                                __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)(first + row) * DP + ch * 32 + e),
-                                       make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]));
-                    } else if (plain && !isnan(all)) {
+                            __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)(first + row) * DP + ch * 32 + e),
+                                   make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]));
+                    } else if (plain) {
                         T *const dst = static_cast<T *>(j.out) + out_row * j.o_ts + out_head * j.o_hs + ch * 32;
 #pragma unroll
                         for (int e = 0; e < 32; e += 8) {
@@ -570,23 +850,17 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                             *reinterpret_cast<uint4 *>(dst + e) = pk;
                         }
                     } else {
-                        float2 ml = make_float2(m, l);
-                        if (isnan(all) && cw.it.causal && cw.it.tokens > 1) {
-                            float o[32];
-                            ml = redo_row<T, 32>(j, cw.it.page0, out_row, out_head, cw.it.kv0, lim, ch * 32, o);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = o[e];
-                        }
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
                             if (ch * 32 + e < D)
                                 finish_row4_call<T>(j, cw.it, cw.p.kv_head, row_base + row, ch * 32 + e,
-                                                    make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]), ml.x, ml.y);
+                                                    make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]), m, l);
                     }
                 }
                 if (plain && real && whole && j.lse)
                     j.lse[out_row * j.n_q_heads + out_head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
                 __syncwarp();
+                if (lost) undefined[w] = 1;
                 tc_fence_before();
             }
             if (two && !x) mbar_arrive(half_read);
@@ -602,6 +876,12 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 while (j.span_begin[c.c1 + 1] < cw.p.tile0 + cw.p.units) ++c.c1;
             }
         }
+        // The softmax warps' part in the pipeline is done, and with it all products and all copies.
+        softmax_sync();
+        bool any = false;
+        for (int k = 0; k < 8; ++k) any |= undefined[k] != 0;
+        if (softmax_all(any && !stop))
+            redo_cuts<T, DP, Sh::kM, Sh::kKeys>(j, span, smem_raw + (base - smem_addr(smem_raw)));
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(Sh::kOtherRegs));
     }

@@ -162,6 +162,12 @@ int launch_many(lsmkv_ctx *ctx, cudaStream_t s, bool follows, AttendJob &job)
 // The tcgen05 kernel takes heads of up to 128 elements.
 bool many_takes(const lsmkv_ctx *ctx) { return ctx->geom.head_dim <= 128; }
 
+// Whether a sequence of max_new new tokens has more rows than one tile of the few-row kernel.
+bool many_rows(const lsmkv_ctx *ctx, uint32_t max_new, uint32_t group)
+{
+    return many_takes(ctx) && (uint64_t)max_new * group > 16;
+}
+
 uint32_t part_dp(const lsmkv_ctx *ctx)
 {
     return ctx->geom.head_dim <= 64 ? 64 : ctx->geom.head_dim <= 128 ? 128 : 256;
@@ -199,7 +205,7 @@ int launch_own(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
     job.parts = job.few_parts;
     const int rc = launch_few<T>(ctx, s, job.skip != nullptr, job, most <= 8);
     job.parts = many_parts;
-    if (rc != LSMKV_OK || !mma || most <= 16) return rc;
+    if (rc != LSMKV_OK || !many_rows(ctx, job.seqs.max_new, job.group)) return rc;
     // side by side, unless a prefix pass is still ahead of both
     job.beside = job.skip == nullptr;
     job.rows_lo = 16;
@@ -309,9 +315,11 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
         job.shared_pages = groups->shared_pages;
     }
     LaunchTimer timer(ctx, s, LSMKV_K_ATTEND);
-    // A row that comes out undefined beside later tokens is computed once more from its query, which
-    // must not have become output by then. One token a sequence has no later tokens.
-    if (seqs->max_new > 1 && rows_meet(*q, *out, seqs->n_new, n_q_heads, ctx->geom.head_dim)) {
+    // A row of a many-row tile that comes out undefined beside later tokens may be computed once more from
+    // its query, which must not have become output by then. One token a sequence has no later tokens, and the
+    // few-row kernel computes none twice.
+    if (many_rows(ctx, seqs->max_new, job.group) && seqs->max_new > 1 &&
+        rows_meet(*q, *out, seqs->n_new, n_q_heads, ctx->geom.head_dim)) {
         const uint64_t pieces = seqs->n_new * n_q_heads * (ctx->geom.head_dim / 8);
         if (!ctx->d_queries || pieces * 16 > ctx->queries_cap) {
             rc = grow_scratch(ctx, &ctx->d_queries, &ctx->queries_cap, pieces * 16, pieces * 16, __LINE__);
