@@ -566,7 +566,8 @@ int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dt
  * A row without any key (padding) is zero, its lse -inf. Scores, statistics and sums are held
  * in 32 bits; weights are rounded to `dtype` before they meet the values.
  * Uses (and may grow) scratch of the context: two attends must be ordered by the caller, and the
- * first of a size comes before any stream capture. A wait that runs out sets
+ * first of a size comes before any stream capture. Scratch that a larger call replaces is kept until
+ * lsmkv_destroy() (all of it no larger than the present one), so graphs captured before stay valid. A wait that runs out sets
  * LSMKV_ST_WAIT_EXPIRED; results are then unspecified until lsmkv_last_status() has been called.
  * Infinities and NaN among the keys and values reach the rows that see them, and no others. (Where
  * a value is undefined that some rows of a tile of 256 see and others do not, those others are

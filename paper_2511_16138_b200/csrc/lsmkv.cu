@@ -66,6 +66,7 @@ struct lsmkv_ctx {
     uint64_t prefix_cap;   // bytes
     void *d_queries;       // copy of queries that share memory with the output
     uint64_t queries_cap;  // bytes
+    struct Kept { void *p; Kept *next; } *kept;   // buffers of theirs that larger ones replaced
     // host-buffer calls: device staging and host scratch
     void *d_io[3];
     uint64_t io_cap[3];
@@ -298,6 +299,36 @@ int grow_scratch(lsmkv_ctx *ctx, T **slot, uint64_t *cap, size_t bytes, uint64_t
     if (rc != LSMKV_OK) { cudaFree(p); return rc; }
     *slot = static_cast<T *>(p);
     *cap = new_cap;
+    return LSMKV_OK;
+}
+
+// enlarge_scratch: as grow_scratch, in bytes, but the buffer that is replaced stays until
+// lsmkv_destroy: a captured graph of an earlier call may still use it. At least twice the size
+// each time, so that all kept buffers together are no larger than the present one.
+int enlarge_scratch(lsmkv_ctx *ctx, void **slot, uint64_t *cap, size_t bytes, int line)
+{
+    lsmkv_ctx::Kept *node = nullptr;
+    if (*slot && !(node = new (std::nothrow) lsmkv_ctx::Kept)) return LSMKV_ENOMEM;
+    size_t want = std::max<size_t>(bytes, 2 * *cap);
+    void *p = nullptr;
+    cudaError_t e = cudaMalloc(&p, want);
+    if (e != cudaSuccess && want > bytes) {
+        cudaGetLastError();
+        want = bytes;
+        e = cudaMalloc(&p, want);
+    }
+    if (e != cudaSuccess) {
+        delete node;
+        cuda_fail(ctx, e, line);
+        return LSMKV_ENOMEM;
+    }
+    if (node) {
+        node->p = *slot;
+        node->next = ctx->kept;
+        ctx->kept = node;
+    }
+    *slot = p;
+    *cap = want;
     return LSMKV_OK;
 }
 
@@ -637,6 +668,11 @@ int lsmkv_destroy(lsmkv_ctx *ctx)
     if (release_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     if (release_scratch(ctx, &ctx->d_prefix, &ctx->prefix_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     if (release_scratch(ctx, &ctx->d_queries, &ctx->queries_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
+    while (lsmkv_ctx::Kept *k = ctx->kept) {
+        ctx->kept = k->next;
+        note(cudaFree(k->p));
+        delete k;
+    }
     for (int k = 0; k < 3; ++k)
         if (release_scratch(ctx, &ctx->d_io[k], &ctx->io_cap[k], __LINE__) != LSMKV_OK)
             note((cudaError_t)ctx->last_cuda);
@@ -1208,9 +1244,6 @@ int lsmkv_last_status(lsmkv_ctx *ctx, void *stream, lsmkv_status_t *out)
     std::memset(&z, 0, sizeof(z));
     z.first_bad = ~0ull;
     CU(ctx, cudaMemcpyAsync(ctx->d_status, &z, sizeof(z), cudaMemcpyHostToDevice, s));
-    // an attend that gave up may have left its counters between two calls' values
-    if ((out->flags & LSMKV_ST_WAIT_EXPIRED) && ctx->d_attend)
-        CU(ctx, cudaMemsetAsync(ctx->d_attend, 0, attend_counter_bytes(ctx), s));
     CU(ctx, cudaStreamSynchronize(s));
     return LSMKV_OK;
 }

@@ -237,11 +237,10 @@ size_t place_attend(const lsmkv_ctx *ctx, void *at, uint32_t n_seq, AttendJob *j
 
 int ensure_attend(lsmkv_ctx *ctx, cudaStream_t s, uint32_t n_seq, AttendJob *job)
 {
-    // room for a few sequences more than asked for: a growing batch does not allocate every time
-    size_t bytes = place_attend(ctx, nullptr, n_seq, job);
+    const size_t bytes = place_attend(ctx, nullptr, n_seq, job);
     if (!ctx->d_attend || bytes > ctx->attend_cap) {
-        bytes += 16384;
-        const int rc = grow_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, bytes, bytes, __LINE__);
+        // room for a few sequences more than asked for: a growing batch does not allocate every time
+        const int rc = enlarge_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, bytes + 16384, __LINE__);
         if (rc != LSMKV_OK) return rc;
         const cudaError_t e = cudaMemsetAsync(ctx->d_attend, 0, attend_counter_bytes(ctx), s);
         if (e != cudaSuccess) {
@@ -306,7 +305,7 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
         };
         const size_t bytes = place(nullptr);
         if (!ctx->d_prefix || bytes > ctx->prefix_cap) {
-            rc = grow_scratch(ctx, &ctx->d_prefix, &ctx->prefix_cap, bytes, bytes, __LINE__);
+            rc = enlarge_scratch(ctx, &ctx->d_prefix, &ctx->prefix_cap, bytes, __LINE__);
             if (rc != LSMKV_OK) return rc;
         }
         place(ctx->d_prefix);
@@ -322,7 +321,7 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
         rows_meet(*q, *out, seqs->n_new, n_q_heads, ctx->geom.head_dim)) {
         const uint64_t pieces = seqs->n_new * n_q_heads * (ctx->geom.head_dim / 8);
         if (!ctx->d_queries || pieces * 16 > ctx->queries_cap) {
-            rc = grow_scratch(ctx, &ctx->d_queries, &ctx->queries_cap, pieces * 16, pieces * 16, __LINE__);
+            rc = enlarge_scratch(ctx, &ctx->d_queries, &ctx->queries_cap, pieces * 16, __LINE__);
             if (rc != LSMKV_OK) return rc;
         }
         k_gather_rows<<<merge_grid(ctx, pieces), 256, 0, s>>>(

@@ -523,3 +523,48 @@ def test_shared_attend_names_the_sequence_that_breaks_the_rules():
     ok = torch.tensor([0, 1, 2, 5, 6], device=DEV)
     check(out[ok], None, tuple(x[ok] for x in ref), torch.bfloat16)
     assert (out[3:5] == 5.0).all()
+
+
+def test_graphs_captured_before_a_larger_call_stay_valid():
+    """Small shared and plain steps (one with its output over the queries) are captured, then larger
+    batches run, twice as large each time, then the small graphs again over other inputs."""
+    small = (torch.bfloat16, 128, 16, 8, 2, [3, 5], [4, 9], 1, (0, 40))
+    geom, pool, q, seqs, groups, new_off, kv, page_off, table = shared_batch(small)
+    plain = (torch.bfloat16, 128, 16, 8, 2, [40, 1, 70], [100, 30, 0])
+    _, pool2, q2, seqs2, new_off2, kv2, page_off2, table2 = setup(plain, n_layers=1)
+    out, out2, over = torch.zeros_like(q), torch.zeros_like(q2), q2.clone()
+    with lsmkv.Context(geom, 0) as ctx:
+        pt, pt2 = lsmkv.pool_table(list(pool)), lsmkv.pool_table(list(pool2))
+
+        def steps():
+            ctx.attend_shared_batch(0, seqs, groups, q, out, pt, 0.08)
+            ctx.attend_batch(0, seqs2, q2, out2, pt2, 0.08)
+            ctx.attend_batch(0, seqs2, over, over, pt2, 0.08)
+
+        steps()                                            # scratch is there before the capture
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            steps()
+        for k in range(1, 6):
+            large = (torch.bfloat16, 128, 16, 8, 2, [2 ** k * 400, 30], [4, 9], 1, (0, 40))
+            _, lpool, lq, lseqs, lgroups, lnew, lkv, lpage, ltable = shared_batch(large, seed=k)
+            lout = torch.zeros_like(lq)
+            ctx.attend_shared_batch(0, lseqs, lgroups, lq, lout, lsmkv.pool_table(list(lpool)), 0.08)
+            wide = (torch.bfloat16, 128, 16, 8, 2, [2 ** k * 100] * 3, [0, 10, 200])
+            _, wpool, wq, wseqs, *_ = setup(wide, n_layers=1)
+            ctx.attend_batch(0, wseqs, wq, wq, lsmkv.pool_table(list(wpool)), 0.08)
+            assert ctx.last_status()["flags"] == 0
+        check(lout, None, reference(lq, lpool, 0, 1, lnew, lkv, lpage, ltable, 16, 0.08), torch.bfloat16)
+        for x in (q, q2, pool, pool2):
+            x.copy_(torch.randn_like(x))
+        over.copy_(q2)
+        junk = torch.full((64 << 20,), 0xFF, dtype=torch.uint8, device=DEV)    # over memory freed since
+        graph.replay()
+        torch.cuda.synchronize()
+        assert ctx.last_status()["flags"] == 0 and ctx.last_cuda_error() == 0
+        del graph, junk
+    check(out, None, reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, 0.08), torch.bfloat16)
+    ref = reference(q2, pool2, 0, 1, new_off2, kv2, page_off2, table2, 16, 0.08)
+    check(out2, None, ref, torch.bfloat16)
+    check(over, None, ref, torch.bfloat16)
