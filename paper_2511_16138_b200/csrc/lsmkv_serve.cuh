@@ -261,6 +261,9 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
     if (seqs->n_new == 0) return LSMKV_OK;
     if (!seqs_ok(seqs) || !rows_ok(q) || !rows_ok(out) || !pool || !pool->kv_ptrs) return LSMKV_EINVAL;
     if (n_q_heads == 0 || n_q_heads % ctx->geom.n_kv_heads != 0 || !std::isfinite(scale)) return LSMKV_EINVAL;
+    // rows are numbered in 32 bits: new tokens, and rows under a KV head up to whole tiles
+    if (seqs->n_new > 0x7FFFFFFFull || seqs->n_new * (n_q_heads / ctx->geom.n_kv_heads) > 0xFFFFFF00ull)
+        return LSMKV_EINVAL;
     if (groups && groups->n_group && (!groups->group_off || !groups->shared_pages)) return LSMKV_EINVAL;
     if (groups && groups->n_group > seqs->n_seq) return LSMKV_EINVAL;
     const bool shared = groups && groups->n_group;

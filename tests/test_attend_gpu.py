@@ -568,3 +568,18 @@ def test_graphs_captured_before_a_larger_call_stay_valid():
     ref = reference(q2, pool2, 0, 1, new_off2, kv2, page_off2, table2, 16, 0.08)
     check(out2, None, ref, torch.bfloat16)
     check(over, None, ref, torch.bfloat16)
+
+
+def test_batches_of_more_rows_than_32_bits_number_are_refused():
+    """Before anything is launched (rows that repeat one token stand in for memory)."""
+    geom = lsmkv.Geom(1, 2, 64, page_tokens=16, chunk_tokens=16)
+    case = (torch.bfloat16, 64, 16, 8, 2, [2], [3])
+    _, pool, q, seqs, *_ = setup(case, n_layers=1)
+    with lsmkv.Context(geom, 0) as ctx:
+        pt = lsmkv.pool_table(list(pool))
+        for n in (2 ** 31, 2 ** 30 - 63):
+            many = lsmkv.Seqs(*seqs.keep, n, 1)
+            rows = q[:1].expand(n, -1, -1)
+            with pytest.raises(lsmkv.LsmkvError) as e:
+                ctx.attend_batch(0, many, rows, rows, pt, 0.1)
+            assert e.value.code == lsmkv.EINVAL
