@@ -515,6 +515,11 @@ def _rows(name, t, n_new: int, heads: int, head_dim: int):
     token, head, element = t.stride()
     if element != 1 and head_dim != 1:
         raise ValueError(f"{name}: the elements of a head must be contiguous, strides {t.stride()}")
+    # the stride of an extent of one is never taken, and may be anything
+    if heads == 1:
+        head = head_dim
+    if n_new == 1:
+        token = heads * head_dim
     return t.data_ptr(), token, head
 
 

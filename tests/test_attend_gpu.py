@@ -583,3 +583,16 @@ def test_batches_of_more_rows_than_32_bits_number_are_refused():
             with pytest.raises(lsmkv.LsmkvError) as e:
                 ctx.attend_batch(0, many, rows, rows, pt, 0.1)
             assert e.value.code == lsmkv.EINVAL
+
+
+def test_one_token_out_of_a_row_of_any_width():
+    """A lone new token whose row has an odd number of elements: the stride is never taken."""
+    case = (torch.bfloat16, 64, 16, 8, 2, [1], [100])
+    geom, pool, q, seqs, new_off, kv, page_off, table = setup(case, n_layers=1)
+    wide = torch.zeros(1, 8 * 64 + 5, dtype=q.dtype, device=DEV)
+    wide[:, :512] = q.flatten(1)
+    odd, out = wide.as_strided((1, 8, 64), (517, 64, 1)), torch.zeros_like(q)
+    with lsmkv.Context(geom, 0) as ctx:
+        ctx.attend_batch(0, seqs, odd, out, lsmkv.pool_table(list(pool)), 0.1)
+        assert ctx.last_status()["flags"] == 0
+    check(out, None, reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, 0.1), torch.bfloat16)

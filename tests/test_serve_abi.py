@@ -72,3 +72,13 @@ def test_rows_and_types_are_checked():
             lsmkv._dtype(t, other)
     with pytest.raises(TypeError):
         lsmkv._dtype(t.float())
+
+
+def test_the_stride_of_an_extent_of_one_does_not_matter():
+    wide = torch.zeros(3, 5 * 16 + 3, dtype=torch.bfloat16)
+    one = wide.as_strided((1, 4, 16), (83, 16, 1))                  # a token of a row of 83 elements
+    assert lsmkv._rows("q", one, 1, 4, 16) == (one.data_ptr(), 64, 16)
+    head = torch.zeros(4, 16, dtype=torch.bfloat16).as_strided((4, 1, 16), (16, 3, 1))
+    assert lsmkv._rows("k", head, 4, 1, 16) == (head.data_ptr(), 16, 16)
+    both = wide[:1, :16].as_strided((1, 1, 16), (83, 5, 1))
+    assert lsmkv._rows("k", both, 1, 1, 16) == (both.data_ptr(), 16, 16)
