@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -504,7 +505,7 @@ def lsmkv_decode_batch_static(geom: Geom, device, stream, n_query, qchunk_off, n
         raise LsmkvError(rc, "lsmkv_decode_batch_static")
 
 
-_NO_ROWS = (None, 0, 0)
+_NO_ROWS = (0, 0, 0)
 
 
 def _rows(name, t, n_new: int, heads: int, head_dim: int):
@@ -521,6 +522,18 @@ def _rows(name, t, n_new: int, heads: int, head_dim: int):
     if n_new == 1:
         token = heads * head_dim
     return t.data_ptr(), token, head
+
+
+def _reachable(*tensors) -> bool:
+    """Whether kernels can read the given tensors (None and raw addresses aside)."""
+    return all(t is None or isinstance(t, int) or t.is_cuda or t.is_pinned() for t in tensors)
+
+
+def _refuse_host(**tensors) -> None:
+    """Raise for a tensor in ordinary host memory, which would fault on the device."""
+    for name, t in tensors.items():
+        if not (t.reachable if isinstance(t, (Seqs, Groups, Rope)) else _reachable(t)):
+            raise ValueError(f"{name}: tensors on the device, got one in host memory")
 
 
 _DTYPES = {}
@@ -560,6 +573,7 @@ class Seqs:
                                  + (f", {n} of them" if n else ""))
         self.n_new, self.max_new, self.n_seq = int(n_new), int(max_new), n_seq
         self.keep = (new_off, kv_len, page_off, page_table)
+        self.reachable = _reachable(*self.keep)
         self.c = SeqsStruct(self.n_new, n_seq, self.max_new, *[t.data_ptr() for t in self.keep])
         self.ref = C.addressof(self.c)
 
@@ -576,6 +590,7 @@ class Groups:
             raise ValueError("group_off: n_group + 1, shared_pages: n_group contiguous 4-byte "
                              "integers")
         self.keep = (group_off, shared_pages)
+        self.reachable = _reachable(*self.keep)
         self.c = GroupsStruct(n, 0, group_off.data_ptr(), shared_pages.data_ptr())
         self.ref = C.addressof(self.c)
 
@@ -592,6 +607,7 @@ class Rope:
                                       not positions.is_contiguous()):
             raise ValueError("positions: contiguous 4-byte integers")
         self.keep = (table, positions)
+        self.reachable = _reachable(*self.keep)
         self.n_positions = None if positions is None else positions.numel()
         self.c = RopeStruct(table.data_ptr(), None if positions is None else positions.data_ptr(),
                             table.shape[0], table.shape[1], int(interleaved))
@@ -615,6 +631,10 @@ class _AppendArgs(C.Structure):
                 for part, kind in (("", C.c_void_p), ("_token", C.c_uint64), ("_head", C.c_uint64))]
     _fields_ += [("kv_ptrs", C.c_void_p), ("num_pages", C.c_uint64)]
     V, Q, OUT, POOL = 24, 48, 72, 96
+
+
+# filled through the bytes of all fields: half the time of the constructor's field by field
+_ATTEND_FIELDS, _APPEND_FIELDS = struct.Struct("=8Q").pack, struct.Struct("=14Q").pack
 
 
 def lsmkv_append_batch(ctx, stream, layer, dtype, seqs, k, v, pool, rope, n_q_heads, q_in, q_out,
@@ -792,7 +812,13 @@ class Context:
         if rope is not None and rope.n_positions not in (None, n):
             raise ValueError(f"{rope.n_positions} positions for {n} new tokens")
         kv_ptrs, num_pages = pool
-        args = _AppendArgs(*kk, *vv, *qq, *oo, _ptr(kv_ptrs), num_pages)
+        if not (k.is_cuda and v.is_cuda and seqs.reachable and (q is None or q.is_cuda and q_out.is_cuda)
+                and (rope is None or rope.reachable) and (q_norm is None or q_norm.is_cuda)
+                and (k_norm is None or k_norm.is_cuda) and (kv_ptrs.__class__ is int or kv_ptrs.is_cuda)):
+            _refuse_host(seqs=seqs, k=k, v=v, q=q, q_out=q_out, rope=rope, pool=kv_ptrs, q_norm=q_norm,
+                         k_norm=k_norm)
+        args = _AppendArgs.from_buffer_copy(
+            _APPEND_FIELDS(*kk, *vv, *qq, *oo, _ptr(kv_ptrs) or 0, num_pages))
         at = _address(args)
         lsmkv_append_batch(self.handle, stream, layer, _dtype(k, v, q, q_out, q_norm, k_norm),
                            seqs.ref, at, at + args.V, at + args.POOL,
@@ -804,8 +830,12 @@ class Context:
         if lse is not None:
             _check_lse(lse, q)
         kv_ptrs, num_pages = pool
-        return heads, _AttendArgs(*_rows("q", q, n, heads, dim), *_rows("out", out, n, heads, dim),
-                                  _ptr(kv_ptrs), num_pages)
+        if not (q.is_cuda and out.is_cuda and seqs.reachable and (lse is None or lse.is_cuda)
+                and (kv_ptrs.__class__ is int or kv_ptrs.is_cuda)):
+            _refuse_host(seqs=seqs, q=q, out=out, pool=kv_ptrs, lse=lse)
+        return heads, _AttendArgs.from_buffer_copy(
+            _ATTEND_FIELDS(*_rows("q", q, n, heads, dim), *_rows("out", out, n, heads, dim),
+                           _ptr(kv_ptrs) or 0, num_pages))
 
     def attend_batch(self, layer, seqs, q, out, pool, scale, lse=None, stream=None):
         """q, out [n_new, n_q_heads, head_dim]; lse float32 [n_new, n_q_heads] or None."""
@@ -816,6 +846,8 @@ class Context:
 
     def attend_shared_batch(self, layer, seqs, groups, q, out, pool, scale, lse=None, stream=None):
         """attend_batch for sequences in groups with common pages ahead (Groups)."""
+        if not groups.reachable:
+            _refuse_host(groups=groups)
         heads, args = self._attend_args(seqs, q, out, pool, lse)
         at = _address(args)
         lsmkv_attend_shared_batch(self.handle, stream, layer, _dtype(q, out), seqs.ref, groups.ref,

@@ -82,3 +82,48 @@ def test_the_stride_of_an_extent_of_one_does_not_matter():
     assert lsmkv._rows("k", head, 4, 1, 16) == (head.data_ptr(), 16, 16)
     both = wide[:1, :16].as_strided((1, 1, 16), (83, 5, 1))
     assert lsmkv._rows("k", both, 1, 1, 16) == (both.data_ptr(), 16, 16)
+
+
+class OnDevice(torch.Tensor):
+    """A host tensor that says it lies on the device: stands in for one here."""
+    is_cuda = True
+
+
+def device(t):
+    return t.as_subclass(OnDevice)
+
+
+def test_tensors_in_host_memory_are_refused_before_the_call():
+    ctx = lsmkv.Context.__new__(lsmkv.Context)          # no device here: a handle that every call refuses
+    ctx.handle, ctx.geom = None, lsmkv.Geom(1, 2, 16)
+
+    def seqs(where=device):
+        return lsmkv.Seqs(where(z(2, dtype=torch.int64)), where(z(1)), where(z(2, dtype=torch.int64)),
+                          where(z(1)), 1, 1)
+
+    def groups(where=device):
+        return lsmkv.Groups(where(z(2)), where(z(1)))
+
+    host = lambda t: t  # noqa: E731
+    rows = lambda heads, where=device: where(torch.zeros(1, heads, 16, dtype=torch.bfloat16))  # noqa: E731
+    pool = (device(z(2, dtype=torch.int64)), 1)
+    good = dict(layer=0, seqs=seqs(), q=rows(4), out=rows(4), pool=pool, scale=1.0, stream=0)
+    bad = [dict(seqs=seqs(host)), dict(q=rows(4, host)), dict(out=rows(4, host)),
+           dict(pool=(z(2, dtype=torch.int64), 1)), dict(lse=torch.zeros(1, 4))]
+    for change, error in [({}, lsmkv.LsmkvError)] + [(b, ValueError) for b in bad]:
+        with pytest.raises(error):
+            ctx.attend_batch(**(good | change))
+        with pytest.raises(error):
+            ctx.attend_shared_batch(groups=groups(), **(good | change))
+    with pytest.raises(ValueError):
+        ctx.attend_shared_batch(groups=groups(host), **good)
+    good = dict(layer=0, seqs=seqs(), k=rows(2), v=rows(2), pool=pool, q=rows(4), stream=0,
+                rope=lsmkv.Rope(device(torch.zeros(3, 16))))
+    weights = torch.zeros(16, dtype=torch.bfloat16)
+    for change, error in ({}, lsmkv.LsmkvError), (dict(pool=(0, 1)), lsmkv.LsmkvError), \
+            (dict(seqs=seqs(host)), ValueError), (dict(k=rows(2, host)), ValueError), \
+            (dict(v=rows(2, host)), ValueError), (dict(q=rows(4, host)), ValueError), \
+            (dict(q_out=rows(4, host)), ValueError), (dict(q_norm=weights), ValueError), \
+            (dict(k_norm=weights), ValueError), (dict(rope=lsmkv.Rope(torch.zeros(3, 16))), ValueError):
+        with pytest.raises(error):
+            ctx.append_batch(**(good | change))
