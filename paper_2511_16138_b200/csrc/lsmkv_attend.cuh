@@ -549,19 +549,22 @@ __device__ __noinline__ Quad sum_parts(const float *parts, uint32_t c0, uint32_t
 
 // A row tile's products also run over keys that only later rows of it see, with weight zero: an
 // infinite or undefined value there would make the sum undefined although the row must not see it.
-// Whether any of eight elements is one.
+// Whether there is one among eight elements: a running sum of zero times each, which stays zero or does not.
 template <typename T>
-__device__ __forceinline__ bool any_undefined(const uint4 &v)
+__device__ __forceinline__ void add_undefined(const uint4 &v, uint32_t &sum)
 {
-    constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
-    bool any = false;
+    using Pair = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+    const uint32_t zero = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t x = (&v.x)[i];
-        any |= (x & kExp) == kExp || (x >> 16 & kExp) == kExp;
+        const Pair r = __hfma2(*reinterpret_cast<const Pair *>(&x), *reinterpret_cast<const Pair *>(&zero),
+                               *reinterpret_cast<const Pair *>(&sum));
+        sum = *reinterpret_cast<const uint32_t *>(&r);
     }
-    return any;
 }
+
+__device__ __forceinline__ bool was_undefined(uint32_t sum) { return (sum & 0x7FFF7FFFu) != 0; }
 
 // Write four elements of finished row R of the item: acc = sum of weighted values relative to
 // 2^m, l the sum of weights. Merges the prefix pass's result first when there is one.
@@ -869,8 +872,7 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
             lim[x >> 1][x & 1] = r < cut.rows ? token_limit(it, (row_base + r) / G) : it.kv0;
         }
         const uint32_t lim_first = token_limit(it, row_base / G);              // least of the tile
-        const uint32_t lim_last = token_limit(it, (row_base + cut.rows - 1) / G);
-        const uint32_t key_end = min(lim_last, it.kv0 + cut.k1 * kTile);
+        const uint32_t key_end = min(token_limit(it, (row_base + cut.rows - 1) / G), it.kv0 + cut.k1 * kTile);
         const uint32_t key0 = it.kv0 + cut.k0 * kTile + w * Sh::kKeys;
 
         // queries as the right operand: 16 elements x 8 rows a fragment, two fragments a load
@@ -994,10 +996,12 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
             // A tile with keys that some rows see and others do not, and an undefined value among them
             // (16 keys at the end of a sequence with several new tokens, at most two warps' tiles)
             bool apart = false;
-            if (lim_first < lim_last && key + Sh::kKeys > lim_first) {
-                for (uint32_t x = lane; x < Sh::kKeys * kChunks; x += 32)
-                    apart |= any_undefined<T>(*reinterpret_cast<const uint4 *>(smem + (vs - q_s) + x * 16));
-                apart = __any_sync(~0u, apart);
+            if (it.tokens > 1 && key + Sh::kKeys > lim_first && it.causal) {
+                uint32_t sum = 0;
+#pragma unroll
+                for (uint32_t x = 0; x < Sh::kKeys * kChunks; x += 32)
+                    add_undefined<T>(*reinterpret_cast<const uint4 *>(smem + (vs - q_s) + (x + lane) * 16), sum);
+                apart = __any_sync(~0u, was_undefined(sum));
             }
             if (!apart) {
 #pragma unroll

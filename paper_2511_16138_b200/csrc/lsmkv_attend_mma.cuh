@@ -288,7 +288,7 @@ __global__ __launch_bounds__(256) void k_attend_merge(const __grid_constant__ At
 
 // ---- rows that came out undefined ---------------------------------------------------------------
 //
-// A row may have come out undefined for a value that only later rows of its tile see (see any_undefined). When
+// A row may have come out undefined for a value that only later rows of its tile see (see add_undefined). When
 // a CTA is done and has met undefined rows, its softmax warps go through its cuts once more: a scan of
 // the values that some rows of the cut see and others do not (at most 256 keys) finds the last undefined
 // one, and only rows that end ahead of it are computed anew, over the cut's keys alone; all others are undefined by
@@ -549,7 +549,9 @@ __device__ __noinline__ void redo_cuts(const AttendJob &j, const Span span, unsi
             const uint32_t k = from + x / pieces, page = j.seqs.page_table[it.page0 + k / j.page_tokens];
             if (page >= j.num_pages) continue;
             const uint64_t at = (((uint64_t)page * j.page_tokens + k % j.page_tokens) * j.n_kv_heads + cw.p.kv_head) * j.head_dim;
-            if (any_undefined<T>(*reinterpret_cast<const uint4 *>(vbuf + at + x % pieces * 8))) atomicMax(behind, k + 1);
+            uint32_t sum = 0;
+            add_undefined<T>(*reinterpret_cast<const uint4 *>(vbuf + at + x % pieces * 8), sum);
+            if (was_undefined(sum)) atomicMax(behind, k + 1);
         }
         softmax_sync();
         const uint32_t last = *behind;
