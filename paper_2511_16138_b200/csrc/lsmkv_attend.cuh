@@ -12,10 +12,14 @@
 // rows of one sequence under one KV head (row r = token r / G, head r % G), and its cost is the
 // number of key tiles that its last row sees. All tiles in a row -- sequence, KV head, row tile,
 // key tile -- form one line of units that is cut into equal spans, one per CTA: no CTA has more
-// than one unit more than another, whatever the lengths. A row tile cut by a span's end leaves
-// parts in scratch, merged in order by whoever comes after (the CTA that delivers the last part
-// in the few-row kernel, a launch of its own behind the many-row kernel), so that results do not depend on timing. Every CTA finds its span by itself, from the lengths: no launch
-// before, and nothing for the host to know.
+// than the total over the CTAs, rounded up, whatever the lengths. (The last spans may be shorter or
+// empty: with few units a CTA the rounding shows, 149 units on 148 CTAs keep half of them busy. In
+// the many-row kernel whole tiles may come first, see find_span; every tile's length holds one unit
+// for what its beginning and end cost, kTileCost.) A row tile cut by a span's end leaves parts in
+// scratch, merged in order by whoever comes after (the CTA that delivers the last part in the few-row
+// kernel, a launch of its own behind the many-row kernel), so that results do not depend on timing.
+// Every CTA finds its span by itself, from the lengths: no launch before, and nothing for the host to
+// know.
 #pragma once
 #include <type_traits>
 
