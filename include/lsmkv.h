@@ -560,9 +560,9 @@ int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dt
  * values of positions 0..p of its sequence under KV head h / (n_q_heads / n_kv_heads), weights
  * softmax(scale * q . k). n_q_heads must be a multiple of n_kv_heads; n_new below 2^31 (as in an
  * append) and n_new * n_q_heads / n_kv_heads below 2^32 - 256 (LSMKV_EINVAL).
- *   q, out   [host] descriptors of n_new x n_q_heads rows of `dtype`; out may be q's rows (where
- *            their memory meets and a sequence may have several new tokens and more than 16 rows
- *            under a KV head, the queries are copied first)
+ *   q, out   [host] descriptors of n_new x n_q_heads rows of `dtype`; out may lie over q (the
+ *            queries are copied first where a sequence may have several new tokens and more than
+ *            16 rows under a KV head, or the rows are not the same ones)
  *   lse_out  [dev] f32[n_new][n_q_heads] or NULL: log(sum exp(scale * q . k)) of every row
  * A row without any key (padding) is zero, its lse -inf. Scores, statistics and sums are held
  * in 32 bits; weights are rounded to `dtype` before they meet the values.

@@ -26,14 +26,28 @@ bool rows_ok(const lsmkv_rows_t *r)
            r->token_stride <= 0xFFFFFFFFull && r->head_stride <= 0xFFFFFFFFull;
 }
 
-// Whether the memory that two sets of rows span meets.
+// Whether two sets of rows are the same ones (strides of an extent of one aside).
+bool rows_same(const lsmkv_rows_t &a, const lsmkv_rows_t &b, uint64_t n_new, uint32_t heads)
+{
+    return a.data == b.data && (n_new == 1 || a.token_stride == b.token_stride) &&
+           (heads == 1 || a.head_stride == b.head_stride);
+}
+
+// Whether the memory of two sets of rows may meet. Rows that lie side by side in the tokens of one
+// buffer do not.
 bool rows_meet(const lsmkv_rows_t &a, const lsmkv_rows_t &b, uint64_t n_new, uint32_t heads, uint32_t head_dim)
 {
-    auto end = [&](const lsmkv_rows_t &r) {
-        return reinterpret_cast<uintptr_t>(r.data) +
-               2 * ((n_new - 1) * r.token_stride + (heads - 1ull) * r.head_stride + head_dim);
-    };
-    return reinterpret_cast<uintptr_t>(a.data) < end(b) && reinterpret_cast<uintptr_t>(b.data) < end(a);
+    auto span = [&](const lsmkv_rows_t &r) { return 2 * ((heads - 1ull) * r.head_stride + head_dim); };
+    auto begin = [&](const lsmkv_rows_t &r) { return reinterpret_cast<uintptr_t>(r.data); };
+    auto end = [&](const lsmkv_rows_t &r) { return begin(r) + 2 * (n_new - 1) * r.token_stride + span(r); };
+    if (begin(a) >= end(b) || begin(b) >= end(a)) return false;
+    const uint64_t period = 2 * a.token_stride;
+    if (a.token_stride == b.token_stride && span(a) <= period && span(b) <= period) {
+        const uint64_t ahead = begin(b) >= begin(a) ? (begin(b) - begin(a)) % period
+                                                    : (period - (begin(a) - begin(b)) % period) % period;
+        return ahead < span(a) || ahead + span(b) > period;      // b's token begins so far behind one of a's
+    }
+    return true;
 }
 
 SeqArgs seq_args(const lsmkv_seqs_t *s)
@@ -317,11 +331,12 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
         job.shared_pages = groups->shared_pages;
     }
     LaunchTimer timer(ctx, s, LSMKV_K_ATTEND);
-    // A row of a many-row tile that comes out undefined beside later tokens may be computed once more from
-    // its query, which must not have become output by then. One token a sequence has no later tokens, and the
-    // few-row kernel computes none twice.
-    if (many_rows(ctx, seqs->max_new, job.group) && seqs->max_new > 1 &&
-        rows_meet(*q, *out, seqs->n_new, n_q_heads, ctx->geom.head_dim)) {
+    // Where the output lies over the queries: rows over themselves are fine, each is written after it was
+    // read. But a row of a many-row tile that comes out undefined beside later tokens may be computed once more from its
+    // query, which must not have become output by then; and in another layout a row lies over other rows.
+    if (rows_meet(*q, *out, seqs->n_new, n_q_heads, ctx->geom.head_dim) &&
+        ((many_rows(ctx, seqs->max_new, job.group) && seqs->max_new > 1) ||
+         !rows_same(*q, *out, seqs->n_new, n_q_heads))) {
         const uint64_t pieces = seqs->n_new * n_q_heads * (ctx->geom.head_dim / 8);
         if (!ctx->d_queries || pieces * 16 > ctx->queries_cap) {
             rc = enlarge_scratch(ctx, &ctx->d_queries, &ctx->queries_cap, pieces * 16, __LINE__);

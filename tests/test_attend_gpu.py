@@ -596,3 +596,24 @@ def test_one_token_out_of_a_row_of_any_width():
         ctx.attend_batch(0, seqs, odd, out, lsmkv.pool_table(list(pool)), 0.1)
         assert ctx.last_status()["flags"] == 0
     check(out, None, reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, 0.1), torch.bfloat16)
+
+
+@pytest.mark.parametrize("new", [[1] * 3000, [2, 1, 4, 3] * 300, [70, 1, 200] * 20], ids=["one", "few", "many"])
+def test_output_over_the_queries_in_another_layout(new):
+    """The queries are every second row of a buffer (and the other way round), the output its first rows;
+    output beside the queries in the tokens of one buffer; output over the queries a few tokens on."""
+    case = (torch.bfloat16, 128, 16, 8, 2, new, [40] * len(new))
+    geom, pool, q, seqs, new_off, kv, page_off, table = setup(case, n_layers=1)
+    n, hq, D = q.shape
+    ref = reference(q, pool, 0, 1, new_off, kv, page_off, table, 16, 0.08)
+    flat = torch.zeros(2 * n + 3, hq, D, dtype=q.dtype, device=DEV)
+    pair = flat[:2 * n].view(n, 2 * hq, D)
+    with lsmkv.Context(geom, 0) as ctx:
+        pt = lsmkv.pool_table(list(pool))
+        for src, dst in ((flat[:2 * n:2], flat[:n]), (flat[:n], flat[1:2 * n:2]), (pair[:, :hq], pair[:, hq:]),
+                         (pair[:, hq:], pair[:, :hq]), (flat[:n], flat[3:n + 3]), (flat[2:n + 2], flat[:n]),
+                         (flat[:n].flip(0).contiguous(), flat[:n])):
+            src.copy_(q)
+            ctx.attend_batch(0, seqs, src, dst, pt, 0.08)
+            assert ctx.last_status()["flags"] == 0
+            check(dst, None, ref, torch.bfloat16)
