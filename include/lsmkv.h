@@ -568,8 +568,8 @@ int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dt
  * in 32 bits; weights are rounded to `dtype` before they meet the values.
  * Uses (and may grow) scratch of the context: two attends must be ordered by the caller, and the
  * first of a size comes before any stream capture. Scratch that a larger call replaces is kept until
- * lsmkv_destroy() (all of it no larger than the present one), so graphs captured before stay valid. A wait that runs out sets
- * LSMKV_ST_WAIT_EXPIRED; results are then unspecified until lsmkv_last_status() has been called.
+ * lsmkv_destroy() (all of it no larger than the present one), so graphs captured before stay valid.
+ * A wait that runs out sets LSMKV_ST_WAIT_EXPIRED; the results of that call are then unspecified.
  * Infinities and NaN among the keys and values reach the rows that see them, and no others. (Where
  * a value is undefined that some rows of a tile of 256 see and others do not, those others are
  * computed twice.)
