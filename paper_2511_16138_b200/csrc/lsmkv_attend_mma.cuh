@@ -317,6 +317,7 @@ struct RedoShape {
     static constexpr uint32_t kHalf = kKeys * kRow;          // keys, then values
     static constexpr uint32_t kOffsets = 4 * kHalf;          // behind two stages: places of two stages' keys
     static constexpr uint32_t kBehind = kOffsets + 2 * kKeys * 8;
+    static_assert(kBehind + 4 <= ManyShape<DP>::kSmem - 1024, "within the pipeline's shared memory");
 };
 
 // 16 rows a warp from row r0 of the cut's tile on, 128 in all; smem: RedoShape's, free.
