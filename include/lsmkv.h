@@ -43,6 +43,14 @@
  *             page_bytes = page_tokens*n_kv_heads*head_dim*elem_bytes is contiguous)
  *   blob    for every page of the chunk, in token order: for l in 0..L-1: K slab of layer l,
  *             V slab of layer l  (chunk_bytes = m*2L*page_bytes)
+ *   8-bit pool  flags = LSMKV_POOL_E4M3(B), elem_bytes = 1, head_dim a multiple of 16; B = 1, 2, 4, 8
+ *             or 16 tokens, dividing page_tokens: a page slab holds e4m3 codes
+ *             [page_tokens][n_kv_heads][head_dim], then one scale byte for each head and block of B
+ *             tokens, [n_kv_heads][page_tokens / B], then as many bytes as make the slab's size a
+ *             multiple of 16. Token t, element d of head h stands for code * 2^(byte - 127) with the
+ *             byte of block t / B; exponents (byte - 127) outside -100..100 are taken as the nearest.
+ *             To the calls that move pages and blobs a slab is bytes, scales included
+ *             (page_bytes = page_tokens*n_kv_heads*head_dim + the scales' part)
  *   A chunk is C = chunk_tokens = m * page_tokens tokens (m >= 1 whole pages); a sequence of len
  *   tokens has floor(len / C) chunks and a trailing partial chunk is never encoded, probed or
  *   decoded. Page tables carry m entries per chunk: entry i*m + k names the pool page of the
@@ -74,11 +82,14 @@ extern "C" {
 #define LSMKV_ST_BAD_COUNT 0x4u    /* chunk_off / qchunk_off / hit disagree with the sequence lengths */
 #define LSMKV_ST_MISALIGNED 0x8u   /* a pool buffer is not 16-byte aligned (skipped) */
 #define LSMKV_ST_WAIT_EXPIRED 0x10u /* a bounded wait inside a kernel gave up */
+#define LSMKV_ST_NO_PAGE 0x40u     /* a fork found no free page left for a child */
 #define LSMKV_ST_OVERFLOW 0x20u    /* compressing codec: a blob did not fit blob_capacity (chunk skipped, empty record) */
 
 /* lsmkv_geom_t.flags */
 #define LSMKV_CODEC_IDENTITY 0u    /* blobs are bit copies of the page slabs */
 #define LSMKV_CODEC_XP12 1u        /* lossless exponent packing of 16-bit float slabs (see below) */
+#define LSMKV_POOL_8BIT 2u         /* set in: */
+#define LSMKV_POOL_E4M3(block_tokens) (LSMKV_POOL_8BIT | ((uint32_t)(block_tokens) << 8)) /* 8-bit pool */
 
 typedef struct lsmkv_ctx lsmkv_ctx;
 
@@ -489,7 +500,8 @@ int lsmkv_decode_batch_static(const lsmkv_geom_t *geom, int device, void *stream
  * The step around a hit: new keys and values enter the paged pool, and queries attend to what
  * the pool holds -- restored prefixes and new tokens alike. These calls work on one layer at a
  * time, on pools of 16-bit floats (elem_bytes == 2, head_dim a multiple of 8 and at most 256,
- * LSMKV_EINVAL otherwise); blobs and codecs play no part in them.
+ * LSMKV_EINVAL otherwise) and on 8-bit pools (head_dim at most 256); blobs and codecs play no
+ * part in them.
  *
  * A batch is described once per step and used for every layer. Sequence i has kv_len[i] tokens,
  * the last n_i = new_off[i+1] - new_off[i] of which are new: new token t of it (row new_off[i] + t
@@ -548,6 +560,13 @@ typedef struct {
  *             n_q_heads rows, both NULL (and n_q_heads 0) to append only
  * Computed in 32 bits and rounded once. V rows, and K rows without norm and rotation, are bit
  * copies. Slots must be distinct within the call.
+ * 8-bit pools (dtype is that of q, k, v and the norms): K and V rows become codes. The exponent of a block's scale
+ * is the least e in -100..100 with |x| <= 448 * 2^e for all finite elements x of the block's new
+ * tokens; where the block holds earlier tokens of the sequence it is not less than it was, and if it grows
+ * their codes are rounded anew (code * 2^(old - new), to nearest even). Codes are x * 2^-e to nearest even;
+ * what is beyond 448 * 2^100 saturates; infinities and NaN become NaN codes. Scales of blocks that a call begins
+ * need no initial value. Blocks of B tokens, not only slots, must be distinct within the call, and no other
+ * sequence may list a block's page that grows (see lsmkv_fork_batch).
  */
 int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype,
                        const lsmkv_seqs_t *seqs, const lsmkv_rows_t *k, const lsmkv_rows_t *v,
@@ -570,6 +589,8 @@ int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dt
  * first of a size comes before any stream capture. Scratch that a larger call replaces is kept until
  * lsmkv_destroy() (all of it no larger than the present one), so graphs captured before stay valid.
  * A wait that runs out sets LSMKV_ST_WAIT_EXPIRED; the results of that call are then unspecified.
+ * 8-bit pools: a key or value is code * 2^exponent, exactly; scale and exponents enter scores and weights in
+ * 32 bits. `dtype` is that of q and out. Limit: |v| below 2^100 or so, as an append leaves them.
  * Infinities and NaN among the keys and values reach the rows that see them, and no others. (Where
  * a value is undefined that some rows of a tile of 256 see and others do not, those others are
  * computed twice.)
@@ -601,6 +622,65 @@ int lsmkv_attend_shared_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint
                               uint32_t n_q_heads, const lsmkv_rows_t *q,
                               const lsmkv_pool_t *pool, float scale, const lsmkv_rows_t *out,
                               float *lse_out);
+
+/*
+ * Pages of a pool and who uses them. refs [dev] u32[num_pages], the caller's: refs[p] = number of page-table
+ * entries, over all sequences, that name page p; 0 = free. Counters stay below 2^31. These calls work on whole
+ * pages of all layers, 8-bit or not, and cost a few microseconds beside the copies they make. Calls on the
+ * same counters, tables or pool must be ordered by the caller; fork and compaction share scratch
+ * of the context (first call of a size before any stream capture, as for an attend).
+ *
+ * Tables: sequence i has kv_len[i] tokens (below 2^31) and entries page_off[i] .. page_off[i+1] of
+ * page_table, the first ceil(kv_len[i] / page_tokens) of them in use. One that breaks these rules, or whose
+ * entries lie beyond n_entries, sets LSMKV_ST_BAD_COUNT (item = sequence) and is left out. A page
+ * id >= num_pages sets LSMKV_ST_BAD_PAGE (item = entry).
+ */
+typedef struct {
+    uint64_t n_entries;
+    uint32_t n_seq, reserved;
+    uint32_t *kv_len;            /* [dev] u32[n_seq] */
+    const uint64_t *page_off;    /* [dev] u64[n_seq + 1], ascending */
+    uint32_t *page_table;        /* [dev] u32[n_entries] */
+} lsmkv_tables_t;
+
+/* Release: the counters of all pages in use by these sequences go down by one an entry. A counter
+ * that would fall below zero stays zero and sets LSMKV_ST_BAD_COUNT (item = sequence). */
+int lsmkv_release_batch(lsmkv_ctx *ctx, void *stream, const lsmkv_tables_t *tables, uint32_t *refs,
+                        uint64_t num_pages);
+
+/*
+ * Fork: child c becomes a copy of sequence parent[c] of `parents`. Its table gets the parent's entries
+ * in use (entries behind them stay as they are), children->kv_len[c] the parent's length. Pages whose tokens are all
+ * filled are shared and counted up; when the parent's length ends inside a page the child gets a free page of its own,
+ * the lowest free ones in the order of the children, counter 1, into which the filled tokens' rows are
+ * copied in every layer (rounded up to 16 bytes; in an 8-bit pool with the page's scales), so that parent
+ * and children may append independently. The parent keeps its pages.
+ *   parent   [dev] u32[children->n_seq]
+ * A child whose parent does not exist or breaks the rules, or whose table is shorter than the parent's entries in
+ * use, sets LSMKV_ST_BAD_COUNT (item = child) and is left out. When no free page is left LSMKV_ST_NO_PAGE is set (item
+ * = child) and the entry is 0xFFFFFFFF; everything else of the child is done. An entry of the parent
+ * that names no page is passed on as it is. Children's tables must not overlap the parents' or each other.
+ */
+int lsmkv_fork_batch(lsmkv_ctx *ctx, void *stream, const lsmkv_tables_t *parents, const uint32_t *parent,
+                     const lsmkv_tables_t *children, uint32_t *refs, const lsmkv_pool_t *pool);
+
+/*
+ * Compaction: with n pages in use (refs[p] > 0), the k-th used page behind the first n, in ascending order, moves to
+ * the k-th free one among the first n, in every layer, and all used pages are then pages 0 .. n-1.
+ * page_table [dev] holds all entries that name pages of the pool, of all sequences, in any order: entries
+ * of moved pages are rewritten, others pass unchanged. refs_out, page_table_out may be refs, page_table themselves or must not
+ * overlap them. n_live_out [dev] receives n (may be NULL). Contents of pages n .. num_pages-1 are
+ * unspecified afterwards. LSMKV_ST_BAD_PAGE: item = entry.
+ */
+int lsmkv_compact_pages(lsmkv_ctx *ctx, void *stream, const uint32_t *refs, uint32_t *refs_out,
+                        const uint32_t *page_table, uint32_t *page_table_out, uint64_t n_entries,
+                        const lsmkv_pool_t *pool, uint64_t *n_live_out);
+
+/* Copy pages src[i] -> dst[i], i < n, in every layer ([dev] u32[n]; n below 2^32). Destinations must be
+ * distinct, and none may be another pair's source. A page id >= num_pages sets LSMKV_ST_BAD_PAGE (item = i)
+ * and the pair is left out. */
+int lsmkv_copy_pages(lsmkv_ctx *ctx, void *stream, const uint32_t *src, const uint32_t *dst, uint64_t n,
+                     const lsmkv_pool_t *pool);
 
 /* Synchronise `stream`, copy the device status block to *out [host] and clear it. */
 int lsmkv_last_status(lsmkv_ctx *ctx, void *stream, lsmkv_status_t *out);

@@ -24,6 +24,9 @@
 #include "lsmkv_append.cuh"
 #include "lsmkv_attend.cuh"
 #include "lsmkv_attend_mma.cuh"
+#include "lsmkv_append8.cuh"
+#include "lsmkv_attend8.cuh"
+#include "lsmkv_pages.cuh"
 
 using namespace lsmkv;
 
@@ -58,6 +61,8 @@ struct lsmkv_ctx {
     int64_t probe_warps_per_cta, simt_ctas_per_sm, host_stage_bytes, xp_generic;
     int64_t xp_one_pass, wait_cycles, host_copy_ctas, host_put_device_placed, test_drop_piece;
     int64_t host_copy_piece;
+    CodeArgs codes;      // 8-bit pools: where a slab's scales lie
+    bool pool8;          // the pool holds e4m3 codes
     uint32_t ppc;        // pages per chunk: chunk_tokens / page_tokens
     // attend: parts of cut tiles with their counters; results of the prefix pass
     void *d_attend;
@@ -66,6 +71,8 @@ struct lsmkv_ctx {
     uint64_t prefix_cap;   // bytes
     void *d_queries;       // copy of queries that share memory with the output
     uint64_t queries_cap;  // bytes
+    void *d_pages;         // fork and compaction: ranks and lists of pages
+    uint64_t pages_cap;    // bytes
     struct Kept { void *p; Kept *next; } *kept;   // buffers of theirs that larger ones replaced
     // host-buffer calls: device staging and host scratch
     void *d_io[3];
@@ -209,6 +216,26 @@ struct LaunchTimer {
     }
 };
 
+// Tokens of a block with a scale of its own, 8-bit pools; 0: none.
+uint32_t pool_block(const lsmkv_geom_t &g) { return g.flags >> 8 & 0xFFu; }
+
+// The flags, and what an 8-bit pool asks of the rest of the geometry.
+bool pool_flags_ok(const lsmkv_geom_t &g)
+{
+    if (!(g.flags & LSMKV_POOL_8BIT)) return g.flags <= LSMKV_CODEC_XP12;
+    const uint32_t b = pool_block(g);
+    return g.flags == LSMKV_POOL_E4M3(b) && b >= 1 && b <= 16 && (b & (b - 1)) == 0 && g.elem_bytes == 1 &&
+           g.head_dim % 16 == 0 && g.page_tokens % b == 0;
+}
+
+// Bytes of a page of one layer's keys or values: elements, and the scales of an 8-bit pool.
+uint64_t slab_bytes(const lsmkv_geom_t &g)
+{
+    const uint64_t body = (uint64_t)g.page_tokens * g.n_kv_heads * g.head_dim * g.elem_bytes;
+    if (!(g.flags & LSMKV_POOL_8BIT)) return body;
+    return body + (((uint64_t)g.page_tokens / pool_block(g) * g.n_kv_heads + 15) & ~15ull);
+}
+
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // The bulk copy kernels and the one-pass encoder take their stages as dynamic shared memory
@@ -244,6 +271,10 @@ cudaError_t set_copy_smem_limit(int max_smem_optin)
     if (e == cudaSuccess)
         e = cudaFuncSetAttribute(k_xpf_encode<XpfShape16k>,
                                  cudaFuncAttributeMaxDynamicSharedMemorySize, (int)XpfShape16k::kSmem);
+    for (auto *kern : {reinterpret_cast<const void *>(k_fork), reinterpret_cast<const void *>(k_compact),
+                       reinterpret_cast<const void *>(k_copy_pages)})
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, max_smem_optin);
     auto raise_few = [&](auto shape, auto *kern) {
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)decltype(shape)::kSmem);
@@ -260,6 +291,18 @@ cudaError_t set_copy_smem_limit(int max_smem_optin)
     raise_few(FewShape<128, 2>(), k_attend_few<__half, 128, 2>);
     raise_few(FewShape<256, 1>(), k_attend_few<__half, 256, 1>);
     raise_few(FewShape<256, 2>(), k_attend_few<__half, 256, 2>);
+    raise_few(Few8Shape<64, 1>(), k_attend_few8<__nv_bfloat16, 64, 1>);
+    raise_few(Few8Shape<64, 2>(), k_attend_few8<__nv_bfloat16, 64, 2>);
+    raise_few(Few8Shape<128, 1>(), k_attend_few8<__nv_bfloat16, 128, 1>);
+    raise_few(Few8Shape<128, 2>(), k_attend_few8<__nv_bfloat16, 128, 2>);
+    raise_few(Few8Shape<256, 1>(), k_attend_few8<__nv_bfloat16, 256, 1>);
+    raise_few(Few8Shape<256, 2>(), k_attend_few8<__nv_bfloat16, 256, 2>);
+    raise_few(Few8Shape<64, 1>(), k_attend_few8<__half, 64, 1>);
+    raise_few(Few8Shape<64, 2>(), k_attend_few8<__half, 64, 2>);
+    raise_few(Few8Shape<128, 1>(), k_attend_few8<__half, 128, 1>);
+    raise_few(Few8Shape<128, 2>(), k_attend_few8<__half, 128, 2>);
+    raise_few(Few8Shape<256, 1>(), k_attend_few8<__half, 256, 1>);
+    raise_few(Few8Shape<256, 2>(), k_attend_few8<__half, 256, 2>);
     for (auto *many : {k_attend_many<__nv_bfloat16, 64, true>, k_attend_many<__half, 64, true>,
                        k_attend_many<__nv_bfloat16, 64, false>, k_attend_many<__half, 64, false>})
         if (e == cudaSuccess)
@@ -581,9 +624,9 @@ int lsmkv_create(lsmkv_ctx **out, const lsmkv_geom_t *g, int device)
     if (!out || !g) return LSMKV_EINVAL;
     *out = nullptr;
     if (!g->n_layers || !g->n_kv_heads || !g->head_dim || !g->elem_bytes || !g->page_tokens ||
-        !g->chunk_tokens || g->chunk_tokens % g->page_tokens != 0 || g->flags > LSMKV_CODEC_XP12)
+        !g->chunk_tokens || g->chunk_tokens % g->page_tokens != 0 || !pool_flags_ok(*g))
         return LSMKV_EINVAL;
-    const uint64_t pb = (uint64_t)g->page_tokens * g->n_kv_heads * g->head_dim * g->elem_bytes;
+    const uint64_t pb = slab_bytes(*g);
     const uint64_t ppc = g->chunk_tokens / g->page_tokens;
     if (pb % 16 != 0 || pb > 0x40000000ull || g->n_layers > 4096 || ppc > 4096 ||
         2ull * g->n_layers * ppc > 0x100000ull)
@@ -601,7 +644,13 @@ int lsmkv_create(lsmkv_ctx **out, const lsmkv_geom_t *g, int device)
     ctx->chunk_bytes = ppc * 2ull * g->n_layers * pb;
     uint64_t key_tab[4 * kKeyTab];
     fill_key_consts(ctx->kc, g->chunk_tokens, key_tab);
-    ctx->codec = g->flags;
+    ctx->codec = g->flags & LSMKV_CODEC_XP12;
+    ctx->pool8 = g->flags & LSMKV_POOL_8BIT;
+    if (ctx->pool8) {
+        ctx->codes.page_bytes = pb;
+        ctx->codes.code_bytes = g->page_tokens * g->n_kv_heads * g->head_dim;
+        while (2u << ctx->codes.block_log2 <= pool_block(*g)) ++ctx->codes.block_log2;
+    }
     ctx->xp_dir_bytes = (uint32_t)((4ull * (ppc * 2ull * g->n_layers + 1) + 15) & ~15ull);
     ctx->copy_mode = 0;
     ctx->copy_stage_bytes = 16384;
@@ -668,6 +717,7 @@ int lsmkv_destroy(lsmkv_ctx *ctx)
     if (release_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     if (release_scratch(ctx, &ctx->d_prefix, &ctx->prefix_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     if (release_scratch(ctx, &ctx->d_queries, &ctx->queries_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
+    if (release_scratch(ctx, &ctx->d_pages, &ctx->pages_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     while (lsmkv_ctx::Kept *k = ctx->kept) {
         ctx->kept = k->next;
         note(cudaFree(k->p));
@@ -1473,9 +1523,9 @@ extern "C" int lsmkv_decode_batch_static(const lsmkv_geom_t *g, int device, void
 {
     if (!g || !g->n_layers || !g->n_kv_heads || !g->head_dim || !g->elem_bytes ||
         !g->page_tokens || !g->chunk_tokens || g->chunk_tokens % g->page_tokens != 0 ||
-        g->flags != 0)
+        (g->flags & LSMKV_CODEC_XP12) || !pool_flags_ok(*g))
         return LSMKV_EINVAL;
-    const uint64_t pb = (uint64_t)g->page_tokens * g->n_kv_heads * g->head_dim * g->elem_bytes;
+    const uint64_t pb = slab_bytes(*g);
     const uint64_t ppc = g->chunk_tokens / g->page_tokens;
     if (pb % 16 != 0 || pb > 0x40000000ull || g->n_layers > 4096 || ppc > 4096 ||
         2ull * g->n_layers * ppc > 0x100000ull)
@@ -1553,3 +1603,4 @@ extern "C" int lsmkv_decode_batch_static(const lsmkv_geom_t *g, int device, void
 
 #include "lsmkv_hostio.cuh"
 #include "lsmkv_serve.cuh"
+#include "lsmkv_pagecalls.cuh"

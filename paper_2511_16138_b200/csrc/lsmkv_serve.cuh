@@ -11,7 +11,7 @@ namespace {
 bool serve_geom_ok(const lsmkv_ctx *ctx, uint32_t layer, uint32_t dtype)
 {
     const lsmkv_geom_t &g = ctx->geom;
-    return g.elem_bytes == 2 && g.head_dim % 8 == 0 && g.head_dim <= 256 && layer < g.n_layers &&
+    return (ctx->pool8 || (g.elem_bytes == 2 && g.head_dim % 8 == 0)) && g.head_dim <= 256 && layer < g.n_layers &&
            (dtype == LSMKV_BF16 || dtype == LSMKV_F16);
 }
 
@@ -90,10 +90,27 @@ cudaError_t start_few(lsmkv_ctx *ctx, cudaStream_t s, bool follows, const Attend
     return start(ctx, s, follows, k_attend_few<T, DP, NB>, (unsigned)ctx->sm_count, Sh::kThreads, Sh::kSmem, job);
 }
 
+template <typename T, int DP, int NB>
+cudaError_t start_few8(lsmkv_ctx *ctx, cudaStream_t s, bool follows, const AttendJob &job)
+{
+    using Sh = Few8Shape<DP, NB>;
+    return start(ctx, s, follows, k_attend_few8<T, DP, NB>, (unsigned)ctx->sm_count, Sh::kThreads, Sh::kSmem, job,
+                 ctx->codes);
+}
+
 // rows8: no row tile has more than 8 rows.
 template <typename T>
 int launch_few(lsmkv_ctx *ctx, cudaStream_t s, bool follows, const AttendJob &job, bool rows8)
 {
+    if (ctx->pool8) {
+        if (job.head_dim <= 64)
+            CU(ctx, (rows8 ? start_few8<T, 64, 1> : start_few8<T, 64, 2>)(ctx, s, follows, job));
+        else if (job.head_dim <= 128)
+            CU(ctx, (rows8 ? start_few8<T, 128, 1> : start_few8<T, 128, 2>)(ctx, s, follows, job));
+        else
+            CU(ctx, (rows8 ? start_few8<T, 256, 1> : start_few8<T, 256, 2>)(ctx, s, follows, job));
+        return LSMKV_OK;
+    }
     if (job.head_dim <= 64)
         CU(ctx, (rows8 ? start_few<T, 64, 1> : start_few<T, 64, 2>)(ctx, s, follows, job));
     else if (job.head_dim <= 128)
@@ -174,7 +191,7 @@ int launch_many(lsmkv_ctx *ctx, cudaStream_t s, bool follows, AttendJob &job)
 }
 
 // The tcgen05 kernel takes heads of up to 128 elements.
-bool many_takes(const lsmkv_ctx *ctx) { return ctx->geom.head_dim <= 128; }
+bool many_takes(const lsmkv_ctx *ctx) { return ctx->geom.head_dim <= 128 && !ctx->pool8; }
 
 // Whether a sequence of max_new new tokens has more rows than one tile of the few-row kernel.
 bool many_rows(const lsmkv_ctx *ctx, uint32_t max_new, uint32_t group)
@@ -359,6 +376,38 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
     return bf ? launch_own<__nv_bfloat16>(ctx, s, job) : launch_own<__half>(ctx, s, job);
 }
 
+// Append to an 8-bit pool: one launch, CTAs for the queries and CTAs for the blocks.
+template <typename T>
+int launch_append8(lsmkv_ctx *ctx, cudaStream_t s, const AppendJob &job, bool vec)
+{
+    Append8Job J;
+    J.a = job;
+    J.c = ctx->codes;
+    const uint64_t B = 1ull << J.c.block_log2, n = job.seqs.n_new, seqs = job.seqs.n_seq;
+    // slots of blocks: the same number for every sequence, or as the sequences' lengths ask for
+    const uint64_t even = std::min<uint64_t>(((uint64_t)job.seqs.max_new + 2 * B - 2) / B, n / B + 2);
+    const uint64_t by_length = n / B + 2 * seqs;
+    J.per_seq = even * seqs <= by_length ? (uint32_t)even : 0u;
+    const uint64_t slots = J.per_seq ? even * seqs : by_length;
+    // queries: as in the 16-bit append, as many tokens a CTA as one round of CTAs, four a SM, leaves
+    const uint64_t round = (uint64_t)ctx->sm_count * 4;
+    J.a.tokens = (uint32_t)std::min<uint64_t>(kAppend8Warps, (n + round - 1) / round);
+    const uint64_t q = job.n_q_heads == 0 ? 0 : vec ? (n + J.a.tokens - 1) / J.a.tokens : (n * job.n_q_heads + 3) / 4;
+    if (q + slots > 0x7FFFFFFFull) return LSMKV_EINVAL;
+    J.q_blocks = (uint32_t)q;
+    J.n_slots = (uint32_t)slots;
+    const unsigned grid = (unsigned)(q + slots);
+    if (!vec)
+        k_append8_elements<T><<<grid, 128, 0, s>>>(J);
+    else if (job.head_dim <= 128)
+        k_append8<T, 4><<<grid, kAppend8Warps * 32, 0, s>>>(J);
+    else
+        k_append8<T, 8><<<grid, kAppend8Warps * 32, 0, s>>>(J);
+    ++ctx->launches;
+    CU(ctx, cudaGetLastError());
+    return LSMKV_OK;
+}
+
 }  // namespace
 
 extern "C" int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype,
@@ -430,6 +479,9 @@ extern "C" int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, 
                                    ? (g.head_dim / 8 + 1) / 2
                                    : job.rot_dim / 16 + (g.head_dim - job.rot_dim + 15) / 16;
         while ((1u << job.lane_log2) < lanes) ++job.lane_log2;
+    }
+    if (ctx->pool8) return bf ? launch_append8<__nv_bfloat16>(ctx, s, job, vec) : launch_append8<__half>(ctx, s, job, vec);
+    if (vec) {
         // as many tokens a block as one round of blocks, four a SM, leaves; at most one a warp
         const uint64_t round = (uint64_t)ctx->sm_count * 4;
         job.tokens = (uint32_t)std::min<uint64_t>(kAppendWarps, (seqs->n_new + round - 1) / round);

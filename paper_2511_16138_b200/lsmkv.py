@@ -30,9 +30,11 @@ EXPORTS = (
     "lsmkv_hindex_buckets", "lsmkv_hindex_build", "lsmkv_xrun_merge", "lsmkv_plan_compaction",
     "lsmkv_relocate_records", "lsmkv_xrun_build", "lsmkv_xprobe_batch",
     "lsmkv_append_batch", "lsmkv_attend_batch", "lsmkv_attend_shared_batch",
+    "lsmkv_release_batch", "lsmkv_fork_batch", "lsmkv_compact_pages", "lsmkv_copy_pages",
 )
-ST_OVERFLOW = 32
+ST_OVERFLOW, ST_NO_PAGE = 32, 64
 CODEC_IDENTITY, CODEC_XP12 = 0, 1
+POOL_8BIT = 2
 ETOOBIG = -5
 STATIC_MAX_QUERIES, STATIC_MAX_CHUNKS = 4096, 262144
 K_KEYS, K_PACK, K_PROBE, K_PLAN, K_UNPACK, K_ATTEND, K_CLASSES = 0, 1, 2, 3, 4, 7, 8
@@ -116,8 +118,18 @@ class GroupsStruct(C.Structure):
                 ("shared_pages", C.c_void_p)]
 
 
+class TablesStruct(C.Structure):
+    _fields_ = [("n_entries", C.c_uint64), ("n_seq", C.c_uint32), ("reserved", C.c_uint32),
+                ("kv_len", C.c_void_p), ("page_off", C.c_void_p), ("page_table", C.c_void_p)]
+
+
 class ProfileStruct(C.Structure):
     _fields_ = [("ms", C.c_double * 8), ("launches", C.c_uint64 * 8)]
+
+
+def pool_e4m3(block_tokens: int) -> int:
+    """Geom.flags of an 8-bit pool: e4m3 codes, a scale for each head and block of so many tokens."""
+    return POOL_8BIT | block_tokens << 8
 
 
 @dataclass(frozen=True)
@@ -132,8 +144,21 @@ class Geom:
     flags: int = 0
 
     @property
-    def page_bytes(self) -> int:
+    def code_bytes(self) -> int:
+        """Bytes of a page slab's elements; an 8-bit pool's scales come behind them."""
         return self.page_tokens * self.n_kv_heads * self.head_dim * self.elem_bytes
+
+    @property
+    def block_tokens(self) -> int:
+        """Tokens that share a scale in an 8-bit pool, 0 in others."""
+        return self.flags >> 8 & 0xFF if self.flags & POOL_8BIT else 0
+
+    @property
+    def page_bytes(self) -> int:
+        if not self.block_tokens:
+            return self.code_bytes
+        scales = self.n_kv_heads * (self.page_tokens // self.block_tokens)
+        return self.code_bytes + -(-scales // 16) * 16
 
     @property
     def pages_per_chunk(self) -> int:
@@ -207,6 +232,14 @@ def lib() -> C.CDLL:
     L.lsmkv_attend_batch.argtypes = [vp, vp, u32, u32, vp, u32, vp, vp, f32, vp, vp]
     L.lsmkv_attend_shared_batch.restype = C.c_int
     L.lsmkv_attend_shared_batch.argtypes = [vp, vp, u32, u32, vp, vp, u32, vp, vp, f32, vp, vp]
+    L.lsmkv_release_batch.restype = C.c_int
+    L.lsmkv_release_batch.argtypes = [vp, vp, vp, vp, u64]
+    L.lsmkv_fork_batch.restype = C.c_int
+    L.lsmkv_fork_batch.argtypes = [vp, vp, vp, vp, vp, vp, C.POINTER(PoolStruct)]
+    L.lsmkv_compact_pages.restype = C.c_int
+    L.lsmkv_compact_pages.argtypes = [vp, vp, vp, vp, vp, vp, u64, C.POINTER(PoolStruct), vp]
+    L.lsmkv_copy_pages.restype = C.c_int
+    L.lsmkv_copy_pages.argtypes = [vp, vp, vp, vp, u64, C.POINTER(PoolStruct)]
     L.lsmkv_encode_bound.restype = u64
     L.lsmkv_encode_bound.argtypes = [vp, u64]
     L.lsmkv_bloom_blocks.restype = u64
@@ -532,7 +565,7 @@ def _reachable(*tensors) -> bool:
 def _refuse_host(**tensors) -> None:
     """Raise for a tensor in ordinary host memory, which would fault on the device."""
     for name, t in tensors.items():
-        if not (t.reachable if isinstance(t, (Seqs, Groups, Rope)) else _reachable(t)):
+        if not (t.reachable if isinstance(t, (Seqs, Groups, Rope, Tables)) else _reachable(t)):
             raise ValueError(f"{name}: tensors on the device, got one in host memory")
 
 
@@ -593,6 +626,32 @@ class Groups:
         self.reachable = _reachable(*self.keep)
         self.c = GroupsStruct(n, 0, group_off.data_ptr(), shared_pages.data_ptr())
         self.ref = C.addressof(self.c)
+
+
+class Tables:
+    """Sequences' page tables (lsmkv_tables_t), for the page calls: kv_len int32[n_seq], page_off
+    int64[n_seq + 1], page_table int32. Keeps its tensors alive."""
+
+    def __init__(self, kv_len, page_off, page_table):
+        n_seq = kv_len.numel()
+        for name, t, size, n in (("kv_len", kv_len, 4, n_seq), ("page_off", page_off, 8, n_seq + 1),
+                                 ("page_table", page_table, 4, None)):
+            if t.element_size() != size or not t.is_contiguous() or (n and t.numel() != n):
+                raise ValueError(f"{name}: contiguous, {size}-byte integers"
+                                 + (f", {n} of them" if n else ""))
+        self.n_seq = n_seq
+        self.keep = (kv_len, page_off, page_table)
+        self.reachable = _reachable(*self.keep)
+        self.c = TablesStruct(page_table.numel(), n_seq, 0, *[t.data_ptr() for t in self.keep])
+        self.ref = C.addressof(self.c)
+
+
+def _words(name, t, n=None):
+    """Address of contiguous 4-byte integers on the device (n of them)."""
+    if t.element_size() != 4 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise ValueError(f"{name}: contiguous 4-byte integers" + ("" if n is None else f", {n} of them"))
+    _refuse_host(**{name: t})
+    return t.data_ptr()
 
 
 class Rope:
@@ -663,6 +722,33 @@ def lsmkv_attend_shared_batch(ctx, stream, layer, dtype, seqs, groups, n_q_heads
                                                    n_q_heads, q, pool, scale, out, _ptr(lse_out))
     if rc:
         _check(ctx, rc, "lsmkv_attend_shared_batch")
+
+
+def lsmkv_release_batch(ctx, stream, tables, refs, num_pages) -> None:
+    """The C call; tables: address of its struct."""
+    _check(ctx, lib().lsmkv_release_batch(ctx, _stream(stream), tables, _ptr(refs), num_pages),
+           "lsmkv_release_batch")
+
+
+def lsmkv_fork_batch(ctx, stream, parents, parent, children, refs, pool) -> None:
+    """The C call; parents, children: addresses of their structs."""
+    p = _pool(pool)
+    _check(ctx, lib().lsmkv_fork_batch(ctx, _stream(stream), parents, _ptr(parent), children, _ptr(refs),
+                                       C.byref(p)), "lsmkv_fork_batch")
+
+
+def lsmkv_compact_pages(ctx, stream, refs, refs_out, page_table, page_table_out, n_entries, pool,
+                        n_live_out=None) -> None:
+    p = _pool(pool)
+    _check(ctx, lib().lsmkv_compact_pages(ctx, _stream(stream), _ptr(refs), _ptr(refs_out), _ptr(page_table),
+                                          _ptr(page_table_out), n_entries, C.byref(p), _ptr(n_live_out)),
+           "lsmkv_compact_pages")
+
+
+def lsmkv_copy_pages(ctx, stream, src, dst, n, pool) -> None:
+    p = _pool(pool)
+    _check(ctx, lib().lsmkv_copy_pages(ctx, _stream(stream), _ptr(src), _ptr(dst), n, C.byref(p)),
+           "lsmkv_copy_pages")
 
 
 def lsmkv_last_status(ctx, stream=None) -> dict:
@@ -852,6 +938,39 @@ class Context:
         at = _address(args)
         lsmkv_attend_shared_batch(self.handle, stream, layer, _dtype(q, out), seqs.ref, groups.ref,
                                   heads, at, at + args.POOL, scale, at + args.OUT, lse)
+
+    def release_batch(self, tables, refs, stream=None):
+        """Count down the pages in use by the sequences of `tables` (Tables); refs int32[num_pages]."""
+        _refuse_host(tables=tables)
+        lsmkv_release_batch(self.handle, stream, tables.ref, _words("refs", refs), refs.numel())
+
+    def fork_batch(self, tables, parent, children, refs, pool, stream=None):
+        """Sequence c of `children` (Tables) becomes a copy of sequence parent[c] of `tables`: whole pages
+        shared, the filled rows of a begun one copied to a free page. parent int32[children], refs
+        int32[num_pages]."""
+        _refuse_host(tables=tables, children=children, pool=pool[0])
+        lsmkv_fork_batch(self.handle, stream, tables.ref, _words("parent", parent, children.n_seq),
+                         children.ref, _words("refs", refs, pool[1]), pool)
+
+    def compact_pages(self, refs, pool, page_table, refs_out=None, table_out=None, n_live=None,
+                      stream=None):
+        """Move the used pages to the pool's beginning; refs int32[num_pages] and page_table int32 (every
+        entry that names a page) follow, in place or into refs_out and table_out. n_live: int64[1] or None."""
+        refs_out = refs if refs_out is None else refs_out
+        table_out = page_table if table_out is None else table_out
+        n = page_table.numel()
+        if n_live is not None and (n_live.element_size() != 8 or n_live.numel() != 1):
+            raise ValueError("n_live: one 8-byte integer")
+        _refuse_host(pool=pool[0], n_live=n_live)
+        lsmkv_compact_pages(self.handle, stream, _words("refs", refs, pool[1]),
+                            _words("refs_out", refs_out, pool[1]), _words("page_table", page_table),
+                            _words("table_out", table_out, n), n, pool, n_live)
+
+    def copy_pages(self, src, dst, pool, stream=None):
+        """Pages src[i] -> dst[i] in every layer; int32."""
+        _refuse_host(pool=pool[0])
+        n = src.numel()
+        lsmkv_copy_pages(self.handle, stream, _words("src", src), _words("dst", dst, n), n, pool)
 
     def last_status(self, stream=None) -> dict:
         return lsmkv_last_status(self.handle, stream)
