@@ -23,9 +23,9 @@
 #include "lsmkv_xrun.cuh"
 #include "lsmkv_append.cuh"
 #include "lsmkv_attend.cuh"
-#include "lsmkv_attend_mma.cuh"
 #include "lsmkv_append8.cuh"
 #include "lsmkv_attend8.cuh"
+#include "lsmkv_attend_mma.cuh"
 #include "lsmkv_pages.cuh"
 
 using namespace lsmkv;
@@ -71,6 +71,13 @@ struct lsmkv_ctx {
     uint64_t prefix_cap;   // bytes
     void *d_queries;       // copy of queries that share memory with the output
     uint64_t queries_cap;  // bytes
+    void *d_gathered;      // queries as the many-row kernel takes them over an 8-bit pool
+    uint64_t gathered_cap; // bytes
+    // of the present call, 8-bit pools: whether the many-row kernel takes the pool, and its queries
+    bool many_blocked;
+    CUtensorMap many_map;
+    __half *many_q;        // null: the caller's own
+    float *many_back;
     void *d_pages;         // fork and compaction: ranks and lists of pages
     uint64_t pages_cap;    // bytes
     struct Kept { void *p; Kept *next; } *kept;   // buffers of theirs that larger ones replaced
@@ -311,6 +318,12 @@ cudaError_t set_copy_smem_limit(int max_smem_optin)
                        k_attend_many<__nv_bfloat16, 128, false>, k_attend_many<__half, 128, false>})
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ManyShape<128>::kSmem);
+    for (auto *many : {k_attend_many<__nv_bfloat16, 64, false, true>, k_attend_many<__half, 64, false, true>})
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ManyShape<64>::kSmem8);
+    for (auto *many : {k_attend_many<__nv_bfloat16, 128, false, true>, k_attend_many<__half, 128, false, true>})
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ManyShape<128>::kSmem8);
     if (e == cudaSuccess) g_smem_limit_set[dev] = true;
     return e;
 }
@@ -717,6 +730,7 @@ int lsmkv_destroy(lsmkv_ctx *ctx)
     if (release_scratch(ctx, &ctx->d_attend, &ctx->attend_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     if (release_scratch(ctx, &ctx->d_prefix, &ctx->prefix_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     if (release_scratch(ctx, &ctx->d_queries, &ctx->queries_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
+    if (release_scratch(ctx, &ctx->d_gathered, &ctx->gathered_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     if (release_scratch(ctx, &ctx->d_pages, &ctx->pages_cap, __LINE__) != LSMKV_OK) note((cudaError_t)ctx->last_cuda);
     while (lsmkv_ctx::Kept *k = ctx->kept) {
         ctx->kept = k->next;

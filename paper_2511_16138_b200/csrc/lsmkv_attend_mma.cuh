@@ -21,12 +21,20 @@
 // Taking some exponentials by a polynomial on the multiply-add units lengthened the chain (1.83 -> 1.84
 // to 1.98 ms).
 // Every wait is bounded; one that runs out ends all roles and is reported.
+//
+// 8-bit pools (kCodes): the products run in f16 (see lsmkv_attend8.cuh), and seven loader warps bring codes from memory to
+// registers and, as f16, to the stages: a tile's 128 keys are stored relative to the largest scale of the
+// tile, code * 2^(a_j - A) with A = max a_j, its values likewise to B. So a row's scores have one factor a tile, and
+// its weights one exponent, known before the exponentials: nothing is added to the softmax warps' chain but a
+// few operations a tile. (f16 holds e4m3 codes exactly down to 2^-15 of the tile's largest scale; what is lost below is under 2^-32 of the
+// largest element.) The sums are relative to M = max (row's largest score + B), the sum of weights is taken
+// back by 2^-B tile by tile.
 #pragma once
 #include <cuda.h>
 
 #include <type_traits>
 
-#include "lsmkv_attend.cuh"
+#include "lsmkv_attend8.cuh"
 
 namespace lsmkv {
 
@@ -36,10 +44,17 @@ struct ManyShape {
     static constexpr int kStages = DP == 128 ? 5 : 8;
     static constexpr uint32_t kTileBytes = 128 * DP * 2;
     static constexpr int kLoaders = 2;         // warps that share a block's rows, by cp.async
+    // 8-bit pools: seven warps load and convert codes. 512 threads start with 128 registers each, all
+    // 65536; 256 x 192 + 256 x 64 are in use afterwards.
+    static constexpr int kConverters = 7, kThreads8 = 16 * 32;
+    // stages, and behind them the codes under way: 128 rows of keys, 128 of values
+    static constexpr int kStages8 = DP == 128 ? 4 : 8;
+    static constexpr size_t kSmem8 = 1024 + (size_t)(2 + kStages8) * kTileBytes + kTileBytes;
     // 8 softmax warps, then a warpgroup of loaders and the issuer. 384 threads start with
     // 168 registers each (64512); 256 x 208 + 128 x 80 = 63488 of them are in use afterwards.
     static constexpr int kThreads = 12 * 32;
     static constexpr int kSoftmaxRegs = 208, kOtherRegs = 80;
+    static constexpr int kSoftmaxRegs8 = 192, kOtherRegs8 = 64;
     static constexpr size_t kSmem = 1024 + (size_t)(2 + kStages) * kTileBytes;
     static_assert(kStages >= 4, "both halves' keys and values in flight");
 };
@@ -286,6 +301,267 @@ __global__ __launch_bounds__(256) void k_attend_merge(const __grid_constant__ At
     }
 }
 
+// ---- 8-bit pools --------------------------------------------------------------------------------
+
+// Number and place of the query of row R of an item under a KV head, as the many-row kernel reads it there.
+__device__ __forceinline__ uint64_t query_row(const AttendJob &j, const Item &it, uint32_t kv_head, uint32_t R)
+{
+    return (uint64_t)kv_head * j.seqs.n_new * j.group + it.row0 * j.group + R;
+}
+
+__device__ __forceinline__ uint64_t query_offset(const AttendJob &j, const Item &it, uint32_t kv_head, uint32_t R)
+{
+    if (j.q_gathered) return query_row(j, it, kv_head, R) * j.head_dim;
+    return (it.row0 + R / j.group) * j.q_ts + (uint64_t)(kv_head * j.group + R % j.group) * j.q_hs;
+}
+
+// Queries as the many-row kernel takes them over an 8-bit pool: f16, a row's largest element at 2^13 and what
+// takes it back in `back`, the rows of a KV head one behind the other. 16 lanes a row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_gather_queries(const T *q, uint64_t q_ts, uint64_t q_hs, uint64_t n_new, uint32_t kv_heads,
+                                                        uint32_t group, uint32_t head_dim, __half *dst, float *back)
+{
+    const uint32_t c = threadIdx.x & 15;
+    const uint64_t per_head = n_new * group, all = per_head * kv_heads;
+    const uint64_t rows = (uint64_t)gridDim.x * 16;
+    // (the lanes of a warp stay together: both of its rows are there, or one is the last row again)
+    for (uint64_t x0 = (uint64_t)blockIdx.x * 16 + (threadIdx.x >> 5) * 2; x0 < all; x0 += rows) {
+        const uint64_t x = min(x0 + (threadIdx.x >> 4 & 1), all - 1);
+        const uint32_t h = (uint32_t)quotient(x, per_head);
+        const uint64_t R = x - h * per_head, t = quotient(R, group);
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (c * 8 < head_dim)
+            v = *reinterpret_cast<const uint4 *>(q + t * q_ts + (uint64_t)(h * group + (uint32_t)(R - t * group)) * q_hs + c * 8);
+        float f = 1.f;
+        if (!std::is_same<T, __half>::value) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = max(top, max((&v.x)[i] & 0x7FFFu, (&v.x)[i] >> 16 & 0x7FFFu));
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(~0u, top, d));
+            int e = (int)(top >> 7) - 127 - 13;
+            e = e < -126 ? -126 : e > 114 ? 114 : e;
+            f = power_of_two(e);
+            const float to = power_of_two(-e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 u = Half2<T>::up((&v.x)[i]);
+                (&v.x)[i] = Half2<__half>::down(u.x * to, u.y * to);
+            }
+        }
+        if (c * 8 < head_dim) *reinterpret_cast<uint4 *>(dst + x * head_dim + c * 8) = v;
+        if (c == 0) back[x] = f;
+    }
+}
+
+// Two equal 16-bit floats 2^d, d <= 0 (zero below their range).
+__device__ __forceinline__ uint32_t power_f16x2(int d)
+{
+    const uint32_t one = d >= -14 ? (uint32_t)(15 + d) << 10 : d >= -24 ? 1u << (24 + d) : 0u;
+    return one | one << 16;
+}
+
+// What the roles tell each other beside the stages. The issuer walks the work for the loaders, a cut ahead of what
+// it issues: they have no registers for it. A tile's exponents go from loader to loader and to the softmax warps,
+// in eight slots in turn (a loader is at most three tiles ahead of the softmax warps, whose weights the
+// products that free its stages wait for).
+struct CodeMail {
+    static constexpr uint32_t kSlots = 8;
+    uint64_t cut_told[2];                    // barriers: a cut is there,
+    uint64_t ready[kSlots], told[kSlots];    // all loaders' parts of a tile's exponents, the tile's
+    const unsigned char *buffer[2];          // the layer's keys, its values
+    uint64_t page0[2];
+    uint4 cut[2];                            // first key, end of the keys, key tiles (0: no cut is left), KV head
+    uint2 q_rows[2];                         // the queries: first row under the KV head, halves
+    uchar2 part[kSlots][8];                  // a loader warp's largest exponents of keys, of values (+ 101; 0: no key)
+    char2 tile[kSlots];                      // the tile's
+    uint32_t q_asked;                        // cuts whose queries were asked for
+};
+
+// Loader warp `me` of kConverters: its rows of key tile after key tile, keys then values, from codes in memory to
+// f16 in the stages; warp 0 brings the queries' boxes too. A lane copies 16 codes a step (whole rows side by side) to a
+// place of its own in `raw` by cp.async, converts them when they have landed, and copies the next half tile's there: no
+// registers are held for what is under way. (Spilled registers cost the L2's latency here, since shared memory
+// takes the whole L1: with the codes under way in registers the kernel took twice as long.)
+template <int DP, typename Wait>
+__device__ __forceinline__ void load_codes(const AttendJob &j, const CodeArgs &cd, const CUtensorMap &q_map, uint32_t me,
+                                           uint32_t q_s, uint32_t ring, uint32_t raw, Wait wait_warp, uint32_t full0,
+                                           uint32_t empty0, uint32_t q_full, uint32_t q_empty, uint32_t spare_bar,
+                                           CodeMail &mail)
+{
+    using Sh = ManyShape<DP>;
+    constexpr uint32_t kBlock = 128 * 128, kStages = Sh::kStages8;
+    constexpr uint32_t kC = DP / 16, kRows = 32 / kC, kSteps = 128 / kRows, W = Sh::kConverters;
+    constexpr uint32_t kMine = (kSteps + W - 1) / W, kOwn = kMine * kRows;     // steps and rows of a warp
+    static_assert(kOwn <= 32, "a lane a row");
+    const uint32_t lane = threadIdx.x & 31, G = j.group;
+    // This lane's 16 codes of a row of a step. Eight lanes take two rows of a block of 64 elements: with the
+    // swizzle (piece p of 8 elements of row r at p ^ r % 8) their stores fill the width of the banks.
+    const uint32_t c = DP == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
+    const uint32_t sub = DP == 128 ? (lane >> 2 & 1) | (lane >> 3 & 2) : lane >> 2;
+    const bool there = c * 16 < j.head_dim;
+    const uint32_t row0 = me * kOwn + sub;               // of step 0; its cell's swizzle, and that of odd steps
+    uint32_t at[2];
+#pragma unroll
+    for (uint32_t y = 0; y < 2; ++y)
+        at[y] = (c >> 2) * kBlock + row0 * 128 + (((2 * (c & 3)) ^ (row0 + y * kRows & 7)) << 4);
+    const uint32_t steps = me * kMine >= kSteps ? 0u : min(kMine, kSteps - me * kMine);
+    raw += (me * kMine * 32 + lane) * 16;                // keys; the values' codes 128 rows on
+    const uint32_t own = me * kOwn + lane;               // this lane's row: its page, place and scales
+    uint32_t half_cnt = 0;                               // half tiles handed over
+    bool alive = true;
+    for (uint32_t cut = 0;; ++cut) {
+        if (!(alive = wait_warp(smem_addr(mail.cut_told + (cut & 1)), (cut >> 1) & 1))) break;
+        const uint4 info = mail.cut[cut & 1];
+        const uint32_t key0 = info.x, key_end = info.y, n = info.z, kv_head = info.w;
+        if (!n) break;
+        constexpr uint32_t kNone = 0xFFFFFFFFu;
+        uint32_t page = kNone, place = kNone;
+        auto find_page = [&](uint32_t t) {
+            const uint32_t k = key0 + t * Sh::kKeys + own;
+            page = kNone;
+            if (lane >= kOwn || own >= Sh::kKeys || k >= key_end) return;
+            const uint64_t entry = mail.page0[cut & 1] + k / j.page_tokens;
+            const uint32_t p = j.seqs.page_table[entry];
+            if (p < j.num_pages) page = p;
+            else st_flag(j.st, LSMKV_ST_BAD_PAGE, entry);
+        };
+        // place of the row's codes in units of 16 bytes, and the exponents of its scales
+        int k_exp, v_exp;
+        auto find_place = [&](uint32_t t) {
+            place = kNone;
+            if (page == kNone) return;
+            const uint32_t slot = (key0 + t * Sh::kKeys + own) % j.page_tokens;
+            const uint64_t slab = page * cd.page_bytes;
+            place = (uint32_t)((slab + (slot * j.n_kv_heads + kv_head) * j.head_dim) >> 4);
+            const uint64_t s = slab + cd.code_bytes + kv_head * (j.page_tokens >> cd.block_log2) + (slot >> cd.block_log2);
+            k_exp = mail.buffer[0][s];
+            v_exp = mail.buffer[1][s];
+        };
+        // this warp's part of a tile's exponents
+        auto tell = [&]() {
+            k_exp = place == kNone ? kScaleMin - 1 : scale_exponent(k_exp);
+            v_exp = place == kNone ? kScaleMin - 1 : scale_exponent(v_exp);
+            const uint32_t k = __reduce_max_sync(~0u, (uint32_t)(k_exp - kScaleMin + 1));
+            const uint32_t v = __reduce_max_sync(~0u, (uint32_t)(v_exp - kScaleMin + 1));
+            if (lane == 0) {
+                const uint32_t slot = half_cnt / 2 % mail.kSlots;
+                mail.part[slot][me] = make_uchar2((unsigned char)k, (unsigned char)v);
+                mbar_arrive(smem_addr(mail.ready + slot));
+            }
+        };
+        auto load = [&](uint32_t i, uint32_t kv) {
+            const uint32_t p = __shfl_sync(~0u, place, i * kRows + sub);
+            const bool in = p != kNone && there;
+            cp_async16(raw + kv * (128 * DP) + i * 512, reinterpret_cast<const uint4 *>(mail.buffer[kv]) + (in ? p + c : 0), in);
+        };
+        auto loaded = [&]() { asm volatile("cp.async.commit_group;" ::: "memory"); };
+        // rows of step i times their factor, to the stage at dst
+        auto convert = [&](uint32_t i, uint32_t kv, uint32_t factor, uint32_t dst) {
+            const uint32_t f = __shfl_sync(~0u, factor, i * kRows + sub);
+            uint4 v, a, b;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(raw + kv * (128 * DP) + i * 512));
+            from_codes4(v.x, a.x, a.y);
+            from_codes4(v.y, a.z, a.w);
+            from_codes4(v.z, b.x, b.y);
+            from_codes4(v.w, b.z, b.w);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                asm("mul.rn.f16x2 %0, %0, %1;" : "+r"((&a.x)[k]) : "r"(f));
+                asm("mul.rn.f16x2 %0, %0, %1;" : "+r"((&b.x)[k]) : "r"(f));
+            }
+            const uint32_t to = dst + at[i * kRows >> 2 & 1] + i * kRows * 128;
+            if (there) {
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(to), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w) : "memory");
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(to ^ 16), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+            }
+        };
+        // The next stage, once its products are done; false: gave up.
+        auto take_stage = [&]() {
+            return alive = wait_warp(empty0 + 8 * (half_cnt % kStages), (half_cnt / kStages & 1) ^ 1);
+        };
+        // (The issuer's proxy fence behind its wait makes the codes visible to the matrix unit.)
+        auto hand_over = [&]() {
+            __syncwarp();
+            // (test hook: a tile of the first CTA that never arrives)
+            const bool drop = blockIdx.x == 0 && half_cnt == j.test_drop;
+            if (lane == 0) mbar_arrive(drop ? spare_bar : full0 + 8 * (half_cnt % kStages));
+            ++half_cnt;
+        };
+        auto load_half = [&](uint32_t kv) {
+#pragma unroll
+            for (uint32_t i = 0; i < kMine; ++i)
+                if (i < steps) load(i, kv);
+            loaded();
+        };
+        find_page(0);
+        find_place(0);
+        load_half(0);
+        load_half(1);
+        if (me == 0) {
+            // the queries, once the products of the cut before have read theirs
+            if (!(alive = wait_warp(q_empty, (cut & 1) ^ 1))) break;
+            if (lane == 0) {
+                const uint2 q = mail.q_rows[cut & 1];
+                mail.q_asked = cut + 1;
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
+                             :: "r"(q_full), "r"(q.y * Sh::kTileBytes) : "memory");
+                for (uint32_t x = 0; x < q.y; ++x)
+                    for (int e = 0; e < DP / 64; ++e) {
+                        const uint32_t R = q.x + x * 128, dst = q_s + x * Sh::kTileBytes + e * kBlock;
+                        if (j.q_gathered) tma_box(dst, &q_map, e * 64, (int)kv_head, (int)R, q_full);
+                        else tma_box(dst, &q_map, e * 64, (int)(kv_head * G), (int)(R / G), q_full);
+                    }
+            }
+            __syncwarp();
+        }
+        tell();
+        if (n > 1) find_page(1);
+        for (uint32_t t = 0; t < n; ++t) {
+            const uint32_t slot = half_cnt / 2 % mail.kSlots;
+            if (!(alive = wait_warp(smem_addr(mail.ready + slot), half_cnt / 2 / mail.kSlots & 1))) break;
+            uint32_t k_factor, v_factor;
+            {
+                const uchar2 part = lane < W ? mail.part[slot][lane] : make_uchar2(0, 0);
+                const int k_top = (int)__reduce_max_sync(~0u, (uint32_t)part.x) + kScaleMin - 1;
+                const int v_top = (int)__reduce_max_sync(~0u, (uint32_t)part.y) + kScaleMin - 1;
+                if (me == 0 && lane == 0) {
+                    mail.tile[slot] = make_char2((char)max(k_top, kScaleMin), (char)max(v_top, kScaleMin));
+                    mbar_arrive(smem_addr(mail.told + slot));
+                }
+                k_factor = power_f16x2(k_exp - k_top);
+                v_factor = power_f16x2(v_exp - v_top);
+            }
+            const bool more = t + 1 < n;
+            if (more) {
+                find_place(t + 1);
+                if (t + 2 < n) find_page(t + 2);
+            }
+#pragma unroll
+            for (uint32_t kv = 0; kv < 2; ++kv) {
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                if (!take_stage()) break;
+                const uint32_t dst = ring + half_cnt % kStages * Sh::kTileBytes;
+#pragma unroll
+                for (uint32_t i = 0; i < kMine; ++i) {
+                    if (i >= steps) continue;
+                    convert(i, kv, kv ? v_factor : k_factor, dst);
+                    if (more) load(i, kv);
+                }
+                loaded();
+                hand_over();
+            }
+            if (!alive) break;
+            if (more) tell();
+        }
+        if (!alive) break;
+    }
+    // boxes of queries still under way write shared memory: let them land (bounded; a box that was never asked for
+    // is not waited for)
+    if (me == 0 && mail.q_asked) (void)mbar_wait_bounded(q_full, (mail.q_asked - 1) & 1, j.wait_cycles);
+}
+
 // ---- rows that came out undefined ---------------------------------------------------------------
 //
 // A row may have come out undefined for a value that only later rows of its tile see (see add_undefined). When
@@ -527,13 +803,206 @@ __device__ __forceinline__ void redo_rows(const AttendJob &j, const Walk<M, TILE
     }
 }
 
-// The cuts of a CTA once more, by its softmax warps.
+// The same over an 8-bit pool: codes as f16 in shared memory, their scales beside them, scores and weights as in
+// the few-row kernel.
 template <typename T, int DP, int M, int TILE>
-__device__ __noinline__ void redo_cuts(const AttendJob &j, const Span span, unsigned char *smem)
+__device__ __forceinline__ void redo_rows8(const AttendJob &j, const CodeArgs &cd, const Walk<M, TILE> &cw, float *slot,
+                                           uint32_t r0, unsigned char *smem, uint32_t behind)
+{
+    using Sh = RedoShape<DP>;
+    using F = __half;
+    const Item &it = cw.it;
+    const uint32_t tid = threadIdx.x, lane = tid & 31, g = lane >> 2, c4 = lane & 3, D = j.head_dim, G = j.group;
+    const uint32_t kv_head = cw.p.kv_head, r1 = min(r0 + 128, cw.p.rows), row_base = cw.p.rt * M;
+    const uint32_t key0 = it.kv0 + cw.p.k0 * TILE;
+    const uint32_t key_end = min(token_limit(it, (row_base + r1 - 1) / G), it.kv0 + cw.p.k1 * TILE);
+    if (key_end <= key0) return;
+    const unsigned char *const kbuf = static_cast<const unsigned char *>(j.kv_ptrs[j.layer]);
+    const unsigned char *const vbuf = static_cast<const unsigned char *>(j.kv_ptrs[j.n_layers + j.layer]);
+    const uint32_t w0 = r0 + (tid >> 5) * 16, n_rows = w0 < r1 ? min(r1 - w0, 16u) : 0;
+    const uint32_t t0 = n_rows ? (row_base + w0) / G : 0, t1 = n_rows ? (row_base + w0 + n_rows - 1) / G : 0;
+    uint32_t lim[2], q[DP / 16][4];
+    float row_scale[2];
+    bool anew[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const bool in = g + 8 * h < n_rows;
+        const uint32_t R = row_base + (in ? w0 + g + 8 * h : 0);
+        lim[h] = in ? token_limit(it, R / G) : it.kv0;
+        anew[h] = in && lim[h] < behind;
+        const uint64_t at = query_row(j, it, kv_head, R);
+        row_scale[h] = j.scale_log2 * (j.q_back ? j.q_back[at] : 1.f);
+        const F *row = static_cast<const F *>(j.q) + query_offset(j, it, kv_head, R);
+#pragma unroll
+        for (int x = 0; x < DP / 8; ++x)
+            q[x >> 1][h + 2 * (x & 1)] =
+                in && x * 8u < D ? *reinterpret_cast<const uint32_t *>(row + x * 8 + c4 * 2) : 0u;
+    }
+    float *const k_scale = reinterpret_cast<float *>(smem + Sh::kOffsets);      // of a stage's keys
+    float *const v_log = k_scale + Sh::kKeys;
+    const uint32_t blocks = j.page_tokens >> cd.block_log2, ks = smem_addr(smem), vs = ks + Sh::kHalf;
+    float o[DP / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < DP / 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
+    bool done = !__any_sync(~0u, anew[0] || anew[1]);
+    for (uint32_t first = key0; first < key_end; first += Sh::kKeys) {
+        if (softmax_all(done)) break;            // (and whatever lay here is read)
+        for (uint32_t x = tid; x < Sh::kKeys * (DP / 16); x += 256) {
+            const uint32_t r = x / (DP / 16), c = x % (DP / 16), k = first + r, s = k % j.page_tokens;
+            const uint32_t page = k < key_end ? j.seqs.page_table[it.page0 + k / j.page_tokens] : 0xFFFFFFFFu;
+            const bool in = page < j.num_pages;
+            const uint64_t slab = in ? page * cd.page_bytes : 0;
+            const uint64_t at = slab + ((uint64_t)s * j.n_kv_heads + kv_head) * D + c * 16;
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                const unsigned char *const buf = kv ? vbuf : kbuf;
+                const uint4 v = in && c * 16 < D ? *reinterpret_cast<const uint4 *>(buf + at) : make_uint4(0, 0, 0, 0);
+                uint4 *const to = reinterpret_cast<uint4 *>(smem + kv * Sh::kHalf + r * Sh::kRow + c * 32);
+                uint4 a, b;
+                from_codes4(v.x, a.x, a.y);
+                from_codes4(v.y, a.z, a.w);
+                from_codes4(v.z, b.x, b.y);
+                from_codes4(v.w, b.z, b.w);
+                to[0] = a;
+                to[1] = b;
+                if (c == 0) {
+                    const int e = in ? scale_exponent(buf[slab + cd.code_bytes + kv_head * blocks + (s >> cd.block_log2)]) : 0;
+                    if (kv) v_log[r] = (float)e;
+                    else k_scale[r] = power_of_two(e);
+                }
+            }
+        }
+        softmax_sync();
+        if (done) continue;
+#pragma unroll 1
+        for (uint32_t sub = 0; sub < Sh::kKeys; sub += 32) {
+            const uint32_t key = first + sub;
+            if (key >= key_end) break;
+            float s[4][4] = {}, u[4][4];
+#pragma unroll
+            for (int x = 0; x < DP / 16; ++x)
+#pragma unroll
+                for (int n = 0; n < 4; n += 2) {
+                    uint32_t f[4];
+                    ldmatrix4(ks + (sub + n * 8 + (lane & 7) + (lane >> 4) * 8) * Sh::kRow + (2 * x + (lane >> 3 & 1)) * 16, f);
+                    mma16816<F>(s[n], q[x], f[0], f[1]);
+                    mma16816<F>(s[n + 1], q[x], f[2], f[3]);
+                }
+            float top[2] = {m[0], m[1]};
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t at = sub + 8 * n + 2 * c4 + (e & 1);
+                    const bool see = first + at < min(lim[e >> 1], key_end);
+                    s[n][e] = see ? s[n][e] * row_scale[e >> 1] * k_scale[at] : -INFINITY;
+                    u[n][e] = see ? s[n][e] + v_log[at] : -INFINITY;
+                    top[e >> 1] = fmaxf(top[e >> 1], u[n][e]);
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                top[h] = fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 1));
+                top[h] = fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 2));
+                const float ref = top[h] == -INFINITY ? 0.f : top[h];
+                if (__any_sync(~0u, top[h] > m[h])) {
+                    const float f = exp2f(m[h] - ref);
+                    m[h] = top[h];
+                    l[h] *= f;
+#pragma unroll
+                    for (int x = 0; x < DP / 8; ++x) {
+                        o[x][2 * h] *= f;
+                        o[x][2 * h + 1] *= f;
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int e = 2 * h; e < 2 * h + 2; ++e) {
+                        l[h] += exp2f(s[n][e] - ref);
+                        u[n][e] = exp2f(u[n][e] - ref);
+                    }
+            }
+            uint32_t p[2][4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                p[n >> 1][2 * (n & 1)] = Half2<F>::down(u[n][0], u[n][1]);
+                p[n >> 1][2 * (n & 1) + 1] = Half2<F>::down(u[n][2], u[n][3]);
+            }
+            // token by token where some of these rows do not see all keys, otherwise all at once
+            const bool apart = key + 32 > token_limit(it, t0);
+            const uint32_t t_end = apart ? t1 : t0;
+            for (uint32_t t = t0; t <= t_end; ++t) {
+                const uint32_t lim_t = apart ? token_limit(it, t) : 0xFFFFFFFFu;
+#pragma unroll
+                for (int x = 0; x < DP / 16; ++x) {
+                    float part[2][4] = {};
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        uint32_t f[4];
+                        ldmatrix4t(vs + (sub + k * 16 + (lane & 15)) * Sh::kRow + (2 * x + (lane >> 4)) * 16, f);
+                        const uint32_t k0 = key + k * 16 + 2 * c4;
+                        const uint32_t m0 = (k0 < lim_t ? 0xFFFFu : 0u) | (k0 + 1 < lim_t ? 0xFFFF0000u : 0u);
+                        const uint32_t m1 = (k0 + 8 < lim_t ? 0xFFFFu : 0u) | (k0 + 9 < lim_t ? 0xFFFF0000u : 0u);
+                        mma16816<F>(part[0], p[k], f[0] & m0, f[1] & m1);
+                        mma16816<F>(part[1], p[k], f[2] & m0, f[3] & m1);
+                    }
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!apart || lim[e >> 1] == lim_t) o[2 * x + n][e] += part[n][e];
+                }
+            }
+        }
+        // rows undefined in all their elements are right as they are
+        bool lost[2] = {true, true};
+#pragma unroll
+        for (int x = 0; x < DP / 8; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) lost[e >> 1] = lost[e >> 1] && (x * 8u >= D || isnan(o[x][e]));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const unsigned votes = __ballot_sync(~0u, lost[h]);
+            if ((votes >> (lane & 28) & 15) == 15) anew[h] = false;
+        }
+        done = !__any_sync(~0u, anew[0] || anew[1]);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        l[h] += __shfl_xor_sync(~0u, l[h], 1);
+        l[h] += __shfl_xor_sync(~0u, l[h], 2);
+        const uint32_t r = w0 + g + 8 * h;
+        // elements 8 x + 2 c4, + 1 of two x: a lane and its neighbour turn them into four of one
+#pragma unroll
+        for (int x = 0; x < DP / 8; x += 2) {
+            const bool odd = c4 & 1;
+            float give[2] = {odd ? o[x][2 * h] : o[x + 1][2 * h], odd ? o[x][2 * h + 1] : o[x + 1][2 * h + 1]};
+            float keep[2] = {odd ? o[x + 1][2 * h] : o[x][2 * h], odd ? o[x + 1][2 * h + 1] : o[x][2 * h + 1]};
+            give[0] = __shfl_xor_sync(~0u, give[0], 1);
+            give[1] = __shfl_xor_sync(~0u, give[1], 1);
+            const float4 acc = odd ? make_float4(give[0], give[1], keep[0], keep[1])
+                                   : make_float4(keep[0], keep[1], give[0], give[1]);
+            const uint32_t d = (x + odd) * 8 + (c4 >> 1) * 4;
+            if (!anew[h] || d >= D) continue;
+            if (slot)
+                __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)r * DP + d), acc);
+            else
+                finish_row4_call<T>(j, it, kv_head, row_base + r, d, acc, m[h], l[h]);
+        }
+        if (slot && anew[h] && c4 == 0) {
+            __stcg(slot + (uint64_t)M * DP + r, m[h]);
+            __stcg(slot + (uint64_t)M * (DP + 1) + r, l[h]);
+        }
+    }
+}
+
+// The cuts of a CTA once more, by its softmax warps.
+template <typename T, int DP, int M, int TILE, bool kCodes>
+__device__ __noinline__ void redo_cuts(const AttendJob &j, const CodeArgs &cd, const Span span, unsigned char *smem)
 {
     uint32_t *const behind = reinterpret_cast<uint32_t *>(smem + RedoShape<DP>::kBehind);
     const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
-    const uint32_t tid = threadIdx.x, pieces = j.head_dim / 8;
+    const uint32_t tid = threadIdx.x, pieces = j.head_dim / (kCodes ? 16 : 8);
     Walk<M, TILE> cw;
     cw.start(j, span);
     while (cw.next(j, span)) {
@@ -549,35 +1018,51 @@ __device__ __noinline__ void redo_cuts(const AttendJob &j, const Span span, unsi
         for (uint32_t x = tid; x < (end - from) * pieces; x += 256) {
             const uint32_t k = from + x / pieces, page = j.seqs.page_table[it.page0 + k / j.page_tokens];
             if (page >= j.num_pages) continue;
-            const uint64_t at = (((uint64_t)page * j.page_tokens + k % j.page_tokens) * j.n_kv_heads + cw.p.kv_head) * j.head_dim;
-            uint32_t sum = 0;
-            add_undefined<T>(*reinterpret_cast<const uint4 *>(vbuf + at + x % pieces * 8), sum);
-            if (was_undefined(sum)) atomicMax(behind, k + 1);
+            if constexpr (kCodes) {
+                const uint64_t at = page * cd.page_bytes +
+                                    ((uint64_t)(k % j.page_tokens) * j.n_kv_heads + cw.p.kv_head) * j.head_dim;
+                const uint4 v = *reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(vbuf) + at +
+                                                                 x % pieces * 16);
+                if (undefined_codes(v.x) | undefined_codes(v.y) | undefined_codes(v.z) | undefined_codes(v.w))
+                    atomicMax(behind, k + 1);
+            } else {
+                const uint64_t at = (((uint64_t)page * j.page_tokens + k % j.page_tokens) * j.n_kv_heads + cw.p.kv_head) * j.head_dim;
+                uint32_t sum = 0;
+                add_undefined<T>(*reinterpret_cast<const uint4 *>(vbuf + at + x % pieces * 8), sum);
+                if (was_undefined(sum)) atomicMax(behind, k + 1);
+            }
         }
         softmax_sync();
         const uint32_t last = *behind;
         const bool whole = cw.p.k0 == 0 && cw.p.k1 == cw.p.units;
         float *slot = whole ? nullptr : part_slot(j, 2ull * span.rank + (cw.p.k0 == 0 ? 1 : 0), M, DP);
         for (uint32_t r0 = 0; r0 < cw.p.rows && token_limit(it, (row_base + r0) / j.group) < last; r0 += 128)
-            redo_rows<T, DP>(j, cw, slot, r0, smem, last);
+            if constexpr (kCodes) redo_rows8<T, DP>(j, cd, cw, slot, r0, smem, last);
+            else redo_rows<T, DP>(j, cw, slot, r0, smem, last);
     }
 }
 
-template <typename T, int DP, bool kBoxes>
-__global__ __launch_bounds__(ManyShape<DP>::kThreads, 1)
+// kCodes: an 8-bit pool (cd; otherwise unused).
+template <typename T, int DP, bool kBoxes, bool kCodes = false>
+__global__ __launch_bounds__(kCodes ? ManyShape<DP>::kThreads8 : ManyShape<DP>::kThreads, 1)
 void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ CUtensorMap map,
-                   const __grid_constant__ CUtensorMap q_map)
+                   const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CodeArgs cd)
 {
+    static_assert(!(kBoxes && kCodes), "codes come by loads");
     using Sh = ManyShape<DP>;
+    using F = typename std::conditional<kCodes, __half, T>::type;     // of the products
     constexpr int kChunks = DP / 8;
     constexpr uint32_t kBlock = 128 * 128;      // bytes of one block of 128 rows x 64 elements
     constexpr uint32_t kIssuer = 10;            // its warp
+    constexpr int kThreads = kCodes ? Sh::kThreads8 : Sh::kThreads;
+    constexpr int kStages = kCodes ? Sh::kStages8 : Sh::kStages;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[3 * Sh::kStages + 14];
+    __shared__ __align__(8) uint64_t bars[3 * kStages + 14];
     __shared__ uint32_t tmem_slot;
     __shared__ __align__(128) unsigned char map_work[128];
     __shared__ volatile uint32_t stop, undefined[8];   // (a softmax warp's rows have come out undefined)
     __shared__ float half_m[128], half_l[128];   // the second half's statistics, when the halves share rows
+    __shared__ CodeMail mail;                    // (8-bit pools)
     const uint32_t tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const uint32_t G = j.group, D = j.head_dim;
     // (what comes behind may count on the launch before this one: nobody leaves ahead of it)
@@ -587,7 +1072,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
 
     const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
     const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
-    const Span span = find_span<Sh::kThreads, true>(j, j.prefix_pass ? j.n_group : j.seqs.n_seq, Sh::kM, Sh::kKeys,
+    const Span span = find_span<kThreads, true>(j, j.prefix_pass ? j.n_group : j.seqs.n_seq, Sh::kM, Sh::kKeys,
                                                     reinterpret_cast<uint32_t *>(smem_raw));
     // the loads of the waves lay where the copy engine writes queries later; ordered by the barrier below
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -605,8 +1090,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     const uint32_t q_s = base, ring = base + 2 * Sh::kTileBytes;
     const uint32_t bar0 = smem_addr(bars);
     auto full = [&](uint32_t s) { return bar0 + 8 * s; };
-    auto empty = [&](uint32_t s) { return bar0 + 8 * (Sh::kStages + s); };
-    const uint32_t q_full = bar0 + 8 * (2 * Sh::kStages), q_empty = q_full + 8;
+    auto empty = [&](uint32_t s) { return bar0 + 8 * (kStages + s); };
+    const uint32_t q_full = bar0 + 8 * (2 * kStages), q_empty = q_full + 8;
     auto s_full = [&](uint32_t x) { return q_empty + 8 + 8 * x; };
     auto p_full = [&](uint32_t x) { return q_empty + 24 + 8 * x; };
     auto o_full = [&](uint32_t x) { return q_empty + 40 + 8 * x; };
@@ -619,12 +1104,21 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         mbar_init(half_read, 128);
         mbar_init(done_bar, 1);
         mbar_init(spare_bar, 32 * Sh::kLoaders);
-        for (int s = 0; s < Sh::kStages; ++s) {
-            mbar_init(full(s), kBoxes ? 1 : 32 * Sh::kLoaders);
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(full(s), kBoxes ? 1 : kCodes ? Sh::kConverters : 32 * Sh::kLoaders);
             mbar_init(empty(s), 1);
             mbar_init(landed(s), 1);
         }
-        mbar_init(q_full, kBoxes && j.q_boxes ? 1 : 32 * Sh::kLoaders);
+        mbar_init(q_full, kCodes || (kBoxes && j.q_boxes) ? 1 : 32 * Sh::kLoaders);
+        if (kCodes)
+            for (uint32_t x = 0; x < mail.kSlots; ++x) {
+                mbar_init(smem_addr(mail.ready + x), Sh::kConverters);
+                mbar_init(smem_addr(mail.told + x), 1);
+                if (x < 2) mbar_init(smem_addr(mail.cut_told + x), 1);
+            }
+        mail.buffer[0] = reinterpret_cast<const unsigned char *>(kbuf);
+        mail.buffer[1] = reinterpret_cast<const unsigned char *>(vbuf);
+        mail.q_asked = 0;
         mbar_init(q_empty, 1);
         for (int x = 0; x < 2; ++x) {
             mbar_init(s_full(x), 1);
@@ -636,7 +1130,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         for (int x = 0; x < 8; ++x) undefined[x] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (w == Sh::kThreads / 32 - 1) {
+    if (w == kThreads / 32 - 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      :: "r"(smem_addr(&tmem_slot)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -662,12 +1156,13 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     using CutWalk = Walk<Sh::kM, Sh::kKeys>;
 
     if (w < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(Sh::kSoftmaxRegs));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kCodes ? Sh::kSoftmaxRegs8 : Sh::kSoftmaxRegs));
         // ---- softmax: a thread owns row `row` of half x
         const uint32_t x = w >> 2, row = tid & 127;
         const uint32_t lane_base = (w & 3) << 21;            // lanes 32 (w % 4) ..
         const uint32_t s_t = tmem + lane_base + x * 128, o_t = tmem + lane_base + 256 + x * 128;
-        const float c = fmaxf(fabsf(j.scale_log2), 1e-37f);  // a negative scale negates the products
+        const float c_all = fmaxf(fabsf(j.scale_log2), 1e-37f);  // a negative scale negates the products
+        uint32_t tiles_before = 0;   // key tiles of the cuts before
         if ((D + 15) / 16 * 16 < DP) {
             // columns of the sums that no product writes: they are read with the others, and an earlier kernel
             // may have left anything there
@@ -688,10 +1183,22 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
             const uint32_t lim_first = token_limit(cw.it, row_base / G);
             float m = -INFINITY, l = 0.f;
             bool alive = true;
+            float c_row = c_all;
+            if (kCodes && j.q_back) c_row *= j.q_back[query_row(j, cw.it, cw.p.kv_head, real ? row_base + row : row_base)];
             for (uint32_t t = 0; t < n; ++t) {
                 if (!(alive = wait_warp(s_full(x), s_cnt & 1))) break;
                 ++s_cnt;
                 tc_fence_after();
+                float c = c_row, value_log = 0.f, l_back = 1.f;
+                if (kCodes) {
+                    // (the loader wrote them ahead of the keys: this barrier only orders the two)
+                    const uint32_t at = tiles_before + (both ? x : 0) + t * step;
+                    if (!(alive = wait_warp(smem_addr(mail.told + at % mail.kSlots), (at / mail.kSlots) & 1))) break;
+                    const char2 e = mail.tile[at % mail.kSlots];
+                    c = fminf(c_row * power_of_two(e.x), kLargest);
+                    value_log = (float)e.y;
+                    l_back = power_of_two(-e.y);
+                }
                 const uint32_t key = cw.it.kv0 + (cw.p.k0 + (both ? x : 0) + t * step) * Sh::kKeys;
                 const bool masked = key + Sh::kKeys > lim_first;
                 const int see = masked ? (int)(lim > key ? lim - key : 0u) : Sh::kKeys;   // keys of the tile
@@ -713,7 +1220,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
 #pragma unroll
                     for (int e = 2; e < 32; e += 2) tops[ch] = max3(tops[ch], v[ch * 32 + e], v[ch * 32 + e + 1]);
                 }
-                const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * c;
+                float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * c;
+                if (kCodes) top += value_log;
                 float fix = 1.f;
                 if (t == 0) {
                     m = top;
@@ -722,7 +1230,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     m = top;
                     l *= fix;
                 }
-                const float neg = m == -INFINITY ? 0.f : -m;
+                const float neg = m == -INFINITY ? 0.f : kCodes ? value_log - m : -m;
                 if (__any_sync(~0u, fix != 1.f)) {
                     // the value product of the tile before is done: its scores came after it
 #pragma unroll 1
@@ -754,7 +1262,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                         x.y = exp2f(x.y);
                         sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], x);
                         // the weights are rounded to the values' type: the tensor cores take both in one
-                        pk[e / 2] = Half2<T>::down(x.x, x.y);
+                        pk[e / 2] = Half2<F>::down(x.x, x.y);
                     }
                     if (ch == 2) {
                         // the weights of the first 64 keys are in place: their product may begin
@@ -765,12 +1273,14 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     }
                     tmem_st16(s_t + ch * 16, pk);
                 }
-                l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                const float all = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                l += kCodes ? all * l_back : all;
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full(x));
             }
+            tiles_before += cw.p.k1 - cw.p.k0;
             if (alive && n) {
                 alive = wait_warp(o_full(x), o_cnt & 1);
                 ++o_cnt;
@@ -884,11 +1394,14 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         bool any = false;
         for (int k = 0; k < 8; ++k) any |= undefined[k] != 0;
         if (softmax_all(any && !stop))
-            redo_cuts<T, DP, Sh::kM, Sh::kKeys>(j, span, smem_raw + (base - smem_addr(smem_raw)));
+            redo_cuts<T, DP, Sh::kM, Sh::kKeys, kCodes>(j, cd, span, smem_raw + (base - smem_addr(smem_raw)));
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(Sh::kOtherRegs));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kCodes ? Sh::kOtherRegs8 : Sh::kOtherRegs));
     }
-    if (w >= 8 && w != kIssuer) {
+    if (kCodes && w >= 8 && w != kIssuer) {
+        load_codes<DP>(j, cd, q_map, w - 8 - (w > kIssuer), q_s, ring, ring + kStages * Sh::kTileBytes, wait_warp,
+                       full(0), empty(0), q_full, q_empty, spare_bar, mail);
+    } else if (w >= 8 && w != kIssuer) {
         // ---- loaders. With boxes: warp 8 keys and values, warp 9 queries (and warp 11, if by
         // cp.async) and what is left to wipe. Otherwise warps 8 and 9 everything, half the rows each.
         constexpr int kSets = 4 / Sh::kLoaders;              // sets of 32 rows a warp takes of a block of 128
@@ -938,10 +1451,10 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         };
         // the barrier of the stage that is filled next (test hook: another one's)
         auto stage_bar = [&]() {
-            return blockIdx.x == 0 && (uint64_t)laps * Sh::kStages + stage == j.test_drop ? spare_bar : full(stage);
+            return blockIdx.x == 0 && (uint64_t)laps * kStages + stage == j.test_drop ? spare_bar : full(stage);
         };
         auto next_stage = [&]() {
-            if (++stage == Sh::kStages) {
+            if (++stage == kStages) {
                 stage = 0;
                 ++laps;
             }
@@ -1002,8 +1515,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 if (w != 9) continue;
                 // the last values of the cut: stage of position 2n - 1 from here
                 stage += 2 * n - 1;
-                laps += stage / Sh::kStages;
-                stage %= Sh::kStages;
+                laps += stage / kStages;
+                stage %= kStages;
                 if (ragged && alive) {
                     if (!(alive = wait_warp(landed(stage), (wiped >> stage) & 1))) break;
                     wiped ^= 1u << stage;
@@ -1083,7 +1596,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         }
         if (kBoxes && w == 8) {
             // boxes still under way write shared memory: let them land
-            for (int s = 0; s < Sh::kStages; ++s) {
+            for (int s = 0; s < kStages; ++s) {
                 const uint32_t lap = laps + (stage > (uint32_t)s ? 1 : 0);        // times this stage was filled
                 if (lap) (void)mbar_wait_bounded(full(s), (lap - 1) & 1, j.wait_cycles);
             }
@@ -1092,7 +1605,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
             (void)mbar_wait_bounded(q_full, (q_cnt - 1) & 1, j.wait_cycles);      // boxes of queries likewise
     } else if (w == kIssuer) {
         // ---- issuer: the warp walks together, one lane waits and issues
-        const uint32_t type = std::is_same<T, __half>::value ? 0u : 1u;
+        const uint32_t type = std::is_same<F, __half>::value ? 0u : 1u;
         const uint32_t common = (1u << 4) | (type << 7) | (type << 10) | (8u << 24);   // f32 sums, M = 128
         const uint32_t k_steps = (D + 15) / 16, n_out = k_steps * 16;
         const uint32_t id_s = common | ((Sh::kKeys / 8) << 17) | (j.scale_log2 < 0.f ? 1u << 13 : 0u);
@@ -1105,8 +1618,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
             __device__ __forceinline__ void step(uint32_t by)
             {
                 st += by;
-                if (st >= Sh::kStages) {
-                    st -= Sh::kStages;
+                if (st >= kStages) {
+                    st -= kStages;
                     ph ^= 1;
                 }
             }
@@ -1152,7 +1665,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
             vp.step(1);
             if (!wait(q_full, q_par)) return false;
             q_par ^= 1;
-            if (!kBoxes || !j.q_boxes) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            if (!kCodes && (!kBoxes || !j.q_boxes)) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             if (both) {
                 // tile t belongs to half t % 2
                 for (uint32_t t = 0; t < n + 2; ++t) {
@@ -1201,12 +1714,33 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         };
         CutWalk cw;
         cw.start(j, span);
-        while (cw.next(j, span)) {
+        // 8-bit pools: the loaders learn of a cut while the one before is issued. (Its slot is free then: the
+        // tiles of the cut that lay there have all been handed over.)
+        uint32_t cut = 0;
+        auto tell_cut = [&](bool there) {
+            if (lane == 0) {
+                const uint32_t row_base = cw.p.rt * Sh::kM, n = cw.p.k1 - cw.p.k0;
+                const uint32_t key0 = cw.it.kv0 + cw.p.k0 * Sh::kKeys;
+                mail.page0[cut & 1] = cw.it.page0;
+                mail.cut[cut & 1] = make_uint4(
+                    key0, min(token_limit(cw.it, (row_base + cw.p.rows - 1) / G), key0 + n * Sh::kKeys), there ? n : 0u, cw.p.kv_head);
+                mail.q_rows[cut & 1] = make_uint2((uint32_t)(cw.it.row0 * G) + row_base, cw.p.rows > 128 ? 2 : 1);
+                mbar_arrive(smem_addr(mail.cut_told + (cut & 1)));
+            }
+            ++cut;
+            __syncwarp();
+        };
+        bool more = cw.next(j, span);
+        if (kCodes) tell_cut(more);
+        while (more) {
+            const uint32_t n = cw.p.k1 - cw.p.k0, n0 = half_tiles(j, cw.it, cw.p, 0, Sh::kM, Sh::kKeys),
+                           n1 = half_tiles(j, cw.it, cw.p, 1, Sh::kM, Sh::kKeys);
+            const bool both = shares_rows(cw.p);
+            if (kCodes) tell_cut(more = cw.next(j, span));
             bool ok = true;
-            if (leader)
-                ok = run_cut(cw.p.k1 - cw.p.k0, half_tiles(j, cw.it, cw.p, 0, Sh::kM, Sh::kKeys),
-                             half_tiles(j, cw.it, cw.p, 1, Sh::kM, Sh::kKeys), shares_rows(cw.p));
+            if (leader) ok = run_cut(n, n0, n1, both);
             if (!__all_sync(~0u, ok)) break;
+            if (!kCodes) more = cw.next(j, span);
         }
         // products still under way read shared memory and write TMEM: let them end
         if (leader) {
@@ -1219,7 +1753,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (w == Sh::kThreads / 32 - 1)
+    if (w == kThreads / 32 - 1)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512u) : "memory");
     if (tid == 0 && stop) st_flag(j.st, LSMKV_ST_WAIT_EXPIRED, blockIdx.x);
     wait_launch();

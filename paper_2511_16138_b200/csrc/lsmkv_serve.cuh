@@ -152,9 +152,35 @@ bool make_map(uint32_t dtype, const void *base, const uint64_t (&dims)[R], const
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The many-row kernel over an 8-bit pool, on queries that gather_queries() left.
+template <typename T>
+int launch_many8(lsmkv_ctx *ctx, cudaStream_t s, bool follows, const AttendJob &few)
+{
+    const unsigned sm = (unsigned)ctx->sm_count;
+    AttendJob job = few;
+    CUtensorMap none;
+    std::memset(&none, 0, sizeof(none));
+    job.q_gathered = ctx->many_q != nullptr;
+    if (job.q_gathered) {
+        job.q = ctx->many_q;
+        job.q_back = ctx->many_back;
+        // (what lies ahead of a kernel that runs beside this one must be over when this one starts)
+        job.beside = 0;
+    }
+    if (job.head_dim <= 64)
+        CU(ctx, start(ctx, s, follows, k_attend_many<T, 64, false, true>, sm, ManyShape<64>::kThreads8,
+                      ManyShape<64>::kSmem8, job, none, ctx->many_map, ctx->codes));
+    else
+        CU(ctx, start(ctx, s, follows, k_attend_many<T, 128, false, true>, sm, ManyShape<128>::kThreads8,
+                      ManyShape<128>::kSmem8, job, none, ctx->many_map, ctx->codes));
+    CU(ctx, start(ctx, s, true, k_attend_merge<T>, dim3(sm, 256 / kMergeBlockRows), 256, 0, job));
+    return LSMKV_OK;
+}
+
 template <typename T>
 int launch_many(lsmkv_ctx *ctx, cudaStream_t s, bool follows, AttendJob &job)
 {
+    if (ctx->pool8) return launch_many8<T>(ctx, s, follows, job);
     const unsigned sm = (unsigned)ctx->sm_count;
     // Tokens of a box: the largest power of two that divides the page, at most 64. The swizzle's
     // unit is 8 rows, so boxes of fewer than 8 are out and cp.async takes such pages.
@@ -182,16 +208,49 @@ int launch_many(lsmkv_ctx *ctx, cudaStream_t s, bool follows, AttendJob &job)
                               {64, job.group, 128 / job.group}, &q_map);
     if (job.head_dim <= 64)
         CU(ctx, start(ctx, s, follows, boxes ? k_attend_many<T, 64, true> : k_attend_many<T, 64, false>, sm,
-                      ManyShape<64>::kThreads, ManyShape<64>::kSmem, job, map, q_map));
+                      ManyShape<64>::kThreads, ManyShape<64>::kSmem, job, map, q_map, ctx->codes));
     else
         CU(ctx, start(ctx, s, follows, boxes ? k_attend_many<T, 128, true> : k_attend_many<T, 128, false>, sm,
-                      ManyShape<128>::kThreads, ManyShape<128>::kSmem, job, map, q_map));
+                      ManyShape<128>::kThreads, ManyShape<128>::kSmem, job, map, q_map, ctx->codes));
     CU(ctx, start(ctx, s, true, k_attend_merge<T>, dim3(sm, 256 / kMergeBlockRows), 256, 0, job));
     return LSMKV_OK;
 }
 
 // The tcgen05 kernel takes heads of up to 128 elements.
-bool many_takes(const lsmkv_ctx *ctx) { return ctx->geom.head_dim <= 128 && !ctx->pool8; }
+bool many_takes(const lsmkv_ctx *ctx) { return ctx->geom.head_dim <= 128 && !ctx->many_blocked; }
+
+// Over an 8-bit pool the many-row kernel wants f16 queries in boxes of 128 rows under a KV head: they are brought to
+// that by a launch ahead of the others, unless they are f16 already and the heads of a KV head divide 128.
+// (8k tokens of 32 heads: 22 us of 520.)
+template <typename T>
+int gather_queries(lsmkv_ctx *ctx, cudaStream_t s, const AttendJob &job)
+{
+    ctx->many_q = nullptr;
+    ctx->many_back = nullptr;
+    const uint64_t rows = job.seqs.n_new * job.n_q_heads, D = job.head_dim;
+    const bool divides = job.group <= 128 && (job.group & (job.group - 1)) == 0;
+    if (std::is_same<T, __half>::value && divides &&
+        make_map<3>(LSMKV_F16, job.q, {D, job.n_q_heads, job.seqs.n_new}, {job.q_hs, job.q_ts},
+                    {64, job.group, 128 / job.group}, &ctx->many_map))
+        return LSMKV_OK;
+    const size_t bytes = rows * job.head_dim * 2 + rows * 4;
+    if (!ctx->d_gathered || bytes > ctx->gathered_cap) {
+        const int rc = enlarge_scratch(ctx, &ctx->d_gathered, &ctx->gathered_cap, bytes, __LINE__);
+        if (rc != LSMKV_OK) return rc;
+    }
+    ctx->many_q = static_cast<__half *>(ctx->d_gathered);
+    ctx->many_back = reinterpret_cast<float *>(ctx->many_q + rows * D);
+    const uint64_t per_head = job.seqs.n_new * job.group;
+    if (!make_map<3>(LSMKV_F16, ctx->many_q, {D, job.n_kv_heads, per_head}, {per_head * D, D}, {64, 1, 128},
+                     &ctx->many_map))
+        return cuda_fail(ctx, cudaErrorNotSupported, __LINE__);
+    k_gather_queries<T><<<merge_grid(ctx, rows * 16), 256, 0, s>>>(
+        static_cast<const T *>(job.q), job.q_ts, job.q_hs, job.seqs.n_new, job.n_kv_heads, job.group, job.head_dim,
+        ctx->many_q, ctx->many_back);
+    ++ctx->launches;
+    CU(ctx, cudaGetLastError());
+    return LSMKV_OK;
+}
 
 // Whether a sequence of max_new new tokens has more rows than one tile of the few-row kernel.
 bool many_rows(const lsmkv_ctx *ctx, uint32_t max_new, uint32_t group)
@@ -208,6 +267,11 @@ uint32_t part_dp(const lsmkv_ctx *ctx)
 // is what counts. A batch of at most 64 rows in all goes by the few-row kernel all the same: its up
 // to four row tiles find the keys in L2, and it starts and ends faster (one group of 8 sequences,
 // G = 4, 1024 common tokens: 26.6 us a call against 30.9).
+bool prefix_many(const lsmkv_ctx *ctx, const AttendJob &job)
+{
+    return many_takes(ctx) && job.seqs.n_new * job.group > 64;
+}
+
 template <typename T>
 int launch_prefix(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
 {
@@ -216,7 +280,7 @@ int launch_prefix(lsmkv_ctx *ctx, cudaStream_t s, AttendJob &job)
     job.rows_hi = 0xFFFFFFFFu;
     const uint64_t rows = job.seqs.n_new * job.group;
     job.beside = 0;
-    const int rc = many_takes(ctx) && rows > 64 ? launch_many<T>(ctx, s, false, job)
+    const int rc = prefix_many(ctx, job) ? launch_many<T>(ctx, s, false, job)
                                                  : launch_few<T>(ctx, s, false, job, rows <= 8);
     job.prefix_pass = 0;
     return rc;
@@ -302,6 +366,8 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     AttendJob job;
     std::memset(&job, 0, sizeof(job));
+    // (the loaders of codes count in units of 16 bytes, in 32 bits: 64 GB a buffer)
+    ctx->many_blocked = ctx->pool8 && pool->num_pages >= (0xFFFFFFFFull << 4) / ctx->page_bytes;
     int rc = ensure_attend(ctx, s, seqs->n_seq, &job);
     if (rc != LSMKV_OK) return rc;
     job.seqs = seq_args(seqs);
@@ -323,6 +389,7 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
     job.o_ts = out->token_stride;
     job.o_hs = out->head_stride;
     job.lse = lse_out;
+    job.pair_bytes = ctx->pool8 ? 2 : 4;
     job.scale_log2 = scale * kLog2e;
     job.dp = part_dp(ctx);
     job.wait_cycles = ctx->wait_cycles;
@@ -369,6 +436,10 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
         job.q_ts = (uint64_t)n_q_heads * ctx->geom.head_dim;
     }
     const bool bf = dtype == LSMKV_BF16;
+    if (ctx->pool8 && (many_rows(ctx, seqs->max_new, job.group) || (shared && prefix_many(ctx, job)))) {
+        rc = bf ? gather_queries<__nv_bfloat16>(ctx, s, job) : gather_queries<__half>(ctx, s, job);
+        if (rc != LSMKV_OK) return rc;
+    }
     if (shared) {
         rc = bf ? launch_prefix<__nv_bfloat16>(ctx, s, job) : launch_prefix<__half>(ctx, s, job);
         if (rc != LSMKV_OK) return rc;

@@ -345,3 +345,21 @@ def test_captured_calls_replay_over_new_tokens():
             ref = reference(turned, values(pool, g), 0, 1, new_off, [length] * n, page_off, table, P, 0.1)
             check(out, None, ref, torch.bfloat16)
         ctx.last_status()
+
+
+def test_a_wait_that_runs_out_is_reported():
+    """A key tile of the first CTA never arrives: the many-row kernel gives up after the limit and says so."""
+    case = (torch.bfloat16, 128, 16, 16, 16, 2, [200], [4000])
+    g, pool, q, seqs, new_off, kv, page_off, table = setup(case, n_layers=1)
+    out = torch.zeros_like(q)
+    with lsmkv.Context(g, 0) as ctx:
+        pt = lsmkv.pool_table(list(pool))
+        ctx.set_tuning("wait_cycles", 1000000)
+        ctx.set_tuning("test_drop_piece", 2)
+        ctx.attend_batch(0, seqs, q, out, pt, 0.1)
+        assert ctx.last_status()["flags"] == lsmkv.ST_WAIT_EXPIRED
+        ctx.set_tuning("test_drop_piece", -1)
+        ctx.set_tuning("wait_cycles", 2000000000)
+        ctx.attend_batch(0, seqs, q, out, pt, 0.1)
+        assert ctx.last_status()["flags"] == 0
+    check(out, None, reference(q, values(pool, g), 0, 1, new_off, kv, page_off, table, 16, 0.1), torch.bfloat16)
