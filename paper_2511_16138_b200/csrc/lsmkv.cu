@@ -663,6 +663,9 @@ int lsmkv_create(lsmkv_ctx **out, const lsmkv_geom_t *g, int device)
         ctx->codes.page_bytes = pb;
         ctx->codes.code_bytes = g->page_tokens * g->n_kv_heads * g->head_dim;
         while (2u << ctx->codes.block_log2 <= pool_block(*g)) ++ctx->codes.block_log2;
+        ctx->codes.page_log2 = 32;
+        for (uint32_t x = 0; x < 32; ++x)
+            if (g->page_tokens == 1u << x) ctx->codes.page_log2 = x;
     }
     ctx->xp_dir_bytes = (uint32_t)((4ull * (ppc * 2ull * g->n_layers + 1) + 15) & ~15ull);
     ctx->copy_mode = 0;

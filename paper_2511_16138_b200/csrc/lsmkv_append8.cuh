@@ -27,7 +27,19 @@ struct CodeArgs {
     uint64_t page_bytes;
     uint32_t code_bytes;     // of a slab: page_tokens * heads * head_dim
     uint32_t block_log2;     // B
+    uint32_t page_log2;      // of page_tokens; 32: it is no power of two
 };
+
+// Page of a sequence's token, and its slot there. (A division takes tens of instructions.)
+__device__ __forceinline__ uint32_t page_of_token(const CodeArgs &c, uint32_t page_tokens, uint32_t t)
+{
+    return c.page_log2 < 32 ? t >> c.page_log2 : t / page_tokens;
+}
+
+__device__ __forceinline__ uint32_t slot_of_token(const CodeArgs &c, uint32_t page_tokens, uint32_t t)
+{
+    return c.page_log2 < 32 ? t & (page_tokens - 1) : t % page_tokens;
+}
 
 __device__ __forceinline__ int scale_exponent(uint32_t byte)
 {

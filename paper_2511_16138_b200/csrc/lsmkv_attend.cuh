@@ -178,6 +178,7 @@ struct Span {
     uint64_t before;             // units ahead of that item
     uint32_t waves;              // whole row tiles that the CTA takes first
     uint32_t rank;               // number of its span among those that are not empty
+    uint32_t heads, tile;        // of the line: KV heads, or groups of them, and keys of a unit
 };
 
 // A call's launches follow each other closely: each lets the next one start while it still runs
@@ -230,7 +231,7 @@ __device__ __forceinline__ uint64_t block_scan(uint64_t mine, uint64_t *scratch,
 // 3000 tokens, 45 MB: 133 us against 147). load: gridDim words of shared memory.
 constexpr uint64_t kL2Keeps = 64ull << 20;   // bytes of keys and values, of 126 MB
 template <int NT, bool kWaves>
-__device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t tile, uint32_t *load)
+__device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t heads, uint32_t M, uint32_t tile, uint32_t *load)
 {
     __shared__ uint64_t scan[NT / 32];
     __shared__ uint64_t found_before, mine_begin, mine_end;
@@ -245,14 +246,14 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
     uint64_t bytes = 0;
     for (uint32_t i = i0; i < i1; ++i) {
         const Item it = load_item(j, i);
-        const uint64_t u = item_units(j, it, M, tile) * j.n_kv_heads;
+        const uint64_t u = item_units(j, it, M, tile) * heads;
         // (a group left out for its offsets holds a sequence that the own pass reports)
         if (!it.ok && !j.prefix_pass && blockIdx.x == 0) st_flag(j.st, LSMKV_ST_BAD_COUNT, i);
         if (i == i0) first = u;
         mine += u;
         if (kWaves && item_tiles(j, it, M)) {
-            tiles += item_tiles(j, it, M) * j.n_kv_heads;
-            bytes += (uint64_t)(it.kv1 - it.kv0) * j.n_kv_heads * j.head_dim * j.pair_bytes;
+            tiles += item_tiles(j, it, M) * heads;
+            bytes += (uint64_t)(it.kv1 - it.kv0) * heads * j.head_dim * j.pair_bytes;
         }
     }
     const bool may_wave = kWaves && !j.prefix_pass;
@@ -277,6 +278,8 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
     if (s.begin > total) s.begin = total;
     s.waves = 0;
     s.rank = blockIdx.x;
+    s.heads = heads;
+    s.tile = tile;
     uint32_t waves = may_wave && all_bytes > kL2Keeps ? all_tiles / N : 0;
     if (kWaves && !waves) {
         // equal spans; every CTA writes all of span_begin, the same values, and reads its own
@@ -288,7 +291,7 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
         // (tile_base likewise)
         for (uint32_t i = i0; i < i1; ++i) {
             j.tile_base[i] = base;
-            base += item_tiles(j, load_item(j, i), M) * j.n_kv_heads;
+            base += item_tiles(j, load_item(j, i), M) * heads;
         }
         if (i1 == n && i0 < i1) j.tile_base[n] = base;
         uint64_t capacity = s.per;                       // of CTA tid, behind its waves
@@ -299,7 +302,7 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
             for (uint32_t i = tid / team; i < n; i += NT / team) {
                 const Item it = load_item(j, i);
                 const uint32_t nt = item_tiles(j, it, M), p0 = j.tile_base[i];
-                for (uint32_t q = tid % team; q < nt * j.n_kv_heads && p0 + q < waves * N; q += team)
+                for (uint32_t q = tid % team; q < nt * heads && p0 + q < waves * N; q += team)
                     atomicAdd(&load[(p0 + q) % N], tile_units(it, q % nt, M, j.group, tile) + kTileCost);
             }
             __syncthreads();
@@ -350,7 +353,7 @@ __device__ Span find_span(const AttendJob &j, uint32_t n, uint32_t M, uint32_t t
         if (each > 1 && at + first <= s.begin) {
             at += first;
             for (i = i0 + 1; i < i1; ++i) {
-                const uint64_t u = item_units(j, load_item(j, i), M, tile) * j.n_kv_heads;
+                const uint64_t u = item_units(j, load_item(j, i), M, tile) * heads;
                 if (at + u > s.begin) break;
                 at += u;
             }
@@ -389,9 +392,11 @@ struct Cut {
     uint32_t k0, k1;             // key tiles [k0, k1) of it are this CTA's
 };
 
-// Walks a CTA's whole tiles and the cuts of its span. All threads of a warp go through it together.
+// Walks a CTA's whole tiles and the cuts of its span. All threads of a warp go through it together. TILE keys a
+// unit, 0: the span says how many, and of how many heads.
 template <int M, int TILE>
 struct Walk {
+    static __device__ __forceinline__ uint32_t tile_keys(const Span &s) { return TILE ? TILE : s.tile; }
     uint64_t u;                  // next unit
     uint32_t i, tiles;           // item, its row tiles
     uint32_t wave;               // whole tiles taken so far
@@ -414,14 +419,14 @@ struct Walk {
         it = load_item(j, i);
         tiles = item_tiles(j, it, M);
         // the tile that holds unit s.begin
-        const uint64_t per_head = item_units(j, it, M, TILE);
+        const uint64_t per_head = item_units(j, it, M, tile_keys(s));
         const uint64_t rel = u - s.before;
         p.kv_head = (uint32_t)quotient(rel, per_head);
         uint64_t at = rel - (uint64_t)p.kv_head * per_head;
         p.tile0 = s.before + (uint64_t)p.kv_head * per_head;
         p.rt = 0;
         while (true) {
-            p.units = tile_units(it, p.rt, M, j.group, TILE);
+            p.units = tile_units(it, p.rt, M, j.group, tile_keys(s));
             if (at < p.units + kTileCost || p.rt + 1 >= tiles) break;
             at -= p.units + kTileCost;
             p.tile0 += p.units + kTileCost;
@@ -434,7 +439,7 @@ struct Walk {
         p.rows = rows < M ? (uint32_t)rows : M;
     }
     // whole tile number `at` of the batch
-    __device__ __forceinline__ void take_tile(const AttendJob &j, uint32_t at)
+    __device__ __forceinline__ void take_tile(const AttendJob &j, const Span &s, uint32_t at)
     {
         uint32_t lo = 0, hi = j.seqs.n_seq;      // tile_base[lo] <= at < tile_base[hi]
         while (hi - lo > 1) {
@@ -451,7 +456,7 @@ struct Walk {
         p.kv_head = rel / tiles;
         p.rt = rel - p.kv_head * tiles;
         p.tile0 = 0;
-        p.units = tile_units(it, p.rt, M, j.group, TILE);
+        p.units = tile_units(it, p.rt, M, j.group, tile_keys(s));
         p.k0 = 0;
         p.k1 = p.units;
         count_rows(j);
@@ -459,7 +464,7 @@ struct Walk {
     __device__ __forceinline__ bool next(const AttendJob &j, const Span &s)
     {
         if (wave < s.waves) {
-            take_tile(j, wave++ * gridDim.x + blockIdx.x);
+            take_tile(j, s, wave++ * gridDim.x + blockIdx.x);
             return true;
         }
         if (s.waves && wave == s.waves) {
@@ -471,13 +476,13 @@ struct Walk {
                 p.tile0 = u;
                 if (++p.rt == tiles) {
                     p.rt = 0;
-                    if (++p.kv_head == j.n_kv_heads) {
+                    if (++p.kv_head == (TILE ? j.n_kv_heads : s.heads)) {
                         p.kv_head = 0;
                         i = next_item(j, i, j.prefix_pass ? j.n_group : j.seqs.n_seq, M, &it);
                         tiles = item_tiles(j, it, M);
                     }
                 }
-                p.units = tile_units(it, p.rt, M, j.group, TILE);
+                p.units = tile_units(it, p.rt, M, j.group, tile_keys(s));
             }
             begun = true;
             p.k0 = (uint32_t)(u - p.tile0);
@@ -667,6 +672,11 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool r
                  :: "r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
+}
+
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4])
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -738,7 +748,7 @@ __global__ __launch_bounds__(FewShape<DP, NB>::kThreads, 1) void k_attend_few(co
     const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
     const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
     const uint32_t n_items = j.prefix_pass ? j.n_group : j.seqs.n_seq;
-    const Span span = find_span<NT, false>(j, n_items, Sh::kM, kTile, nullptr);
+    const Span span = find_span<NT, false>(j, n_items, j.n_kv_heads, Sh::kM, kTile, nullptr);
     if ((reinterpret_cast<uintptr_t>(kbuf) | reinterpret_cast<uintptr_t>(vbuf)) & 15u) {
         if (blockIdx.x == 0 && tid == 0) st_flag(j.st, LSMKV_ST_MISALIGNED, 0);
         return;

@@ -11,6 +11,12 @@
 // to 448), in registers behind the load of a fragment: one conversion for two codes. So the products run
 // in f16 whatever the type of the queries; bfloat16 queries are brought to it row by row with a power of two
 // that puts a row's largest element at 2^13 (what lies below 2^-27 of it loses bits, far below the products' 32 bits).
+//
+// A token's codes of one head are 128 bytes or fewer, and read head by head -- the whole of a sequence under one
+// head, then under the next -- memory gives half of its rate: 256 requests of 1k to 8k tokens, 8 heads, 687 us for
+// the loads alone. So up to eight heads are read side by side where the batch is large enough: the warps of a CTA
+// take a head each (or two or more a head), over the same keys, and a page's codes are read whole. Then nothing is
+// merged among the warps but what shares a head. Small batches cut each head's keys for themselves (see few8_heads()).
 #pragma once
 #include "lsmkv_append8.cuh"
 #include "lsmkv_attend.cuh"
@@ -21,13 +27,14 @@ template <int DP, int NB>
 struct Few8Shape {
     static constexpr int kM = 8 * NB;                      // rows of a tile
     static constexpr int kKeys = 16;                       // keys a warp takes at a time
-    static constexpr int kWarps = DP <= 128 ? 8 : 4;
+    static constexpr int kWarps = DP > 128 ? 4 : 8;
     static constexpr int kStages = DP <= 64 ? 10 : 5;      // 160 KB of keys and values a SM
+    static constexpr int kHeads = DP <= 128 ? 8 : 1;       // heads of a CTA, at most
     static constexpr int kThreads = kWarps * 32;
-    static constexpr uint32_t kCodes = kKeys * DP * 2;     // K then V
-    static constexpr uint32_t kStage = kCodes + 32 * 4;    // and a word with the scale of each key, each value
-    static constexpr size_t kQBytes = kM * DP * 2;
-    static constexpr uint32_t kMergeRows = (NB == 1 && DP <= 128 ? 32768 : 24576) / (kWarps * DP * 4);
+    static constexpr uint32_t kCodes = 16 * DP * 2;        // sixteen keys, their values,
+    static constexpr uint32_t kStage = kCodes + 32 * 8;    // and of each a word with its scale and the byte's place
+    static constexpr size_t kQBytes = (size_t)kHeads * kM * DP * 2;
+    static constexpr uint32_t kMergeRows = (DP == 128 && NB == 1 ? 32768 : DP <= 128 ? 16384 : 24576) / (kWarps * DP * 4);
     static constexpr size_t kMergeBytes = (size_t)kMergeRows * kWarps * DP * 4;
     static constexpr size_t kSmem = kQBytes + kMergeBytes + (size_t)kWarps * kStages * kStage;
     static constexpr bool kQInRegs = DP * NB <= 256;
@@ -38,17 +45,16 @@ __device__ __forceinline__ uint32_t undefined_codes(uint32_t c) { return ((c & 0
 
 template <typename T, int DP, int NB>
 __global__ __launch_bounds__(Few8Shape<DP, NB>::kThreads, 1)
-void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ CodeArgs cd)
+void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ CodeArgs cd, const uint32_t most_log2)
 {
     using Sh = Few8Shape<DP, NB>;
     using F = __half;
     constexpr int NT = Sh::kThreads, NW = Sh::kWarps, ST = Sh::kStages;
     constexpr int kChunks = DP / 16;           // 16-byte pieces of a row of codes
     constexpr int kQChunks = DP / 8;           // of a row of queries
-    constexpr uint32_t kTile = Sh::kKeys * NW, kNone = 0xFFFFFFFFu;
+    constexpr uint32_t kNone = 0xFFFFFFFFu;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ float sm_m[NW][Sh::kM], sm_l[NW][Sh::kM], sm_q[Sh::kM];
-    __shared__ unsigned char which[NW][ST][32];            // the scale's byte in its word
+    __shared__ float sm_m[NW][Sh::kM], sm_l[NW][Sh::kM], sm_q[Sh::kHeads * Sh::kM];
     const uint32_t tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const uint32_t G = j.group, D = j.head_dim;
 
@@ -56,7 +62,24 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
     const unsigned char *const kbuf = static_cast<const unsigned char *>(j.kv_ptrs[j.layer]);
     const unsigned char *const vbuf = static_cast<const unsigned char *>(j.kv_ptrs[j.n_layers + j.layer]);
     const uint32_t n_items = j.prefix_pass ? j.n_group : j.seqs.n_seq;
-    const Span span = find_span<NT, false>(j, n_items, Sh::kM, kTile, nullptr);
+    // Heads side by side: as many as the host allows while the row tiles under a group of heads are no fewer than
+    // an eighth of the CTAs, so that a cut tile has no more than about eight parts for its last CTA to merge. (What
+    // this launch takes of the batch is known here only. Four short chats, 8 heads: 12 us one by one, 25 side by side.)
+    uint32_t heads_log2 = most_log2;
+    if (most_log2) {
+        uint32_t tiles = 0;
+        for (uint32_t i = tid; i < n_items; i += NT) tiles += item_tiles(j, load_item(j, i), Sh::kM);
+        __shared__ uint32_t all_tiles;
+        if (tid == 0) all_tiles = 0;
+        __syncthreads();
+        if (tiles) atomicAdd(&all_tiles, tiles);
+        __syncthreads();
+        while (heads_log2 && (uint64_t)all_tiles * (j.n_kv_heads >> heads_log2) * 8 < gridDim.x) --heads_log2;
+    }
+    const uint32_t HC = 1u << heads_log2, per_head = NW >> heads_log2, kv_heads = j.n_kv_heads;
+    const uint32_t kTile = Sh::kKeys * per_head;
+    const uint32_t my_head = w / per_head, my_part = w % per_head;         // of the group; of its keys
+    const Span span = find_span<NT, false>(j, n_items, kv_heads >> heads_log2, Sh::kM, kTile, nullptr);
     if ((reinterpret_cast<uintptr_t>(kbuf) | reinterpret_cast<uintptr_t>(vbuf)) & 15u) {
         if (blockIdx.x == 0 && tid == 0) st_flag(j.st, LSMKV_ST_MISALIGNED, 0);
         return;
@@ -67,9 +90,9 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
     float *const merge = reinterpret_cast<float *>(smem + Sh::kQBytes);
     const uint32_t ring_at = (uint32_t)(Sh::kQBytes + Sh::kMergeBytes) + w * (ST * Sh::kStage);
     const uint32_t ring = q_s + ring_at;
-    const uint32_t tok_stride = j.n_kv_heads * D;          // bytes of a token's codes
+    const uint32_t tok_stride = kv_heads * D;          // bytes of a token's codes
     const uint32_t blocks = j.page_tokens >> cd.block_log2;
-    using CutWalk = Walk<Sh::kM, (int)kTile>;
+    using CutWalk = Walk<Sh::kM, 0>;
 
     CutWalk walk;
     walk.start(j, span);
@@ -94,7 +117,7 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
     };
     auto take_load_cut = [&]() {
         const Item &on = ahead.it;
-        load_key = on.kv0 + ahead.p.k0 * kTile + w * Sh::kKeys;
+        load_key = on.kv0 + ahead.p.k0 * kTile + my_part * Sh::kKeys;
         load_end = min(token_limit(on, (ahead.p.rt * Sh::kM + ahead.p.rows - 1) / G), on.kv0 + ahead.p.k1 * kTile);
     };
     auto next_load_cut = [&]() {
@@ -106,56 +129,62 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
     constexpr int kCopies = 16 * kChunks / 32;
     auto swizzle = [](uint32_t r) { return kChunks == 4 ? (r >> 1) & 3 : r & 7; };
     const uint32_t piece_r = lane / kChunks, piece_c = lane % kChunks;
+    // (piece c of row x kRows + piece_r: only the row's bit 2 depends on x, where rows are 128 bytes)
+    const uint32_t piece_at = (piece_r * kChunks + (piece_c ^ swizzle(piece_r))) * 16;
+    const uint32_t row_off = piece_r * tok_stride + piece_c * 16;
+    const bool chunk_there = piece_c * 16 < D;
     auto fetch = [&](uint32_t stage) {
         if (load_key < load_end) {
-            const uint32_t k = load_key + (lane & 15);         // this lane's key, for the scale
+            const uint32_t kv_head = (ahead.p.kv_head << heads_log2) + my_head;
             const uint32_t page = one_page ? __shfl_sync(~0u, load_page, 32 - tiles_known) : load_page;
             const uint32_t left = load_end - load_key;
+            const uint32_t slot0 = slot_of_token(cd, j.page_tokens, load_key);
+            // this lane's key, for the scale (and for its codes, where a page does not hold sixteen)
+            const uint32_t slot = one_page ? slot0 + (lane & 15) : slot_of_token(cd, j.page_tokens, load_key + (lane & 15));
             const bool real = page != kNone && (lane & 15) < left;
-            const uint32_t slot = k % j.page_tokens;
-            const uint64_t slab = real ? page * cd.page_bytes : 0;
-            const uint32_t kv_head = ahead.p.kv_head;
+            const uint64_t slab = page != kNone ? page * cd.page_bytes : 0;
+            const unsigned char *const kp = kbuf + slab, *const vp = vbuf + slab;
             const uint32_t dst = ring + stage * Sh::kStage;
             {
-                // the word that holds the scale: a copy takes four bytes
-                const uint64_t at = slab + cd.code_bytes + kv_head * blocks + (slot >> cd.block_log2);
-                const uint32_t to = dst + Sh::kCodes + lane * 4;
-                if (real) {
-                    which[w][stage][lane] = (unsigned char)(at & 3);
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;"
-                                 :: "r"(to), "l"((lane < 16 ? kbuf : vbuf) + (at & ~3ull)) : "memory");
-                } else {
-                    // a page that is not there reads as zeros of scale one
-                    which[w][stage][lane] = 0;
-                    asm volatile("st.shared.b32 [%0], %1;" :: "r"(to), "r"(0x7F7F7F7F) : "memory");
-                }
+                // the word that holds the scale (a copy takes four bytes), and which byte it is
+                const uint32_t at = cd.code_bytes + kv_head * blocks + (slot >> cd.block_log2), to = dst + Sh::kCodes + lane * 8;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;"
+                             :: "r"(to), "l"((lane < 16 ? kp : vp) + (real ? at & ~3u : 0u)), "r"(real ? 4 : 0) : "memory");
+                asm volatile("st.shared.b32 [%0], %1;" :: "r"(to + 4), "r"((at & 3u) * 8) : "memory");
             }
-            if (one_page) {
-                const bool there = page != kNone && piece_c * 16 < D;
-                const uint64_t off = (page != kNone ? page * cd.page_bytes : 0) +
-                                     (load_key % j.page_tokens + piece_r) * tok_stride + kv_head * D + piece_c * 16;
+            if (one_page && page != kNone && left >= 16) {
+                const uint32_t off = slot0 * tok_stride + kv_head * D + row_off;
+                if (chunk_there) {
+                    const unsigned char *k = kp + off, *v = vp + off;
 #pragma unroll
-                for (int x = 0; x < kCopies; ++x) {
-                    const uint32_t r = x * kRows + piece_r;
-                    const bool in = there && r < left;
-                    const uint64_t e = in ? off + x * kRows * tok_stride : 0;
-                    const uint32_t to = dst + (r * kChunks + (piece_c ^ swizzle(r))) * 16;
-                    cp_async16(to, kbuf + e, in);
-                    cp_async16(to + Sh::kKeys * DP, vbuf + e, in);
+                    for (int x = 0; x < kCopies; ++x) {
+                        const uint32_t to = dst + (piece_at ^ (swizzle(x * kRows) << 4)) + x * kRows * kChunks * 16;
+                        cp_async16(to, k);
+                        cp_async16(to + 16 * DP, v);
+                        k += kRows * tok_stride;
+                        v += kRows * tok_stride;
+                    }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < kCopies; ++x) {
+                        const uint32_t to = dst + (piece_at ^ (swizzle(x * kRows) << 4)) + x * kRows * kChunks * 16;
+                        cp_async16(to, kbuf, false);
+                        cp_async16(to + 16 * DP, vbuf, false);
+                    }
                 }
             } else {
                 const uint64_t mine = slab + slot * tok_stride + kv_head * D;
                 const uint32_t lo = (uint32_t)mine, hi = (uint32_t)(mine >> 32) | (real ? 0u : 0x80000000u);
-#pragma unroll
+#pragma unroll 1
                 for (int x = 0; x < kCopies; ++x) {
                     const uint32_t r = x * kRows + piece_r;
                     const uint32_t h = __shfl_sync(~0u, hi, r);
                     const uint64_t o = ((uint64_t)(h & 0x7FFFFFFFu) << 32) | __shfl_sync(~0u, lo, r);
-                    const bool in = !(h >> 31) && piece_c * 16 < D;
+                    const bool in = !(h >> 31) && chunk_there;
                     const uint64_t e = in ? o + piece_c * 16 : 0;
                     const uint32_t to = dst + (r * kChunks + (piece_c ^ swizzle(r))) * 16;
                     cp_async16(to, kbuf + e, in);
-                    cp_async16(to + Sh::kKeys * DP, vbuf + e, in);
+                    cp_async16(to + 16 * DP, vbuf + e, in);
                 }
             }
             load_key += kTile;
@@ -164,17 +193,20 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    constexpr int kPieces = (Sh::kM * kQChunks + NT - 1) / NT;
+    // Pieces of 16 bytes of the cut's queries, of all its heads; rows beyond the tile are zero.
+    constexpr int kPieces = (Sh::kHeads * Sh::kM * kQChunks + NT - 1) / NT;
+    const uint32_t n_pieces = HC * Sh::kM * kQChunks;
     uint4 q_piece[kPieces];
     auto load_queries = [&]() {
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) {
-            const uint32_t x = tid + y * NT, r = x / kQChunks, c = x % kQChunks;
+            const uint32_t x = tid + y * NT, r = x / kQChunks % Sh::kM, h = x / (kQChunks * Sh::kM), c = x % kQChunks;
             q_piece[y] = make_uint4(0, 0, 0, 0);
-            if (r < p.rows && c * 8 < D) {
+            if (y * NT < n_pieces && h < HC && r < p.rows && c * 8 < D) {
                 const uint32_t R = p.rt * Sh::kM + r;
-                q_piece[y] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(j.q) + (it.row0 + R / G) * j.q_ts +
-                                                              (uint64_t)(p.kv_head * G + R % G) * j.q_hs + c * 8);
+                q_piece[y] = *reinterpret_cast<const uint4 *>(
+                    static_cast<const T *>(j.q) + (it.row0 + R / G) * j.q_ts +
+                    (uint64_t)(((p.kv_head << heads_log2) + h) * G + R % G) * j.q_hs + c * 8);
             }
         }
     };
@@ -183,6 +215,7 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
     auto store_queries = [&]() {
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) {
+            if (y * NT >= n_pieces) break;
             const uint32_t x = tid + y * NT, r = x / kQChunks, c = x % kQChunks;
             uint4 v = q_piece[y];
             float back = 1.f;
@@ -202,7 +235,7 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     (&v.x)[i] = Half2<F>::down(u.x * f, u.y * f);
                 }
             }
-            if (r < Sh::kM) {
+            if (x < n_pieces) {
                 *reinterpret_cast<uint4 *>(smem + (r * kQChunks + (c ^ (r & 7))) * 16) = v;
                 if (c == 0) sm_q[r] = back * j.scale_log2;
             }
@@ -228,11 +261,11 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
         for (int x = 0; x < 2 * NB; ++x) {
             const uint32_t r = (x >> 1) * 8 + 2 * (lane & 3) + (x & 1);
             lim[x >> 1][x & 1] = r < cut.rows ? token_limit(it, (row_base + r) / G) : it.kv0;
-            row_scale[x >> 1][x & 1] = sm_q[r];
+            row_scale[x >> 1][x & 1] = sm_q[my_head * Sh::kM + r];
         }
         const uint32_t lim_first = token_limit(it, row_base / G);              // least of the tile
         const uint32_t key_end = min(token_limit(it, (row_base + cut.rows - 1) / G), it.kv0 + cut.k1 * kTile);
-        const uint32_t key0 = it.kv0 + cut.k0 * kTile + w * Sh::kKeys;
+        const uint32_t key0 = it.kv0 + cut.k0 * kTile + my_part * Sh::kKeys;
 
         // Queries as the right operand. The elements of a piece of 16 are taken in the order in which a lane
         // finds the codes of a key: its elements 4 t .. 4 t + 3 (t = lane % 4) stand for 2 t, 2 t + 1, 2 t + 8, 2 t + 9.
@@ -240,7 +273,7 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
         auto load_q = [&](int x, uint32_t (&f)[NB][2]) {          // elements 16 x ..
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                const uint32_t r = nb * 8 + (lane >> 2), c = 2 * x + ((lane & 3) >> 1);
+                const uint32_t r = my_head * Sh::kM + nb * 8 + (lane >> 2), c = 2 * x + ((lane & 3) >> 1);
                 const uint2 q = *reinterpret_cast<const uint2 *>(smem + (r * kQChunks + (c ^ (r & 7))) * 16 + (lane & 1) * 8);
                 f[nb][0] = q.x;
                 f[nb][1] = q.y;
@@ -268,23 +301,13 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
             stage_load = stage_load + 1 == ST ? 0 : stage_load + 1;
             asm volatile("cp.async.wait_group %0;" :: "n"(ST - 1) : "memory");
             __syncwarp();
-            const uint32_t ks = ring + stage * Sh::kStage;
-            const uint32_t vs = ks + Sh::kKeys * DP;
-            // exponents of this lane's keys, lane / 4 and 8 more
-            float k_scale[2], v_log[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t r = (lane >> 2) + 8 * h;
-                const unsigned char *const words = smem + ring_at + stage * Sh::kStage + Sh::kCodes;
-                k_scale[h] = power_of_two(scale_exponent(words[r * 4 + which[w][stage][r]]));
-                v_log[h] = (float)scale_exponent(words[(r + 16) * 4 + which[w][stage][r + 16]]);
-            }
-
-            // scores of 16 keys (lane/4 and lane/4 + 8) x 8 rows
-            float s[NB][4];
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.f;
+            const uint32_t first = ring + stage * Sh::kStage;
+            // scores of 16 keys (lane/4 and lane/4 + 8) x 8 rows; u: with the logarithm of what multiplies the value
+            float s[NB][4], u[NB][4];
             {
+                const uint32_t ks = first;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.f;
                 const uint32_t kr = lane & 15;
 #pragma unroll
                 for (int x = 0; x < DP / 16; x += 2) {
@@ -303,35 +326,46 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
                         }
                     }
                 }
-            }
-            float u[NB][4];
+                // exponents of this lane's keys: a byte each of their words
+                const uint2 *const words = reinterpret_cast<const uint2 *>(smem + (ks - q_s) + Sh::kCodes);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+                for (int h = 0; h < 2; ++h) {
+                    const uint2 kw = words[(lane >> 2) + 8 * h], vw = words[(lane >> 2) + 8 * h + 16];
+                    const float k_scale = power_of_two(scale_exponent(kw.x >> kw.y & 0xFF));
+                    const float v_log = (float)scale_exponent(vw.x >> vw.y & 0xFF);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[nb][e] = s[nb][e] * row_scale[nb][e & 1] * k_scale[e >> 1];
-                    u[nb][e] = s[nb][e] + v_log[e >> 1];
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int e = 2 * h; e < 2 * h + 2; ++e) {
+                            s[nb][e] = s[nb][e] * row_scale[nb][e & 1] * k_scale;
+                            u[nb][e] = s[nb][e] + v_log;
+                        }
                 }
-            if (key + Sh::kKeys > lim_first) {
+                if (key + 16 > lim_first) {
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
+                    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (key + (lane >> 2) + 8 * (e >> 1) >= lim[nb][e & 1]) s[nb][e] = u[nb][e] = -INFINITY;
+                        for (int e = 0; e < 4; ++e)
+                            if (key + (lane >> 2) + 8 * (e >> 1) >= lim[nb][e & 1]) s[nb][e] = u[nb][e] = -INFINITY;
+                }
             }
             // the maximum moves only when passed by more than 2^8, as in the 16-bit kernel
+            float top[NB][2];
             bool over = false;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) over |= fmaxf(u[nb][x], u[nb][2 + x]) > m[nb][x] + 8.f;
+                for (int x = 0; x < 2; ++x) {
+                    top[nb][x] = fmaxf(u[nb][x], u[nb][2 + x]);
+                    over |= top[nb][x] > m[nb][x] + 8.f;
+                }
             if (__any_sync(~0u, over)) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     float fix[2];
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        float t = fmaxf(u[nb][x], u[nb][2 + x]);
+                        float t = top[nb][x];
                         t = fmaxf(t, __shfl_xor_sync(~0u, t, 4));
                         t = fmaxf(t, __shfl_xor_sync(~0u, t, 8));
                         t = fmaxf(t, __shfl_xor_sync(~0u, t, 16));
@@ -349,76 +383,80 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     }
                 }
             }
-            uint32_t pf[NB][2];
+            {
+                const uint32_t vs = first + 16 * DP;
+                uint32_t pf[NB][2];
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
+                for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float base = m[nb][e & 1] == -INFINITY ? 0.f : m[nb][e & 1];
-                    l[nb][e & 1] += exp2f(s[nb][e] - base);
-                    u[nb][e] = exp2f(u[nb][e] - base);
-                }
-                // the weights are rounded to f16, the codes' type: the tensor cores take both in one
-                pf[nb][0] = transpose8x8(Half2<F>::down(u[nb][0], u[nb][1]));
-                pf[nb][1] = transpose8x8(Half2<F>::down(u[nb][2], u[nb][3]));
-            }
-            // Values as the left operand: a transposed load gives two elements of two keys, whose codes are
-            // sorted by element and converted. Rows of the fragment: elements 2 g and 2 g + 1 of a piece at g and g + 8.
-            const uint32_t vr = lane & 15;
-            auto value_fragments = [&](int x, uint32_t (&a)[2][4]) {      // pieces x and x + 1
-                uint32_t c[4];
-                ldmatrix4t(vs + (vr * kChunks + ((x + (lane >> 4)) ^ swizzle(vr))) * 16, c);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    from_codes4(__byte_perm(c[i], 0, 0x3120), a[i >> 1][2 * (i & 1)], a[i >> 1][2 * (i & 1) + 1]);
-            };
-            // A tile with keys that some rows see and others do not, and a NaN among its values
-            bool apart = false;
-            if (it.tokens > 1 && key + Sh::kKeys > lim_first && it.causal) {
-                uint32_t any = 0;
-#pragma unroll
-                for (uint32_t x = 0; x < Sh::kKeys * kChunks; x += 32) {
-                    const uint4 v = *reinterpret_cast<const uint4 *>(smem + (vs - q_s) + (x + lane) * 16);
-                    any |= undefined_codes(v.x) | undefined_codes(v.y) | undefined_codes(v.z) | undefined_codes(v.w);
-                }
-                apart = __any_sync(~0u, any != 0);
-            }
-            if (!apart) {
-#pragma unroll
-                for (int x = 0; x < DP / 16; x += 2) {
-                    uint32_t a[2][4];
-                    value_fragments(x, a);
-#pragma unroll
-                    for (int y = 0; y < 2; ++y)
-#pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) mma16816<F>(o[x + y][nb], a[y], pf[nb][0], pf[nb][1]);
-                }
-            } else {
-                // token by token, over the keys that it sees
-                const uint32_t t1 = (row_base + cut.rows - 1) / G;
-                for (uint32_t t = row_base / G; t <= t1; ++t) {
-                    const uint32_t lim_t = token_limit(it, t), see = lim_t > key ? lim_t - key : 0;
-                    uint32_t mask[2];                // of this lane's keys 2 (lane % 4), + 1, + 8, + 9
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t k = 8 * h + 2 * (lane & 3);
-                        mask[h] = (k < see ? 0xFFFFu : 0u) | (k + 1 < see ? 0xFFFF0000u : 0u);
+                    for (int e = 0; e < 4; ++e) {
+                        const float base = m[nb][e & 1] == -INFINITY ? 0.f : m[nb][e & 1];
+                        l[nb][e & 1] += exp2f(s[nb][e] - base);
+                        u[nb][e] = exp2f(u[nb][e] - base);
                     }
+                    // the weights are rounded to f16, the codes' type: the tensor cores take both in one
+                    pf[nb][0] = transpose8x8(Half2<F>::down(u[nb][0], u[nb][1]));
+                    pf[nb][1] = transpose8x8(Half2<F>::down(u[nb][2], u[nb][3]));
+                }
+                // Values as the left operand: a transposed load gives two elements of two keys, whose codes are
+                // sorted by element and converted. Rows of the fragment: elements 2 g and 2 g + 1 of a piece at g and g + 8.
+                const uint32_t vr = lane & 15;
+                auto value_fragments = [&](int x, uint32_t (&a)[2][4]) {      // pieces x and x + 1
+                    uint32_t c[4];
+                    ldmatrix4t(vs + (vr * kChunks + ((x + (lane >> 4)) ^ swizzle(vr))) * 16, c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        from_codes4(__byte_perm(c[i], 0, 0x3120), a[i >> 1][2 * (i & 1)], a[i >> 1][2 * (i & 1) + 1]);
+                };
+                // keys that some rows see and others do not, and a NaN among their values
+                bool apart = false;
+                if (it.tokens > 1 && key + 16 > lim_first && it.causal) {
+                    uint32_t any = 0;
+#pragma unroll
+                    for (uint32_t x = 0; x < 16 * kChunks; x += 32) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(smem + (vs - q_s) + (x + lane) * 16);
+                        any |= undefined_codes(v.x) | undefined_codes(v.y) | undefined_codes(v.z) | undefined_codes(v.w);
+                    }
+                    apart = __any_sync(~0u, any != 0);
+                }
+                if (!apart) {
 #pragma unroll
                     for (int x = 0; x < DP / 16; x += 2) {
                         uint32_t a[2][4];
                         value_fragments(x, a);
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
+                        for (int y = 0; y < 2; ++y)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) a[y][e] &= mask[e >> 1];
+                            for (int nb = 0; nb < NB; ++nb) mma16816<F>(o[x + y][nb], a[y], pf[nb][0], pf[nb][1]);
+                    }
+                } else {
+                    // token by token, over the keys that it sees
+                    const uint32_t t1 = (row_base + cut.rows - 1) / G;
+#pragma unroll 1
+                    for (uint32_t t = row_base / G; t <= t1; ++t) {
+                        const uint32_t lim_t = token_limit(it, t), see = lim_t > key ? lim_t - key : 0;
+                        uint32_t mask[2];                // of this lane's keys 2 (lane % 4), + 1, + 8, + 9
 #pragma unroll
-                            for (int nb = 0; nb < NB; ++nb) {
-                                float part[4] = {0.f, 0.f, 0.f, 0.f};
-                                mma16816<F>(part, a[y], pf[nb][0], pf[nb][1]);
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t k = 8 * h + 2 * (lane & 3);
+                            mask[h] = (k < see ? 0xFFFFu : 0u) | (k + 1 < see ? 0xFFFF0000u : 0u);
+                        }
 #pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    if (lim[nb][e & 1] == lim_t) o[x + y][nb][e] += part[e];
+                        for (int x = 0; x < DP / 16; x += 2) {
+                            uint32_t a[2][4];
+                            value_fragments(x, a);
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) a[y][e] &= mask[e >> 1];
+#pragma unroll
+                                for (int nb = 0; nb < NB; ++nb) {
+                                    float part_o[4] = {0.f, 0.f, 0.f, 0.f};
+                                    mma16816<F>(part_o, a[y], pf[nb][0], pf[nb][1]);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        if (lim[nb][e & 1] == lim_t) o[x + y][nb][e] += part_o[e];
+                                }
                             }
                         }
                     }
@@ -444,9 +482,9 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
             }
         }
         const bool whole = cut.k0 == 0 && cut.k1 == cut.units;
-        const uint32_t quads = D / 4;
+        const uint32_t quads = D / 4, part_rows = HC * Sh::kM;       // a part's row: head of the group * kM + row
         float *slot = whole ? nullptr
-                            : part_slot(j, 2ull * blockIdx.x + (cut.k0 == 0 ? 1 : 0), Sh::kM, DP);
+                            : part_slot(j, 2ull * blockIdx.x + (cut.k0 == 0 ? 1 : 0), part_rows, DP);
         for (uint32_t r0 = 0; r0 < cut.rows; r0 += Sh::kMergeRows) {
             const uint32_t r1 = min(r0 + Sh::kMergeRows, cut.rows);
 #pragma unroll
@@ -462,14 +500,19 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
             }
             __syncthreads();
             if (r0 == 0 && more) store_queries();      // all warps are done with this cut's
-            for (uint32_t x = tid; x < (r1 - r0) * quads; x += NT) {
-                const uint32_t r = r0 + x / quads, d = x % quads * 4;
+            const uint32_t per = (r1 - r0) * quads;
+            for (uint32_t x = tid; x < per << heads_log2; x += NT) {
+                const uint32_t h = x / per, y = x - h * per, r = r0 + y / quads, d = y % quads * 4;
+                const uint32_t k0 = h * per_head;                            // the head's warps
                 float top = -INFINITY, sum = 0.f;
 #pragma unroll
-                for (int k = 0; k < NW; ++k) top = fmaxf(top, sm_m[k][r]);
+                for (uint32_t i = 0; i < NW; ++i)
+                    if (i < per_head) top = fmaxf(top, sm_m[k0 + i][r]);
                 float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int k = 0; k < NW; ++k) {
+                for (uint32_t i = 0; i < NW; ++i) {
+                    if (i >= per_head) break;
+                    const uint32_t k = k0 + i;
                     const float f = part_weight(sm_m[k][r], top);
                     const float4 v = *reinterpret_cast<const float4 *>(
                         merge + ((r - r0) * NW + k) * DP + (d ^ ((r & 6) << 3)));
@@ -480,12 +523,13 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     sum += f * sm_l[k][r];
                 }
                 if (whole) {
-                    finish_row4<T>(j, done, cut.kv_head, row_base + r, d, acc, top, sum);
+                    finish_row4<T>(j, done, (cut.kv_head << heads_log2) + h, row_base + r, d, acc, top, sum);
                 } else {
-                    __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)r * DP + d), acc);
+                    const uint32_t at = h * Sh::kM + r;
+                    __stcg(reinterpret_cast<float4 *>(slot + (uint64_t)at * DP + d), acc);
                     if (d == 0) {
-                        __stcg(slot + (uint64_t)Sh::kM * DP + r, top);
-                        __stcg(slot + (uint64_t)Sh::kM * (DP + 1) + r, sum);
+                        __stcg(slot + (uint64_t)part_rows * DP + at, top);
+                        __stcg(slot + (uint64_t)part_rows * (DP + 1) + at, sum);
                     }
                 }
             }
@@ -494,7 +538,14 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
         if (!whole) {
             const uint32_t c0 = (uint32_t)quotient(cut.tile0, span.per),
                            c1 = (uint32_t)quotient(cut.tile0 + cut.units - 1, span.per);
-            if (deliver_part(j, c0, c1)) merge_parts<T, NT>(j, done, cut, c0, c1, Sh::kM, 0, cut.rows);
+            if (deliver_part(j, c0, c1)) {
+                const uint32_t per = cut.rows * quads;
+                for (uint32_t x = tid; x < per << heads_log2; x += NT) {
+                    const uint32_t h = x / per, y = x - h * per, r = y / quads, d = y % quads * 4;
+                    const Quad q = sum_parts(j.parts, c0, c1, part_rows, j.dp, h * Sh::kM + r, d);
+                    finish_row4<T>(j, done, (cut.kv_head << heads_log2) + h, row_base + r, d, q.acc, q.m, q.l);
+                }
+            }
         }
     }
 }

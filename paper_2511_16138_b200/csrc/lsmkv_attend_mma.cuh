@@ -369,7 +369,6 @@ struct CodeMail {
     static constexpr uint32_t kSlots = 8;
     uint64_t cut_told[2];                    // barriers: a cut is there,
     uint64_t ready[kSlots], told[kSlots];    // all loaders' parts of a tile's exponents, the tile's
-    const unsigned char *buffer[2];          // the layer's keys, its values
     uint64_t page0[2];
     uint4 cut[2];                            // first key, end of the keys, key tiles (0: no cut is left), KV head
     uint2 q_rows[2];                         // the queries: first row under the KV head, halves
@@ -406,6 +405,8 @@ __device__ __forceinline__ void load_codes(const AttendJob &j, const CodeArgs &c
     for (uint32_t y = 0; y < 2; ++y)
         at[y] = (c >> 2) * kBlock + row0 * 128 + (((2 * (c & 3)) ^ (row0 + y * kRows & 7)) << 4);
     const uint32_t steps = me * kMine >= kSteps ? 0u : min(kMine, kSteps - me * kMine);
+    const unsigned char *const kbuf = static_cast<const unsigned char *>(j.kv_ptrs[j.layer]);
+    const unsigned char *const vbuf = static_cast<const unsigned char *>(j.kv_ptrs[j.n_layers + j.layer]);
     raw += (me * kMine * 32 + lane) * 16;                // keys; the values' codes 128 rows on
     const uint32_t own = me * kOwn + lane;               // this lane's row: its page, place and scales
     uint32_t half_cnt = 0;                               // half tiles handed over
@@ -421,22 +422,24 @@ __device__ __forceinline__ void load_codes(const AttendJob &j, const CodeArgs &c
             const uint32_t k = key0 + t * Sh::kKeys + own;
             page = kNone;
             if (lane >= kOwn || own >= Sh::kKeys || k >= key_end) return;
-            const uint64_t entry = mail.page0[cut & 1] + k / j.page_tokens;
-            const uint32_t p = j.seqs.page_table[entry];
-            if (p < j.num_pages) page = p;
-            else st_flag(j.st, LSMKV_ST_BAD_PAGE, entry);
+            page = j.seqs.page_table[mail.page0[cut & 1] + page_of_token(cd, j.page_tokens, k)];   // (looked at a tile later)
         };
         // place of the row's codes in units of 16 bytes, and the exponents of its scales
         int k_exp, v_exp;
         auto find_place = [&](uint32_t t) {
             place = kNone;
-            if (page == kNone) return;
-            const uint32_t slot = (key0 + t * Sh::kKeys + own) % j.page_tokens;
+            const uint32_t k = key0 + t * Sh::kKeys + own;
+            if (page >= j.num_pages) {
+                if (lane < kOwn && own < Sh::kKeys && k < key_end)
+                    st_flag(j.st, LSMKV_ST_BAD_PAGE, mail.page0[cut & 1] + page_of_token(cd, j.page_tokens, k));
+                return;
+            }
+            const uint32_t slot = slot_of_token(cd, j.page_tokens, k);
             const uint64_t slab = page * cd.page_bytes;
             place = (uint32_t)((slab + (slot * j.n_kv_heads + kv_head) * j.head_dim) >> 4);
             const uint64_t s = slab + cd.code_bytes + kv_head * (j.page_tokens >> cd.block_log2) + (slot >> cd.block_log2);
-            k_exp = mail.buffer[0][s];
-            v_exp = mail.buffer[1][s];
+            k_exp = kbuf[s];
+            v_exp = vbuf[s];
         };
         // this warp's part of a tile's exponents
         auto tell = [&]() {
@@ -450,10 +453,17 @@ __device__ __forceinline__ void load_codes(const AttendJob &j, const CodeArgs &c
                 mbar_arrive(smem_addr(mail.ready + slot));
             }
         };
+        uint32_t from[kMine];                            // this lane's codes of a step, likewise
+        auto find_codes = [&]() {
+#pragma unroll
+            for (uint32_t i = 0; i < kMine; ++i) {
+                const uint32_t p = __shfl_sync(~0u, place, i * kRows + sub);
+                from[i] = p != kNone && there ? p + c : kNone;
+            }
+        };
         auto load = [&](uint32_t i, uint32_t kv) {
-            const uint32_t p = __shfl_sync(~0u, place, i * kRows + sub);
-            const bool in = p != kNone && there;
-            cp_async16(raw + kv * (128 * DP) + i * 512, reinterpret_cast<const uint4 *>(mail.buffer[kv]) + (in ? p + c : 0), in);
+            const bool in = from[i] != kNone;
+            cp_async16(raw + kv * (128 * DP) + i * 512, reinterpret_cast<const uint4 *>(kv ? vbuf : kbuf) + (in ? from[i] : 0), in);
         };
         auto loaded = [&]() { asm volatile("cp.async.commit_group;" ::: "memory"); };
         // rows of step i times their factor, to the stage at dst
@@ -497,6 +507,7 @@ __device__ __forceinline__ void load_codes(const AttendJob &j, const CodeArgs &c
         };
         find_page(0);
         find_place(0);
+        find_codes();
         load_half(0);
         load_half(1);
         if (me == 0) {
@@ -537,6 +548,7 @@ __device__ __forceinline__ void load_codes(const AttendJob &j, const CodeArgs &c
             if (more) {
                 find_place(t + 1);
                 if (t + 2 < n) find_page(t + 2);
+                find_codes();
             }
 #pragma unroll
             for (uint32_t kv = 0; kv < 2; ++kv) {
@@ -1072,7 +1084,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
 
     const T *const kbuf = static_cast<const T *>(j.kv_ptrs[j.layer]);
     const T *const vbuf = static_cast<const T *>(j.kv_ptrs[j.n_layers + j.layer]);
-    const Span span = find_span<kThreads, true>(j, j.prefix_pass ? j.n_group : j.seqs.n_seq, Sh::kM, Sh::kKeys,
+    const Span span = find_span<kThreads, true>(j, j.prefix_pass ? j.n_group : j.seqs.n_seq, j.n_kv_heads, Sh::kM, Sh::kKeys,
                                                     reinterpret_cast<uint32_t *>(smem_raw));
     // the loads of the waves lay where the copy engine writes queries later; ordered by the barrier below
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1116,8 +1128,6 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 mbar_init(smem_addr(mail.told + x), 1);
                 if (x < 2) mbar_init(smem_addr(mail.cut_told + x), 1);
             }
-        mail.buffer[0] = reinterpret_cast<const unsigned char *>(kbuf);
-        mail.buffer[1] = reinterpret_cast<const unsigned char *>(vbuf);
         mail.q_asked = 0;
         mbar_init(q_empty, 1);
         for (int x = 0; x < 2; ++x) {

@@ -94,8 +94,15 @@ template <typename T, int DP, int NB>
 cudaError_t start_few8(lsmkv_ctx *ctx, cudaStream_t s, bool follows, const AttendJob &job)
 {
     using Sh = Few8Shape<DP, NB>;
+    // Heads that a CTA reads side by side, at most: as many as the KV heads divide into, unless even all items could not
+    // keep the cut tiles' parts few (the kernel looks at what it takes of them).
+    const uint64_t items = job.prefix_pass ? job.n_group : job.seqs.n_new;
+    uint32_t log2 = 0;
+    while ((2 << log2) <= Sh::kHeads && job.n_kv_heads % (2u << log2) == 0 &&
+           items * (job.n_kv_heads >> (log2 + 1)) * 8 >= (uint64_t)ctx->sm_count)
+        ++log2;
     return start(ctx, s, follows, k_attend_few8<T, DP, NB>, (unsigned)ctx->sm_count, Sh::kThreads, Sh::kSmem, job,
-                 ctx->codes);
+                 ctx->codes, log2);
 }
 
 // rows8: no row tile has more than 8 rows.
@@ -324,7 +331,7 @@ size_t place_attend(const lsmkv_ctx *ctx, void *at, uint32_t n_seq, AttendJob *j
     job->cuts = l.take<CutDesc>(sm);
     job->maps = l.take<unsigned char>(sm * 256);
     job->span_begin = l.take<uint64_t>(sm + 1);
-    job->few_parts = l.take<float>(part_bytes(ctx, 16) / 4);
+    job->few_parts = l.take<float>(part_bytes(ctx, ctx->pool8 ? 128 : 16) / 4);      // (8-bit: of up to eight heads)
     job->parts = many_takes(ctx) ? l.take<float>(part_bytes(ctx, 256) / 4) : job->few_parts;
     job->tile_base = l.take<uint32_t>((size_t)n_seq + 1);
     return l.at;
