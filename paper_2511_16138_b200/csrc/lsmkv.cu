@@ -298,18 +298,26 @@ cudaError_t set_copy_smem_limit(int max_smem_optin)
     raise_few(FewShape<128, 2>(), k_attend_few<__half, 128, 2>);
     raise_few(FewShape<256, 1>(), k_attend_few<__half, 256, 1>);
     raise_few(FewShape<256, 2>(), k_attend_few<__half, 256, 2>);
-    raise_few(Few8Shape<64, 1>(), k_attend_few8<__nv_bfloat16, 64, 1>);
-    raise_few(Few8Shape<64, 2>(), k_attend_few8<__nv_bfloat16, 64, 2>);
-    raise_few(Few8Shape<128, 1>(), k_attend_few8<__nv_bfloat16, 128, 1>);
-    raise_few(Few8Shape<128, 2>(), k_attend_few8<__nv_bfloat16, 128, 2>);
-    raise_few(Few8Shape<256, 1>(), k_attend_few8<__nv_bfloat16, 256, 1>);
-    raise_few(Few8Shape<256, 2>(), k_attend_few8<__nv_bfloat16, 256, 2>);
-    raise_few(Few8Shape<64, 1>(), k_attend_few8<__half, 64, 1>);
-    raise_few(Few8Shape<64, 2>(), k_attend_few8<__half, 64, 2>);
-    raise_few(Few8Shape<128, 1>(), k_attend_few8<__half, 128, 1>);
-    raise_few(Few8Shape<128, 2>(), k_attend_few8<__half, 128, 2>);
-    raise_few(Few8Shape<256, 1>(), k_attend_few8<__half, 256, 1>);
-    raise_few(Few8Shape<256, 2>(), k_attend_few8<__half, 256, 2>);
+    raise_few(Few8Shape<64, 1>(), k_attend_few8<__nv_bfloat16, 64, 1, false>);
+    raise_few(Few8Shape<64, 1>(), k_attend_few8<__nv_bfloat16, 64, 1, true>);
+    raise_few(Few8Shape<64, 2>(), k_attend_few8<__nv_bfloat16, 64, 2, false>);
+    raise_few(Few8Shape<64, 2>(), k_attend_few8<__nv_bfloat16, 64, 2, true>);
+    raise_few(Few8Shape<128, 1>(), k_attend_few8<__nv_bfloat16, 128, 1, false>);
+    raise_few(Few8Shape<128, 1>(), k_attend_few8<__nv_bfloat16, 128, 1, true>);
+    raise_few(Few8Shape<128, 2>(), k_attend_few8<__nv_bfloat16, 128, 2, false>);
+    raise_few(Few8Shape<128, 2>(), k_attend_few8<__nv_bfloat16, 128, 2, true>);
+    raise_few(Few8Shape<256, 1>(), k_attend_few8<__nv_bfloat16, 256, 1, false>);
+    raise_few(Few8Shape<256, 2>(), k_attend_few8<__nv_bfloat16, 256, 2, false>);
+    raise_few(Few8Shape<64, 1>(), k_attend_few8<__half, 64, 1, false>);
+    raise_few(Few8Shape<64, 1>(), k_attend_few8<__half, 64, 1, true>);
+    raise_few(Few8Shape<64, 2>(), k_attend_few8<__half, 64, 2, false>);
+    raise_few(Few8Shape<64, 2>(), k_attend_few8<__half, 64, 2, true>);
+    raise_few(Few8Shape<128, 1>(), k_attend_few8<__half, 128, 1, false>);
+    raise_few(Few8Shape<128, 1>(), k_attend_few8<__half, 128, 1, true>);
+    raise_few(Few8Shape<128, 2>(), k_attend_few8<__half, 128, 2, false>);
+    raise_few(Few8Shape<128, 2>(), k_attend_few8<__half, 128, 2, true>);
+    raise_few(Few8Shape<256, 1>(), k_attend_few8<__half, 256, 1, false>);
+    raise_few(Few8Shape<256, 2>(), k_attend_few8<__half, 256, 2, false>);
     for (auto *many : {k_attend_many<__nv_bfloat16, 64, true>, k_attend_many<__half, 64, true>,
                        k_attend_many<__nv_bfloat16, 64, false>, k_attend_many<__half, 64, false>})
         if (e == cudaSuccess)

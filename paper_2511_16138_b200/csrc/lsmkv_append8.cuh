@@ -15,7 +15,7 @@
 // maximum by shuffles, and keeps them in registers until they are written. A CTA takes a block of all heads, keys and
 // values, and looks up place and angles once; other CTAs of the launch take the queries, a few tokens each.
 #pragma once
-#include "lsmkv_append.cuh"
+#include "lsmkv_attend.cuh"
 
 namespace lsmkv {
 
@@ -309,68 +309,95 @@ __device__ __forceinline__ int settle_scale(unsigned char *block, uint64_t row_b
     return e;
 }
 
-// kPasses: passes of a warp over the rows of a block of 16 tokens, at most.
 constexpr int kAppend8Warps = 8;
+
+// Queries of j.tokens tokens from row t0 on, by a CTA: places and angles looked up first, then a head a lane group and
+// pass, the next pass's pieces loaded ahead.
+template <typename T>
+__device__ __forceinline__ void append_queries(const AppendJob &j, uint32_t t0, float (*angles)[256], TokenPlace *places)
+{
+    const unsigned lane = lane_id(), w = threadIdx.x >> 5;
+    const uint32_t half = j.rot_dim / 2, groups = 32u >> j.lane_log2, sub = lane >> j.lane_log2;
+    const LanePieces lp(j, lane);
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    const uint32_t here = min((uint32_t)j.seqs.n_new - t0, j.tokens);
+    const uint32_t n = j.n_q_heads, rows = here * n, stride = kAppend8Warps * groups;
+    const T *const q = static_cast<const T *>(j.q);
+    T *const out = static_cast<T *>(j.q_out);
+    uint32_t r = w * groups + sub, tok = r / n, h = r - tok * n;
+    uint4 a = none, b = none;
+    auto fetch = [&](uint4 &x, uint4 &y) {
+        x = y = none;
+        if (tok >= here) return;
+        const uint4 *src = reinterpret_cast<const uint4 *>(q + (uint64_t)(t0 + tok) * j.q_ts + (uint64_t)h * j.q_hs);
+        if (lp.has_a) x = src[lp.pa];
+        if (lp.has_b) y = src[lp.pb];
+    };
+    fetch(a, b);
+    if (w < here) {
+        const TokenPlace at = place_token(j, t0 + w, lane, false);
+        if (lane == 0) places[w] = at;
+        if (at.state == 2)
+            for (uint32_t e = lane * 4; e < j.rot_dim; e += 128)
+                *reinterpret_cast<float4 *>(&angles[w][e]) =
+                    *reinterpret_cast<const float4 *>(j.table + at.angle * j.rot_dim + e);
+    }
+    __syncthreads();
+    float2 wa[4], wb[4];
+    if (j.q_norm) load_weights<T>(j.q_norm, lp, wa, wb);
+    for (uint32_t r0 = w * groups; r0 < rows; r0 += stride) {
+        const uint32_t on = tok, head = h;
+        h += stride;
+        while (h >= n) {
+            h -= n;
+            ++tok;
+        }
+        uint4 na, nb;
+        fetch(na, nb);
+        const int state = on < here ? places[on].state : 0;
+        LaneRow<T> v;
+        v.take(a, b);
+        if (j.q_norm) v.norm(j, wa, wb);
+        if (half && state == 2) v.turn(lp, angles[on], half);
+        if (state) {
+            // what neither norm nor rotation touched keeps its bits; padding is zero
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (j.q_norm || (uint32_t)e < lp.turned) (&a.x)[e] = Half2<T>::down(v.x[e].x, v.x[e].y);
+                if (j.q_norm || (uint32_t)e + 4 < lp.turned) (&b.x)[e] = Half2<T>::down(v.y[e].x, v.y[e].y);
+            }
+            if (state == 1) a = b = none;
+            uint4 *dst = reinterpret_cast<uint4 *>(out + (uint64_t)(t0 + on) * j.o_ts + (uint64_t)head * j.o_hs);
+            if (lp.has_a) dst[lp.pa] = a;
+            if (lp.has_b) dst[lp.pb] = b;
+        }
+        a = na;
+        b = nb;
+    }
+}
+
+// The queries alone, of large batches: at 80 registers three CTAs a SM, where the blocks of keys and values take
+// 128. (64 turns of 256 to 1024 tokens, 28 + 2 x 4 heads of 128, norms: 260 us in one launch.)
+template <typename T>
+__global__ __launch_bounds__(kAppend8Warps * 32, 3) void k_append8_queries(const __grid_constant__ AppendJob j)
+{
+    __shared__ __align__(16) float angles[kAppend8Warps][256];
+    __shared__ TokenPlace places[kAppend8Warps];
+    follow_launch();             // (the blocks of keys and values may start beside)
+    append_queries<T>(j, blockIdx.x * j.tokens, angles, places);
+}
+
+// Keys and values of block slot g, by a CTA: a warp takes a head's keys or values at a time.
 template <typename T, int kPasses>
-__global__ __launch_bounds__(kAppend8Warps * 32, kPasses <= 4 ? 2 : 1) void k_append8(const __grid_constant__ Append8Job J)
+__device__ __forceinline__ void append_block(const Append8Job &J, uint32_t g, float (*angles)[256], uint32_t &stored)
 {
     const AppendJob &j = J.a;
-    __shared__ __align__(16) float angles[16][256];          // cosines and sines of the tokens
-    __shared__ TokenPlace places[kAppend8Warps];
-    __shared__ uint32_t stored;                              // bit k: token k of the block has its angles
     const unsigned lane = lane_id(), w = threadIdx.x >> 5;
     const uint32_t half = j.rot_dim / 2, D = j.head_dim, H = j.n_kv_heads;
     const uint32_t groups = 32u >> j.lane_log2, sub = lane >> j.lane_log2;
     const LanePieces lp(j, lane);
     const uint4 none = make_uint4(0, 0, 0, 0);
 
-    if (blockIdx.x < J.q_blocks) {
-        // ---- queries of a few tokens
-        const uint32_t t0 = blockIdx.x * j.tokens, here = min((uint32_t)j.seqs.n_new - t0, j.tokens);
-        if (w < here) {
-            const TokenPlace at = place_token(j, t0 + w, lane, false);
-            if (lane == 0) places[w] = at;
-            if (at.state == 2)
-                for (uint32_t e = lane * 4; e < j.rot_dim; e += 128)
-                    *reinterpret_cast<float4 *>(&angles[w][e]) =
-                        *reinterpret_cast<const float4 *>(j.table + at.angle * j.rot_dim + e);
-        }
-        __syncthreads();
-        float2 wa[4], wb[4];
-        if (j.q_norm) load_weights<T>(j.q_norm, lp, wa, wb);
-        const uint32_t n = j.n_q_heads, rows = here * n, stride = kAppend8Warps * groups;
-        const T *const q = static_cast<const T *>(j.q);
-        T *const out = static_cast<T *>(j.q_out);
-        for (uint32_t r0 = w * groups; r0 < rows; r0 += stride) {
-            const uint32_t r = r0 + sub, tok = r / n, h = r - tok * n;
-            const int state = r < rows ? places[tok].state : 0;
-            uint4 a = none, b = none;
-            if (state == 2) {
-                const uint4 *src = reinterpret_cast<const uint4 *>(q + (uint64_t)(t0 + tok) * j.q_ts + h * j.q_hs);
-                if (lp.has_a) a = src[lp.pa];
-                if (lp.has_b) b = src[lp.pb];
-            }
-            LaneRow<T> v;
-            v.take(a, b);
-            if (j.q_norm) v.norm(j, wa, wb);
-            if (half && state == 2) v.turn(lp, angles[tok], half);
-            if (!state) continue;
-            if (state == 2) {
-                // what neither norm nor rotation touched keeps its bits
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (j.q_norm || (uint32_t)e < lp.turned) (&a.x)[e] = Half2<T>::down(v.x[e].x, v.x[e].y);
-                    if (j.q_norm || (uint32_t)e + 4 < lp.turned) (&b.x)[e] = Half2<T>::down(v.y[e].x, v.y[e].y);
-                }
-            }
-            uint4 *dst = reinterpret_cast<uint4 *>(out + (uint64_t)(t0 + tok) * j.o_ts + h * j.o_hs);
-            if (lp.has_a) dst[lp.pa] = a;
-            if (lp.has_b) dst[lp.pb] = b;
-        }
-        return;
-    }
-
-    // ---- keys and values of a block
     unsigned char *const kbuf = static_cast<unsigned char *>(j.kv_ptrs[j.layer]);
     unsigned char *const vbuf = static_cast<unsigned char *>(j.kv_ptrs[j.n_layers + j.layer]);
     if ((reinterpret_cast<uintptr_t>(kbuf) | reinterpret_cast<uintptr_t>(vbuf)) & 15u) {
@@ -378,7 +405,25 @@ __global__ __launch_bounds__(kAppend8Warps * 32, kPasses <= 4 ? 2 : 1) void k_ap
         return;
     }
     BlockPlace p;
-    if (!find_block(J, blockIdx.x - J.q_blocks, &p, threadIdx.x == 0)) return;
+    if (!find_block(J, g, &p, threadIdx.x == 0)) return;
+    // a unit: a head's keys, or its values; the first one's rows are under way while the angles are looked up
+    uint4 a[kPasses], b[kPasses];
+    auto fetch = [&](uint32_t u) {
+        const uint32_t h = u < H ? u : u - H;
+        const T *const src = u < H ? static_cast<const T *>(j.k) + h * j.k_hs : static_cast<const T *>(j.v) + h * j.v_hs;
+        const uint64_t ts = u < H ? j.k_ts : j.v_ts;
+#pragma unroll
+        for (int s = 0; s < kPasses; ++s) {
+            const uint32_t k = s * groups + sub;
+            a[s] = b[s] = none;
+            if (k < p.count) {
+                const uint4 *row = reinterpret_cast<const uint4 *>(src + (p.t0 + k) * ts);
+                if (lp.has_a) a[s] = row[lp.pa];
+                if (lp.has_b) b[s] = row[lp.pb];
+            }
+        }
+    };
+    if (w < 2 * H) fetch(w);
     if (threadIdx.x == 0) stored = 0;
     __syncthreads();
     for (uint32_t k = w; k < p.count; k += kAppend8Warps) {
@@ -397,30 +442,19 @@ __global__ __launch_bounds__(kAppend8Warps * 32, kPasses <= 4 ? 2 : 1) void k_ap
     for (uint32_t u = w; u < 2 * H; u += kAppend8Warps) {
         const bool key = u < H;
         const uint32_t h = key ? u : u - H;
-        const T *const src = key ? static_cast<const T *>(j.k) + h * j.k_hs : static_cast<const T *>(j.v) + h * j.v_hs;
-        const uint64_t ts = key ? j.k_ts : j.v_ts;
-        uint4 a[kPasses], b[kPasses];
-#pragma unroll
-        for (int s = 0; s < kPasses; ++s) {
-            const uint32_t k = s * groups + sub;
-            a[s] = b[s] = none;
-            if (k < 16 && (real >> k & 1)) {
-                const uint4 *row = reinterpret_cast<const uint4 *>(src + (p.t0 + k) * ts);
-                if (lp.has_a) a[s] = row[lp.pa];
-                if (lp.has_b) b[s] = row[lp.pb];
-            }
-        }
+        if (u != w) fetch(u);
         LaneRow<T> v[kPasses];
         float top = 0.f;
         bool undefined = false;
 #pragma unroll
         for (int s = 0; s < kPasses; ++s) {
             if (s * groups >= p.count) break;                // (the same for all lanes)
+            const uint32_t k = s * groups + sub;
+            const bool in = k < 16 && (real >> k & 1);
+            if (!in) a[s] = b[s] = none;                     // (a token left out counts for nothing)
             v[s].take(a[s], b[s]);
             if (key && j.k_norm) v[s].norm(j, wa, wb);
-            // (rows of tokens that are not there are zero)
-            const uint32_t k = s * groups + sub;
-            if (key && half && k < 16 && (real >> k & 1)) v[s].turn(lp, angles[k], half);
+            if (key && half && in) v[s].turn(lp, angles[k], half);
             top = fmaxf(top, v[s].largest(undefined));
         }
 #pragma unroll
@@ -456,6 +490,20 @@ __global__ __launch_bounds__(kAppend8Warps * 32, kPasses <= 4 ? 2 : 1) void k_ap
                     to_codes4(y[0].x, y[0].y, y[1].x, y[1].y), to_codes4(y[2].x, y[2].y, y[3].x, y[3].y));
         }
     }
+}
+
+// kPasses: passes of a warp over the rows of a block of tokens, at most; one is enough for single tokens, whose
+// CTAs then fit four to a SM.
+template <typename T, int kPasses>
+__global__ __launch_bounds__(kAppend8Warps * 32, kPasses == 1 ? 4 : kPasses <= 4 ? 2 : 1)
+void k_append8(const __grid_constant__ Append8Job J)
+{
+    __shared__ __align__(16) float angles[16][256];          // cosines and sines of the tokens
+    __shared__ TokenPlace places[kAppend8Warps];
+    __shared__ uint32_t stored;                              // bit k: token k of the block has its angles
+    if (blockIdx.x < J.q_blocks) append_queries<T>(J.a, blockIdx.x * J.a.tokens, angles, places);
+    else append_block<T, kPasses>(J, blockIdx.x - J.q_blocks, angles, stored);
+    wait_launch();               // what comes behind may count on the queries' launch too
 }
 
 // Element form, for rotations whose halves are not whole 16-byte pieces: a warp takes a block of a head,

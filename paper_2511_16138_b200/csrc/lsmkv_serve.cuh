@@ -101,8 +101,8 @@ cudaError_t start_few8(lsmkv_ctx *ctx, cudaStream_t s, bool follows, const Atten
     while ((2 << log2) <= Sh::kHeads && job.n_kv_heads % (2u << log2) == 0 &&
            items * (job.n_kv_heads >> (log2 + 1)) * 8 >= (uint64_t)ctx->sm_count)
         ++log2;
-    return start(ctx, s, follows, k_attend_few8<T, DP, NB>, (unsigned)ctx->sm_count, Sh::kThreads, Sh::kSmem, job,
-                 ctx->codes, log2);
+    return start(ctx, s, follows, log2 ? k_attend_few8<T, DP, NB, (DP <= 128)> : k_attend_few8<T, DP, NB, false>,
+                 (unsigned)ctx->sm_count, Sh::kThreads, Sh::kSmem, job, ctx->codes, log2);
 }
 
 // rows8: no row tile has more than 8 rows.
@@ -454,7 +454,7 @@ int attend(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype, const l
     return bf ? launch_own<__nv_bfloat16>(ctx, s, job) : launch_own<__half>(ctx, s, job);
 }
 
-// Append to an 8-bit pool: one launch, CTAs for the queries and CTAs for the blocks.
+// Append to an 8-bit pool: CTAs for the queries and CTAs for the blocks, in one launch or, large batches, one each.
 template <typename T>
 int launch_append8(lsmkv_ctx *ctx, cudaStream_t s, const AppendJob &job, bool vec)
 {
@@ -470,19 +470,20 @@ int launch_append8(lsmkv_ctx *ctx, cudaStream_t s, const AppendJob &job, bool ve
     // queries: as in the 16-bit append, as many tokens a CTA as one round of CTAs, four a SM, leaves
     const uint64_t round = (uint64_t)ctx->sm_count * 4;
     J.a.tokens = (uint32_t)std::min<uint64_t>(kAppend8Warps, (n + round - 1) / round);
-    const uint64_t q = job.n_q_heads == 0 ? 0 : vec ? (n + J.a.tokens - 1) / J.a.tokens : (n * job.n_q_heads + 3) / 4;
+    uint64_t q = job.n_q_heads == 0 ? 0 : vec ? (n + J.a.tokens - 1) / J.a.tokens : (n * job.n_q_heads + 3) / 4;
     if (q + slots > 0x7FFFFFFFull) return LSMKV_EINVAL;
-    J.q_blocks = (uint32_t)q;
     J.n_slots = (uint32_t)slots;
-    const unsigned grid = (unsigned)(q + slots);
-    if (!vec)
-        k_append8_elements<T><<<grid, 128, 0, s>>>(J);
-    else if (job.head_dim <= 128)
-        k_append8<T, 4><<<grid, kAppend8Warps * 32, 0, s>>>(J);
-    else
-        k_append8<T, 8><<<grid, kAppend8Warps * 32, 0, s>>>(J);
-    ++ctx->launches;
-    CU(ctx, cudaGetLastError());
+    // rows of a block's new tokens that a warp takes in one pass
+    const bool one_pass = std::min<uint64_t>(B, job.seqs.max_new) <= 32u >> job.lane_log2;
+    bool follows = false;
+    if (vec && !one_pass && q > 2 * (uint64_t)ctx->sm_count) {
+        CU(ctx, start(ctx, s, false, k_append8_queries<T>, (unsigned)q, kAppend8Warps * 32, 0, J.a));
+        q = 0;
+        follows = true;
+    }
+    J.q_blocks = (uint32_t)q;
+    auto kern = !vec ? k_append8_elements<T> : one_pass ? k_append8<T, 1> : job.head_dim <= 128 ? k_append8<T, 4> : k_append8<T, 8>;
+    CU(ctx, start(ctx, s, follows, kern, (unsigned)(q + slots), vec ? kAppend8Warps * 32 : 128, 0, J));
     return LSMKV_OK;
 }
 
