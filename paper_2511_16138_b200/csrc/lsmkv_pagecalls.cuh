@@ -83,6 +83,7 @@ extern "C" int lsmkv_fork_batch(lsmkv_ctx *ctx, void *stream, const lsmkv_tables
     if (!ctx || !parents || !children) return LSMKV_EINVAL;
     if (children->n_seq == 0) return LSMKV_OK;
     if (!tables_ok(parents) || !tables_ok(children) || !parent || !refs || !pool_ok(pool)) return LSMKV_EINVAL;
+    if (children->n_seq > 0x7FFFFFFFu) return LSMKV_EINVAL;
     DeviceGuard guard(ctx->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const size_t n = children->n_seq;

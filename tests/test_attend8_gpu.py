@@ -78,6 +78,16 @@ CASES = [
     (torch.bfloat16, 128, 16, 16, 4, 1, [1], [40000]),
     (torch.float16, 128, 16, 16, 8, 1, [40], [20000]),
     (torch.bfloat16, 128, 16, 16, 8, 2, [1, 33, 70, 2, 150, 0, 4, 5] * 40, [300, 0, 90, 1000, 40, 7, 16, 31] * 40),
+    # heads side by side, eight, four and two at a time; tiles cut by the spans' ends
+    (torch.bfloat16, 128, 16, 16, 32, 8, [1] * 60, [1000 + 37 * i for i in range(60)]),
+    (torch.float16, 96, 16, 4, 16, 8, [1, 2, 8, 0, 3] * 20, [5, 700, 64, 9, 2000] * 20),
+    (torch.bfloat16, 64, 32, 8, 36, 12, [1, 1, 5] * 30, [0, 1500, 33] * 30),
+    (torch.float16, 128, 8, 8, 18, 6, [1] * 70, [31 * i for i in range(70)]),
+    (torch.bfloat16, 128, 16, 16, 56, 8, [1, 2] * 30, [400, 3000] * 30),
+    (torch.bfloat16, 32, 16, 1, 24, 8, [1] * 90, [17 * i for i in range(90)]),
+    # one long sequence among many that another kernel takes
+    (torch.bfloat16, 128, 16, 16, 32, 8, [1] + [40] * 30, [9000] + [10 * i for i in range(30)]),
+    (torch.float16, 48, 16, 8, 12, 4, [20, 1, 300], [77, 800, 0]),
 ]
 
 
