@@ -89,7 +89,8 @@ extern "C" {
 #define LSMKV_CODEC_IDENTITY 0u    /* blobs are bit copies of the page slabs */
 #define LSMKV_CODEC_XP12 1u        /* lossless exponent packing of 16-bit float slabs (see below) */
 #define LSMKV_POOL_8BIT 2u         /* set in: */
-#define LSMKV_POOL_E4M3(block_tokens) (LSMKV_POOL_8BIT | ((uint32_t)(block_tokens) << 8)) /* 8-bit pool */
+/* 8-bit pool, a scale for each head and block of so many tokens */
+#define LSMKV_POOL_E4M3(block_tokens) (LSMKV_POOL_8BIT | ((uint32_t)(block_tokens) << 8))
 
 typedef struct lsmkv_ctx lsmkv_ctx;
 
@@ -560,13 +561,14 @@ typedef struct {
  *             n_q_heads rows, both NULL (and n_q_heads 0) to append only
  * Computed in 32 bits and rounded once. V rows, and K rows without norm and rotation, are bit
  * copies. Slots must be distinct within the call.
- * 8-bit pools (dtype is that of q, k, v and the norms): K and V rows become codes. The exponent of a block's scale
- * is the least e in -100..100 with |x| <= 448 * 2^e for all finite elements x of the block's new
- * tokens; where the block holds earlier tokens of the sequence it is not less than it was, and if it grows
- * their codes are rounded anew (code * 2^(old - new), to nearest even). Codes are x * 2^-e to nearest even;
- * what is beyond 448 * 2^100 saturates; infinities and NaN become NaN codes. Scales of blocks that a call begins
- * need no initial value. Blocks of B tokens, not only slots, must be distinct within the call, and no other
- * sequence may list a block's page that grows (see lsmkv_fork_batch).
+ * 8-bit pools (dtype is that of q, k, v and the norms): K and V rows become codes. The exponent of
+ * a block's scale is the least e in -100..100 with |x| <= 448 * 2^e for all finite elements x of
+ * the block's new tokens; where the block holds earlier tokens of the sequence it is not less than
+ * it was, and if it grows their codes are rounded anew (code * 2^(old - new), to nearest even).
+ * Codes are x * 2^-e to nearest even; what is beyond 448 * 2^100 saturates; infinities and NaN
+ * become NaN codes. Scales of blocks that a call begins need no initial value. Blocks of B tokens,
+ * not only slots, must be distinct within the call, and a page that a sequence appends to must not
+ * be another sequence's too (lsmkv_fork_batch sees to that).
  */
 int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dtype,
                        const lsmkv_seqs_t *seqs, const lsmkv_rows_t *k, const lsmkv_rows_t *v,
@@ -589,8 +591,11 @@ int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dt
  * first of a size comes before any stream capture. Scratch that a larger call replaces is kept until
  * lsmkv_destroy() (all of it no larger than the present one), so graphs captured before stay valid.
  * A wait that runs out sets LSMKV_ST_WAIT_EXPIRED; the results of that call are then unspecified.
- * 8-bit pools: a key or value is code * 2^exponent, exactly; scale and exponents enter scores and weights in
- * 32 bits. `dtype` is that of q and out. Limit: |v| below 2^100 or so, as an append leaves them.
+ * 8-bit pools: a key or value is code * 2^exponent, and the scales enter scores and weights in 32
+ * bits; `dtype` is that of q and out, and the weights are rounded to 11 bits, whichever it is. (In
+ * the kernel for many rows a code that lies more than 2^15 below the largest scale among 128 keys
+ * may lose bits: under 2^-32 of the largest element.) Buffers of 64 GB or more go by the kernel for
+ * few rows whatever their rows.
  * Infinities and NaN among the keys and values reach the rows that see them, and no others. (Where
  * a value is undefined that some rows of a tile of 256 see and others do not, those others are
  * computed twice.)
@@ -624,16 +629,19 @@ int lsmkv_attend_shared_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint
                               float *lse_out);
 
 /*
- * Pages of a pool and who uses them. refs [dev] u32[num_pages], the caller's: refs[p] = number of page-table
- * entries, over all sequences, that name page p; 0 = free. Counters stay below 2^31. These calls work on whole
- * pages of all layers, 8-bit or not, and cost a few microseconds beside the copies they make. Calls on the
- * same counters, tables or pool must be ordered by the caller; fork and compaction share scratch
- * of the context (first call of a size before any stream capture, as for an attend).
+ * Pages of a pool and who uses them. refs [dev] u32[num_pages], the caller's: refs[p] = number of
+ * page-table entries, over all sequences, that name page p; 0 = free. Counters stay below 2^31.
+ * num_pages below 2^32 - 1. These calls work on whole pages of all layers, 8-bit or not, and cost a
+ * few microseconds beside the copies they make (fork and compaction look through the counters with
+ * one SM: under half a millisecond for a million pages). Calls on the same counters, tables or pool must be ordered by
+ * the caller; fork and compaction share scratch of the context (the first call of a size comes before
+ * any stream capture; scratch that a larger call replaces is kept until lsmkv_destroy()). A wait that
+ * runs out sets LSMKV_ST_WAIT_EXPIRED; the copies of that call are then unspecified.
  *
  * Tables: sequence i has kv_len[i] tokens (below 2^31) and entries page_off[i] .. page_off[i+1] of
- * page_table, the first ceil(kv_len[i] / page_tokens) of them in use. One that breaks these rules, or whose
- * entries lie beyond n_entries, sets LSMKV_ST_BAD_COUNT (item = sequence) and is left out. A page
- * id >= num_pages sets LSMKV_ST_BAD_PAGE (item = entry).
+ * page_table, the first ceil(kv_len[i] / page_tokens) of them in use. One that breaks these rules,
+ * or whose entries lie beyond n_entries, sets LSMKV_ST_BAD_COUNT (item = sequence) and is left out.
+ * A page id >= num_pages sets LSMKV_ST_BAD_PAGE (item = entry).
  */
 typedef struct {
     uint64_t n_entries;
@@ -649,28 +657,31 @@ int lsmkv_release_batch(lsmkv_ctx *ctx, void *stream, const lsmkv_tables_t *tabl
                         uint64_t num_pages);
 
 /*
- * Fork: child c becomes a copy of sequence parent[c] of `parents`. Its table gets the parent's entries
- * in use (entries behind them stay as they are), children->kv_len[c] the parent's length. Pages whose tokens are all
- * filled are shared and counted up; when the parent's length ends inside a page the child gets a free page of its own,
- * the lowest free ones in the order of the children, counter 1, into which the filled tokens' rows are
- * copied in every layer (rounded up to 16 bytes; in an 8-bit pool with the page's scales), so that parent
- * and children may append independently. The parent keeps its pages.
- *   parent   [dev] u32[children->n_seq]
- * A child whose parent does not exist or breaks the rules, or whose table is shorter than the parent's entries in
- * use, sets LSMKV_ST_BAD_COUNT (item = child) and is left out. When no free page is left LSMKV_ST_NO_PAGE is set (item
- * = child) and the entry is 0xFFFFFFFF; everything else of the child is done. An entry of the parent
- * that names no page is passed on as it is. Children's tables must not overlap the parents' or each other.
+ * Fork: child c becomes a copy of sequence parent[c] of `parents`. Its table gets the parent's
+ * entries in use (entries behind them stay as they are), children->kv_len[c] the parent's length.
+ * Pages whose tokens are all filled are shared and counted up; when the parent's length ends inside
+ * a page the child gets a free page of its own, the lowest free ones in the order of the children,
+ * counter 1, into which the filled tokens' rows are copied in every layer (rounded up to 16 bytes;
+ * in an 8-bit pool with the page's scales), so that parent and children may append independently.
+ * The parent keeps its pages.
+ *   parent   [dev] u32[children->n_seq]; n_seq below 2^31
+ * A child whose parent does not exist or breaks the rules, or whose table is shorter than the
+ * parent's entries in use, sets LSMKV_ST_BAD_COUNT (item = child) and is left out. When no free
+ * page is left LSMKV_ST_NO_PAGE is set (item = child) and the entry is 0xFFFFFFFF; everything else
+ * of the child is done. An entry of the parent that names no page is passed on as it is. Children's
+ * tables must not overlap the parents' or each other.
  */
 int lsmkv_fork_batch(lsmkv_ctx *ctx, void *stream, const lsmkv_tables_t *parents, const uint32_t *parent,
                      const lsmkv_tables_t *children, uint32_t *refs, const lsmkv_pool_t *pool);
 
 /*
- * Compaction: with n pages in use (refs[p] > 0), the k-th used page behind the first n, in ascending order, moves to
- * the k-th free one among the first n, in every layer, and all used pages are then pages 0 .. n-1.
- * page_table [dev] holds all entries that name pages of the pool, of all sequences, in any order: entries
- * of moved pages are rewritten, others pass unchanged. refs_out, page_table_out may be refs, page_table themselves or must not
- * overlap them. n_live_out [dev] receives n (may be NULL). Contents of pages n .. num_pages-1 are
- * unspecified afterwards. LSMKV_ST_BAD_PAGE: item = entry.
+ * Compaction: with n pages in use (refs[p] > 0), the k-th used page behind the first n, in ascending
+ * order, moves to the k-th free one among the first n, in every layer, and all used pages are then
+ * pages 0 .. n-1. page_table [dev] holds all entries that name pages of the pool, of all sequences,
+ * in any order: entries of moved pages are rewritten, others pass unchanged. refs_out and
+ * page_table_out may be refs and page_table themselves, or must not overlap them. n_live_out [dev]
+ * receives n (may be NULL). Contents of pages n .. num_pages-1 are unspecified afterwards.
+ * LSMKV_ST_BAD_PAGE: item = entry.
  */
 int lsmkv_compact_pages(lsmkv_ctx *ctx, void *stream, const uint32_t *refs, uint32_t *refs_out,
                         const uint32_t *page_table, uint32_t *page_table_out, uint64_t n_entries,
@@ -690,7 +701,8 @@ int lsmkv_last_status(lsmkv_ctx *ctx, void *stream, lsmkv_status_t *out);
  * by CUDA events on the launching stream (no synchronisation). lsmkv_profile_read() waits for
  * the recorded events, returns the summed device time and launch count per kernel class since
  * the previous read, and clears them. Class LSMKV_K_PLAN covers the two small kernels that
- * turn hit lengths into the list of chunks to copy.
+ * turn hit lengths into the list of chunks to copy, and releases of pages; forks, compactions and
+ * copies of pages are of class LSMKV_K_PACK.
  * Independently of that switch the launches of every call of a context sit inside an NVTX
  * range named after their class ("lsmkv:keys", "lsmkv:pack", "lsmkv:probe", "lsmkv:plan",
  * "lsmkv:unpack", "lsmkv:flush", "lsmkv:merge", "lsmkv:attend"): a timeline tool that collects NVTX shows

@@ -28,7 +28,8 @@
 // its weights one exponent, known before the exponentials: nothing is added to the softmax warps' chain but a
 // few operations a tile. (f16 holds e4m3 codes exactly down to 2^-15 of the tile's largest scale; what is lost below is under 2^-32 of the
 // largest element.) The sums are relative to M = max (row's largest score + B), the sum of weights is taken
-// back by 2^-B tile by tile.
+// back by 2^-B tile by tile. Measured: the two requests above 2.3 to 2.4 ms (1.99 without the conversion): the loaders
+// take 4.9k cycles a tile, 2.7k of them in conversions and copies.
 #pragma once
 #include <cuda.h>
 
@@ -843,7 +844,7 @@ __device__ __forceinline__ void redo_rows8(const AttendJob &j, const CodeArgs &c
         lim[h] = in ? token_limit(it, R / G) : it.kv0;
         anew[h] = in && lim[h] < behind;
         const uint64_t at = query_row(j, it, kv_head, R);
-        row_scale[h] = j.scale_log2 * (j.q_back ? j.q_back[at] : 1.f);
+        row_scale[h] = j.scale_log2 * (j.q_back ? __ldcg(j.q_back + at) : 1.f);
         const F *row = static_cast<const F *>(j.q) + query_offset(j, it, kv_head, R);
 #pragma unroll
         for (int x = 0; x < DP / 8; ++x)
@@ -1194,7 +1195,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
             float m = -INFINITY, l = 0.f;
             bool alive = true;
             float c_row = c_all;
-            if (kCodes && j.q_back) c_row *= j.q_back[query_row(j, cw.it, cw.p.kv_head, real ? row_base + row : row_base)];
+            if (kCodes && j.q_back) c_row *= __ldcg(j.q_back + query_row(j, cw.it, cw.p.kv_head, real ? row_base + row : row_base));
             for (uint32_t t = 0; t < n; ++t) {
                 if (!(alive = wait_warp(s_full(x), s_cnt & 1))) break;
                 ++s_cnt;

@@ -170,9 +170,7 @@ int launch_many8(lsmkv_ctx *ctx, cudaStream_t s, bool follows, const AttendJob &
     job.q_gathered = ctx->many_q != nullptr;
     if (job.q_gathered) {
         job.q = ctx->many_q;
-        job.q_back = ctx->many_back;
-        // (what lies ahead of a kernel that runs beside this one must be over when this one starts)
-        job.beside = 0;
+        job.q_back = ctx->many_back;     // (the gather is over when the launch that this one may run beside starts)
     }
     if (job.head_dim <= 64)
         CU(ctx, start(ctx, s, follows, k_attend_many<T, 64, false, true>, sm, ManyShape<64>::kThreads8,
@@ -228,7 +226,7 @@ bool many_takes(const lsmkv_ctx *ctx) { return ctx->geom.head_dim <= 128 && !ctx
 
 // Over an 8-bit pool the many-row kernel wants f16 queries in boxes of 128 rows under a KV head: they are brought to
 // that by a launch ahead of the others, unless they are f16 already and the heads of a KV head divide 128.
-// (8k tokens of 32 heads: 22 us of 520.)
+// (8k tokens of 32 heads of 128: 32 us of 671, with cold caches.)
 template <typename T>
 int gather_queries(lsmkv_ctx *ctx, cudaStream_t s, const AttendJob &job)
 {
