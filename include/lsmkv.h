@@ -99,7 +99,8 @@ typedef struct { uint32_t file_id, reserved; uint64_t offset; } lsmkv_val_t; /* 
 
 typedef struct {
     uint32_t n_layers, n_kv_heads, head_dim, elem_bytes;
-    uint32_t page_tokens, chunk_tokens, ns, flags; /* chunk_tokens = m * page_tokens, m >= 1; flags = LSMKV_CODEC_* */
+    uint32_t page_tokens, chunk_tokens, ns, flags; /* chunk_tokens = m * page_tokens, m >= 1; flags = LSMKV_CODEC_*
+                                                      or LSMKV_POOL_E4M3(B) */
 } lsmkv_geom_t;
 
 /* One immutable sorted run of the index: keys ascending and unique, vals[i] belongs to keys[i].

@@ -882,7 +882,8 @@ class Context:
     def append_batch(self, layer, seqs, k, v, pool, rope=None, q=None, q_out=None, q_norm=None,
                      k_norm=None, eps=1e-6, stream=None):
         """k, v [n_new, n_kv_heads, head_dim] into the pool; q [n_new, n_q_heads, head_dim] ->
-        q_out (q itself when None). Strided views are fine."""
+        q_out (q itself when None). Strided views are fine. In an 8-bit pool (Geom.flags =
+        pool_e4m3(...)) k and v become codes with a scale for each block of tokens and head."""
         g = self.geom
         dim, n = g.head_dim, seqs.n_new
         kk, vv = _rows("k", k, n, g.n_kv_heads, dim), _rows("v", v, n, g.n_kv_heads, dim)
@@ -924,7 +925,8 @@ class Context:
                            _ptr(kv_ptrs) or 0, num_pages))
 
     def attend_batch(self, layer, seqs, q, out, pool, scale, lse=None, stream=None):
-        """q, out [n_new, n_q_heads, head_dim]; lse float32 [n_new, n_q_heads] or None."""
+        """q, out [n_new, n_q_heads, head_dim], 16-bit whether the pool is or not; lse float32
+        [n_new, n_q_heads] or None."""
         heads, args = self._attend_args(seqs, q, out, pool, lse)
         at = _address(args)
         lsmkv_attend_batch(self.handle, stream, layer, _dtype(q, out), seqs.ref, heads, at,
