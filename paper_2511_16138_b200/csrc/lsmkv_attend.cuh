@@ -62,12 +62,12 @@ struct AttendJob {
     uint32_t beside;             // the launch before has nothing for this one: wait for it at the end
     uint32_t wide_boxes;         // a box has all elements of a head, not 64
     uint32_t q_boxes;            // the queries come by boxes too
-    uint32_t pair_bytes;         // of an element of a key and its value: 4, or 2 in an 8-bit pool
-    uint32_t q_gathered;         // 8-bit pools, many rows: the queries are f16 rows [kv_head][token, head of the group]
-    const float *q_back;         // their rows' factors (null: 1)
     long long wait_cycles;
     uint64_t test_drop;          // test hook: ~0 = off
     DevStatus *st;
+    uint32_t pair_bytes;         // of an element of a key and its value: 4, or 2 in an 8-bit pool
+    uint32_t q_gathered;         // 8-bit pools, many rows: the queries are f16 rows [kv_head][token, head of the group]
+    const float *q_back;         // their rows' factors (null: 1)
 };
 
 // An item: a sequence, or in the prefix pass a group.

@@ -1129,7 +1129,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                 mbar_init(smem_addr(mail.told + x), 1);
                 if (x < 2) mbar_init(smem_addr(mail.cut_told + x), 1);
             }
-        mail.q_asked = 0;
+        if (kCodes) mail.q_asked = 0;
         mbar_init(q_empty, 1);
         for (int x = 0; x < 2; ++x) {
             mbar_init(s_full(x), 1);
@@ -1725,33 +1725,42 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         };
         CutWalk cw;
         cw.start(j, span);
-        // 8-bit pools: the loaders learn of a cut while the one before is issued. (Its slot is free then: the
-        // tiles of the cut that lay there have all been handed over.)
-        uint32_t cut = 0;
-        auto tell_cut = [&](bool there) {
-            if (lane == 0) {
-                const uint32_t row_base = cw.p.rt * Sh::kM, n = cw.p.k1 - cw.p.k0;
-                const uint32_t key0 = cw.it.kv0 + cw.p.k0 * Sh::kKeys;
-                mail.page0[cut & 1] = cw.it.page0;
-                mail.cut[cut & 1] = make_uint4(
-                    key0, min(token_limit(cw.it, (row_base + cw.p.rows - 1) / G), key0 + n * Sh::kKeys), there ? n : 0u, cw.p.kv_head);
-                mail.q_rows[cut & 1] = make_uint2((uint32_t)(cw.it.row0 * G) + row_base, cw.p.rows > 128 ? 2 : 1);
-                mbar_arrive(smem_addr(mail.cut_told + (cut & 1)));
+        if constexpr (!kCodes) {
+            while (cw.next(j, span)) {
+                bool ok = true;
+                if (leader)
+                    ok = run_cut(cw.p.k1 - cw.p.k0, half_tiles(j, cw.it, cw.p, 0, Sh::kM, Sh::kKeys),
+                                 half_tiles(j, cw.it, cw.p, 1, Sh::kM, Sh::kKeys), shares_rows(cw.p));
+                if (!__all_sync(~0u, ok)) break;
             }
-            ++cut;
-            __syncwarp();
-        };
-        bool more = cw.next(j, span);
-        if (kCodes) tell_cut(more);
-        while (more) {
-            const uint32_t n = cw.p.k1 - cw.p.k0, n0 = half_tiles(j, cw.it, cw.p, 0, Sh::kM, Sh::kKeys),
-                           n1 = half_tiles(j, cw.it, cw.p, 1, Sh::kM, Sh::kKeys);
-            const bool both = shares_rows(cw.p);
-            if (kCodes) tell_cut(more = cw.next(j, span));
-            bool ok = true;
-            if (leader) ok = run_cut(n, n0, n1, both);
-            if (!__all_sync(~0u, ok)) break;
-            if (!kCodes) more = cw.next(j, span);
+        } else {
+            // The loaders learn of a cut while the one before is issued. (Its slot is free then: the tiles of the cut
+            // that lay there have all been handed over.)
+            uint32_t cut = 0;
+            auto tell_cut = [&](bool there) {
+                if (lane == 0) {
+                    const uint32_t row_base = cw.p.rt * Sh::kM, n = cw.p.k1 - cw.p.k0;
+                    const uint32_t key0 = cw.it.kv0 + cw.p.k0 * Sh::kKeys;
+                    const uint32_t last = token_limit(cw.it, (row_base + cw.p.rows - 1) / G);
+                    mail.page0[cut & 1] = cw.it.page0;
+                    mail.cut[cut & 1] = make_uint4(key0, min(last, key0 + n * Sh::kKeys), there ? n : 0u, cw.p.kv_head);
+                    mail.q_rows[cut & 1] = make_uint2((uint32_t)(cw.it.row0 * G) + row_base, cw.p.rows > 128 ? 2 : 1);
+                    mbar_arrive(smem_addr(mail.cut_told + (cut & 1)));
+                }
+                ++cut;
+                __syncwarp();
+            };
+            bool more = cw.next(j, span);
+            tell_cut(more);
+            while (more) {
+                const uint32_t n = cw.p.k1 - cw.p.k0, n0 = half_tiles(j, cw.it, cw.p, 0, Sh::kM, Sh::kKeys),
+                               n1 = half_tiles(j, cw.it, cw.p, 1, Sh::kM, Sh::kKeys);
+                const bool both = shares_rows(cw.p);
+                tell_cut(more = cw.next(j, span));
+                bool ok = true;
+                if (leader) ok = run_cut(n, n0, n1, both);
+                if (!__all_sync(~0u, ok)) break;
+            }
         }
         // products still under way read shared memory and write TMEM: let them end
         if (leader) {
