@@ -103,7 +103,6 @@ struct Append8Job {
     CodeArgs c;
     uint32_t q_blocks;       // CTAs that take queries
     uint32_t per_seq;        // block slots a sequence, 0: as many as its length asks for (see find_block)
-    uint32_t n_slots;
 };
 
 // The block that a CTA takes: `count` new tokens from row t0 on, in slots [slot, slot + count) of a page, of

@@ -470,7 +470,6 @@ int launch_append8(lsmkv_ctx *ctx, cudaStream_t s, const AppendJob &job, bool ve
     J.a.tokens = (uint32_t)std::min<uint64_t>(kAppend8Warps, (n + round - 1) / round);
     uint64_t q = job.n_q_heads == 0 ? 0 : vec ? (n + J.a.tokens - 1) / J.a.tokens : (n * job.n_q_heads + 3) / 4;
     if (q + slots > 0x7FFFFFFFull) return LSMKV_EINVAL;
-    J.n_slots = (uint32_t)slots;
     // rows of a block's new tokens that a warp takes in one pass
     const bool one_pass = std::min<uint64_t>(B, job.seqs.max_new) <= 32u >> job.lane_log2;
     bool follows = false;
