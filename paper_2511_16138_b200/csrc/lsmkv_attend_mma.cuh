@@ -1172,7 +1172,10 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         const uint32_t x = w >> 2, row = tid & 127;
         const uint32_t lane_base = (w & 3) << 21;            // lanes 32 (w % 4) ..
         const uint32_t s_t = tmem + lane_base + x * 128, o_t = tmem + lane_base + 256 + x * 128;
-        const float c_all = fmaxf(fabsf(j.scale_log2), 1e-37f);  // a negative scale negates the products
+        // A negative scale negates the products. The factor of the scores stays above zero and finite, whatever the
+        // scale, a row's and a tile's factors: a masked score of -inf stays one, and a row of zeros counts its keys.
+        constexpr float kLeast = 1e-37f;
+        const float c_all = kCodes ? fabsf(j.scale_log2) : fmaxf(fabsf(j.scale_log2), kLeast);
         uint32_t tiles_before = 0;   // key tiles of the cuts before
         if ((D + 15) / 16 * 16 < DP) {
             // columns of the sums that no product writes: they are read with the others, and an earlier kernel
@@ -1194,8 +1197,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
             const uint32_t lim_first = token_limit(cw.it, row_base / G);
             float m = -INFINITY, l = 0.f;
             bool alive = true;
-            float c_row = c_all;
-            if (kCodes && j.q_back) c_row *= __ldcg(j.q_back + query_row(j, cw.it, cw.p.kv_head, real ? row_base + row : row_base));
+            float c_row = kCodes ? 1.f : c_all;
+            if (kCodes && j.q_back) c_row = __ldcg(j.q_back + query_row(j, cw.it, cw.p.kv_head, real ? row_base + row : row_base));
             for (uint32_t t = 0; t < n; ++t) {
                 if (!(alive = wait_warp(s_full(x), s_cnt & 1))) break;
                 ++s_cnt;
@@ -1206,7 +1209,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     const uint32_t at = tiles_before + (both ? x : 0) + t * step;
                     if (!(alive = wait_warp(smem_addr(mail.told + at % mail.kSlots), (at / mail.kSlots) & 1))) break;
                     const char2 e = mail.tile[at % mail.kSlots];
-                    c = fminf(c_row * power_of_two(e.x), kLargest);
+                    c = fmaxf(fminf(c_all * fminf(c_row * power_of_two(e.x), kLargest), kLargest), kLeast);
                     value_log = (float)e.y;
                     l_back = power_of_two(-e.y);
                 }
