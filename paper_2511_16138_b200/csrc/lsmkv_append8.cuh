@@ -78,13 +78,14 @@ __device__ __forceinline__ void from_codes4(uint32_t c, uint32_t &lo, uint32_t &
         : "=r"(lo), "=r"(hi) : "r"(c));
 }
 
-// Four codes times 2^-by: exact in 16-bit floats wherever the result is not zero in e4m3.
+// Four codes times 2^-by, by in 1..200. (From 2^-19 on every code becomes zero: 448 2^-19 is less than half of the
+// least one, 2^-9. 2^-126 is the least factor that 32 bits hold.)
 __device__ __forceinline__ uint32_t shrink_codes4(uint32_t c, int by)
 {
     uint32_t lo, hi;
     from_codes4(c, lo, hi);
     const float2 a = Half2<__half>::up(lo), b = Half2<__half>::up(hi);
-    const float f = power_of_two(-by);
+    const float f = power_of_two(-min(by, 126));
     return to_codes4(a.x * f, a.y * f, b.x * f, b.y * f);
 }
 

@@ -152,3 +152,40 @@ def test_append_and_attend_with_padding():
     assert not turned[:33].any() and not turned[40:70].any()
     assert not out[:33].any() and not out[40:70].any()
     check(out, None, exact(turned, pool, g, 0, new_off, kv, page_off, table, 0.1), torch.bfloat16)
+
+
+# ---- exponents that grow by up to the whole range --------------------------------------------------
+
+@pytest.mark.parametrize("rot", [0, 20])                     # 20: element by element
+@pytest.mark.parametrize("grow", [126, 127, 128, 129, 160, 200])
+@pytest.mark.parametrize("at_once", [False, True])
+def test_a_begun_block_whose_exponent_grows_by_the_range(grow, rot, at_once):
+    """Tokens of zeros and of the least size, then a large one: the codes of the earlier tokens become zeros."""
+    D, H, B, P = 80, 2, 16, 16
+    g = geom8(1, H, D, P, B)
+    e = grow - 100
+    k = torch.zeros(6, H, D, dtype=torch.bfloat16, device=DEV)
+    k[1] = 300 * 2.0 ** -100
+    k[2] = -448 * 2.0 ** -100
+    k[3, 0] = 2.0 ** -105
+    k[4] = 448.0 * 2.0 ** e
+    k[5] = -3.5 * 2.0 ** (e + 2)
+    pool = torch.full((2, 1, g.page_bytes), 0xFF, dtype=torch.uint8, device=DEV)
+    tab = torch.cat([torch.ones(P, 10), torch.zeros(P, 10)], 1).to(DEV)          # turns nothing
+    with lsmkv.Context(g, 0) as ctx:
+        pt = lsmkv.pool_table(list(pool))
+        for a, b in ([(0, 4), (4, 6)] if at_once else [(t, t + 1) for t in range(6)]):
+            seqs, *_ = batch([b - a], [b], P, spare=0)
+            ctx.append_batch(0, seqs, k[a:b], k[a:b], pt, rope=lsmkv.Rope(tab) if rot else None)
+            if b == 4:
+                codes, scales = views(pool, g)
+                assert (exponents(scales) == -100).all()
+                # (300 is not a code; even neighbours lie at 288 and 320)
+                want = (k[:4].double() * 2.0 ** 100).float().to(torch.float8_e4m3fn)
+                assert torch.equal(codes[:, 0, :4].float(), want.float().expand(2, -1, -1, -1))
+        assert ctx.last_status()["flags"] == 0
+    codes, scales = views(pool, g)
+    assert (exponents(scales) == e).all()
+    got = codes[:, 0, :6].float()
+    assert not got[:, :4].any()                                                 # (NaN would count)
+    assert (got[:, 4] == 448).all() and (got[:, 5] == -14).all()
