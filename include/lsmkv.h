@@ -593,10 +593,12 @@ int lsmkv_append_batch(lsmkv_ctx *ctx, void *stream, uint32_t layer, uint32_t dt
  * lsmkv_destroy() (all of it no larger than the present one), so graphs captured before stay valid.
  * A wait that runs out sets LSMKV_ST_WAIT_EXPIRED; the results of that call are then unspecified.
  * 8-bit pools: a key or value is code * 2^exponent, and the scales enter scores and weights in 32
- * bits; `dtype` is that of q and out, and the weights are rounded to 11 bits, whichever it is. (In
- * the kernel for many rows a code that lies more than 2^15 below the largest scale among 128 keys
- * may lose bits: under 2^-32 of the largest element.) Buffers of 64 GB or more go by the kernel for
- * few rows whatever their rows.
+ * bits; `dtype` is that of q and out. Whichever it is, weights meet the codes as 16-bit floats of 11
+ * bits that hold w * 2^exponent relative to the largest one among the keys that the row sees (with
+ * exponents under -40 taken as -40 for the largest): under 2^-14 of it they lose bits, under 2^-25 they
+ * count as zero. Likewise the elements of a bfloat16 query relative to the largest one of its row: under
+ * 2^-27 of it they lose bits, and rows of 2^96 or more may overflow. Buffers of 64 GB or more go by the
+ * kernel for few rows whatever their rows.
  * Infinities and NaN among the keys and values reach the rows that see them, and no others. (Where
  * a value is undefined that some rows of a tile of 256 see and others do not, those others are
  * computed twice.)

@@ -245,6 +245,18 @@ uint64_t slab_bytes(const lsmkv_geom_t &g)
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Dynamic shared memory of the many-row kernel over an 8-bit pool: its tiles, on a boundary of 1 KB. At heads of 128 these
+// and its variables fill all that a block may have, and how much the boundary costs goes by the variables' size.
+template <typename T, int DP>
+size_t many8_smem(int max_smem_optin)
+{
+    static const size_t variables = [] {
+        cudaFuncAttributes a;
+        return cudaFuncGetAttributes(&a, k_attend_many<T, DP, false, true>) == cudaSuccess ? a.sharedSizeBytes : 0;
+    }();
+    return std::min(ManyShape<DP>::kSmem8, (size_t)max_smem_optin - variables);
+}
+
 // The bulk copy kernels and the one-pass encoder take their stages as dynamic shared memory
 // beyond the default limit.
 // The limit is a per-device attribute of the function: it is raised once per device, to the
@@ -326,12 +338,13 @@ cudaError_t set_copy_smem_limit(int max_smem_optin)
                        k_attend_many<__nv_bfloat16, 128, false>, k_attend_many<__half, 128, false>})
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ManyShape<128>::kSmem);
-    for (auto *many : {k_attend_many<__nv_bfloat16, 64, false, true>, k_attend_many<__half, 64, false, true>})
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ManyShape<64>::kSmem8);
-    for (auto *many : {k_attend_many<__nv_bfloat16, 128, false, true>, k_attend_many<__half, 128, false, true>})
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(many, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ManyShape<128>::kSmem8);
+    auto raise_many8 = [&](auto *kern, size_t bytes) {
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    };
+    raise_many8(k_attend_many<__nv_bfloat16, 64, false, true>, many8_smem<__nv_bfloat16, 64>(max_smem_optin));
+    raise_many8(k_attend_many<__half, 64, false, true>, many8_smem<__half, 64>(max_smem_optin));
+    raise_many8(k_attend_many<__nv_bfloat16, 128, false, true>, many8_smem<__nv_bfloat16, 128>(max_smem_optin));
+    raise_many8(k_attend_many<__half, 128, false, true>, many8_smem<__half, 128>(max_smem_optin));
     if (e == cudaSuccess) g_smem_limit_set[dev] = true;
     return e;
 }

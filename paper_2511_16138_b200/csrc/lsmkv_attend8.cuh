@@ -43,6 +43,11 @@ struct Few8Shape {
     static constexpr bool kQInRegs = DP * NB <= 256;
 };
 
+// The reference M lies no more than 2^40 below the largest 2^(s_j), whatever the values' exponents: the sum of weights, which are
+// relative to M too, stays in range beside blocks of zeros, whose exponent is the least there is. (Contributions
+// under 2^-54 of a code's size times the largest weight lose bits for it.)
+constexpr float kLeastLog = -40.f;
+
 // Whether one of four codes is NaN.
 __device__ __forceinline__ uint32_t undefined_codes(uint32_t c) { return ((c & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 

@@ -26,10 +26,13 @@
 // registers and, as f16, to the stages: a tile's 128 keys are stored relative to the largest scale of the
 // tile, code * 2^(a_j - A) with A = max a_j, its values likewise to B. So a row's scores have one factor a tile, and
 // its weights one exponent, known before the exponentials: nothing is added to the softmax warps' chain but a
-// few operations a tile. (f16 holds e4m3 codes exactly down to 2^-15 of the tile's largest scale; what is lost below is under 2^-32 of the
-// largest element.) The sums are relative to M = max (row's largest score + B), the sum of weights is taken
-// back by 2^-B tile by tile. Measured: the two requests above 2.3 to 2.4 ms (1.99 without the conversion): the loaders
-// take 4.9k cycles a tile, 2.7k of them in conversions and copies.
+// few operations a tile. The sums are relative to M = max (row's largest score + B), less kLead, the sum of weights is taken
+// back by 2^-B tile by tile. That is exact, and M no further from the largest contribution than in the few-row
+// kernel, where a tile's exponents lie within kKeySpread and kValueSpread of the largest. A loader warp whose rows do
+// not stores them with their own scales, and the softmax warps take such a tile's scores key by key, as the
+// few-row kernel does: no row depends on the size of keys and values that it does not see, nor on its tile's.
+// Measured: the two requests above 2.42 ms (1.99 without the conversion, 2.38 without the look for such tiles): the
+// loaders take 4.9k cycles a tile, 2.7k of them in conversions and copies.
 #pragma once
 #include <cuda.h>
 
@@ -50,7 +53,8 @@ struct ManyShape {
     static constexpr int kConverters = 7, kThreads8 = 16 * 32;
     // stages, and behind them the codes under way: 128 rows of keys, 128 of values
     static constexpr int kStages8 = DP == 128 ? 4 : 8;
-    static constexpr size_t kSmem8 = 1024 + (size_t)(2 + kStages8) * kTileBytes + kTileBytes;
+    static constexpr size_t kTiles8 = (size_t)(2 + kStages8) * kTileBytes + kTileBytes;
+    static constexpr size_t kSmem8 = 1024 + kTiles8;       // or what there is behind the variables (the kernel looks)
     // 8 softmax warps, then a warpgroup of loaders and the issuer. 384 threads start with
     // 168 registers each (64512); 256 x 208 + 128 x 80 = 63488 of them are in use afterwards.
     static constexpr int kThreads = 12 * 32;
@@ -362,19 +366,33 @@ __device__ __forceinline__ uint32_t power_f16x2(int d)
     return one | one << 16;
 }
 
+// How far the exponents of a tile's scales may lie below the largest for its codes to be stored with a common one. Keys: f16
+// holds every code exactly down to 2^-15 of the largest scale (the least code is 2^-9, the least f16 2^-24). Values:
+// M goes by the tile's largest exponent, which may be that of a key that hardly counts for a row or that it does not
+// see, and is then too high by up to that much; all weights lie 2^kLead higher to make up for it.
+constexpr int kKeySpread = 15, kLead = 7, kValueSpread = kLead;
+
 // What the roles tell each other beside the stages. The issuer walks the work for the loaders, a cut ahead of what
 // it issues: they have no registers for it. A tile's exponents go from loader to loader and to the softmax warps,
-// in eight slots in turn (a loader is at most three tiles ahead of the softmax warps, whose weights the
-// products that free its stages wait for).
+// in eight slots in turn, those of its keys one by one in fewer. How far a loader can be ahead of a half's softmax warps in tile t:
+// their scores' place is taken, so a stage with keys that they are to see next stays taken too. Those are the
+// keys of tile t + 1, or of t + 2 when t is the half's last of a cut and only the other half sees t + 1 (the
+// cut behind the next is not told before both halves are done with this one). So a stage for keys is found
+// for tiles up to t + 1 + kStages8 / 2, and a tile's keys' exponents are written when its stage is found.
+template <int DP>
 struct CodeMail {
-    static constexpr uint32_t kSlots = 8;
+    static constexpr uint32_t kSlots = 8, kKeySlots = ManyShape<DP>::kStages8;
+    static_assert(2 + ManyShape<DP>::kStages8 / 2 <= kKeySlots && 3 + ManyShape<DP>::kStages8 / 2 <= kSlots,
+                  "nothing is written over before it is read");
     uint64_t cut_told[2];                    // barriers: a cut is there,
     uint64_t ready[kSlots], told[kSlots];    // all loaders' parts of a tile's exponents, the tile's
     uint64_t page0[2];
     uint4 cut[2];                            // first key, end of the keys, key tiles (0: no cut is left), KV head
     uint2 q_rows[2];                         // the queries: first row under the KV head, halves
     uchar2 part[kSlots][8];                  // a loader warp's largest exponents of keys, of values (+ 101; 0: no key)
-    char2 tile[kSlots];                      // the tile's
+    // x, y: a byte a loader warp, whether its rows are stored with their own scales, not the tile's; z, w: the tile's exponents
+    uint4 tile[kSlots];
+    alignas(16) uint16_t key[kKeySlots][128];    // exponents + 127 that every key is stored with, then its value
     uint32_t q_asked;                        // cuts whose queries were asked for
 };
 
@@ -387,7 +405,7 @@ template <int DP, typename Wait>
 __device__ __forceinline__ void load_codes(const AttendJob &j, const CodeArgs &cd, const CUtensorMap &q_map, uint32_t me,
                                            uint32_t q_s, uint32_t ring, uint32_t raw, Wait wait_warp, uint32_t full0,
                                            uint32_t empty0, uint32_t q_full, uint32_t q_empty, uint32_t spare_bar,
-                                           CodeMail &mail)
+                                           CodeMail<DP> &mail)
 {
     using Sh = ManyShape<DP>;
     constexpr uint32_t kBlock = 128 * 128, kStages = Sh::kStages8;
@@ -493,11 +511,14 @@ __device__ __forceinline__ void load_codes(const AttendJob &j, const CodeArgs &c
             return alive = wait_warp(empty0 + 8 * (half_cnt % kStages), (half_cnt / kStages & 1) ^ 1);
         };
         // (The issuer's proxy fence behind its wait makes the codes visible to the matrix unit.)
-        auto hand_over = [&]() {
+        auto hand_over = [&](uint32_t kv) {
             __syncwarp();
             // (test hook: a tile of the first CTA that never arrives)
             const bool drop = blockIdx.x == 0 && half_cnt == j.test_drop;
-            if (lane == 0) mbar_arrive(drop ? spare_bar : full0 + 8 * (half_cnt % kStages));
+            if (lane == 0) {
+                if (!kv) mbar_arrive(smem_addr(mail.told + half_cnt / 2 % mail.kSlots));
+                mbar_arrive(drop ? spare_bar : full0 + 8 * (half_cnt % kStages));
+            }
             ++half_cnt;
         };
         auto load_half = [&](uint32_t kv) {
@@ -534,16 +555,22 @@ __device__ __forceinline__ void load_codes(const AttendJob &j, const CodeArgs &c
             const uint32_t slot = half_cnt / 2 % mail.kSlots;
             if (!(alive = wait_warp(smem_addr(mail.ready + slot), half_cnt / 2 / mail.kSlots & 1))) break;
             uint32_t k_factor, v_factor;
+            uint32_t mine;                                   // exponents with which this lane's row is stored
+            bool apart;                                      // the warp's rows keep their own scales
             {
                 const uchar2 part = lane < W ? mail.part[slot][lane] : make_uchar2(0, 0);
-                const int k_top = (int)__reduce_max_sync(~0u, (uint32_t)part.x) + kScaleMin - 1;
-                const int v_top = (int)__reduce_max_sync(~0u, (uint32_t)part.y) + kScaleMin - 1;
+                const int k_top = max((int)__reduce_max_sync(~0u, (uint32_t)part.x) + kScaleMin - 1, kScaleMin);
+                const int v_top = max((int)__reduce_max_sync(~0u, (uint32_t)part.y) + kScaleMin - 1, kScaleMin);
                 if (me == 0 && lane == 0) {
-                    mail.tile[slot] = make_char2((char)max(k_top, kScaleMin), (char)max(v_top, kScaleMin));
-                    mbar_arrive(smem_addr(mail.told + slot));
+                    mail.tile[slot].z = (uint32_t)k_top;
+                    mail.tile[slot].w = (uint32_t)v_top;
                 }
-                k_factor = power_f16x2(k_exp - k_top);
-                v_factor = power_f16x2(v_exp - v_top);
+                // (a row without a key has the exponent kScaleMin - 1, and zeros as its codes)
+                apart = __any_sync(~0u, k_exp >= kScaleMin && (k_top - k_exp > kKeySpread || v_top - v_exp > kValueSpread));
+                const int k_own = apart ? k_exp : k_top, v_own = apart ? v_exp : v_top;
+                k_factor = power_f16x2(k_exp - k_own);
+                v_factor = power_f16x2(v_exp - v_own);
+                mine = (uint32_t)(k_own + 127) | (uint32_t)(v_own + 127) << 8;
             }
             const bool more = t + 1 < n;
             if (more) {
@@ -555,6 +582,10 @@ __device__ __forceinline__ void load_codes(const AttendJob &j, const CodeArgs &c
             for (uint32_t kv = 0; kv < 2; ++kv) {
                 asm volatile("cp.async.wait_group 1;" ::: "memory");
                 if (!take_stage()) break;
+                if (!kv) {
+                    if (lane < kOwn && own < Sh::kKeys) mail.key[half_cnt / 2 % mail.kKeySlots][own] = (uint16_t)mine;
+                    if (lane == 0) reinterpret_cast<unsigned char *>(mail.tile + slot)[me] = apart;
+                }
                 const uint32_t dst = ring + half_cnt % kStages * Sh::kTileBytes;
 #pragma unroll
                 for (uint32_t i = 0; i < kMine; ++i) {
@@ -563,7 +594,7 @@ __device__ __forceinline__ void load_codes(const AttendJob &j, const CodeArgs &c
                     if (more) load(i, kv);
                 }
                 loaded();
-                hand_over();
+                hand_over(kv);
             }
             if (!alive) break;
             if (more) tell();
@@ -1055,6 +1086,54 @@ __device__ __noinline__ void redo_cuts(const AttendJob &j, const CodeArgs &cd, c
     }
 }
 
+// What the product of a query and a key's codes is multiplied by: scale, way back of the query's row, exponent + 127
+// of the key's scale. It stays above zero and finite, whatever they are: a masked score of -inf stays one, and a row of zeros
+// counts its keys.
+constexpr float kLeast = 1e-37f;
+
+__device__ __forceinline__ float score_factor(float scale, float back, uint32_t e)
+{
+    return fmaxf(fminf(scale * fminf(back * __uint_as_float(e << 23), kLargest), kLargest), kLeast);
+}
+
+// A row's scores of a tile whose keys and values keep their own scales: products in TMEM to u_j = s_j + b_j in their place,
+// base 2, -inf from key `see` on. es: exponents + 127 of every key, then of its value. Returns the largest s_j, the
+// largest s_j + max(b_j, kLeastLog), and the sum of 2^(s_j) relative to the former. Out of line, since few tiles are like
+// that and the others' registers and instruction cache count (32 suffixes: 692 us, in line 714).
+__device__ __noinline__ float3 scores_apart(uint32_t s_t, const uint16_t *es, float scale, float back, int see)
+{
+    float s_top = -INFINITY, u_top = -INFINITY, sum = 0.f;
+#pragma unroll 1
+    for (int ch = 0; ch < 128; ch += 32) {
+        float u[32];
+        tmem_ld32(s_t + ch, u);
+        tmem_wait_ld();
+        tmem_pin32(u);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+            const uint32_t e = es[ch + k];
+            const float log = (float)(int)(e >> 8) - 127.f;
+            u[k] = ch + k < see ? u[k] * score_factor(scale, back, e & 0xFF) : -INFINITY;
+            s_top = fmaxf(s_top, u[k]);
+            u_top = fmaxf(u_top, u[k] + fmaxf(log, kLeastLog));
+            u[k] += log;
+        }
+        tmem_st32(s_t + ch, u);
+    }
+    tmem_wait_st();
+    const float ref = s_top == -INFINITY ? 0.f : s_top;
+#pragma unroll 1
+    for (int ch = 0; ch < 128; ch += 32) {
+        float u[32];
+        tmem_ld32(s_t + ch, u);
+        tmem_wait_ld();
+        tmem_pin32(u);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) sum += exp2f(u[k] - ((float)(int)(es[ch + k] >> 8) - 127.f) - ref);
+    }
+    return make_float3(s_top, u_top, sum);
+}
+
 // kCodes: an 8-bit pool (cd; otherwise unused).
 template <typename T, int DP, bool kBoxes, bool kCodes = false>
 __global__ __launch_bounds__(kCodes ? ManyShape<DP>::kThreads8 : ManyShape<DP>::kThreads, 1)
@@ -1075,7 +1154,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     __shared__ __align__(128) unsigned char map_work[128];
     __shared__ volatile uint32_t stop, undefined[8];   // (a softmax warp's rows have come out undefined)
     __shared__ float half_m[128], half_l[128];   // the second half's statistics, when the halves share rows
-    __shared__ CodeMail mail;                    // (8-bit pools)
+    __shared__ CodeMail<DP> mail;                // (8-bit pools)
     const uint32_t tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const uint32_t G = j.group, D = j.head_dim;
     // (what comes behind may count on the launch before this one: nobody leaves ahead of it)
@@ -1100,6 +1179,15 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
     }
 
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    if (kCodes) {
+        uint32_t size;
+        asm("mov.u32 %0, %%dynamic_smem_size;" : "=r"(size));
+        if (base + Sh::kTiles8 > smem_addr(smem_raw) + size) {
+            if (blockIdx.x == 0 && tid == 0) st_flag(j.st, LSMKV_ST_WAIT_EXPIRED, 0);
+            wait_launch();
+            return;
+        }
+    }
     const uint32_t q_s = base, ring = base + 2 * Sh::kTileBytes;
     const uint32_t bar0 = smem_addr(bars);
     auto full = [&](uint32_t s) { return bar0 + 8 * s; };
@@ -1126,10 +1214,13 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         if (kCodes)
             for (uint32_t x = 0; x < mail.kSlots; ++x) {
                 mbar_init(smem_addr(mail.ready + x), Sh::kConverters);
-                mbar_init(smem_addr(mail.told + x), 1);
+                mbar_init(smem_addr(mail.told + x), Sh::kConverters);
                 if (x < 2) mbar_init(smem_addr(mail.cut_told + x), 1);
             }
-        if (kCodes) mail.q_asked = 0;
+        if (kCodes) {
+            mail.q_asked = 0;
+            for (uint32_t x = 0; x < mail.kSlots; ++x) mail.tile[x].y = 0;      // (there are seven loaders, eight bytes)
+        }
         mbar_init(q_empty, 1);
         for (int x = 0; x < 2; ++x) {
             mbar_init(s_full(x), 1);
@@ -1172,9 +1263,7 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
         const uint32_t x = w >> 2, row = tid & 127;
         const uint32_t lane_base = (w & 3) << 21;            // lanes 32 (w % 4) ..
         const uint32_t s_t = tmem + lane_base + x * 128, o_t = tmem + lane_base + 256 + x * 128;
-        // A negative scale negates the products. The factor of the scores stays above zero and finite, whatever the
-        // scale, a row's and a tile's factors: a masked score of -inf stays one, and a row of zeros counts its keys.
-        constexpr float kLeast = 1e-37f;
+        // a negative scale negates the products
         const float c_all = kCodes ? fabsf(j.scale_log2) : fmaxf(fabsf(j.scale_log2), kLeast);
         uint32_t tiles_before = 0;   // key tiles of the cuts before
         if ((D + 15) / 16 * 16 < DP) {
@@ -1200,22 +1289,44 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
             float c_row = kCodes ? 1.f : c_all;
             if (kCodes && j.q_back) c_row = __ldcg(j.q_back + query_row(j, cw.it, cw.p.kv_head, real ? row_base + row : row_base));
             for (uint32_t t = 0; t < n; ++t) {
+                float c = c_row, value_log = 0.f, l_back = 1.f;
+                const uint16_t *apart = nullptr;
+                if (kCodes) {
+                    // (the loaders wrote these ahead of the keys)
+                    const uint32_t at = tiles_before + (both ? x : 0) + t * step, slot = at % mail.kSlots;
+                    if (!(alive = wait_warp(smem_addr(mail.told + slot), (at / mail.kSlots) & 1))) break;
+                    const uint4 e = mail.tile[slot];
+                    c = score_factor(c_all, c_row, e.z + 127);
+                    value_log = (float)(int)e.w;
+                    l_back = power_of_two(-(int)e.w);
+                    if (__any_sync(~0u, (e.x | e.y) != 0)) apart = mail.key[at % mail.kKeySlots];
+                }
                 if (!(alive = wait_warp(s_full(x), s_cnt & 1))) break;
                 ++s_cnt;
                 tc_fence_after();
-                float c = c_row, value_log = 0.f, l_back = 1.f;
-                if (kCodes) {
-                    // (the loader wrote them ahead of the keys: this barrier only orders the two)
-                    const uint32_t at = tiles_before + (both ? x : 0) + t * step;
-                    if (!(alive = wait_warp(smem_addr(mail.told + at % mail.kSlots), (at / mail.kSlots) & 1))) break;
-                    const char2 e = mail.tile[at % mail.kSlots];
-                    c = fmaxf(fminf(c_all * fminf(c_row * power_of_two(e.x), kLargest), kLargest), kLeast);
-                    value_log = (float)e.y;
-                    l_back = power_of_two(-e.y);
-                }
+                // The reference moves only when passed by more than 2^8: then what was summed takes the factor fix.
+                constexpr float lead = kCodes ? (float)kLead : 0.f;
+                float fix = 1.f;
+                auto raise = [&](float top) {
+                    if (t == 0) {
+                        m = kCodes ? fmaxf(m, top - lead) : top;
+                    } else if (top > m + (8.f + lead)) {
+                        fix = exp2f(m + lead - top);
+                        m = top - lead;
+                        l *= fix;
+                    }
+                };
                 const uint32_t key = cw.it.kv0 + (cw.p.k0 + (both ? x : 0) + t * step) * Sh::kKeys;
                 const bool masked = key + Sh::kKeys > lim_first;
                 const int see = masked ? (int)(lim > key ? lim - key : 0u) : Sh::kKeys;   // keys of the tile
+                if (kCodes && apart) {
+                    // scores to what multiplies a code; the sum of weights is taken here, without the values' scales
+                    const float3 r = scores_apart(s_t, apart, c_all, c_row, see);
+                    raise(r.y);
+                    l += r.z * exp2f(r.x + (m == -INFINITY ? 0.f : -m));
+                    c = 1.f;
+                    value_log = l_back = 0.f;
+                }
                 float v[Sh::kKeys];
 #pragma unroll
                 for (int ch = 0; ch < 4; ++ch) tmem_ld32(s_t + ch * 32, v + ch * 32);
@@ -1235,15 +1346,8 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     for (int e = 2; e < 32; e += 2) tops[ch] = max3(tops[ch], v[ch * 32 + e], v[ch * 32 + e + 1]);
                 }
                 float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * c;
-                if (kCodes) top += value_log;
-                float fix = 1.f;
-                if (t == 0) {
-                    m = top;
-                } else if (top > m + 8.f) {
-                    fix = exp2f(m - top);
-                    m = top;
-                    l *= fix;
-                }
+                if (kCodes) top += fmaxf(value_log, kLeastLog);
+                raise(top);
                 const float neg = m == -INFINITY ? 0.f : kCodes ? value_log - m : -m;
                 if (__any_sync(~0u, fix != 1.f)) {
                     // the value product of the tile before is done: its scores came after it

@@ -174,10 +174,10 @@ int launch_many8(lsmkv_ctx *ctx, cudaStream_t s, bool follows, const AttendJob &
     }
     if (job.head_dim <= 64)
         CU(ctx, start(ctx, s, follows, k_attend_many<T, 64, false, true>, sm, ManyShape<64>::kThreads8,
-                      ManyShape<64>::kSmem8, job, none, ctx->many_map, ctx->codes));
+                      many8_smem<T, 64>(ctx->max_smem_optin), job, none, ctx->many_map, ctx->codes));
     else
         CU(ctx, start(ctx, s, follows, k_attend_many<T, 128, false, true>, sm, ManyShape<128>::kThreads8,
-                      ManyShape<128>::kSmem8, job, none, ctx->many_map, ctx->codes));
+                      many8_smem<T, 128>(ctx->max_smem_optin), job, none, ctx->many_map, ctx->codes));
     CU(ctx, start(ctx, s, true, k_attend_merge<T>, dim3(sm, 256 / kMergeBlockRows), 256, 0, job));
     return LSMKV_OK;
 }

@@ -189,3 +189,114 @@ def test_a_begun_block_whose_exponent_grows_by_the_range(grow, rot, at_once):
     got = codes[:, 0, :6].float()
     assert not got[:, :4].any()                                                 # (NaN would count)
     assert (got[:, 4] == 448).all() and (got[:, 5] == -14).all()
+
+
+# ---- scales far apart ----------------------------------------------------------------------------
+
+def raw_codes(pool, g):
+    return pool[..., :g.code_bytes].unflatten(-1, (g.page_tokens, g.n_kv_heads, g.head_dim))
+
+
+def spread_setup(dt, D, B, hq, hkv, new, hist, seed=0):
+    kv = [a + b for a, b in zip(new, hist)]
+    seqs, new_off, page_off, table, num = batch(new, kv, 16, seed)
+    gen = torch.Generator(device=DEV).manual_seed(seed + 7)
+    g = geom8(1, hkv, D, 16, B)
+    pool = filled(g, num, gen)
+    q = torch.randn(sum(new), hq, D, generator=gen, device=DEV).to(dt)
+    return g, pool, q, seqs, new_off, kv, page_off, table, gen
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("up", [9, 20, 30, 40])
+@pytest.mark.parametrize("new", [4, 5, 90, 300])
+def test_rows_do_not_depend_on_tokens_behind_them(dt, up, new):
+    """A late token far larger than the others, in its key, its value or both: the rows before it are what they are
+    without it, whichever kernel takes them."""
+    for B, hq, which in ((1, 8, (0, 1)), (1, 8, (0,)), (16, 8, (1,)), (1, 2, (0, 1))):
+        g, pool, q, seqs, new_off, kv, page_off, table, gen = spread_setup(dt, 128, B, hq, 2, [new, 20], [500, 30])
+        last = kv[0] - 1
+        _, scales = views(pool, g)
+        for x in which:
+            # (a block of 16 holds tokens that the rows before see)
+            scales[x, int(table[last // 16]), :, last % 16 // B] += min(up, 11) if B > 1 and dt == torch.float16 else up
+        ref = exact(q, pool, g, 0, new_off, kv, page_off, table, 0.08)
+        out, lse = attend(g, pool, q, seqs, 0.08)
+        first = new - 1                                     # (the row that sees it has scores of any size)
+        rows = [r for r in range(len(q)) if r != first]
+        check(out, lse, ref, dt, rows)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("new", [1, 4, 5, 40, 300])
+@pytest.mark.parametrize("B", [1, 16])
+def test_a_large_value_that_hardly_weighs(dt, new, B):
+    """An early token (or block) whose values are 2^23 times the others' and whose weight is nothing: what comes behind it keeps its bits.
+    And the other way round, a token that weighs nearly everything and whose values are small."""
+    for large in (True, False):
+        g, pool, q, seqs, new_off, kv, page_off, table, gen = spread_setup(dt, 128, B, 8, 2, [new, 1], [3000, 300])
+        codes, scales = raw_codes(pool, g), views(pool, g)[1]
+        q[..., 0] = 16
+        codes[0, ..., 0] = 0x66                            # 56
+        for i in (0, 1):
+            page = int(table[page_off[i]])
+            codes[0, page, :B, :, 0] = 0xFE if large else 0x7E                      # 448, less or more than 200 nats away
+            scales[0, page, :, 0] += 6
+            scales[1, page, :, 0] += 23 if large else -23
+        ref = exact(q, pool, g, 0, new_off, kv, page_off, table, 0.08)
+        out, lse = attend(g, pool, q, seqs, 0.08)
+        check(out, lse, ref, dt)
+
+
+@pytest.mark.parametrize("case", [
+    (torch.bfloat16, 128, 1, 8, 2, [300, 1, 40, 5], [900, 600, 100, 3]),
+    (torch.float16, 128, 4, 16, 2, [33, 8, 17], [2000, 40, 129]),
+    (torch.bfloat16, 64, 2, 8, 4, [70, 300], [3000, 5]),
+    (torch.float16, 96, 1, 12, 4, [128, 30], [700, 0]),
+    (torch.float16, 128, 1, 2, 2, [200], [6000]),
+    (torch.bfloat16, 80, 8, 56, 8, [37, 90], [64, 700]),
+    (torch.bfloat16, 128, 1, 8, 8, [150], [40000]),
+], ids=range(7))
+@pytest.mark.parametrize("span", [6, 12, 30])
+def test_scales_far_apart_everywhere(case, span):
+    """A scale drawn for every block, keys and values apart; bad weights or codes of any one key would show."""
+    dt, D, B, hq, hkv, new, hist = case
+    g, pool, q, seqs, new_off, kv, page_off, table, gen = spread_setup(dt, D, B, hq, hkv, new, hist)
+    _, scales = views(pool, g)
+    for x, top in ((0, 120), (1, 130)):
+        scales[x] = torch.randint(top - span, top + 1, scales[x].shape, generator=gen, device=DEV).to(torch.uint8)
+    ref = exact(q, pool, g, 0, new_off, kv, page_off, table, 0.08)
+    out, lse = attend(g, pool, q, seqs, 0.08)
+    check(out, lse, ref, dt)
+    out, _ = attend(g, pool, q, seqs, -0.08)
+    check(out, None, exact(q, pool, g, 0, new_off, kv, page_off, table, -0.08), dt)
+
+
+@pytest.mark.parametrize("B", [1, 16])
+def test_scales_far_apart_over_shared_prefixes(B):
+    for dt, members, pages, new in ((torch.bfloat16, [6, 4], [9, 5], 5), (torch.float16, [33], [70], 1), (torch.float16, [3, 5], [20, 7], 30)):
+        case = (dt, 128, 16, 16, 2, members, pages, new, (0, 30))
+        g, pool, q, seqs, groups, new_off, kv, page_off, table = shared_setup(case, B)
+        _, scales = views(pool, g)
+        gen = torch.Generator(device=DEV).manual_seed(5)
+        for x, top in ((0, 119), (1, 130)):
+            scales[x] = torch.randint(top - 20, top + 1, scales[x].shape, generator=gen, device=DEV).to(torch.uint8)
+        out, lse = attend(g, pool, q, seqs, 0.08, groups)
+        check(out, lse, exact(q, pool, g, 0, new_off, kv, page_off, table, 0.08), dt)
+
+
+def test_nan_beside_scales_far_apart():
+    """An undefined value among blocks whose scales lie far apart reaches the rows that see it, and no others."""
+    for new in (3, 70, 300):
+        g, pool, q, seqs, new_off, kv, page_off, table, gen = spread_setup(torch.bfloat16, 128, 1, 8, 2, [new], [500])
+        _, scales = views(pool, g)
+        for x, top in ((0, 120), (1, 130)):
+            scales[x] = torch.randint(top - 25, top + 1, scales[x].shape, generator=gen, device=DEV).to(torch.uint8)
+        ref = exact(q, pool, g, 0, new_off, kv, page_off, table, 0.08)
+        p = kv[0] - 2
+        raw_codes(pool, g)[1, int(table[p // 16]), p % 16, :, 7] = 0x7F
+        out = torch.zeros_like(q)
+        with lsmkv.Context(g, 0) as ctx:
+            ctx.attend_batch(0, seqs, q, out, lsmkv.pool_table(list(pool)), 0.08)
+        check(out, None, ref, torch.bfloat16, slice(0, new - 2))
+        assert torch.isnan(out[new - 2:, :, 7]).all() and torch.isfinite(out[:new - 2]).all()
