@@ -376,7 +376,7 @@ void k_attend_few8(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     float fix[2];
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        float t = top[nb][x];
+                        float t = fmaxf(top[nb][x], fmaxf(s[nb][x], s[nb][2 + x]) + kLeastLog);
                         t = fmaxf(t, __shfl_xor_sync(~0u, t, 4));
                         t = fmaxf(t, __shfl_xor_sync(~0u, t, 8));
                         t = fmaxf(t, __shfl_xor_sync(~0u, t, 16));

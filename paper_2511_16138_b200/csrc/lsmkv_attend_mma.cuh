@@ -941,7 +941,7 @@ __device__ __forceinline__ void redo_rows8(const AttendJob &j, const CodeArgs &c
                     const bool see = first + at < min(lim[e >> 1], key_end);
                     s[n][e] = see ? s[n][e] * row_scale[e >> 1] * k_scale[at] : -INFINITY;
                     u[n][e] = see ? s[n][e] + v_log[at] : -INFINITY;
-                    top[e >> 1] = fmaxf(top[e >> 1], u[n][e]);
+                    top[e >> 1] = fmaxf(top[e >> 1], s[n][e] + (see ? fmaxf(v_log[at], kLeastLog) : 0.f));
                 }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {

@@ -300,3 +300,23 @@ def test_nan_beside_scales_far_apart():
             ctx.attend_batch(0, seqs, q, out, lsmkv.pool_table(list(pool)), 0.08)
         check(out, None, ref, torch.bfloat16, slice(0, new - 2))
         assert torch.isnan(out[new - 2:, :, 7]).all() and torch.isfinite(out[:new - 2]).all()
+
+
+@pytest.mark.parametrize("up", [5, 30, 45])
+@pytest.mark.parametrize("new", [1, 40])
+def test_zeros_ahead_of_large_values(new, up):
+    """Blocks of zeros have the least exponent; their tokens weigh as much as others', whatever comes behind."""
+    g, pool, q, seqs, new_off, kv, page_off, table, gen = spread_setup(torch.bfloat16, 128, 16, 8, 2, [new], [20000])
+    codes, scales = raw_codes(pool, g), views(pool, g)[1]
+    zero = torch.tensor(table[:1000], device=DEV)
+    codes[1, zero] = 0
+    scales[1, zero] = 27
+    rest = torch.tensor(table[1000:], device=DEV)
+    scales[1, rest] += up
+    # the first keys fit worse than the others, by six nats
+    q[..., 0] = 32
+    codes[0, ..., 0] = 0x50                                # 8
+    codes[0, torch.tensor(table[:8], device=DEV), :, :, 0] = 0xFA           # -320
+    ref = exact(q, pool, g, 0, new_off, kv, page_off, table, 0.08)
+    out, lse = attend(g, pool, q, seqs, 0.08)
+    check(out, lse, ref, torch.bfloat16)
