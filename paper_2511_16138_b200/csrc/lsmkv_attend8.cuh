@@ -3,7 +3,7 @@
 //
 //   k_j = c_j 2^a_j, v_j = d_j 2^b_j   (codes c, d; exponents a, b of their blocks)
 //   s_j = scale * q . c_j * 2^a_j;  weights in base 2;  u_j = s_j + b_j (log2 of what multiplies d_j)
-//   with M = max_j u_j:  o = sum_j 2^(u_j - M) d_j / sum_j 2^(s_j - M)
+//   with M = max_j u_j (at least max_j s_j - 40):  o = sum_j 2^(u_j - M) d_j / sum_j 2^(s_j - M)
 // so the scales cost one multiplication and one addition a score, nothing a code, and the weights that meet
 // the codes are the true contributions relative to their largest, whatever the scales of the values.
 //
@@ -18,7 +18,7 @@
 // take a head each (or two or more a head), over the same keys, and a page's codes are read whole. Then nothing is
 // merged among the warps but what shares a head. Small batches cut each head's keys for themselves.
 // Measured: that batch 510 to 565 us (2.38 GB, up to 4.7 TB/s; the loads alone 405, head by head 730); 512 sequences of
-// 256 to 4096 tokens, 28/4 heads, 1.16 GB, 256 us (loads alone 198). What lies between is instructions, 370 for 16 keys of
+// 256 to 4096 tokens, 28/4 heads, 1.16 GB, 258 us (loads alone 198). What lies between is instructions, 370 for 16 keys of
 // a head, 64 of them conversions; 16 warps with 128 registers instead of 8 take as long.
 #pragma once
 #include "lsmkv_append8.cuh"
