@@ -31,7 +31,7 @@
 // kernel, where a tile's exponents lie within kKeySpread and kValueSpread of the largest. A loader warp whose rows do
 // not stores them with their own scales, and the softmax warps take such a tile's scores key by key, as the
 // few-row kernel does: no row depends on the size of keys and values that it does not see, nor on its tile's.
-// Measured: the two requests above 2.42 ms (1.99 without the conversion, 2.38 without the look for such tiles): the
+// Measured: the two requests above 2.45 ms (1.99 without the conversion, 2.39 without the look for such tiles): the
 // loaders take 4.9k cycles a tile, 2.7k of them in conversions and copies.
 #pragma once
 #include <cuda.h>
@@ -1102,8 +1102,8 @@ __device__ __forceinline__ float exponent_of(uint32_t e) { return __uint_as_floa
 // A row's scores of a tile whose keys and values keep their own scales: products in TMEM to u_j = s_j + b_j in their
 // place, base 2, -inf from key `see` on. es: exponents + 127 of every key, then of its value; scale: with the row's way
 // back. Returns the largest s_j, the largest s_j + max(b_j, kLeastLog), and the sum of 2^(s_j) relative to the former. Out
-// of line, since few tiles are like that and the others' registers and instruction cache count (32 suffixes: 692 us, in
-// line 714). Where all tiles are like that they take 1300 us, and the long suffix 6.1 ms.
+// of line, since few tiles are like that and the others' registers and instruction cache count (32 suffixes: 697 us, in
+// line 710). Where all tiles are like that they take 1300 us, and the long suffix 6.1 ms.
 __device__ __noinline__ float3 scores_apart(uint32_t s_t, const uint16_t *es, float scale, int see)
 {
     const uint4 *const eights = reinterpret_cast<const uint4 *>(es);
@@ -1298,10 +1298,14 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
             float c_row = kCodes ? 1.f : c_all;
             if (kCodes && j.q_back) c_row = __ldcg(j.q_back + query_row(j, cw.it, cw.p.kv_head, real ? row_base + row : row_base));
             for (uint32_t t = 0; t < n; ++t) {
+                if (!(alive = wait_warp(s_full(x), s_cnt & 1))) break;
+                ++s_cnt;
+                tc_fence_after();
                 float c = c_row, value_log = 0.f, l_back = 1.f;
                 const uint16_t *apart = nullptr;
                 if (kCodes) {
-                    // (the loaders wrote these ahead of the keys)
+                    // (The loaders wrote these ahead of the keys: this barrier only orders the two. It comes behind the scores', since a
+                    // half that had no tile in many cuts may be further ahead than its phases tell apart.)
                     const uint32_t at = tiles_before + (both ? x : 0) + t * step, slot = at % mail.kSlots;
                     if (!(alive = wait_warp(smem_addr(mail.told + slot), (at / mail.kSlots) & 1))) break;
                     const uint4 e = mail.tile[slot];
@@ -1310,9 +1314,6 @@ void k_attend_many(const __grid_constant__ AttendJob j, const __grid_constant__ 
                     l_back = power_of_two(-(int)e.w);
                     if (__any_sync(~0u, (e.x | e.y) != 0)) apart = mail.key[at % mail.kKeySlots];
                 }
-                if (!(alive = wait_warp(s_full(x), s_cnt & 1))) break;
-                ++s_cnt;
-                tc_fence_after();
                 // The reference moves only when passed by more than 2^8: then what was summed takes the factor fix.
                 constexpr float lead = kCodes ? (float)kLead : 0.f;
                 float fix = 1.f;

@@ -226,7 +226,7 @@ bool many_takes(const lsmkv_ctx *ctx) { return ctx->geom.head_dim <= 128 && !ctx
 
 // Over an 8-bit pool the many-row kernel wants f16 queries in boxes of 128 rows under a KV head: they are brought to
 // that by a launch ahead of the others, unless they are f16 already and the heads of a KV head divide 128.
-// (8k tokens of 32 heads of 128: 32 us of 692, with cold caches.)
+// (8k tokens of 32 heads of 128: 32 us of 697, with cold caches.)
 template <typename T>
 int gather_queries(lsmkv_ctx *ctx, cudaStream_t s, const AttendJob &job)
 {

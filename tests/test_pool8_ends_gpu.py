@@ -320,3 +320,17 @@ def test_zeros_ahead_of_large_values(new, up):
     ref = exact(q, pool, g, 0, new_off, kv, page_off, table, 0.08)
     out, lse = attend(g, pool, q, seqs, 0.08)
     check(out, lse, ref, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("D,every", [(128, 30), (64, 17), (128, 9)])
+def test_short_sequences_ahead_of_longer_ones(dt, D, every):
+    """Row tiles that see one key tile give the second half of a CTA's rows nothing to do: it goes ahead to the next one that
+    does, and takes that one's scales all the same."""
+    n = 1500
+    hist = [1000 if i % every == every - 1 else 60 + i % 60 for i in range(n)]
+    g, pool, q, seqs, new_off, kv, page_off, table, gen = spread_setup(dt, D, 16, 8, 2, [5] * n, hist)
+    _, scales = views(pool, g)
+    scales += torch.randint(0, 6, scales.shape, generator=gen, device=DEV).to(torch.uint8)
+    out, lse = attend(g, pool, q, seqs, D ** -0.5)
+    check(out, lse, exact(q, pool, g, 0, new_off, kv, page_off, table, D ** -0.5), dt)
